@@ -299,6 +299,101 @@ dark_status dark_decode_step(const dark_params* p, const void* q, const void* k,
                              void* out, void* hip_stream);
 
 /*
+ * Linear attention with a decay for each head (no feature map, no normaliser: q and k are taken as they are, features of
+ * dark_featurize or any other rows).  Per (b, h), with g = exp(log_decay[h]), from a state S_0 [dk, dv]:
+ *   S_t = g S_(t-1) + k_t v_t^T,      out_t = scale S_t^T q_t,      t = 1 ... n.
+ * Chunked form (prompts, training): dark_decay_fwd, dark_decay_bwd; recurrent form (single tokens): dark_decay_step.
+ *
+ *   Q, K: [B, H, L, dk], V, out: [B, H, L, dv] in io_dtype with layout DARK_BHLD, or [B, L, H, dk] and [B, L, H, dv] with
+ *   DARK_BLHD (as a projection lays them out); all of them in the same layout.
+ *   log_decay: [H] float32, the natural logarithm of the decay: 0 keeps everything, -infinity nothing but the token itself.
+ *   A decay is a constant of the model: there is no gradient with respect to it.  Values above 0 are computed as they are.
+ *   lengths: [B] int32 or NULL (every sequence has L tokens).  Sequence b has its first lengths[b] rows, values outside
+ *   0 ... L count as the nearer of the two.  What lies behind a sequence in Q, K, V and dOut is not read; out and the
+ *   gradients are 0 there.
+ *   States are float32, [B, H, dk, dv].  S_in NULL: zero.  S_out NULL: not wanted.  S_out is the state behind the last
+ *   token; S_out == S_in updates a state in place, any other overlap is DARK_EINVAL.
+ * dk and dv up to 256 (else DARK_EUNSUPPORTED), of any size; rows of whole 16 bytes are faster.  L == 0: the state is passed on.
+ *
+ * Arithmetic: fp32 operands are multiplied and summed in fp32.  bf16 operands go through the matrix units with fp32 sums; the
+ * weights (q_t . k_l) g^(t-l) inside a chunk of 64 rows, and the state where it is read, are rounded to bf16 (2^-8 relative)
+ * on their way into an output of that type, the state itself keeps 24 bits.  An element of K or V that is not finite makes the outputs
+ * from its row on not finite, in its column at least; one of V also those of up to 63 rows before it.
+ */
+typedef enum { DARK_BHLD = 0, DARK_BLHD = 1 } dark_layout;
+
+typedef struct {
+  int32_t B, H, L;        /* batch, heads, rows of a sequence */
+  int32_t dk, dv;         /* width of queries and keys, of values */
+  int32_t io_dtype;       /* dark_dtype of Q, K, V, out, dOut, dQ, dK, dV */
+  int32_t layout;         /* dark_layout */
+  float scale;            /* 0 = 1/sqrt(dk) */
+  int32_t sched_segments; /* segments to cut a sequence into, 0 = the library's choice; a schedule, not semantics */
+} dark_decay_params;
+
+/* Bytes of scratch of dark_decay_fwd (backward == 0) or dark_decay_bwd; 0 on invalid parameters, and where none is needed
+ * (ws may then be NULL). */
+size_t dark_decay_workspace_bytes(const dark_decay_params* p, int backward);
+
+dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,
+                           const int32_t* lengths, const float* S_in, void* out, float* S_out,
+                           void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * Gradients of sum(out dOut) + sum(S_out dS_out).  dS_out NULL: zero.  dQ, dK, dV have the element type and layout of what
+ * they belong to (a product of bf16 operands has no more than its precision); dS_in: float32.  All are overwritten; each may be
+ * NULL (skipped).  dS_in may not overlap dS_out or S_in (DARK_EINVAL).  Nothing is needed from the forward call.
+ */
+dark_status dark_decay_bwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,
+                           const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out,
+                           void* dQ, void* dK, void* dV, float* dS_in, void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * One token: q, k [B, H, dk], v, out [B, H, dv] in io_dtype; p->L and p->layout are ignored; q, k, v and out need
+ * the alignment of their elements only.  No workspace.  fp32 arithmetic.
+ * parent NULL: row b of S_out is the next state of row b of S_in (state_rows == B; S_out == S_in updates in place).
+ * parent [B] int32: row b continues row parent[b] of S_in [state_rows, H, dk, dv], so that beams change places, and one
+ * prompt's state becomes several beams', without a copy of their own; S_out then must not overlap S_in (DARK_EINVAL).  A parent
+ * outside 0 ... state_rows - 1 stands for an empty state.
+ */
+dark_status dark_decay_step(const dark_decay_params* p, const void* q, const void* k, const void* v, const float* log_decay,
+                            const int32_t* parent, int state_rows, const float* S_in, float* S_out, void* out, void* hip_stream);
+
+/*
+ * Beam search: the next n beams of each batch entry.  Candidate (j, t), beam j going on with token t, is worth
+ *   scores[j] + logits[j][t] - log sum_u exp logits[j][u];
+ * the n largest are taken, of equal ones that with the lowest j, then the lowest t.
+ *   logits [B, n, V] in io_dtype, scores [B, n] float32 (log-probabilities so far), finished [B, n] bytes or NULL.
+ *   out_scores [B, n] float32, out_parent and out_token [B, n] int32, best first; with keep_slots != 0 instead so that a beam's best
+ *   successor has the beam's own place (then out_parent[j] == j wherever beam j survives, and dark_state_reorder moves
+ *   the other places only), the further ones, best first, the places left over, lowest first.  out_scores may be scores.
+ *   A finished beam has the one candidate (j, eos) of value scores[j]; its logits are not read.  Logits that are -infinity or
+ *   NaN, a score that is not finite (a beam not in use: -infinity), and rows whose logits are all -infinity or
+ *   hold +infinity make candidates of value -infinity: such ones are taken, in the order of j and t, only where there are too few others.
+ * n <= 32 and n V < 2^31, B n <= 65535 (else DARK_EUNSUPPORTED; V too, beyond some millions); eos in 0 ... V - 1 if finished is given.
+ */
+typedef struct {
+  int32_t B, n, V;     /* batch entries, beams of each, vocabulary */
+  int32_t io_dtype;    /* dark_dtype of logits */
+  int32_t eos;
+  int32_t keep_slots;
+} dark_beam_params;
+size_t dark_beam_workspace_bytes(const dark_beam_params* p);
+dark_status dark_beam_select(const dark_beam_params* p, const void* logits, const float* scores, const unsigned char* finished,
+                             float* out_scores, int32_t* out_parent, int32_t* out_token,
+                             void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * The states of the beams follow their parents, in place: of each of the `count` tensors [B, n, ...] of row_bytes[i] bytes for one beam
+ * (the recurrent states of dark_decode_step and dark_decay_step, or anything else kept for a beam) row (b, j) becomes what row
+ * (b, parent[b][j]) was before the call.  A parent outside 0 ... n - 1 leaves its row as it is.
+ *   parent: [B, n] int32 in device memory; states and row_bytes: host arrays, read before the call returns; tensors must not overlap.
+ * n <= 32, B <= 65535 (else DARK_EUNSUPPORTED).  Sixteen tensors a launch.
+ */
+dark_status dark_state_reorder(int B, int n, const int32_t* parent, int count, void* const* states, const size_t* row_bytes,
+                               void* hip_stream);
+
+/*
  * Per-kernel device timing for benchmarks.  While enabled (on != 0) every kernel
  * launch of the library carries a start and a stop event that the launch itself
  * stamps with the kernel's begin and end on the device, and the launch stream is

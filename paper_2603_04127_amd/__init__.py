@@ -7,6 +7,7 @@ missing the import of this binding's functions raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import math
 import os
@@ -20,6 +21,7 @@ DARK_OK, DARK_EINVAL, DARK_EUNSUPPORTED, DARK_EWORKSPACE, DARK_EALIGN, DARK_EHIP
 DARK_F32, DARK_BF16 = 0, 1
 OP_FEATURIZE, OP_ATTN_FWD, OP_ATTN_CAUSAL_FWD, OP_ATTN_BWD, OP_WHITEN = range(5)
 PATH_AUTO, PATH_F32, PATH_FUSED = range(3)
+BHLD, BLHD = range(2)
 
 
 class DarkParams(ctypes.Structure):
@@ -30,6 +32,20 @@ class DarkParams(ctypes.Structure):
         ("scale", ctypes.c_float), ("w_shared", ctypes.c_int32), ("path", ctypes.c_int32),
         ("sched_kv_wgs", ctypes.c_int32), ("sched_ro_wgs", ctypes.c_int32), ("sched_cs_wgs", ctypes.c_int32),
         ("sched_cs_state", ctypes.c_int32),
+    ]
+
+
+class DecayParams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("dk", ctypes.c_int32), ("dv", ctypes.c_int32),
+        ("io_dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("scale", ctypes.c_float), ("sched_segments", ctypes.c_int32),
+    ]
+
+
+class BeamParams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("n", ctypes.c_int32), ("V", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("eos", ctypes.c_int32),
+        ("keep_slots", ctypes.c_int32),
     ]
 
 
@@ -80,6 +96,21 @@ def lib() -> ctypes.CDLL:
     L.dark_attn_causal_fwd_save.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, sz, vp, sz, vp]
     L.dark_attn_bwd_saved.restype = i32
     L.dark_attn_bwd_saved.argtypes = [pp, vp, vp, vp, vp, vp, vp, vp, sz, vp, vp, vp, vp, vp, vp, sz, vp]
+    dp, bp = ctypes.POINTER(DecayParams), ctypes.POINTER(BeamParams)
+    L.dark_decay_workspace_bytes.restype = sz
+    L.dark_decay_workspace_bytes.argtypes = [dp, i32]
+    L.dark_decay_fwd.restype = i32
+    L.dark_decay_fwd.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.dark_decay_bwd.restype = i32
+    L.dark_decay_bwd.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.dark_decay_step.restype = i32
+    L.dark_decay_step.argtypes = [dp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+    L.dark_beam_workspace_bytes.restype = sz
+    L.dark_beam_workspace_bytes.argtypes = [bp]
+    L.dark_beam_select.restype = i32
+    L.dark_beam_select.argtypes = [bp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.dark_state_reorder.restype = i32
+    L.dark_state_reorder.argtypes = [i32, i32, vp, i32, ctypes.POINTER(vp), ctypes.POINTER(sz), vp]
     L.dark_timing_enable.argtypes = [i32]
     L.dark_timing_enable.restype = None
     L.dark_timing_reset.restype = None
@@ -402,6 +433,214 @@ def dark_attn_bwd(Q, K, V, M, W, dOut, causal: bool, *, chunk=0, scale=0.0, path
                                _ptr(g["dQ"]), _ptr(g["dK"]), _ptr(g["dV"]), _ptr(g["dM"]), ws.data_ptr(), ws.numel(),
                                stream), "dark_attn_bwd")
     return g
+
+
+# ----------------------------------------------------------------------------
+# linear attention with a decay for each head; beam search over recurrent states
+# ----------------------------------------------------------------------------
+def _on_device(*tensors):
+    """The device that all given tensors (None: not given) are on; refuses host tensors and mixed devices."""
+    index = None
+    for t in tensors:
+        if t is None:
+            continue
+        i = t.get_device()
+        if i < 0 or (index is not None and i != index):
+            raise ValueError("tensors must be on one GPU")
+        index = i
+    return index
+
+
+def _on(index):
+    """Calls are enqueued on the current stream of the tensors' device, whichever is current."""
+    torch = _torch()
+    return _HERE_ALREADY if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
+
+
+_HERE_ALREADY = contextlib.nullcontext()
+_LAYOUTS = {"bhld": BHLD, "blhd": BLHD}
+
+
+def _f32(t, shape, what):
+    if t is not None and (t.dtype != _torch().float32 or tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what} must be float32 of shape {tuple(shape)}")
+
+
+def _i32(t, shape, what):
+    if t is not None and (t.dtype != _torch().int32 or tuple(t.shape) != tuple(shape)):
+        raise ValueError(f"{what} must be int32 of shape {tuple(shape)}")
+
+
+def _like(t, x, what):
+    if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
+        raise ValueError(f"{what} must have the shape and type of what it belongs to")
+
+
+def _decay_plan(Q, K, V, layout, scale, segments, backward):
+    """(DecayParams, workspace bytes) of a call."""
+    key = ("decay", Q.shape, Q.dtype, K.shape, K.dtype, V.shape, V.dtype, layout, scale, segments, segments.__class__, backward)
+    plan = _plans.get(key)
+    if plan is None:
+        if layout not in _LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}")
+        if Q.dim() != 4 or K.shape != Q.shape or V.dim() != 4 or V.shape[:3] != Q.shape[:3]:
+            raise ValueError("Q, K and V must have the same batch, heads and length, Q and K the same width")
+        if K.dtype != Q.dtype or V.dtype != Q.dtype:
+            raise TypeError("Q, K and V must have one type")
+        B, H, L, dk = Q.shape if layout == "bhld" else (Q.shape[0], Q.shape[2], Q.shape[1], Q.shape[3])
+        p = DecayParams(B, H, L, dk, V.shape[3], _dtype_code(Q), _LAYOUTS[layout], scale, segments)
+        plan = (p, int(lib().dark_decay_workspace_bytes(ctypes.byref(p), int(backward))))
+        _keep_plan(key, plan)
+    return plan
+
+
+def _decay_checks(p, log_decay, lengths):
+    _f32(log_decay, (p.H,), "log_decay")
+    _i32(lengths, (p.B,), "lengths")
+
+
+def dark_decay_fwd(Q, K, V, log_decay, *, lengths=None, state=None, out=None, state_out=None, want_state=False, scale=0.0,
+                   layout="bhld", segments=0):
+    """Linear attention with the decay exp(log_decay[h]) of each head, from `state` [B,H,dk,dv] (None: empty):
+    S_t = g S_{t-1} + k_t v_t^T, out_t = scale S_t^T q_t.  Q, K [B,H,L,dk], V [B,H,L,dv] (layout "blhd": [B,L,H,..]).
+    Returns out, or (out, state after the last token) with want_state or a `state_out` (which may be `state`).
+    `lengths` [B] int32: rows of each sequence; out is 0 behind them.  `segments`: a schedule override (0: none)."""
+    torch = _torch()
+    p, nb = _decay_plan(Q, K, V, layout, float(scale), segments, False)
+    _decay_checks(p, log_decay, lengths)
+    shape = (p.B, p.H, p.dk, p.dv)
+    _f32(state, shape, "state")
+    _f32(state_out, shape, "state_out")
+    _like(out, V, "out")
+    index = _on_device(Q, K, V, log_decay, lengths, state, out, state_out)
+    with _on(index):
+        if out is None:
+            out = _result(V, V.dtype, Q)
+        if want_state and state_out is None:
+            state_out = torch.empty(shape, dtype=torch.float32, device=Q.device)
+        ws, stream = _workspace(nb, Q.device) if nb else (None, _stream())
+        _check(lib().dark_decay_fwd(ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(lengths), _ptr(state), _ptr(out),
+                                    _ptr(state_out), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream),
+               "dark_decay_fwd")
+    return out if state_out is None else (out, state_out)
+
+
+def dark_decay_bwd(Q, K, V, log_decay, dOut, *, lengths=None, state=None, dstate=None, need=("dQ", "dK", "dV", "dstate"), grads=None,
+                   scale=0.0, layout="bhld", segments=0):
+    """Gradients of sum(out dOut) + sum(state_out dstate) of dark_decay_fwd: a dict of those named in `need` ("dstate", the gradient
+    of the incoming state, only where `state` is given), in the types and layouts of what they belong to.
+    `grads`: a dict of preallocated tensors to write into instead."""
+    torch = _torch()
+    p, nb = _decay_plan(Q, K, V, layout, float(scale), segments, True)
+    _decay_checks(p, log_decay, lengths)
+    shape = (p.B, p.H, p.dk, p.dv)
+    _f32(state, shape, "state")
+    _f32(dstate, shape, "dstate")
+    if dOut.dtype != V.dtype or dOut.shape != V.shape:
+        raise ValueError("dOut must have the shape and type of V")
+    like = {"dQ": Q, "dK": K, "dV": V}
+    unknown = set(need if grads is None else grads) - {"dQ", "dK", "dV", "dstate"}
+    if unknown:
+        raise ValueError(f"unknown gradient(s) {sorted(unknown)}")
+    if grads is not None:
+        g = {k: t for k, t in grads.items() if t is not None}
+        for k, t in g.items():
+            _f32(t, shape, k) if k == "dstate" else _like(t, like[k], k)
+    index = _on_device(Q, K, V, log_decay, dOut, lengths, state, dstate, *(g.values() if grads is not None else ()))
+    with _on(index):
+        if grads is None:
+            g = {k: _result(x, x.dtype, Q) for k, x in like.items() if k in need}
+            if "dstate" in need and state is not None:
+                g["dstate"] = torch.empty(shape, dtype=torch.float32, device=Q.device)
+        ws, stream = _workspace(nb, Q.device) if nb else (None, _stream())
+        _check(lib().dark_decay_bwd(ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(lengths), _ptr(state), _ptr(dOut),
+                                    _ptr(dstate), _ptr(g.get("dQ")), _ptr(g.get("dK")), _ptr(g.get("dV")), _ptr(g.get("dstate")),
+                                    None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream), "dark_decay_bwd")
+    return g
+
+
+def dark_decay_step(q, k, v, log_decay, state, *, parent=None, state_out=None, out=None, scale=0.0):
+    """One token of dark_decay_fwd: q, k [B,H,dk], v [B,H,dv]; returns out [B,H,dv].  `state` [B,H,dk,dv] is updated in place,
+    or left alone and the new one written to `state_out`.  With `parent` [B] int32 (and a `state_out`) row b continues row
+    parent[b] of `state` [any number of rows,H,dk,dv]; a parent that is no row of it stands for an empty state."""
+    scale = float(scale)
+    key = ("decay_step", q.shape, q.dtype, k.shape, k.dtype, v.shape, v.dtype, scale)
+    plan = _plans.get(key)
+    if plan is None:
+        if q.dim() != 3 or k.shape != q.shape or v.dim() != 3 or v.shape[:2] != q.shape[:2]:
+            raise ValueError("q and k must be [B, H, dk], v [B, H, dv]")
+        if k.dtype != q.dtype or v.dtype != q.dtype:
+            raise TypeError("q, k and v must have one type")
+        plan = (DecayParams(q.shape[0], q.shape[1], 1, q.shape[2], v.shape[2], _dtype_code(q), BHLD, scale, 0), 0)
+        _keep_plan(key, plan)
+    p = plan[0]
+    shape = (p.B, p.H, p.dk, p.dv)
+    _f32(log_decay, (p.H,), "log_decay")
+    _i32(parent, (p.B,), "parent")
+    if state_out is None:
+        if parent is not None:
+            raise ValueError("a step that reads its states through `parent` needs a state_out")
+        state_out = state
+    rows = state.shape[0]
+    _f32(state, (rows,) + shape[1:], "state")
+    _f32(state_out, shape, "state_out")
+    _like(out, v, "out")
+    with _on(_on_device(q, k, v, log_decay, state, parent, state_out, out)):
+        if out is None:
+            out = _result(v, v.dtype, q)
+        _check(lib().dark_decay_step(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(parent), rows, _ptr(state),
+                                     _ptr(state_out), _ptr(out), _stream()), "dark_decay_step")
+    return out
+
+
+def dark_beam_select(logits, scores, *, finished=None, eos=0, keep_slots=False, out=None):
+    """The next n beams of each batch entry from logits [B,n,V] and scores [B,n] (float32): (scores, parent, token), [B,n] each,
+    parent and token int32.  Candidate (j, t) is worth scores[j] + log_softmax(logits[j])[t]; best first, equal ones by the lowest j, then
+    the lowest t; with keep_slots a surviving beam's best successor has the beam's own place.  `finished` [B,n] (uint8 or bool): such a
+    beam goes on with `eos` at its score.  `out`: the three tensors to write into."""
+    torch = _torch()
+    key = ("beam", logits.shape, logits.dtype, int(eos), bool(keep_slots))
+    plan = _plans.get(key)
+    if plan is None:
+        B, n, V = logits.shape
+        p = BeamParams(B, n, V, _dtype_code(logits), int(eos), int(bool(keep_slots)))
+        plan = (p, int(lib().dark_beam_workspace_bytes(ctypes.byref(p))))
+        _keep_plan(key, plan)
+    p, nb = plan
+    shape = (p.B, p.n)
+    _f32(scores, shape, "scores")
+    if finished is not None and (finished.dtype not in (torch.uint8, torch.bool) or tuple(finished.shape) != shape):
+        raise ValueError(f"finished must be uint8 or bool of shape {shape}")
+    if out is not None:
+        _f32(out[0], shape, "the scores of out")
+        _i32(out[1], shape, "the parents of out")
+        _i32(out[2], shape, "the tokens of out")
+    with _on(_on_device(logits, scores, finished, *(out or ()))):
+        if out is None:
+            out = (torch.empty(shape, dtype=torch.float32, device=logits.device), torch.empty(shape, dtype=torch.int32, device=logits.device),
+                   torch.empty(shape, dtype=torch.int32, device=logits.device))
+        ws, stream = _workspace(nb, logits.device)
+        _check(lib().dark_beam_select(ctypes.byref(p), _ptr(logits), _ptr(scores), _ptr(finished), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
+                                      ws.data_ptr(), ws.numel(), stream), "dark_beam_select")
+    return tuple(out)
+
+
+def dark_state_reorder(states, parent):
+    """States of beams follow their parents, in place: row (b, j) of every tensor [B*n, ...] (or [B, n, ...]) becomes row
+    (b, parent[b, j]) of before.  parent [B, n] int32; an entry outside 0 ... n - 1 leaves its row as it is.  The tensors may not overlap."""
+    if parent.dim() != 2:
+        raise ValueError("parent must be [B, n]")
+    B, n = parent.shape
+    _i32(parent, (B, n), "parent")
+    count = len(states)
+    ptrs, sizes = (ctypes.c_void_p * count)(), (ctypes.c_size_t * count)()
+    for i, t in enumerate(states):
+        if t.shape[0] != B * n and tuple(t.shape[:2]) != (B, n):
+            raise ValueError("a state must have a row for each beam")
+        ptrs[i] = _ptr(t)
+        sizes[i] = t.numel() * t.element_size() // (B * n) if B else 0
+    with _on(_on_device(parent, *states)):
+        _check(lib().dark_state_reorder(B, n, _ptr(parent), count, ptrs, sizes, _stream()), "dark_state_reorder")
 
 
 # ----------------------------------------------------------------------------

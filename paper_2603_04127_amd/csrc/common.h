@@ -40,6 +40,13 @@ enum KernelId : int {
   KID_WHITEN_MOMENTS,  // whitening geometry: second moments of the rows of Q and K
   KID_WHITEN_EIG,      // whitening geometry: eigen-decomposition, M = Lambda^-1/2
   KID_DECODE,          // one-token recurrence of causal attention
+  KID_DECAY_STATE,     // decayed linear attention: states of the segments
+  KID_DECAY_PREFIX,    // decayed linear attention: states before every segment
+  KID_DECAY_SCAN,      // decayed linear attention: outputs, or gradients, of a segment chunk by chunk
+  KID_DECAY_STEP,      // decayed linear attention: one token
+  KID_BEAM_ROWS,       // beam search: sums and largest logits of every slice of a row
+  KID_BEAM_PICK,       // beam search: the next beams of a batch entry
+  KID_STATE_REORDER,   // recurrent states follow their beams
   KID_COUNT
 };
 

@@ -1,0 +1,371 @@
+// Linear attention with a decay for each head: argument checks, the plan of a call, the prefix over segment states and the
+// one-token recurrence.  The scan itself is in decay_scan.h.
+#include <cmath>
+
+#include "decay.h"
+
+namespace dark {
+namespace decay {
+namespace {
+
+using fz::f32x4;
+using fz::fast_exp2;
+using fz::kLog2e;
+
+// The states before every segment, in place of the segments' own: U_0 = u_in, U_(s+1) = g^len U_s + seg_s.  One thread an element
+// (four where they divide), segment by segment; bound by reading and writing the states once.
+template <int W>
+__global__ __launch_bounds__(256) void k_decay_prefix(States A) {
+  typedef float vec __attribute__((ext_vector_type(W)));
+  State a = A.s[0];
+  if (blockIdx.z == 1) a = A.s[1];
+  const long long size = (long long)a.d1 * a.d2, e = ((long long)blockIdx.y * 256 + threadIdx.x) * W;
+  if (e >= size) return;
+  const int bh = blockIdx.x, b = bh / A.H, h = bh % A.H;
+  const int n = A.lengths != nullptr ? min(max(A.lengths[b], 0), A.L) : A.L;
+  const int used = max(1, (n + A.seg_len - 1) / A.seg_len);
+  const float gl = fast_exp2(fmaxf(A.log_decay[h] * kLog2e, -1e30f) * (float)A.seg_len);
+  vec U = 0.f;
+  if (a.u_in != nullptr) U = *reinterpret_cast<const vec*>(a.u_in + bh * size + e);
+  float* const s = a.seg + (long long)bh * A.nseg * size + e;
+#pragma unroll 4
+  for (int i = 0; i < used - 1; ++i) {
+    const vec own = *reinterpret_cast<const vec*>(s + i * size);
+    *reinterpret_cast<vec*>(s + i * size) = U;
+    U = gl * U + own;
+  }
+  *reinterpret_cast<vec*>(s + (long long)(used - 1) * size) = U;
+}
+
+// ---------------------------------------------------------------------------
+// One token: S <- g S + k v^T, out = scale S^T q, for the columns of a workgroup.  Bound by reading and writing the state once.
+// 256 threads as `tx` units of W columns by 256 / tx rows; every thread sums its rows' share of the output, LDS joins the shares.
+// ---------------------------------------------------------------------------
+template <typename T>
+__device__ __forceinline__ float ld(const T* p);
+template <>
+__device__ __forceinline__ float ld<float>(const float* p) { return *p; }
+template <>
+__device__ __forceinline__ float ld<unsigned short>(const unsigned short* p) { return __uint_as_float((unsigned)*p << 16); }
+__device__ __forceinline__ void st(float* p, float v) { *p = v; }
+__device__ __forceinline__ void st(unsigned short* p, float v) { *p = (unsigned short)fz::pack_bf16(v, 0.f); }
+
+constexpr int kMostWidth = 256;
+constexpr int kAhead = 8;   // rows in flight a thread
+
+template <typename T, int W>
+__global__ __launch_bounds__(256) void k_decay_step(const T* __restrict__ q, const T* __restrict__ k, const T* __restrict__ v,
+                                                    const float* __restrict__ log_decay, const int32_t* __restrict__ parent, int state_rows,
+                                                    const float* S_in, float* S_out, T* __restrict__ out, int H, int dk, int dv, int tx,
+                                                    float scale) {
+  typedef float vec __attribute__((ext_vector_type(W)));
+  __shared__ float qs[kMostWidth], ks[kMostWidth];
+  __shared__ vec part[256];
+  const int tid = threadIdx.x, b = blockIdx.x / H, h = blockIdx.x % H, x = tid % tx, row0 = tid / tx, rows = 256 / tx;
+  const int c = (blockIdx.y * tx + x) * W;
+  const bool mine = c < dv;
+  const int from = parent != nullptr ? parent[b] : b;
+  const bool there = (unsigned)from < (unsigned)state_rows;   // no such row: an empty state
+  const long long size = (long long)dk * dv;
+  const float* const Si = S_in + ((long long)(there ? from : 0) * H + h) * size + c;
+  float* const So = S_out + (long long)blockIdx.x * size + c;
+  vec s[kAhead];
+#pragma unroll
+  for (int u = 0; u < kAhead; ++u) {
+    const int i = row0 + u * rows;
+    s[u] = 0.f;
+    if (mine && there && i < dk) s[u] = *reinterpret_cast<const vec*>(Si + (long long)i * dv);
+  }
+  const float gam = fast_exp2(fmaxf(log_decay[h] * kLog2e, -1e30f));
+  vec vv = 0.f;
+  if (mine) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) vv[j] = ld<T>(v + (long long)blockIdx.x * dv + c + j);
+  }
+  if (tid < dk) {
+    qs[tid] = scale * ld<T>(q + (long long)blockIdx.x * dk + tid);
+    ks[tid] = ld<T>(k + (long long)blockIdx.x * dk + tid);
+  }
+  __syncthreads();
+  vec acc = 0.f;
+  for (int i0 = row0; i0 < dk; i0 += kAhead * rows) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + u * rows;
+      if (i < dk) {
+        const vec n = gam * s[u] + ks[i] * vv;
+        if (mine) *reinterpret_cast<vec*>(So + (long long)i * dv) = n;
+        acc += qs[i] * n;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      const int i = i0 + (kAhead + u) * rows;
+      if (mine && there && i < dk) s[u] = *reinterpret_cast<const vec*>(Si + (long long)i * dv);
+    }
+  }
+  part[tid] = acc;
+  __syncthreads();
+  for (int o = 128; o >= tx; o >>= 1) {   // tx is a power of two
+    if (tid < o) part[tid] += part[tid + o];
+    __syncthreads();
+  }
+  if (tid < tx && mine) {
+#pragma unroll
+    for (int j = 0; j < W; ++j) st(out + (long long)blockIdx.x * dv + c + j, part[tid][j]);
+  }
+}
+
+}  // namespace
+
+dark_status check_params(const dark_decay_params* p, Problem* out) {
+  if (p == nullptr) return DARK_EINVAL;
+  if (p->B < 0 || p->L < 0 || p->H <= 0 || p->dk <= 0 || p->dv <= 0) return DARK_EINVAL;
+  if (p->io_dtype != DARK_F32 && p->io_dtype != DARK_BF16) return DARK_EINVAL;
+  if (p->layout != DARK_BHLD && p->layout != DARK_BLHD) return DARK_EINVAL;
+  if (!(p->scale >= 0.f) || std::isinf(p->scale) || p->sched_segments < 0) return DARK_EINVAL;
+  if (p->dk > kMostWidth || p->dv > kMostWidth || (long long)p->B * p->H > (1 << 22) || p->L > (1 << 30)) return DARK_EUNSUPPORTED;
+  out->p = *p;
+  out->scale = p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)p->dk);
+  out->st = nullptr;
+  return DARK_OK;
+}
+
+namespace {
+
+int blocks_of(int d1, int d2) { return d1 > 128 || d2 <= 64 ? (d2 + 63) / 64 : (d2 + 127) / 128; }
+
+// Segments of a sequence: about two workgroups a CU over all (b,h), column blocks and scans, of at least four chunks.
+void segments(const Problem& pb, int scans, int d1, int d2, int* nseg, int* seg_len) {
+  const int C = pb.p.io_dtype == DARK_BF16 ? kChunkBf16 : kChunkF32;
+  const long long have = pb.BH() * blocks_of(d1, d2) * scans;
+  const int chunks = pb.p.L > 0 ? (pb.p.L + C - 1) / C : 1;
+  long long want = pb.p.sched_segments > 0 ? pb.p.sched_segments : 512 / (have > 0 ? have : 1);
+  if (pb.p.sched_segments == 0 && want > (chunks + 3) / 4) want = (chunks + 3) / 4;
+  if (want > chunks) want = chunks;
+  if (want > 64) want = 64;
+  if (want < 1) want = 1;
+  const int each = (int)((chunks + want - 1) / want);
+  *seg_len = each * C;
+  *nseg = (chunks + each - 1) / each;
+}
+
+dark_status run_scan(const Problem& pb, const Scans& a, int n) {
+  return pb.p.io_dtype == DARK_BF16 ? launch_scan_bf16(a, n, pb.st) : launch_scan_f32(a, n, pb.st);
+}
+
+// The states before every segment, for `n` states of the same widths.
+dark_status run_states(const Problem& pb, const States& a, int n) {
+  DARK_TRY(pb.p.io_dtype == DARK_BF16 ? launch_state_bf16(a, n, pb.st) : launch_state_f32(a, n, pb.st));
+  const long long size = (long long)a.s[0].d1 * a.s[0].d2;
+  if (size % 4 == 0) {
+    const dim3 grid((unsigned)pb.BH(), (unsigned)((size / 4 + 255) / 256), n);
+    DARK_LAUNCH(KID_DECAY_PREFIX, pb.st, k_decay_prefix<4>, grid, dim3(256), 0, a);
+  } else {
+    const dim3 grid((unsigned)pb.BH(), (unsigned)((size + 255) / 256), n);
+    DARK_LAUNCH(KID_DECAY_PREFIX, pb.st, k_decay_prefix<1>, grid, dim3(256), 0, a);
+  }
+  return DARK_OK;
+}
+
+template <typename A>
+void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* lengths, int nseg, int seg_len) {
+  a.log_decay = log_decay;
+  a.lengths = lengths;
+  a.B = pb.p.B;
+  a.H = pb.p.H;
+  a.L = pb.p.L;
+  a.layout = pb.p.layout;
+  a.nseg = nseg;
+  a.seg_len = seg_len;
+}
+
+}  // namespace
+
+dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, const void* V, const float* log_decay,
+                    const int32_t* lengths, const float* S_in, void* out, float* S_out) {
+  const int dk = pb.p.dk, dv = pb.p.dv;
+  int nseg, seg_len;
+  segments(pb, 1, dk, dv, &nseg, &seg_len);
+  float* const seg = nseg > 1 ? ar.take<float>((size_t)pb.BH() * nseg * dk * dv) : nullptr;
+  if (ar.base == nullptr && nseg > 1) return DARK_OK;   // measuring
+  if (ar.overflow) return DARK_EWORKSPACE;
+  if (nseg > 1) {
+    States st;
+    fill(pb, st, log_decay, lengths, nseg, seg_len);
+    st.s[0] = st.s[1] = State{K, V, S_in, seg, dk, dv, 0, 0, 1.f};
+    DARK_TRY(run_states(pb, st, 1));
+  }
+  Scans a;
+  fill(pb, a, log_decay, lengths, nseg, seg_len);
+  a.s[0] = a.s[1] = a.s[2] = Scan{Q, K, V, out, nseg > 1 ? seg : S_in, S_out, dk, dv, 0, 0, 0, pb.scale, pb.scale, 1.f};
+  return run_scan(pb, a, 1);
+}
+
+dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K, const void* V, const float* log_decay,
+                     const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out, void* dQ, void* dK,
+                     void* dV, float* dS_in) {
+  const int dk = pb.p.dk, dv = pb.p.dv;
+  int nseg, seg_len;
+  segments(pb, 3, dk > dv ? dk : dv, dk > dv ? dk : dv, &nseg, &seg_len);
+  const size_t states = (size_t)pb.BH() * nseg * dk * dv;
+  float* const sseg = nseg > 1 ? ar.take<float>(states) : nullptr;
+  float* const gseg = nseg > 1 ? ar.take<float>(states) : nullptr;
+  if (ar.base == nullptr && nseg > 1) return DARK_OK;
+  if (ar.overflow) return DARK_EWORKSPACE;
+  const float s = pb.scale;
+  const bool rev = dK != nullptr || dV != nullptr || dS_in != nullptr;
+  if (nseg > 1) {
+    States st;
+    fill(pb, st, log_decay, lengths, nseg, seg_len);
+    int n = 0;
+    if (dQ != nullptr) st.s[n++] = State{K, V, S_in, sseg, dk, dv, 0, 0, 1.f};
+    if (rev) st.s[n++] = State{Q, dOut, dS_out, gseg, dk, dv, 1, 1, s};
+    if (n == 1) st.s[1] = st.s[0];
+    if (n > 0) DARK_TRY(run_states(pb, st, n));
+  }
+  const float* const Su = nseg > 1 ? sseg : S_in;
+  const float* const Gu = nseg > 1 ? gseg : dS_out;
+  const Scan q{dOut, V, K, dQ, Su, nullptr, dv, dk, 1, 0, 0, s, s, 1.f};
+  const Scan k{V, dOut, Q, dK, Gu, nullptr, dv, dk, 1, 1, 1, s, 1.f, s};
+  const Scan v{K, Q, dOut, dV, Gu, dS_in, dk, dv, 0, 1, 1, s, 1.f, s};
+  Scans a;
+  fill(pb, a, log_decay, lengths, nseg, seg_len);
+  int n = 0;
+  if (dQ != nullptr) a.s[n++] = q;
+  if (dK != nullptr) a.s[n++] = k;
+  if (dk != dv && n > 0) {   // dV has other widths: a launch of its own
+    for (int i = n; i < kMostScans; ++i) a.s[i] = a.s[0];
+    DARK_TRY(run_scan(pb, a, n));
+    n = 0;
+  }
+  if (dV != nullptr || dS_in != nullptr) a.s[n++] = v;
+  if (n == 0) return DARK_OK;
+  for (int i = n; i < kMostScans; ++i) a.s[i] = a.s[0];
+  return run_scan(pb, a, n);
+}
+
+dark_status step(const Problem& pb, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* parent,
+                 int state_rows, const float* S_in, float* S_out, void* out) {
+  const int dk = pb.p.dk, dv = pb.p.dv, H = pb.p.H;
+  const int W = dv % 4 == 0 ? 4 : 1, units = (dv + W - 1) / W;
+  // Columns of a workgroup: all of them, or fewer (16 at least, 64 bytes of a row) until there are four workgroups a CU.
+  int tx = 1;
+  while (tx < units) tx *= 2;
+  const int least = 16 / W;
+  while (tx > least && pb.BH() * ((units + tx - 1) / tx) < 1024) tx /= 2;
+  const dim3 grid((unsigned)pb.BH(), (unsigned)((units + tx - 1) / tx));
+#define DARK_STEP(T, WW)                                                                                                        \
+  DARK_LAUNCH(KID_DECAY_STEP, pb.st, (k_decay_step<T, WW>), grid, dim3(256), 0, static_cast<const T*>(q), static_cast<const T*>(k), \
+              static_cast<const T*>(v), log_decay, parent, state_rows, S_in, S_out, static_cast<T*>(out), H, dk, dv, tx, pb.scale)
+  if (pb.p.io_dtype == DARK_BF16) {
+    if (W == 4) DARK_STEP(unsigned short, 4);
+    else DARK_STEP(unsigned short, 1);
+  } else {
+    if (W == 4) DARK_STEP(float, 4);
+    else DARK_STEP(float, 1);
+  }
+#undef DARK_STEP
+  return DARK_OK;
+}
+
+}  // namespace decay
+}  // namespace dark
+
+// ---------------------------------------------------------------------------
+// C ABI
+// ---------------------------------------------------------------------------
+using namespace dark;
+
+namespace {
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a != nullptr && b != nullptr && x < y + nb && y < x + na;
+}
+dark_status check_workspace(const void* ws, size_t ws_bytes, size_t need) {
+  if (need == 0) return DARK_OK;
+  if (ws == nullptr || ws_bytes < need) return DARK_EWORKSPACE;
+  return aligned(ws, 256) ? DARK_OK : DARK_EALIGN;
+}
+size_t measure(const decay::Problem& pb, bool bwd) {
+  int nseg, seg_len;
+  if (bwd) {
+    const int w = pb.p.dk > pb.p.dv ? pb.p.dk : pb.p.dv;
+    decay::segments(pb, 3, w, w, &nseg, &seg_len);
+  } else {
+    decay::segments(pb, 1, pb.p.dk, pb.p.dv, &nseg, &seg_len);
+  }
+  if (nseg == 1) return 0;
+  Arena ar(nullptr, 0);
+  const size_t states = (size_t)pb.BH() * nseg * pb.p.dk * pb.p.dv;
+  for (int i = 0; i < (bwd ? 2 : 1); ++i) (void)ar.take<float>(states);
+  return ar.off;
+}
+}  // namespace
+
+extern "C" {
+
+size_t dark_decay_workspace_bytes(const dark_decay_params* p, int backward) {
+  decay::Problem pb;
+  if (decay::check_params(p, &pb) != DARK_OK || pb.p.B == 0) return 0;
+  return measure(pb, backward != 0);
+}
+
+dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,
+                           const int32_t* lengths, const float* S_in, void* out, float* S_out, void* ws, size_t ws_bytes,
+                           void* hip_stream) {
+  decay::Problem pb;
+  DARK_TRY(decay::check_params(p, &pb));
+  if (pb.p.B == 0 || (pb.p.L == 0 && S_out == nullptr)) return DARK_OK;
+  if (log_decay == nullptr) return DARK_EINVAL;
+  if (pb.p.L > 0 && (!Q || !K || !V || !out)) return DARK_EINVAL;
+  if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(S_in, 16) || !aligned(S_out, 16) ||
+      !aligned(log_decay, 4) || !aligned(lengths, 4))
+    return DARK_EALIGN;
+  const size_t state = (size_t)pb.BH() * pb.p.dk * pb.p.dv * sizeof(float);
+  if (S_in != S_out && overlap(S_in, state, S_out, state)) return DARK_EINVAL;
+  const size_t need = measure(pb, false);
+  DARK_TRY(check_workspace(ws, ws_bytes, need));
+  pb.st = static_cast<hipStream_t>(hip_stream);
+  Arena ar(ws, ws_bytes);
+  return decay::forward(pb, ar, Q, K, V, log_decay, lengths, S_in, out, S_out);
+}
+
+dark_status dark_decay_bwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,
+                           const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out, void* dQ, void* dK,
+                           void* dV, float* dS_in, void* ws, size_t ws_bytes, void* hip_stream) {
+  decay::Problem pb;
+  DARK_TRY(decay::check_params(p, &pb));
+  if (pb.p.B == 0 || (pb.p.L == 0 && dS_in == nullptr)) return DARK_OK;
+  if (log_decay == nullptr) return DARK_EINVAL;
+  if (pb.p.L > 0 && (!Q || !K || !V || !dOut)) return DARK_EINVAL;
+  if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(dOut, 16) || !aligned(S_in, 16) || !aligned(dS_out, 16) ||
+      !aligned(dQ, 16) || !aligned(dK, 16) || !aligned(dV, 16) || !aligned(dS_in, 16) || !aligned(log_decay, 4) || !aligned(lengths, 4))
+    return DARK_EALIGN;
+  const size_t state = (size_t)pb.BH() * pb.p.dk * pb.p.dv * sizeof(float);
+  if (overlap(dS_in, state, dS_out, state) || overlap(dS_in, state, S_in, state)) return DARK_EINVAL;
+  const size_t need = measure(pb, true);
+  DARK_TRY(check_workspace(ws, ws_bytes, need));
+  pb.st = static_cast<hipStream_t>(hip_stream);
+  Arena ar(ws, ws_bytes);
+  return decay::backward(pb, ar, Q, K, V, log_decay, lengths, S_in, dOut, dS_out, dQ, dK, dV, dS_in);
+}
+
+dark_status dark_decay_step(const dark_decay_params* p, const void* q, const void* k, const void* v, const float* log_decay,
+                            const int32_t* parent, int state_rows, const float* S_in, float* S_out, void* out, void* hip_stream) {
+  decay::Problem pb;
+  DARK_TRY(decay::check_params(p, &pb));
+  if (pb.p.B == 0) return DARK_OK;
+  if (!q || !k || !v || !log_decay || !S_in || !S_out || !out) return DARK_EINVAL;
+  if (parent == nullptr ? state_rows != pb.p.B : state_rows <= 0) return DARK_EINVAL;
+  const size_t elem = pb.p.io_dtype == DARK_BF16 ? 2 : 4;   // rows of one tensor, slices of a longer one: no more is asked of them
+  if (!aligned(q, elem) || !aligned(k, elem) || !aligned(v, elem) || !aligned(out, elem) || !aligned(S_in, 16) || !aligned(S_out, 16) ||
+      !aligned(log_decay, 4) || !aligned(parent, 4))
+    return DARK_EALIGN;
+  const size_t row = (size_t)pb.p.H * pb.p.dk * pb.p.dv * sizeof(float);
+  if ((parent != nullptr || S_in != S_out) && overlap(S_in, row * state_rows, S_out, row * pb.p.B)) return DARK_EINVAL;
+  pb.st = static_cast<hipStream_t>(hip_stream);
+  return decay::step(pb, q, k, v, log_decay, parent, state_rows, S_in, S_out, out);
+}
+
+}  // extern "C"

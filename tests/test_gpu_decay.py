@@ -1,0 +1,254 @@
+"""Linear attention with a decay for each head: chunked forward, backward and single tokens against the fp64 oracle."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2603_04127_amd as dk
+from tests import decay_util as U
+
+pytestmark = pytest.mark.gpu
+NAMES = ("Q", "K", "V", "dOut")
+
+
+def _device(p, layout="bhld"):
+    d = {k: (p[k] if layout == "bhld" else p[k].transpose(1, 2)).contiguous().cuda() for k in NAMES}
+    d.update({k: None if p[k] is None else p[k].cuda() for k in ("a", "lengths", "state", "dstate")})
+    return d
+
+
+def _forward(d, **kw):
+    return dk.dark_decay_fwd(d["Q"], d["K"], d["V"], d["a"], lengths=d["lengths"], state=d["state"], want_state=True, **kw)
+
+
+def _backward(d, **kw):
+    return dk.dark_decay_bwd(d["Q"], d["K"], d["V"], d["a"], d["dOut"], lengths=d["lengths"], state=d["state"], dstate=d["dstate"], **kw)
+
+
+def _heads_first(t, layout):
+    return t if layout == "bhld" else t.transpose(1, 2)
+
+
+def _run(p, layout="bhld", segments=0, scale=0.0, backward=True):
+    d = _device(p, layout)
+    want, size = U.oracle(p, scale), U.oracle(p, scale, magnitude=True)
+    out, last = _forward(d, layout=layout, segments=segments, scale=scale)
+    g = _backward(d, layout=layout, segments=segments, scale=scale) if backward else {}
+    torch.cuda.synchronize()
+    U.check(_heads_first(out, layout), want["out"], size["out"], p["dtype"], "out")
+    U.check(last, want["last"], size["last"], "f32", "last")
+    for k, t in g.items():
+        U.check(t if k == "dstate" else _heads_first(t, layout), want[k], size[k], "f32" if k == "dstate" else p["dtype"], k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [1, 2, 31, 33, 64, 65, 200])
+def test_lengths(L, dtype):
+    _run(U.problem(L, 2, 3, L, 64, 64, dtype, state=True, dstate=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("widths", [(1, 1), (64, 128), (128, 64), (128, 128), (96, 80), (33, 65), (7, 200), (256, 64), (64, 256), (256, 256), (250, 131)])
+def test_widths(widths, dtype):
+    _run(U.problem(3, 1, 2, 150, *widths, dtype, state=True, dstate=True))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["bhld", "blhd"])
+@pytest.mark.parametrize("segments", [1, 2, 3, 100])
+def test_segments_and_layouts(segments, layout, dtype):
+    _run(U.problem(4, 2, 3, 333, 64, 64, dtype, lengths=[333, 191], state=True, dstate=True), layout, segments)
+    _run(U.problem(5, 1, 2, 260, 40, 72, dtype), layout, segments)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("decay", [0.0, -1e-4, -1.0, -30.0, -1e5, -np.inf])
+def test_decays(decay, dtype):
+    _run(U.problem(6, 1, 2, 170, 64, 64, dtype, decay=[decay], state=True, dstate=True), segments=2)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lengths", [[0, 1, 64, 140], [140, 65, 0, 63], [-3, 1000, 128, 127]])
+def test_ragged_batches_read_nothing_behind_a_sequence(lengths, dtype):
+    p = U.problem(7, 4, 2, 140, 64, 64, dtype, lengths=lengths, state=True, dstate=True)
+    for b in range(4):
+        n = min(max(lengths[b], 0), 140)
+        for k, bad in zip(NAMES, (float("nan"), float("inf"), float("-inf"), float("nan"))):
+            p[k][b, :, n:] = 0.0
+    want = {k: U.f64(p[k]) for k in NAMES}   # the oracle sees zeros there
+    d = _device(p)
+    for b in range(4):
+        n = min(max(lengths[b], 0), 140)
+        for k, bad in zip(NAMES, (float("nan"), float("inf"), float("-inf"), float("nan"))):
+            d[k][b, :, n:] = bad
+    ref, size = U.oracle(p), U.oracle(p, magnitude=True)
+    for segments in (1, 3):
+        out, last = _forward(d, segments=segments)
+        g = _backward(d, segments=segments)
+        torch.cuda.synchronize()
+        U.check(out, ref["out"], size["out"], dtype, "out")
+        U.check(last, ref["last"], size["last"], "f32", "last")
+        for k in ("dQ", "dK", "dV", "dstate"):
+            U.check(g[k], ref[k], size[k], "f32" if k == "dstate" else dtype, k)
+        for b in range(4):
+            n = min(max(lengths[b], 0), 140)
+            for t in (out, g["dQ"], g["dK"], g["dV"]):
+                assert (t[b, :, n:] == 0).all()
+    assert all((U.f64(p[k]) == want[k]).all() for k in NAMES)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_no_rows_pass_the_state_on(dtype):
+    p = U.problem(8, 2, 2, 0, 64, 48, dtype, state=True, dstate=True)
+    d = _device(p)
+    out, last = _forward(d)
+    g = _backward(d)
+    assert out.shape == (2, 2, 0, 48) and torch.equal(last, d["state"]) and torch.equal(g["dstate"], d["dstate"])
+    d["state"] = None
+    assert (_forward(d)[1] == 0).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_long_sequences_by_the_library_s_own_segments(dtype):
+    p = U.problem(9, 1, 2, 3000, 64, 64, dtype, state=True, dstate=True)
+    assert dk._decay_plan(p["Q"], p["K"], p["V"], "bhld", 0.0, 0, False)[1] > 0   # several segments
+    _run(p)
+
+
+def test_state_in_place_and_continued_prompts():
+    p = U.problem(10, 2, 2, 300, 64, 64, "bf16", state=True)
+    d = _device(p)
+    out, last = _forward(d)
+    for segments in (1, 3):
+        S = d["state"].clone()
+        got, same = dk.dark_decay_fwd(d["Q"], d["K"], d["V"], d["a"], state=S, state_out=S, segments=segments)
+        assert same is S
+        assert torch.allclose(got.float(), out.float(), rtol=2.0 ** -6, atol=2e-2) and torch.allclose(S, last, rtol=1e-4, atol=1e-4)
+    # the same prompt in two calls
+    first, S = dk.dark_decay_fwd(*(d[k][:, :, :111].contiguous() for k in "QKV"), d["a"], state=d["state"], want_state=True)
+    second, S = dk.dark_decay_fwd(*(d[k][:, :, 111:].contiguous() for k in "QKV"), d["a"], state=S, want_state=True)
+    want, size = U.oracle(p), U.oracle(p, magnitude=True)
+    U.check(torch.cat([first, second], 2), want["out"], size["out"], "bf16", "two calls")
+    U.check(S, want["last"], size["last"], "f32", "state of two calls")
+
+
+def test_needed_gradients_only():
+    d = _device(U.problem(11, 1, 2, 200, 64, 32, "bf16", state=True, dstate=True))
+    whole = _backward(d)
+    for need in (("dQ",), ("dK",), ("dV",), ("dstate",), ("dK", "dstate")):
+        got = _backward(d, need=need)
+        assert set(got) == set(need) and all(torch.equal(got[k], whole[k]) for k in need)
+    own = {"dQ": torch.empty_like(d["Q"]), "dV": torch.empty_like(d["V"])}
+    assert _backward(d, grads=own)["dQ"] is own["dQ"] and torch.equal(own["dV"], whole["dV"])
+
+
+def test_scale_and_repeatability():
+    p = U.problem(12, 2, 4, 500, 64, 64, "bf16", state=True, dstate=True)
+    _run(p, scale=0.75)
+    d = _device(p)
+    a, b = (_forward(d) + tuple(_backward(d).values()) for _ in range(2))
+    assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_far_positions():
+    # the last token of a long sequence against the sum written out: 64-bit row offsets, many chunks of a state
+    L, d = 70000, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    Q, K, V = (torch.randn(1, 2, L, d, generator=g, device="cuda").bfloat16() for _ in range(3))
+    a = torch.tensor([0.0, -1e-4], device="cuda")
+    out, last = dk.dark_decay_fwd(Q, K, V, a, want_state=True)
+    w = torch.exp(a.double()[:, None] * torch.arange(L - 1, -1, -1, device="cuda").double())
+    for h in range(2):
+        S = (K[0, h].double() * w[h][:, None]).T @ V[0, h].double()
+        assert ((last[0, h].double() - S).norm() / S.norm()).item() <= U.L2["f32"]
+        want = (Q[0, h, -64:].double() @ S) * d ** -0.5
+        assert ((out[0, h, -1].double() - want[-1]).norm() / want[-1].norm()).item() <= 2 * U.L2["bf16"]   # one row, not the whole tensor
+
+
+def test_infinity_and_nan_stay_behind_their_row():
+    # a key that is not finite reaches no earlier row; a value may reach the rows of its own chunk (64 rows)
+    for dtype in ("f32", "bf16"):
+        p = U.problem(13, 1, 1, 200, 64, 64, dtype)
+        d = _device(p)
+        clean = _forward(d)[0]
+        for name, bad in (("K", float("nan")), ("K", float("inf")), ("Q", float("nan"))):
+            e = {**d, name: d[name].clone()}
+            e[name][0, 0, 100, 3] = bad
+            out = _forward(e)[0]
+            assert torch.equal(out[:, :, :100], clean[:, :, :100]) and not torch.isfinite(out[0, 0, 100]).any()
+        e = {**d, "V": d["V"].clone()}
+        e["V"][0, 0, 100, 3] = float("inf")
+        out = _forward(e)[0]
+        assert torch.equal(out[:, :, :64], clean[:, :, :64]) and not torch.isfinite(out[0, 0, 100:, 3]).any()
+
+
+# ---------------------------------------------------------------------------
+# single tokens
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 3, 64, 64), (1, 1, 1, 1), (3, 2, 33, 65), (1, 2, 256, 256), (2, 2, 128, 20), (70, 16, 128, 128), (1, 5, 100, 200)])
+def test_steps_are_the_forward(shape, dtype):
+    B, H, dkey, dval = shape
+    p = U.problem(20, B, H, 3 if B * H > 100 else 20, dkey, dval, dtype, state=True)
+    d = _device(p)
+    S = d["state"].clone()
+    out = torch.stack([dk.dark_decay_step(*(d[k][:, :, t].contiguous() for k in "QKV"), d["a"], S) for t in range(p["Q"].shape[2])], 2)
+    want, size = U.oracle(p), U.oracle(p, magnitude=True)
+    U.check(out, want["out"], size["out"], dtype, "out")
+    U.check(S, want["last"], size["last"], "f32", "state")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_steps_from_parents(dtype):
+    p = U.problem(21, 6, 2, 1, 48, 72, dtype)
+    d = _device(p)
+    past = torch.randn(4, 2, 48, 72, device="cuda")
+    parent = torch.tensor([3, 0, 0, -1, 4, 2], dtype=torch.int32, device="cuda")   # -1 and 4 are no rows: empty states
+    S = torch.full((6, 2, 48, 72), float("nan"), device="cuda")
+    before = past.clone()
+    out = dk.dark_decay_step(*(d[k][:, :, 0].contiguous() for k in "QKV"), d["a"], past, parent=parent, state_out=S)
+    p["state"] = torch.stack([past[r].cpu() if 0 <= r < 4 else torch.zeros(2, 48, 72) for r in parent.tolist()])
+    want, size = U.oracle(p), U.oracle(p, magnitude=True)
+    U.check(out[:, :, None], want["out"], size["out"], dtype, "out")
+    U.check(S, want["last"], size["last"], "f32", "state")
+    assert torch.equal(past, before)
+
+
+# ---------------------------------------------------------------------------
+# streams and graphs
+# ---------------------------------------------------------------------------
+def test_two_streams_at_once():
+    ds = [_device(U.problem(30 + i, 1, 4, 2000, 64, 64, "bf16", state=True, dstate=True)) for i in range(2)]
+    want = [(*_forward(d), *_backward(d).values()) for d in ds]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ds]
+    for _ in range(3):
+        got = []
+        for d, s in zip(ds, streams):
+            with torch.cuda.stream(s):
+                got.append((*_forward(d), *_backward(d).values()))
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))
+
+
+def test_captured_calls_replay():
+    d = _device(U.problem(40, 1, 4, 1500, 64, 64, "bf16", state=True, dstate=True))
+    other = _device(U.problem(41, 1, 4, 1500, 64, 64, "bf16", state=True, dstate=True))
+    step = [d[k][:, :, 0].contiguous() for k in "QKV"]
+    S2 = torch.empty_like(d["state"])
+
+    def work():
+        return (*_forward(d), *_backward(d).values(), dk.dark_decay_step(*step, d["a"], d["state"], state_out=S2), S2)
+
+    work()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = work()
+    for i in range(3):
+        for k in NAMES + ("state", "dstate"):
+            d[k].copy_(other[k] if i % 2 else torch.randn_like(d[k]))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in held]
+        _forward(other)   # eager work between the replays
+        assert all(torch.equal(x, y) for x, y in zip(got, work()))
