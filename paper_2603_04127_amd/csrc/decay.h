@@ -33,7 +33,7 @@ struct Scan {
   const float* u_in;          // state before row 0 of the sequence (one segment) or of every segment (several); null: zero
   float* u_out;               // state behind the last row; null: not asked for
   int d1, d2;
-  int transposed;             // u_in and u_out are [.., d2, d1] instead of [.., d1, d2]
+  int transposed;             // u_in is [.., d2, d1] instead of [.., d1, d2] (u_out never)
   int reverse, off;
   float sp, sr, su;
 };

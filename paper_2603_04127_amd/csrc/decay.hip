@@ -125,6 +125,8 @@ dark_status check_params(const dark_decay_params* p, Problem* out) {
   if (p->layout != DARK_BHLD && p->layout != DARK_BLHD) return DARK_EINVAL;
   if (!(p->scale >= 0.f) || std::isinf(p->scale) || p->sched_segments < 0) return DARK_EINVAL;
   if (p->dk > kMostWidth || p->dv > kMostWidth || (long long)p->B * p->H > (1 << 22) || p->L > (1 << 30)) return DARK_EUNSUPPORTED;
+  // a chunk's rows are addressed by 32-bit offsets: 64 rows of all heads stay under 2^31 bytes
+  if (p->layout == DARK_BLHD && (long long)p->H * (p->dk > p->dv ? p->dk : p->dv) > (1 << 22)) return DARK_EUNSUPPORTED;
   out->p = *p;
   out->scale = p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)p->dk);
   out->st = nullptr;

@@ -1,11 +1,12 @@
 // The chunked scan of decayed linear attention and the states of its segments, for one element type (see decay.h for the mathematics).
 //
-// A workgroup of four waves walks the rows of a segment of one (b,h) in chunks of C rows, for a block of D2 columns of x3 and y.
-// The state U [D1, D2] stays in the accumulators of the products that update it: each wave owns D2 / 4 of its columns, and what it
+// A workgroup of D2 / 16 waves walks the rows of a segment of one (b,h) in chunks of C rows, for a block of D2 columns of x3 and y.
+// The state U [D1, D2] stays in the accumulators of the products that update it: each wave owns 16 of its columns, and what it
 // owns serves the next chunk's readout as an operand without leaving the registers: an accumulator tile holds four consecutive
 // rows of a column in a lane, and as the order in which a product runs over its inner dimension is free as long as both operands
 // keep to it, two such tiles are one operand of 32, met by x1 rows that are read in the same order (`row_perm`).
 // Per chunk: P = x1 x2^T, decayed and masked, by all waves together through LDS; y^T = U^T x1^T + x3^T P^T; U' = g^C U + x2^T (w x3).
+// The next chunk's rows are on their way into registers meanwhile.
 #pragma once
 
 #include "decay.h"
@@ -15,20 +16,29 @@ namespace decay {
 
 using namespace fz;
 
-// 16-byte chunk q of row `row` of a tile in LDS whose rows are RB bytes long lies at position q ^ swz<RB>(row).  Rows read side by
-// side (16 rows, one chunk each) and columns read by the transposing reads (four rows, two neighbouring chunks; the other half of
-// the 32 lanes that the LDS serves together eight rows further on) both fall onto distinct banks: with rows of 256 bytes the four
-// low bits of the row permute all 16 chunks, neighbours of four rows two chunks apart.
+// 16-byte chunk q of row `row` of a tile in LDS whose rows are RB bytes long lies at position q ^ swz<RB>(row).  The LDS serves a
+// 16-byte read of rows (lane l: row l % 16, chunk l / 16) in groups of lanes {0-3, 12-15, 20-27} and {4-11, 16-19, 28-31}: rows
+// 0-3 and 12-15 of one chunk together with rows 4-11 of its neighbour, and the other way round.  The transposing reads fetch two
+// neighbouring chunks of four rows r ... r + 3 and of r + 8 ... r + 11 together.  Both fall onto distinct banks if the position's lowest
+// bit is free within each of the two row sets, that is if bit 2 ^ bit 3 of the row lies above it, and the bits above it tell the
+// eight rows of a transposing read apart.  (With bit 3 alone there, the former two-way: a third of the LDS's busy cycles.)
+// The mapping is linear over xor, so that constants of a tile's position are one xor with a lane's base.
 template <int RB>
-__device__ static inline int swz(int row) {
+__device__ constexpr int swz(int row) {
   static_assert(RB == 128 || RB % 256 == 0, "rows of 128 or whole 256 bytes");
-  if (RB == 128) return ((row >> 2) & 1) | ((row >> 1) & 1) << 1 | ((row >> 3) & 1) << 2;
-  return ((row >> 2) & 1) | (row & 3) << 1 | ((row >> 3) & 1) << 3;
+  if (RB == 128) return ((row >> 2) & 1) | ((row >> 1) & 1) << 1 | (((row >> 3) ^ (row >> 2)) & 1) << 2;
+  return ((row >> 2) & 1) | (row & 3) << 1 | (((row >> 3) ^ (row >> 2)) & 1) << 3;
 }
-template <int RB>
-__device__ static inline int at(int row, int q) { return row * RB + ((q ^ swz<RB>(row)) << 4); }
 
-// Operands of a product over 32 values of the inner dimension: eight a lane, those of lane group g = lane / 16.
+// A lane's bases into tiles of RB bytes a row, from which every operand is one xor (and an immediate) away.
+struct Lane {
+  int i, g;   // lane % 16, lane / 16
+};
+
+template <typename V>
+__device__ static inline V lds_get(const char* smem, int at) { return *reinterpret_cast<const V*>(smem + at); }
+
+// Operands of a product over 32 values of the inner dimension: eight a lane, those of lane group g.
 template <typename T>
 struct Op;
 
@@ -40,53 +50,60 @@ struct Op<unsigned short> {
   __device__ static f32x4 mma(frag a, frag b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(*reinterpret_cast<bf16x8*>(&a), *reinterpret_cast<bf16x8*>(&b), c, 0, 0, 0);
   }
-  // values k0 + 8 g ... + 7 of a row
+  // values 32 k + 8 g ... + 7 of row i of 16
   template <int RB>
-  __device__ static frag row(const char* tile, int r, int k0, int g) {
-    return *reinterpret_cast<const u32x4*>(tile + at<RB>(r, k0 / 8 + g));
-  }
-  // values k0 + 4 g ... + 3 and k0 + 16 + 4 g ... + 3: the order of two accumulator tiles
+  __device__ static int row_base(Lane l) { return l.i * RB + ((l.g ^ swz<RB>(l.i)) << 4); }
+  __device__ static frag row(const char* tile, int base, int k) { return lds_get<u32x4>(tile, base ^ (k << 6)); }
+  // values 32 k + 4 g ... + 3 and 32 k + 16 + 4 g ... + 3: the order of two accumulator tiles
   template <int RB>
-  __device__ static frag row_perm(const char* tile, int r, int k0, int g) {
-    const u32x2 a = *reinterpret_cast<const u32x2*>(tile + at<RB>(r, k0 / 8 + (g >> 1)) + 8 * (g & 1));
-    const u32x2 b = *reinterpret_cast<const u32x2*>(tile + at<RB>(r, k0 / 8 + 2 + (g >> 1)) + 8 * (g & 1));
+  __device__ static int perm_base(Lane l) { return l.i * RB + (((l.g >> 1) ^ swz<RB>(l.i)) << 4) + 8 * (l.g & 1); }
+  __device__ static frag row_perm(const char* tile, int base, int k) {
+    const u32x2 a = lds_get<u32x2>(tile, base ^ (k << 6)), b = lds_get<u32x2>(tile, base ^ (k << 6) ^ 32);
     return frag{a[0], a[1], b[0], b[1]};
   }
-  // rows r0 + 8 g ... + 7 of column c0 + lane % 16
+  // rows 8 g ... + 7 (of 32) of column 16 t + i: the lane points at row 8 g + i / 4 (+ 4), columns 16 t + 4 (i % 4) ... + 3
   template <int RB>
-  __device__ static frag col(const char* tile, int r0, int c0, int lane) {
-    const int i = lane & 15, r = r0 + 8 * (lane >> 4) + (i >> 2), q = c0 / 8 + ((i >> 1) & 1);
-    const u32x2 a = lds_read_tr16(reinterpret_cast<const unsigned short*>(tile + at<RB>(r, q) + 8 * (i & 1)));
-    const u32x2 b = lds_read_tr16(reinterpret_cast<const unsigned short*>(tile + at<RB>(r + 4, q) + 8 * (i & 1)));
+  __device__ static int col_base(Lane l) {
+    const int r = 8 * l.g + (l.i >> 2);
+    return r * RB + ((((l.i >> 1) & 1) ^ swz<RB>(r)) << 4) + 8 * (l.i & 1);
+  }
+  template <int RB>
+  __device__ static frag col(const char* tile, int base, int t) {
+    const u32x2 a = lds_read_tr16(reinterpret_cast<const unsigned short*>(tile + (base ^ (t << 5))));
+    const u32x2 b = lds_read_tr16(reinterpret_cast<const unsigned short*>(tile + 4 * RB + (base ^ (t << 5) ^ (swz<RB>(4) << 4))));
     return frag{a[0], a[1], b[0], b[1]};
   }
   // Two accumulator tiles as an operand.  Rounded to bf16 once (2^-8 relative): the product goes into an output of that type.
   __device__ static frag state(f32x4 a, f32x4 b) {
     return frag{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
   }
-  // w x as the sum of three bf16 operands: the state is a 32-bit result, so its terms keep their 24 bits (8 + 8 + 8).
-  __device__ static void weighted(frag x, const float* w, frag* out) {
+  // w x as the sum of three bf16 operands: the state is a 32-bit result, so its terms keep their 24 bits.  Cut off, not rounded: what
+  // is left behind eight leading bits, and again behind the next eight, is exact, and so is the sum of the three.
+  __device__ static void weighted(frag x, f32x4 w0, f32x4 w1, frag* out) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      float lo = __uint_as_float(x[i] << 16) * w[2 * i], hi = __uint_as_float(x[i] & 0xffff0000u) * w[2 * i + 1];
+      const f32x4 w = i < 2 ? w0 : w1;
+      float lo = __uint_as_float(x[i] << 16) * w[2 * (i & 1)], hi = __uint_as_float(x[i] & 0xffff0000u) * w[2 * (i & 1) + 1];
 #pragma unroll
       for (int p = 0; p < kPlanes; ++p) {
-        const unsigned u = pack_bf16(lo, hi);
-        out[p][i] = u;
-        lo -= __uint_as_float(u << 16);
-        hi -= __uint_as_float(u & 0xffff0000u);
+        out[p][i] = __builtin_amdgcn_perm(__float_as_uint(hi), __float_as_uint(lo), 0x07060302u);
+        lo -= __uint_as_float(__float_as_uint(lo) & 0xffff0000u);
+        hi -= __uint_as_float(__float_as_uint(hi) & 0xffff0000u);
       }
     }
   }
-  // four values of P, columns c ... c + 3 of row r
+  // four values of P: columns 16 kt + 4 g ... + 3 of row i
   template <int RB>
-  __device__ static void put4(char* tile, int r, int c, f32x4 v) {
-    *reinterpret_cast<u32x2*>(tile + at<RB>(r, c / 8) + 2 * (c & 7)) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  __device__ static int put_base(Lane l) { return perm_base<RB>(l); }
+  __device__ static void put4(char* tile, int base, int kt, f32x4 v) {
+    *reinterpret_cast<u32x2*>(tile + (base ^ (kt << 5))) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
   }
-  __device__ static void store4(unsigned short* p, f32x4 v) {
-    *reinterpret_cast<u32x2*>(p) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  __device__ static void store4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
+    __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, b, at, 0, 0);
   }
-  __device__ static void store1(unsigned short* p, float v) { *p = (unsigned short)pack_bf16(v, 0.f); }
+  __device__ static void store1(__amdgpu_buffer_rsrc_t b, unsigned at, float v) {
+    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)pack_bf16(v, 0.f), b, at, 0, 0);
+  }
 };
 
 template <>
@@ -103,190 +120,251 @@ struct Op<float> {
     return c;
   }
   template <int RB>
-  __device__ static frag row(const char* tile, int r, int k0, int g) {
-    return frag{{*reinterpret_cast<const f32x4*>(tile + at<RB>(r, k0 / 4 + 2 * g)),
-                 *reinterpret_cast<const f32x4*>(tile + at<RB>(r, k0 / 4 + 2 * g + 1))}};
+  __device__ static int row_base(Lane l) { return l.i * RB + (((2 * l.g) ^ swz<RB>(l.i)) << 4); }
+  __device__ static frag row(const char* tile, int base, int k) {
+    return frag{{lds_get<f32x4>(tile, base ^ (k << 7)), lds_get<f32x4>(tile, base ^ (k << 7) ^ 16)}};
   }
   template <int RB>
-  __device__ static frag row_perm(const char* tile, int r, int k0, int g) {
-    return frag{{*reinterpret_cast<const f32x4*>(tile + at<RB>(r, k0 / 4 + g)),
-                 *reinterpret_cast<const f32x4*>(tile + at<RB>(r, k0 / 4 + 4 + g))}};
+  __device__ static int perm_base(Lane l) { return l.i * RB + ((l.g ^ swz<RB>(l.i)) << 4); }
+  __device__ static frag row_perm(const char* tile, int base, int k) {
+    return frag{{lds_get<f32x4>(tile, base ^ (k << 7)), lds_get<f32x4>(tile, base ^ (k << 7) ^ 64)}};
   }
   template <int RB>
-  __device__ static frag col(const char* tile, int r0, int c0, int lane) {
+  __device__ static int col_base(Lane l) { return 8 * l.g * RB + (((l.i >> 2) ^ swz<RB>(8 * l.g)) << 4) + 4 * (l.i & 3); }
+  template <int RB>
+  __device__ static frag col(const char* tile, int base, int t) {
     frag f;
-    const int i = lane & 15, r = r0 + 8 * (lane >> 4);
 #pragma unroll
-    for (int j = 0; j < 8; ++j)
-      f.v[j >> 2][j & 3] = *reinterpret_cast<const float*>(tile + at<RB>(r + j, c0 / 4 + (i >> 2)) + 4 * (i & 3));
+    for (int j = 0; j < 8; ++j) f.v[j >> 2][j & 3] = lds_get<float>(tile + j * RB, base ^ (t << 6) ^ (swz<RB>(j) << 4));
     return f;
   }
   __device__ static frag state(f32x4 a, f32x4 b) { return frag{{a, b}}; }
-  __device__ static void weighted(const frag& x, const float* w, frag* out) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j) out[0].v[j >> 2][j & 3] = x.v[j >> 2][j & 3] * w[j];
+  __device__ static void weighted(const frag& x, f32x4 w0, f32x4 w1, frag* out) {
+    out[0].v[0] = x.v[0] * w0;
+    out[0].v[1] = x.v[1] * w1;
   }
   template <int RB>
-  __device__ static void put4(char* tile, int r, int c, f32x4 v) {
-    *reinterpret_cast<f32x4*>(tile + at<RB>(r, c / 4)) = v;
+  __device__ static int put_base(Lane l) { return perm_base<RB>(l); }
+  __device__ static void put4(char* tile, int base, int kt, f32x4 v) { *reinterpret_cast<f32x4*>(tile + (base ^ (kt << 6))) = v; }
+  __device__ static void store4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
+    __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, b, at, 0, 0);
   }
-  __device__ static void store4(float* p, f32x4 v) { *reinterpret_cast<f32x4*>(p) = v; }
-  __device__ static void store1(float* p, float v) { *p = v; }
+  __device__ static void store1(__amdgpu_buffer_rsrc_t b, unsigned at, float v) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), b, at, 0, 0); }
 };
 
-// Where the rows of a (b,h) lie: row r is token r, or counted from the end token n - 1 - r.
-template <typename T>
+// Memory by buffer instructions: a wave-uniform address and extent, 32-bit offsets of the lanes.  What lies at or behind the extent
+// reads as zero and is not written, so that rows behind a sequence, columns behind the last and parts of a tile need no branches:
+// they are given offsets that are too large.
+typedef __amdgpu_buffer_rsrc_t Buffer;
+__device__ static inline Buffer buffer(const void* p, unsigned bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000);
+}
+constexpr unsigned kNowhere = 0x80000000u;   // every extent is smaller (check_params)
+
+// Rows of a (b,h), chunk by chunk.  Row r is token r, or counted from the end token n - 1 - r.
 struct Rows {
-  const T* base;
-  long long stride;   // elements from one row to the next (negative: counted from the end)
+  const char* head;   // token 0
+  unsigned row;       // bytes from one token to the next
+  unsigned width;     // bytes of a row that exist from the tile's first column on
+  int n, reverse;
+  // the tokens of rows r0 ... r0 + nr - 1
+  __device__ Buffer rows(int r0, int nr) const {
+    return buffer(head + (long long)(reverse ? n - r0 - nr : r0) * row, nr > 0 ? (unsigned)(nr - 1) * row + width : 0u);
+  }
+  // offset of the chunk's row `row`, of nr; too large for a row that does not exist (negative, read as unsigned, where counted from the end)
+  __device__ unsigned offset(int r, int nr) const { return (unsigned)(reverse ? nr - 1 - r : r) * row; }
+  // from there to the row `by` rows further on
+  __device__ int step(int by) const { return reverse ? -by * (int)row : by * (int)row; }
 };
 template <typename T>
-__device__ static inline Rows<T> rows_of(const void* x, int b, int h, int H, int L, int d, int layout, int reverse, int n) {
-  const long long stride = layout == DARK_BHLD ? d : (long long)H * d;
-  const T* base = static_cast<const T*>(x) + (layout == DARK_BHLD ? ((long long)b * H + h) * L * d : ((long long)b * L * H + h) * d);
-  if (!reverse) return {base, stride};
-  return {base + (n > 0 ? (n - 1) * stride : 0), -stride};
+__device__ static inline Rows rows_of(const void* x, int b, int h, int H, int L, int d, int layout, int reverse, int n, int col0, int cols) {
+  const long long first = layout == DARK_BHLD ? ((long long)b * H + h) * L * d : ((long long)b * L * H + h) * d;
+  return {static_cast<const char*>(x) + (first + col0) * (long long)sizeof(T), (unsigned)(layout == DARK_BHLD ? d : H * d) * (unsigned)sizeof(T),
+          (unsigned)(cols * (int)sizeof(T)), n, reverse};
 }
 
-// A tile of C rows and D columns on its way to LDS: NCH = C D sizeof(T) / 16 / 256 pieces of 16 bytes a thread, zeros behind the last
+// A tile of C rows and D columns on its way to LDS: some pieces of 16 bytes for each of NTH threads, zeros behind the last
 // row and column (what lies there in memory is never read).  VEC: rows begin at multiples of 16 bytes and are whole pieces long.
-template <typename T, int C, int D, bool VEC>
+template <typename T, int C, int D, int NTH, bool VEC>
 struct Tile {
   static constexpr int kPieces = D * (int)sizeof(T) / 16;   // of a row
-  static constexpr int kEach = C * kPieces / 256;
+  static constexpr int kEach = C * kPieces / NTH;
+  static constexpr int kStep = NTH / kPieces;               // rows from one piece of a thread to its next
   static constexpr int kPer = 16 / (int)sizeof(T);
-  static_assert(C * kPieces % 256 == 0, "whole pieces a thread");
+  static constexpr int RB = D * (int)sizeof(T);
+  static_assert(C * kPieces % NTH == 0 && NTH % kPieces == 0 && (kStep & (kStep - 1)) == 0, "whole pieces a thread");
   u32x4 r[kEach];
-  __device__ void load(Rows<T> x, int r0, int nr, int col0, int d, int tid) {
+  __device__ void load(const Rows& x, int r0, int nr, int tid) {
+    const Buffer b = x.rows(r0, nr);
+    const unsigned c = (unsigned)(tid % kPieces) * 16u, row = x.offset(tid / kPieces, nr);
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      const int e = tid + 256 * i, row = e / kPieces, c = col0 + (e % kPieces) * kPer;
-      r[i] = u32x4{0, 0, 0, 0};
-      if (row >= nr || c >= d) continue;
-      const T* p = x.base + (long long)(r0 + row) * x.stride + c;
+      const unsigned at = row + (unsigned)x.step(i * kStep);   // wraps around to far behind the extent where rows are counted from the end
       if (VEC) {
-        r[i] = *reinterpret_cast<const u32x4*>(p);
+        r[i] = __builtin_amdgcn_raw_buffer_load_b128(b, c < x.width ? at + c : kNowhere, 0, 0);
       } else {
         T v[kPer];
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) v[j] = c + j < d ? p[j] : (T)0;
+        for (int j = 0; j < kPer; ++j) {
+          const unsigned cj = c + j * (unsigned)sizeof(T), off = cj < x.width ? at + cj : kNowhere;
+          if constexpr (sizeof(T) == 2) v[j] = __builtin_amdgcn_raw_buffer_load_b16(b, off, 0, 0);
+          else v[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
+        }
         __builtin_memcpy(&r[i], v, 16);
       }
     }
   }
   __device__ void store(char* tile, int tid) const {
+    const int row0 = tid / kPieces, base = row0 * RB + (((tid % kPieces) ^ swz<RB>(row0)) << 4);
+    // kStep is a power of two and row0 below it: further rows are one xor with a constant away
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const int e = tid + 256 * i;
-      *reinterpret_cast<u32x4*>(tile + at<D * (int)sizeof(T)>(e / kPieces, e % kPieces)) = r[i];
-    }
+    for (int i = 0; i < kEach; ++i) *reinterpret_cast<u32x4*>(tile + i * kStep * RB + (base ^ (swz<RB>((i * kStep) & 15) << 4))) = r[i];
   }
 };
+
+// A wave's columns of a state [d1, d2] in memory (or of its transpose): rows 16 kt + 4 g ... + 3 of column c (behind the last: c >= d2).
+template <int KT, bool VEC>
+__device__ static inline void load_state(f32x4 (&U)[KT], const float* p, int d1, int d2, int transposed, int c, int g) {
+  const Buffer b = buffer(p, (unsigned)(d1 * d2) * 4u);
+  if (!transposed) {
+    const unsigned off = c < d2 ? (unsigned)(4 * g * d2 + c) * 4u : kNowhere;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) U[kt][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off + (unsigned)((16 * kt + j) * d2) * 4u, 0, 0));
+  } else {
+    const unsigned off = c < d2 ? (unsigned)(c * d1 + 4 * g) * 4u : kNowhere;
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      const int row = 16 * kt + 4 * g;   // rows behind the last would be the next column
+      if (VEC) {
+        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, row < d1 ? off + 64u * kt : kNowhere, 0, 0);
+        __builtin_memcpy(&U[kt], &v, 16);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) U[kt][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, row + j < d1 ? off + 64u * kt + 4u * j : kNowhere, 0, 0));
+      }
+    }
+  }
+}
+template <int KT>
+__device__ static inline void store_state(const f32x4 (&U)[KT], float* p, int d1, int d2, int c, int g) {
+  const Buffer b = buffer(p, (unsigned)(d1 * d2) * 4u);
+  const unsigned off = c < d2 ? (unsigned)(4 * g * d2 + c) * 4u : kNowhere;
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(U[kt][j]), b, off + (unsigned)((16 * kt + j) * d2) * 4u, 0, 0);
+}
 
 // The decay in the log2 domain.  exp(-inf) = 0 as a large negative number, so that 0 * -inf does not arise: g^0 = 1.
 __device__ static inline float decay_log2(const float* log_decay, int h) { return fmaxf(log_decay[h] * kLog2e, -1e30f); }
 __device__ static inline float power(float a2, int n) { return fast_exp2(a2 * (float)n); }
 
-// Weights g^(nr-1-key+off) su of the lane's keys; 0 behind the last row.
-template <int KS>
-__device__ static inline void key_weights(float (&w)[KS][8], float a2, int nr, int off, float su, int g) {
-#pragma unroll
-  for (int ks = 0; ks < KS; ++ks)
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      const int n = nr - 1 - (32 * ks + 8 * g + j);
-      w[ks][j] = n >= 0 ? su * power(a2, n + off) : 0.f;
-    }
+// Weights su g^(nr-1-key+off) of the chunk's keys, 0 behind the last row: C floats in LDS.
+template <int C>
+__device__ static inline void put_weights(char* tw, float a2, int nr, int off, float su, int tid) {
+  if (tid < C) *reinterpret_cast<float*>(tw + 4 * tid) = tid < nr ? su * power(a2, max(nr - 1 - tid, 0) + off) : 0.f;
 }
 
-// U <- g^nr U + x2^T (w x3): the columns of U that the wave owns.
-template <typename T, int C, int D1, int D2, int NT>
-__device__ static inline void update(f32x4 (&U)[D1 / 16][NT], const char* t2, const char* t3, const float (&w)[C / 32][8], float gn, int wave, int lane) {
+// U <- g^nr U + x2^T (w x3): the 16 columns of U that the wave owns.
+template <typename T, int C, int D1, int D2>
+__device__ static inline void update(f32x4 (&U)[D1 / 16], const char* t2, const char* t3, const char* tw, float gn, int wave, Lane l) {
   typedef Op<T> O;
+  constexpr int RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T);
+  const int b2 = O::template col_base<RB1>(l), b3 = O::template col_base<RB2>(l);
 #pragma unroll
-  for (int kt = 0; kt < D1 / 16; ++kt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) U[kt][nt] *= gn;
+  for (int kt = 0; kt < D1 / 16; ++kt) U[kt] *= gn;
 #pragma unroll
   for (int ks = 0; ks < C / 32; ++ks) {
-    typename O::frag x[NT][O::kPlanes];
+    typename O::frag x[O::kPlanes];
+    const f32x4 w0 = lds_get<f32x4>(tw, 128 * ks + 32 * l.g), w1 = lds_get<f32x4>(tw, 128 * ks + 32 * l.g + 16);
+    O::weighted(O::template col<RB2>(t3 + 32 * ks * RB2, b3, wave), w0, w1, x);
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-      O::weighted(O::template col<D2 * (int)sizeof(T)>(t3, 32 * ks, 16 * (wave * NT + nt), lane), w[ks], x[nt]);
+    for (int k0 = 0; k0 < D1 / 16; k0 += 4) {   // four sums at a time: a product does not wait for the one before it
+      typename O::frag k[4];
 #pragma unroll
-    for (int kt = 0; kt < D1 / 16; ++kt) {
-      const typename O::frag k = O::template col<D1 * (int)sizeof(T)>(t2, 32 * ks, 16 * kt, lane);
+      for (int i = 0; i < 4; ++i) k[i] = O::template col<RB1>(t2 + 32 * ks * RB1, b2, k0 + i);
 #pragma unroll
       for (int p = O::kPlanes - 1; p >= 0; --p)   // the smallest terms first
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) U[kt][nt] = O::mma(k, x[nt][p], U[kt][nt]);
+        for (int i = 0; i < 4; ++i) U[k0 + i] = O::mma(k[i], x[p], U[k0 + i]);
+      __builtin_amdgcn_sched_barrier(0);
     }
   }
 }
 
 template <typename T, int D1, int D2>
-constexpr int scan_lds() { return Op<T>::kChunk * (2 * D1 + D2 + Op<T>::kChunk) * (int)sizeof(T); }
+constexpr int scan_lds() { return Op<T>::kChunk * ((2 * D1 + D2 + Op<T>::kChunk) * (int)sizeof(T) + 4); }
 template <typename T, int D1, int D2>
-constexpr int state_lds() { return Op<T>::kChunk * (D1 + D2) * (int)sizeof(T); }
+constexpr int state_lds() { return Op<T>::kChunk * ((D1 + D2) * (int)sizeof(T) + 4); }
+
+// Waves a SIMD that the registers have to leave room for: as many as the LDS takes workgroups.
+constexpr int scan_waves(int d1, int d2) { return d1 == 256 ? 2 : d1 == 128 && d2 == 64 ? 3 : 4; }
+constexpr int state_waves(int d1) { return d1 == 256 ? 2 : 4; }
+
+// The lane index anew: what is derived from it is computed where it is used, instead of held in registers all along.
+__device__ static inline Lane fresh(int lane) {
+  asm volatile("" : "+v"(lane));
+  return {lane & 15, lane >> 4};
+}
 
 template <typename T, int D1, int D2, bool VEC>
-__global__ __launch_bounds__(256) void k_decay_scan(Scans A) {
+__global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans A) {
   typedef Op<T> O;
-  constexpr int C = O::kChunk, QT = C / 16, KS = C / 32, NT = D2 / 64, KT = D1 / 16, K1 = D1 / 32;
+  constexpr int C = O::kChunk, QT = C / 16, KS = C / 32, KT = D1 / 16, K1 = D1 / 32, W = D2 / 16, NTH = 64 * W;
   constexpr int RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T), RBP = C * (int)sizeof(T);
   extern __shared__ __attribute__((aligned(256))) char smem[];
   char* const t1 = smem;
   char* const t2 = t1 + C * RB1;
   char* const t3 = t2 + C * RB1;
   char* const tp = t3 + C * RB2;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l15 = lane & 15, g = lane >> 4;
+  char* const tw = tp + C * RBP;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   Scan a = A.s[0];
   if (blockIdx.z == 1) a = A.s[1];
   if (blockIdx.z == 2) a = A.s[2];
   const int bh = blockIdx.x / A.nseg, seg = blockIdx.x % A.nseg, b = bh / A.H, h = bh % A.H, col0 = blockIdx.y * D2;
   const int n = A.lengths != nullptr ? min(max(A.lengths[b], 0), A.L) : A.L;
   const float a2 = decay_log2(A.log_decay, h);
-  const int begin = seg * A.seg_len, end = min(begin + A.seg_len, A.L);
-  T* const ybase = const_cast<T*>(rows_of<T>(a.y, b, h, A.H, A.L, a.d2, A.layout, 0, n).base);
-  const long long ystride = A.layout == DARK_BHLD ? a.d2 : (long long)A.H * a.d2;
+  const int begin = seg * A.seg_len, end = min(begin + A.seg_len, A.L), cols = min(a.d2 - col0, D2);
   // rows behind the sequence
-  for (int r = a.y != nullptr ? max(begin, n) + (tid >> 6) : end; r < end; r += 4)
-    for (int c = col0 + lane; c < min(col0 + D2, a.d2); c += 64) ybase[r * ystride + c] = (T)0;
+  if (a.y != nullptr && end > n) {
+    const Rows y = rows_of<T>(a.y, b, h, A.H, A.L, a.d2, A.layout, 0, n, col0, cols);
+    for (int r = max(begin, n) + wave; r < end; r += W)
+      for (int c = lane; c < cols; c += 64) reinterpret_cast<T*>(const_cast<char*>(y.head) + (long long)r * y.row)[c] = (T)0;
+  }
   if (begin >= n && seg > 0) return;   // segment 0 passes the state on even when there are no rows
-
-  const Rows<T> x1 = rows_of<T>(a.x1, b, h, A.H, A.L, a.d1, A.layout, a.reverse, n);
-  const Rows<T> x2 = rows_of<T>(a.x2, b, h, A.H, A.L, a.d1, A.layout, a.reverse, n);
-  const Rows<T> x3 = rows_of<T>(a.x3, b, h, A.H, A.L, a.d2, A.layout, a.reverse, n);
   const int last = min(end, n);
-  Tile<T, C, D1, VEC> p1, p2;
-  Tile<T, C, D2, VEC> p3;
-  p1.load(x1, begin, last - begin, 0, a.d1, tid);
-  p2.load(x2, begin, last - begin, 0, a.d1, tid);
-  p3.load(x3, begin, last - begin, col0, a.d2, tid);
 
-  // the state: rows 16 kt + 4 g ... + 3 of column col0 + 16 (wave NT + nt) + lane % 16
-  f32x4 U[KT][NT];
-  const long long uat = A.nseg > 1 ? (long long)bh * A.nseg + seg : bh;
-  const float* const uin = a.u_in != nullptr ? a.u_in + uat * a.d1 * a.d2 : nullptr;
-  bool carried = uin != nullptr;
+  const Rows x1 = rows_of<T>(a.x1, b, h, A.H, A.L, a.d1, A.layout, a.reverse, n, 0, a.d1);
+  const Rows x2 = rows_of<T>(a.x2, b, h, A.H, A.L, a.d1, A.layout, a.reverse, n, 0, a.d1);
+  const Rows x3 = rows_of<T>(a.x3, b, h, A.H, A.L, a.d2, A.layout, a.reverse, n, col0, cols);
+  const Rows y = rows_of<T>(a.y, b, h, A.H, A.L, a.d2, A.layout, a.reverse, n, col0, cols);
+  Tile<T, C, D1, NTH, VEC> p1, p2;
+  Tile<T, C, D2, NTH, VEC> p3;
+  p1.load(x1, begin, min(C, last - begin), tid);
+  p2.load(x2, begin, min(C, last - begin), tid);
+  p3.load(x3, begin, min(C, last - begin), tid);
+
+  // the state: rows 16 kt + 4 g ... + 3 of column col0 + 16 wave + lane % 16
+  f32x4 U[KT];
+  const long long uat = (A.nseg > 1 ? (long long)bh * A.nseg + seg : bh) * a.d1 * a.d2;
+  bool carried = a.u_in != nullptr;
+  const int uc = col0 + 16 * wave + (lane & 15);
+  if (carried) {
+    load_state<KT, VEC>(U, a.u_in + uat, a.d1, a.d2, a.transposed, uc, lane >> 4);
+  } else {
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = 16 * kt + 4 * g, c = col0 + 16 * (wave * NT + nt) + l15;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        U[kt][nt][j] = carried && row + j < a.d1 && c < a.d2 ? uin[a.transposed ? (long long)c * a.d1 + row + j : (long long)(row + j) * a.d2 + c] : 0.f;
-    }
+    for (int kt = 0; kt < KT; ++kt) U[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
   // Tiles of P above the diagonal that a product over 32 keys reads: zero from here on, never written again.
-  for (int e = tid; e < C * RBP / 16; e += 256) *reinterpret_cast<u32x4*>(tp + 16 * e) = u32x4{0, 0, 0, 0};
-
-  float w[KS][8];
-  key_weights<KS>(w, a2, C, a.off, a.su, g);
+  for (int e = tid; e < C * RBP / 16; e += NTH) *reinterpret_cast<u32x4*>(tp + 16 * e) = u32x4{0, 0, 0, 0};
+  put_weights<C>(tw, a2, C, a.off, a.su, tid);
   float lead[QT];   // sr g^(r+1-off) of the lane's rows
 #pragma unroll
-  for (int qt = 0; qt < QT; ++qt) lead[qt] = a.sr * power(a2, 16 * qt + l15 + 1 - a.off);
-  float gn = power(a2, C);
+  for (int qt = 0; qt < QT; ++qt) lead[qt] = a.sr * power(a2, 16 * qt + (lane & 15) + 1 - a.off);
+  const float gC = power(a2, C);
 
   for (int r0 = begin; r0 < last; r0 += C) {
     const int nr = min(C, last - r0);
@@ -294,156 +372,121 @@ __global__ __launch_bounds__(256) void k_decay_scan(Scans A) {
     p1.store(t1, tid);
     p2.store(t2, tid);
     p3.store(t3, tid);
+    if (nr < C) put_weights<C>(tw, a2, nr, a.off, a.su, tid);
     lds_barrier();
     if (r0 + C < last) {
-      p1.load(x1, r0 + C, last - r0 - C, 0, a.d1, tid);
-      p2.load(x2, r0 + C, last - r0 - C, 0, a.d1, tid);
-      p3.load(x3, r0 + C, last - r0 - C, col0, a.d2, tid);
+      const int next = min(C, last - r0 - C);
+      p1.load(x1, r0 + C, next, tid);
+      p2.load(x2, r0 + C, next, tid);
+      p3.load(x3, r0 + C, next, tid);
     }
     // P: the tiles on and below the diagonal, dealt out to the waves
+    const Lane l = fresh(lane);
+    const int b1 = O::template row_base<RB1>(l);
 #pragma unroll
-    for (int i = 0; i < (QT * (QT + 1) / 2 + 3) / 4; ++i) {
-      const int t = wave + 4 * i;
+    for (int i = 0; i < (QT * (QT + 1) / 2 + W - 1) / W; ++i) {
+      const int t = wave + W * i;
       if (t < QT * (QT + 1) / 2) {
         const int qt = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, kt = t - qt * (qt + 1) / 2;
         f32x4 s = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < K1; ++k)
-          s = O::mma(O::template row<RB1>(t2, 16 * kt + l15, 32 * k, g), O::template row<RB1>(t1, 16 * qt + l15, 32 * k, g), s);
+        for (int k = 0; k < K1; ++k) s = O::mma(O::row(t2 + kt * 16 * RB1, b1, k), O::row(t1 + qt * 16 * RB1, b1, k), s);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-          const int apart = 16 * (qt - kt) + l15 - 4 * g - j;
+          const int apart = 16 * (qt - kt) + l.i - 4 * l.g - j;
           s[j] = apart >= 0 ? s[j] * (a.sp * power(a2, max(apart, 0))) : 0.f;
         }
-        O::template put4<RBP>(tp, 16 * qt + l15, 16 * kt + 4 * g, s);
+        O::put4(tp + qt * 16 * RBP, O::template put_base<RBP>(l), kt, s);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
-    f32x4 y[NT][QT];
+    f32x4 out[QT];
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) y[nt][qt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int qt = 0; qt < QT; ++qt) out[qt] = f32x4{0.f, 0.f, 0.f, 0.f};
     if (carried) {
+      const int bp = O::template perm_base<RB1>(l);
 #pragma unroll
       for (int k = 0; k < K1; ++k) {
-        typename O::frag u[NT];
+        const typename O::frag u = O::state(U[2 * k], U[2 * k + 1]);
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) u[nt] = O::state(U[2 * k][nt], U[2 * k + 1][nt]);
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) {
-          const typename O::frag x = O::template row_perm<RB1>(t1, 16 * qt + l15, 32 * k, g);
-#pragma unroll
-          for (int nt = 0; nt < NT; ++nt) y[nt][qt] = O::mma(u[nt], x, y[nt][qt]);
-        }
+        for (int qt = 0; qt < QT; ++qt) out[qt] = O::mma(u, O::row_perm(t1 + qt * 16 * RB1, bp, k), out[qt]);
+        __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) y[nt][qt] *= lead[qt];
+      for (int qt = 0; qt < QT; ++qt) out[qt] *= lead[qt];
     }
     lds_barrier();   // P is there
+    {
+      const int b3 = O::template col_base<RB2>(l), bp = O::template row_base<RBP>(l);
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks) {
-      typename O::frag v[NT];
+      for (int ks = 0; ks < KS; ++ks) {
+        const typename O::frag v = O::template col<RB2>(t3 + 32 * ks * RB2, b3, wave);
 #pragma unroll
-      for (int nt = 0; nt < NT; ++nt) v[nt] = O::template col<RB2>(t3, 32 * ks, 16 * (wave * NT + nt), lane);
-#pragma unroll
-      for (int qt = 2 * ks; qt < QT; ++qt) {
-        const typename O::frag p = O::template row<RBP>(tp, 16 * qt + l15, 32 * ks, g);
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt) y[nt][qt] = O::mma(v[nt], p, y[nt][qt]);
+        for (int qt = 2 * ks; qt < QT; ++qt) out[qt] = O::mma(v, O::row(tp + qt * 16 * RBP, bp, ks), out[qt]);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
+    if (a.y != nullptr) {
+      const Buffer yb = y.rows(r0, nr);
+      const unsigned c = (unsigned)((16 * wave + 4 * l.g) * (int)sizeof(T)), row = y.offset(l.i, nr);
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) {
-      const int r = r0 + 16 * qt + l15;
-      if (r < last && a.y != nullptr) {
-        T* const row = ybase + (a.reverse ? n - 1 - r : r) * ystride;
+      for (int qt = 0; qt < QT; ++qt) {
+        const unsigned at = row + (unsigned)y.step(16 * qt);
+        if (VEC) {
+          O::store4(yb, c < y.width ? at + c : kNowhere, out[qt]);
+        } else {
 #pragma unroll
-        for (int nt = 0; nt < NT; ++nt) {
-          const int c = col0 + 16 * (wave * NT + nt) + 4 * g;
-          if (VEC) {
-            if (c < a.d2) O::store4(row + c, y[nt][qt]);
-          } else {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (c + j < a.d2) O::store1(row + c + j, y[nt][qt][j]);
-          }
+          for (unsigned j = 0; j < 4; ++j) O::store1(yb, c + j * (unsigned)sizeof(T) < y.width ? at + c + j * (unsigned)sizeof(T) : kNowhere, out[qt][j]);
         }
       }
     }
     if (r0 + C < last || (last == n && a.u_out != nullptr)) {
-      if (nr < C) {
-        key_weights<KS>(w, a2, nr, a.off, a.su, g);
-        gn = power(a2, nr);
-      }
-      update<T, C, D1, D2, NT>(U, t2, t3, w, gn, wave, lane);
+      update<T, C, D1, D2>(U, t2, t3, tw, nr < C ? power(a2, nr) : gC, wave, l);
       carried = true;
     }
   }
-  if (last != n || a.u_out == nullptr) return;
-  float* const uo = a.u_out + (long long)bh * a.d1 * a.d2;
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = 16 * kt + 4 * g, c = col0 + 16 * (wave * NT + nt) + l15;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (row + j < a.d1 && c < a.d2) uo[a.transposed ? (long long)c * a.d1 + row + j : (long long)(row + j) * a.d2 + c] = U[kt][nt][j];
-    }
+  if (last == n && a.u_out != nullptr) store_state<KT>(U, a.u_out + (long long)bh * a.d1 * a.d2, a.d1, a.d2, uc, lane >> 4);
 }
 
 template <typename T, int D1, int D2, bool VEC>
-__global__ __launch_bounds__(256) void k_decay_state(States A) {
+__global__ __launch_bounds__(4 * D2, state_waves(D1)) void k_decay_state(States A) {
   typedef Op<T> O;
-  constexpr int C = O::kChunk, KS = C / 32, NT = D2 / 64, KT = D1 / 16;
+  constexpr int C = O::kChunk, KT = D1 / 16, NTH = 4 * D2;
   extern __shared__ __attribute__((aligned(256))) char smem[];
   char* const t2 = smem;
   char* const t3 = t2 + C * D1 * (int)sizeof(T);
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, l15 = lane & 15, g = lane >> 4;
+  char* const tw = t3 + C * D2 * (int)sizeof(T);
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   State a = A.s[0];
   if (blockIdx.z == 1) a = A.s[1];
   const int segs = A.nseg - 1, bh = blockIdx.x / segs, seg = blockIdx.x % segs, b = bh / A.H, h = bh % A.H, col0 = blockIdx.y * D2;
   const int n = A.lengths != nullptr ? min(max(A.lengths[b], 0), A.L) : A.L;
-  const int begin = seg * A.seg_len, end = begin + A.seg_len;
+  const int begin = seg * A.seg_len, end = begin + A.seg_len, cols = min(a.d2 - col0, D2);
   if (end >= n) return;   // nothing follows
   const float a2 = decay_log2(A.log_decay, h);
-  const Rows<T> x2 = rows_of<T>(a.x2, b, h, A.H, A.L, a.d1, A.layout, a.reverse, n);
-  const Rows<T> x3 = rows_of<T>(a.x3, b, h, A.H, A.L, a.d2, A.layout, a.reverse, n);
-  Tile<T, C, D1, VEC> p2;
-  Tile<T, C, D2, VEC> p3;
-  p2.load(x2, begin, C, 0, a.d1, tid);
-  p3.load(x3, begin, C, col0, a.d2, tid);
-  f32x4 U[KT][NT];
+  const Rows x2 = rows_of<T>(a.x2, b, h, A.H, A.L, a.d1, A.layout, a.reverse, n, 0, a.d1);
+  const Rows x3 = rows_of<T>(a.x3, b, h, A.H, A.L, a.d2, A.layout, a.reverse, n, col0, cols);
+  Tile<T, C, D1, NTH, VEC> p2;
+  Tile<T, C, D2, NTH, VEC> p3;
+  p2.load(x2, begin, C, tid);
+  p3.load(x3, begin, C, tid);
+  f32x4 U[KT];
 #pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) U[kt][nt] = f32x4{0.f, 0.f, 0.f, 0.f};
-  float w[KS][8];
-  key_weights<KS>(w, a2, C, a.off, a.su, g);
-  const float gn = power(a2, C);
+  for (int kt = 0; kt < KT; ++kt) U[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+  put_weights<C>(tw, a2, C, a.off, a.su, tid);
+  const float gC = power(a2, C);
   for (int r0 = begin; r0 < end; r0 += C) {
     lds_barrier();
     p2.store(t2, tid);
     p3.store(t3, tid);
     lds_barrier();
     if (r0 + C < end) {
-      p2.load(x2, r0 + C, C, 0, a.d1, tid);
-      p3.load(x3, r0 + C, C, col0, a.d2, tid);
+      p2.load(x2, r0 + C, C, tid);
+      p3.load(x3, r0 + C, C, tid);
     }
-    update<T, C, D1, D2, NT>(U, t2, t3, w, gn, wave, lane);
+    update<T, C, D1, D2>(U, t2, t3, tw, gC, wave, fresh(lane));
   }
-  float* const uo = a.seg + ((long long)bh * A.nseg + seg) * a.d1 * a.d2;
-#pragma unroll
-  for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-      const int row = 16 * kt + 4 * g, c = col0 + 16 * (wave * NT + nt) + l15;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-        if (row + j < a.d1 && c < a.d2) uo[(long long)(row + j) * a.d2 + c] = U[kt][nt][j];
-    }
+  store_state<KT>(U, a.seg + ((long long)bh * A.nseg + seg) * a.d1 * a.d2, a.d1, a.d2, col0 + 16 * wave + (lane & 15), lane >> 4);
 }
 
 template <typename T, int D1, int D2, bool VEC>
@@ -451,7 +494,7 @@ static dark_status launch_scan(const Scans& a, int n, hipStream_t st) {
   constexpr int lds = scan_lds<T, D1, D2>();
   DARK_TRY(allow_lds(k_decay_scan<T, D1, D2, VEC>, lds));
   const dim3 grid((unsigned)((long long)a.B * a.H * a.nseg), (unsigned)((a.s[0].d2 + D2 - 1) / D2), (unsigned)n);
-  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_scan<T, D1, D2, VEC>), grid, dim3(256), lds, a);
+  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_scan<T, D1, D2, VEC>), grid, dim3(4 * D2), lds, a);
   return DARK_OK;
 }
 template <typename T, int D1, int D2, bool VEC>
@@ -459,7 +502,7 @@ static dark_status launch_state(const States& a, int n, hipStream_t st) {
   constexpr int lds = state_lds<T, D1, D2>();
   DARK_TRY(allow_lds(k_decay_state<T, D1, D2, VEC>, lds));
   const dim3 grid((unsigned)((long long)a.B * a.H * (a.nseg - 1)), (unsigned)((a.s[0].d2 + D2 - 1) / D2), (unsigned)n);
-  DARK_LAUNCH(KID_DECAY_STATE, st, (k_decay_state<T, D1, D2, VEC>), grid, dim3(256), lds, a);
+  DARK_LAUNCH(KID_DECAY_STATE, st, (k_decay_state<T, D1, D2, VEC>), grid, dim3(4 * D2), lds, a);
   return DARK_OK;
 }
 
