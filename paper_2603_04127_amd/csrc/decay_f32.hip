@@ -4,8 +4,8 @@
 namespace dark {
 namespace decay {
 
-dark_status launch_scan_f32(const Scans& a, int n, hipStream_t st) { DARK_DECAY_PICK(launch_scan, float, a, n, st); }
-dark_status launch_state_f32(const States& a, int n, hipStream_t st) { DARK_DECAY_PICK(launch_state, float, a, n, st); }
+dark_status launch_scan_f32(const Scans& a, int n, hipStream_t st) { return pick<float>(a, n, st); }
+dark_status launch_state_f32(const States& a, int n, hipStream_t st) { return pick<float>(a, n, st); }
 
 }  // namespace decay
 }  // namespace dark

@@ -2,9 +2,8 @@
 //
 // A workgroup of D2 / 16 waves walks the rows of a segment of one (b,h) in chunks of C rows, for a block of D2 columns of x3 and y.
 // The state U [D1, D2] stays in the accumulators of the products that update it: each wave owns 16 of its columns, and what it
-// owns serves the next chunk's readout as an operand without leaving the registers: an accumulator tile holds four consecutive
-// rows of a column in a lane, and as the order in which a product runs over its inner dimension is free as long as both operands
-// keep to it, two such tiles are one operand of 32, met by x1 rows that are read in the same order (`row_perm`).
+// owns serves the next chunk's readout as an operand without a way through LDS: an accumulator tile holds rows 4 g ... + 3 of a column in
+// lane group g, an operand of two such tiles wants rows 8 g ... + 7, and two exchanges between the lane groups make one of the other.
 // Per chunk: P = x1 x2^T, decayed and masked, by all waves together through LDS; y^T = U^T x1^T + x3^T P^T; U' = g^C U + x2^T (w x3).
 // The next chunk's rows are on their way into registers meanwhile.
 #pragma once
@@ -38,6 +37,15 @@ struct Lane {
 template <typename V>
 __device__ static inline V lds_get(const char* smem, int at) { return *reinterpret_cast<const V*>(smem + at); }
 
+// a: values of rows 4 g ... of a tile in lane group g, b: those of the tile below it.  Afterwards lane group g has rows 8 g ... in a
+// and 8 g + 4 ... in b (of the 32).
+__device__ static inline void spread(unsigned& a, unsigned& b) {
+  const auto h = __builtin_amdgcn_permlane32_swap(a, b, false, false);      // {a0, a1, b0, b1}, {a2, a3, b2, b3}
+  const auto q = __builtin_amdgcn_permlane16_swap(h[0], h[1], false, false);   // {a0, a2, b0, b2}, {a1, a3, b1, b3}
+  a = q[0];
+  b = q[1];
+}
+
 // Operands of a product over 32 values of the inner dimension: eight a lane, those of lane group g.
 template <typename T>
 struct Op;
@@ -54,13 +62,6 @@ struct Op<unsigned short> {
   template <int RB>
   __device__ static int row_base(Lane l) { return l.i * RB + ((l.g ^ swz<RB>(l.i)) << 4); }
   __device__ static frag row(const char* tile, int base, int k) { return lds_get<u32x4>(tile, base ^ (k << 6)); }
-  // values 32 k + 4 g ... + 3 and 32 k + 16 + 4 g ... + 3: the order of two accumulator tiles
-  template <int RB>
-  __device__ static int perm_base(Lane l) { return l.i * RB + (((l.g >> 1) ^ swz<RB>(l.i)) << 4) + 8 * (l.g & 1); }
-  __device__ static frag row_perm(const char* tile, int base, int k) {
-    const u32x2 a = lds_get<u32x2>(tile, base ^ (k << 6)), b = lds_get<u32x2>(tile, base ^ (k << 6) ^ 32);
-    return frag{a[0], a[1], b[0], b[1]};
-  }
   // rows 8 g ... + 7 (of 32) of column 16 t + i: the lane points at row 8 g + i / 4 (+ 4), columns 16 t + 4 (i % 4) ... + 3
   template <int RB>
   __device__ static int col_base(Lane l) {
@@ -75,10 +76,14 @@ struct Op<unsigned short> {
   }
   // Two accumulator tiles as an operand.  Rounded to bf16 once (2^-8 relative): the product goes into an output of that type.
   __device__ static frag state(f32x4 a, f32x4 b) {
-    return frag{pack_bf16(a[0], a[1]), pack_bf16(a[2], a[3]), pack_bf16(b[0], b[1]), pack_bf16(b[2], b[3])};
+    unsigned a0 = pack_bf16(a[0], a[1]), a1 = pack_bf16(a[2], a[3]), b0 = pack_bf16(b[0], b[1]), b1 = pack_bf16(b[2], b[3]);
+    spread(a0, b0);
+    spread(a1, b1);
+    return frag{a0, a1, b0, b1};
   }
-  // w x as the sum of three bf16 operands: the state is a 32-bit result, so its terms keep their 24 bits.  Cut off, not rounded: what
-  // is left behind eight leading bits, and again behind the next eight, is exact, and so is the sum of the three.
+  // w x as the sum of three bf16 operands: a state that is handed out is a 32-bit result, so its terms keep their 24 bits.  Cut off, not
+  // rounded: what is left behind eight leading bits, and again behind the next eight, is exact, and so is the sum of the three.  A
+  // state that only goes into outputs of 8 bits does without the third (16 bits).
   __device__ static void weighted(frag x, f32x4 w0, f32x4 w1, frag* out) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -94,7 +99,7 @@ struct Op<unsigned short> {
   }
   // four values of P: columns 16 kt + 4 g ... + 3 of row i
   template <int RB>
-  __device__ static int put_base(Lane l) { return perm_base<RB>(l); }
+  __device__ static int put_base(Lane l) { return l.i * RB + (((l.g >> 1) ^ swz<RB>(l.i)) << 4) + 8 * (l.g & 1); }
   __device__ static void put4(char* tile, int base, int kt, f32x4 v) {
     *reinterpret_cast<u32x2*>(tile + (base ^ (kt << 5))) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
   }
@@ -125,11 +130,6 @@ struct Op<float> {
     return frag{{lds_get<f32x4>(tile, base ^ (k << 7)), lds_get<f32x4>(tile, base ^ (k << 7) ^ 16)}};
   }
   template <int RB>
-  __device__ static int perm_base(Lane l) { return l.i * RB + ((l.g ^ swz<RB>(l.i)) << 4); }
-  __device__ static frag row_perm(const char* tile, int base, int k) {
-    return frag{{lds_get<f32x4>(tile, base ^ (k << 7)), lds_get<f32x4>(tile, base ^ (k << 7) ^ 64)}};
-  }
-  template <int RB>
   __device__ static int col_base(Lane l) { return 8 * l.g * RB + (((l.i >> 2) ^ swz<RB>(8 * l.g)) << 4) + 4 * (l.i & 3); }
   template <int RB>
   __device__ static frag col(const char* tile, int base, int t) {
@@ -138,13 +138,22 @@ struct Op<float> {
     for (int j = 0; j < 8; ++j) f.v[j >> 2][j & 3] = lds_get<float>(tile + j * RB, base ^ (t << 6) ^ (swz<RB>(j) << 4));
     return f;
   }
-  __device__ static frag state(f32x4 a, f32x4 b) { return frag{{a, b}}; }
+  __device__ static frag state(f32x4 a, f32x4 b) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      unsigned x = __float_as_uint(a[j]), y = __float_as_uint(b[j]);
+      spread(x, y);
+      a[j] = __uint_as_float(x);
+      b[j] = __uint_as_float(y);
+    }
+    return frag{{a, b}};
+  }
   __device__ static void weighted(const frag& x, f32x4 w0, f32x4 w1, frag* out) {
     out[0].v[0] = x.v[0] * w0;
     out[0].v[1] = x.v[1] * w1;
   }
   template <int RB>
-  __device__ static int put_base(Lane l) { return perm_base<RB>(l); }
+  __device__ static int put_base(Lane l) { return l.i * RB + ((l.g ^ swz<RB>(l.i)) << 4); }
   __device__ static void put4(char* tile, int base, int kt, f32x4 v) { *reinterpret_cast<f32x4*>(tile + (base ^ (kt << 6))) = v; }
   __device__ static void store4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, b, at, 0, 0);
@@ -267,18 +276,23 @@ __device__ static inline void put_weights(char* tw, float a2, int nr, int off, f
   if (tid < C) *reinterpret_cast<float*>(tw + 4 * tid) = tid < nr ? su * power(a2, max(nr - 1 - tid, 0) + off) : 0.f;
 }
 
-// U <- g^nr U + x2^T (w x3): the 16 columns of U that the wave owns.
-template <typename T, int C, int D1, int D2>
-__device__ static inline void update(f32x4 (&U)[D1 / 16], const char* t2, const char* t3, const char* tw, float gn, int wave, Lane l) {
+// Nothing is moved across: what one step has read is used up before the next step reads, so that 128 registers are enough.
+__device__ static inline void hold() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// U <- U + x2^T (f w x3): the 16 columns of U that the wave owns.
+template <typename T, int C, int D1, int D2, bool EXACT>
+__device__ static inline void update(f32x4 (&U)[D1 / 16], const char* t2, const char* t3, const char* tw, float f, int wave, Lane l) {
   typedef Op<T> O;
+  constexpr int kUsed = O::kPlanes == 3 && !EXACT ? 2 : O::kPlanes;
   constexpr int RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T);
   const int b2 = O::template col_base<RB1>(l), b3 = O::template col_base<RB2>(l);
 #pragma unroll
-  for (int kt = 0; kt < D1 / 16; ++kt) U[kt] *= gn;
-#pragma unroll
   for (int ks = 0; ks < C / 32; ++ks) {
     typename O::frag x[O::kPlanes];
-    const f32x4 w0 = lds_get<f32x4>(tw, 128 * ks + 32 * l.g), w1 = lds_get<f32x4>(tw, 128 * ks + 32 * l.g + 16);
+    const f32x4 w0 = f * lds_get<f32x4>(tw, 128 * ks + 32 * l.g), w1 = f * lds_get<f32x4>(tw, 128 * ks + 32 * l.g + 16);
     O::weighted(O::template col<RB2>(t3 + 32 * ks * RB2, b3, wave), w0, w1, x);
 #pragma unroll
     for (int k0 = 0; k0 < D1 / 16; k0 += 4) {   // four sums at a time: a product does not wait for the one before it
@@ -286,16 +300,16 @@ __device__ static inline void update(f32x4 (&U)[D1 / 16], const char* t2, const 
 #pragma unroll
       for (int i = 0; i < 4; ++i) k[i] = O::template col<RB1>(t2 + 32 * ks * RB1, b2, k0 + i);
 #pragma unroll
-      for (int p = O::kPlanes - 1; p >= 0; --p)   // the smallest terms first
+      for (int p = kUsed - 1; p >= 0; --p)   // the smallest terms first
 #pragma unroll
         for (int i = 0; i < 4; ++i) U[k0 + i] = O::mma(k[i], x[p], U[k0 + i]);
-      __builtin_amdgcn_sched_barrier(0);
+      hold();
     }
   }
 }
 
 template <typename T, int D1, int D2>
-constexpr int scan_lds() { return Op<T>::kChunk * ((2 * D1 + D2 + Op<T>::kChunk) * (int)sizeof(T) + 4); }
+constexpr int scan_lds() { return Op<T>::kChunk * ((2 * D1 + D2 + Op<T>::kChunk) * (int)sizeof(T) + 12) + 64; }
 template <typename T, int D1, int D2>
 constexpr int state_lds() { return Op<T>::kChunk * ((D1 + D2) * (int)sizeof(T) + 4); }
 
@@ -309,7 +323,7 @@ __device__ static inline Lane fresh(int lane) {
   return {lane & 15, lane >> 4};
 }
 
-template <typename T, int D1, int D2, bool VEC>
+template <typename T, int D1, int D2, bool VEC, bool EXACT>
 __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans A) {
   typedef Op<T> O;
   constexpr int C = O::kChunk, QT = C / 16, KS = C / 32, KT = D1 / 16, K1 = D1 / 32, W = D2 / 16, NTH = 64 * W;
@@ -320,6 +334,8 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
   char* const t3 = t2 + C * RB1;
   char* const tp = t3 + C * RB2;
   char* const tw = tp + C * RBP;
+  char* const tl = tw + 4 * C;   // sr g^(r+1-off) of the chunk's rows
+  char* const td = tl + 4 * C;   // sp g^(n - 15), n = 0 ... C + 14 (what stands before g^0 is not used)
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   Scan a = A.s[0];
   if (blockIdx.z == 1) a = A.s[1];
@@ -350,9 +366,8 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
   // the state: rows 16 kt + 4 g ... + 3 of column col0 + 16 wave + lane % 16
   f32x4 U[KT];
   const long long uat = (A.nseg > 1 ? (long long)bh * A.nseg + seg : bh) * a.d1 * a.d2;
-  bool carried = a.u_in != nullptr;
   const int uc = col0 + 16 * wave + (lane & 15);
-  if (carried) {
+  if (a.u_in != nullptr) {
     load_state<KT, VEC>(U, a.u_in + uat, a.d1, a.d2, a.transposed, uc, lane >> 4);
   } else {
 #pragma unroll
@@ -361,9 +376,8 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
   // Tiles of P above the diagonal that a product over 32 keys reads: zero from here on, never written again.
   for (int e = tid; e < C * RBP / 16; e += NTH) *reinterpret_cast<u32x4*>(tp + 16 * e) = u32x4{0, 0, 0, 0};
   put_weights<C>(tw, a2, C, a.off, a.su, tid);
-  float lead[QT];   // sr g^(r+1-off) of the lane's rows
-#pragma unroll
-  for (int qt = 0; qt < QT; ++qt) lead[qt] = a.sr * power(a2, 16 * qt + (lane & 15) + 1 - a.off);
+  if (tid < C + 15) *reinterpret_cast<float*>(td + 4 * tid) = a.sp * power(a2, max(tid - 15, 0));
+  if (tid < C) *reinterpret_cast<float*>(tl + 4 * tid) = a.sr * power(a2, tid + 1 - a.off);
   const float gC = power(a2, C);
 
   for (int r0 = begin; r0 < last; r0 += C) {
@@ -388,33 +402,30 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
       const int t = wave + W * i;
       if (t < QT * (QT + 1) / 2) {
         const int qt = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, kt = t - qt * (qt + 1) / 2;
-        f32x4 s = {0.f, 0.f, 0.f, 0.f};
+        f32x4 s;
 #pragma unroll
-        for (int k = 0; k < K1; ++k) s = O::mma(O::row(t2 + kt * 16 * RB1, b1, k), O::row(t1 + qt * 16 * RB1, b1, k), s);
+        for (int k = 0; k < K1; ++k) s = O::mma(O::row(t2 + kt * 16 * RB1, b1, k), O::row(t1 + qt * 16 * RB1, b1, k), k > 0 ? s : f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int apart = 16 * (qt - kt) + l.i - 4 * l.g - j;
-          s[j] = apart >= 0 ? s[j] * (a.sp * power(a2, max(apart, 0))) : 0.f;
+        for (int j = 0; j < 4; ++j) s[j] *= lds_get<float>(td + 64 * (qt - kt) + 4 * (3 - j), 4 * (l.i - 4 * l.g + 12));
+        if (qt == kt) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) s[j] = l.i - 4 * l.g - j >= 0 ? s[j] : 0.f;
         }
         O::put4(tp + qt * 16 * RBP, O::template put_base<RBP>(l), kt, s);
-        __builtin_amdgcn_sched_barrier(0);
+        hold();
       }
     }
     f32x4 out[QT];
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) out[qt] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (carried) {
-      const int bp = O::template perm_base<RB1>(l);
+    for (int k = 0; k < K1; ++k) {
+      const typename O::frag u = O::state(U[2 * k], U[2 * k + 1]);
 #pragma unroll
-      for (int k = 0; k < K1; ++k) {
-        const typename O::frag u = O::state(U[2 * k], U[2 * k + 1]);
-#pragma unroll
-        for (int qt = 0; qt < QT; ++qt) out[qt] = O::mma(u, O::row_perm(t1 + qt * 16 * RB1, bp, k), out[qt]);
-        __builtin_amdgcn_sched_barrier(0);
-      }
-#pragma unroll
-      for (int qt = 0; qt < QT; ++qt) out[qt] *= lead[qt];
+      for (int qt = 0; qt < QT; ++qt)
+        out[qt] = O::mma(u, O::row(t1 + qt * 16 * RB1, b1, k), k > 0 ? out[qt] : f32x4{0.f, 0.f, 0.f, 0.f});
+      hold();
     }
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) out[qt] *= lds_get<float>(tl + 64 * qt, 4 * l.i);
     lds_barrier();   // P is there
     {
       const int b3 = O::template col_base<RB2>(l), bp = O::template row_base<RBP>(l);
@@ -423,7 +434,7 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
         const typename O::frag v = O::template col<RB2>(t3 + 32 * ks * RB2, b3, wave);
 #pragma unroll
         for (int qt = 2 * ks; qt < QT; ++qt) out[qt] = O::mma(v, O::row(tp + qt * 16 * RBP, bp, ks), out[qt]);
-        __builtin_amdgcn_sched_barrier(0);
+        hold();
       }
     }
     if (a.y != nullptr) {
@@ -441,14 +452,16 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
       }
     }
     if (r0 + C < last || (last == n && a.u_out != nullptr)) {
-      update<T, C, D1, D2>(U, t2, t3, tw, nr < C ? power(a2, nr) : gC, wave, l);
-      carried = true;
+      const float gn = nr < C ? power(a2, nr) : gC;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) U[kt] *= gn;
+      update<T, C, D1, D2, EXACT>(U, t2, t3, tw, 1.f, wave, l);
     }
   }
   if (last == n && a.u_out != nullptr) store_state<KT>(U, a.u_out + (long long)bh * a.d1 * a.d2, a.d1, a.d2, uc, lane >> 4);
 }
 
-template <typename T, int D1, int D2, bool VEC>
+template <typename T, int D1, int D2, bool VEC, bool EXACT>
 __global__ __launch_bounds__(4 * D2, state_waves(D1)) void k_decay_state(States A) {
   typedef Op<T> O;
   constexpr int C = O::kChunk, KT = D1 / 16, NTH = 4 * D2;
@@ -468,56 +481,61 @@ __global__ __launch_bounds__(4 * D2, state_waves(D1)) void k_decay_state(States 
   const Rows x3 = rows_of<T>(a.x3, b, h, A.H, A.L, a.d2, A.layout, a.reverse, n, col0, cols);
   Tile<T, C, D1, NTH, VEC> p2;
   Tile<T, C, D2, NTH, VEC> p3;
-  p2.load(x2, begin, C, tid);
-  p3.load(x3, begin, C, tid);
+  // From the segment's end to its beginning, where the scan starts: what was read last is still in the memory-side cache then.
+  p2.load(x2, end - C, C, tid);
+  p3.load(x3, end - C, C, tid);
   f32x4 U[KT];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) U[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
   put_weights<C>(tw, a2, C, a.off, a.su, tid);
-  const float gC = power(a2, C);
-  for (int r0 = begin; r0 < end; r0 += C) {
+  for (int r0 = end - C; r0 >= begin; r0 -= C) {
     lds_barrier();
     p2.store(t2, tid);
     p3.store(t3, tid);
     lds_barrier();
-    if (r0 + C < end) {
-      p2.load(x2, r0 + C, C, tid);
-      p3.load(x3, r0 + C, C, tid);
+    if (r0 > begin) {
+      p2.load(x2, r0 - C, C, tid);
+      p3.load(x3, r0 - C, C, tid);
     }
-    update<T, C, D1, D2>(U, t2, t3, tw, gC, wave, fresh(lane));
+    update<T, C, D1, D2, EXACT>(U, t2, t3, tw, power(a2, end - C - r0), wave, fresh(lane));
   }
   store_state<KT>(U, a.seg + ((long long)bh * A.nseg + seg) * a.d1 * a.d2, a.d1, a.d2, col0 + 16 * wave + (lane & 15), lane >> 4);
 }
 
-template <typename T, int D1, int D2, bool VEC>
-static dark_status launch_scan(const Scans& a, int n, hipStream_t st) {
+template <typename T, int D1, int D2, bool VEC, bool EXACT>
+static dark_status launch(const Scans& a, int n, hipStream_t st) {
   constexpr int lds = scan_lds<T, D1, D2>();
-  DARK_TRY(allow_lds(k_decay_scan<T, D1, D2, VEC>, lds));
+  DARK_TRY(allow_lds(k_decay_scan<T, D1, D2, VEC, EXACT>, lds));
   const dim3 grid((unsigned)((long long)a.B * a.H * a.nseg), (unsigned)((a.s[0].d2 + D2 - 1) / D2), (unsigned)n);
-  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_scan<T, D1, D2, VEC>), grid, dim3(4 * D2), lds, a);
+  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_scan<T, D1, D2, VEC, EXACT>), grid, dim3(4 * D2), lds, a);
   return DARK_OK;
 }
-template <typename T, int D1, int D2, bool VEC>
-static dark_status launch_state(const States& a, int n, hipStream_t st) {
+template <typename T, int D1, int D2, bool VEC, bool EXACT>
+static dark_status launch(const States& a, int n, hipStream_t st) {
   constexpr int lds = state_lds<T, D1, D2>();
-  DARK_TRY(allow_lds(k_decay_state<T, D1, D2, VEC>, lds));
+  DARK_TRY(allow_lds(k_decay_state<T, D1, D2, VEC, EXACT>, lds));
   const dim3 grid((unsigned)((long long)a.B * a.H * (a.nseg - 1)), (unsigned)((a.s[0].d2 + D2 - 1) / D2), (unsigned)n);
-  DARK_LAUNCH(KID_DECAY_STATE, st, (k_decay_state<T, D1, D2, VEC>), grid, dim3(4 * D2), lds, a);
+  DARK_LAUNCH(KID_DECAY_STATE, st, (k_decay_state<T, D1, D2, VEC, EXACT>), grid, dim3(4 * D2), lds, a);
   return DARK_OK;
 }
 
 // The instance that holds d1 inner values, with 64 columns a workgroup where x3 has no more (or the state of 256 x 128 would take
 // half of the registers), else 128.
-#define DARK_DECAY_PICK(what, T, a, n, st)                                                                  \
-  do {                                                                                                      \
-    const int d1 = (a).s[0].d1, d2 = (a).s[0].d2;                                                           \
-    const bool vec = d1 * (int)sizeof(T) % 16 == 0 && d2 * (int)sizeof(T) % 16 == 0;                        \
-    if (d1 <= 64 && d2 <= 64) return vec ? what<T, 64, 64, true>(a, n, st) : what<T, 64, 64, false>(a, n, st);      \
-    if (d1 <= 64) return vec ? what<T, 64, 128, true>(a, n, st) : what<T, 64, 128, false>(a, n, st);        \
-    if (d1 <= 128 && d2 <= 64) return vec ? what<T, 128, 64, true>(a, n, st) : what<T, 128, 64, false>(a, n, st);   \
-    if (d1 <= 128) return vec ? what<T, 128, 128, true>(a, n, st) : what<T, 128, 128, false>(a, n, st);     \
-    return vec ? what<T, 256, 64, true>(a, n, st) : what<T, 256, 64, false>(a, n, st);                      \
-  } while (0)
+template <typename T, int D1, int D2, typename A>
+static dark_status pick(const A& a, int n, hipStream_t st) {
+  const bool vec = a.s[0].d1 * sizeof(T) % 16 == 0 && a.s[0].d2 * sizeof(T) % 16 == 0;
+  if constexpr (Op<T>::kPlanes == 3) {
+    if (a.exact) return vec ? launch<T, D1, D2, true, true>(a, n, st) : launch<T, D1, D2, false, true>(a, n, st);
+  }
+  return vec ? launch<T, D1, D2, true, false>(a, n, st) : launch<T, D1, D2, false, false>(a, n, st);
+}
+template <typename T, typename A>
+static dark_status pick(const A& a, int n, hipStream_t st) {
+  const int d1 = a.s[0].d1, d2 = a.s[0].d2;
+  if (d1 > 128) return pick<T, 256, 64>(a, n, st);
+  if (d1 > 64) return d2 <= 64 ? pick<T, 128, 64>(a, n, st) : pick<T, 128, 128>(a, n, st);
+  return d2 <= 64 ? pick<T, 64, 64>(a, n, st) : pick<T, 64, 128>(a, n, st);
+}
 
 }  // namespace decay
 }  // namespace dark
