@@ -34,8 +34,18 @@ struct Lane {
   int i, g;   // lane % 16, lane / 16
 };
 
+// LDS by its address.  These kernels have dynamic LDS alone, which begins at 0; by way of a pointer to it the compiler adds that
+// 0 to every address, a sixth of the scan's vector instructions.
 template <typename V>
-__device__ static inline V lds_get(const char* smem, int at) { return *reinterpret_cast<const V*>(smem + at); }
+using Lds = __attribute__((address_space(3))) V;
+template <typename V>
+__device__ static inline V lds_get(int at) { return *reinterpret_cast<const Lds<V>*>((unsigned)at); }
+template <typename V>
+__device__ static inline void lds_put(int at, V v) { *reinterpret_cast<Lds<V>*>((unsigned)at) = v; }
+__device__ static inline u32x2 lds_get_tr16(int at) {
+  const s16x4 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(reinterpret_cast<Lds<s16x4>*>((unsigned)at));
+  return *reinterpret_cast<const u32x2*>(&v);
+}
 
 // a: values of rows 4 g ... of a tile in lane group g, b: those of the tile below it.  Afterwards lane group g has rows 8 g ... in a
 // and 8 g + 4 ... in b (of the 32).
@@ -61,7 +71,7 @@ struct Op<unsigned short> {
   // values 32 k + 8 g ... + 7 of row i of 16
   template <int RB>
   __device__ static int row_base(Lane l) { return l.i * RB + ((l.g ^ swz<RB>(l.i)) << 4); }
-  __device__ static frag row(const char* tile, int base, int k) { return lds_get<u32x4>(tile, base ^ (k << 6)); }
+  __device__ static frag row(int tile, int base, int k) { return lds_get<u32x4>(tile + (base ^ (k << 6))); }
   // rows 8 g ... + 7 (of 32) of column 16 t + i: the lane points at row 8 g + i / 4 (+ 4), columns 16 t + 4 (i % 4) ... + 3
   template <int RB>
   __device__ static int col_base(Lane l) {
@@ -69,9 +79,8 @@ struct Op<unsigned short> {
     return r * RB + ((((l.i >> 1) & 1) ^ swz<RB>(r)) << 4) + 8 * (l.i & 1);
   }
   template <int RB>
-  __device__ static frag col(const char* tile, int base, int t) {
-    const u32x2 a = lds_read_tr16(reinterpret_cast<const unsigned short*>(tile + (base ^ (t << 5))));
-    const u32x2 b = lds_read_tr16(reinterpret_cast<const unsigned short*>(tile + 4 * RB + (base ^ (t << 5) ^ (swz<RB>(4) << 4))));
+  __device__ static frag col(int tile, int base, int t) {
+    const u32x2 a = lds_get_tr16(tile + (base ^ (t << 5))), b = lds_get_tr16(tile + 4 * RB + (base ^ (t << 5) ^ (swz<RB>(4) << 4)));
     return frag{a[0], a[1], b[0], b[1]};
   }
   // Two accumulator tiles as an operand.  Rounded to bf16 once (2^-8 relative): the product goes into an output of that type.
@@ -100,8 +109,8 @@ struct Op<unsigned short> {
   // four values of P: columns 16 kt + 4 g ... + 3 of row i
   template <int RB>
   __device__ static int put_base(Lane l) { return l.i * RB + (((l.g >> 1) ^ swz<RB>(l.i)) << 4) + 8 * (l.g & 1); }
-  __device__ static void put4(char* tile, int base, int kt, f32x4 v) {
-    *reinterpret_cast<u32x2*>(tile + (base ^ (kt << 5))) = u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+  __device__ static void put4(int tile, int base, int kt, f32x4 v) {
+    lds_put(tile + (base ^ (kt << 5)), u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])});
   }
   __device__ static void store4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, b, at, 0, 0);
@@ -126,16 +135,16 @@ struct Op<float> {
   }
   template <int RB>
   __device__ static int row_base(Lane l) { return l.i * RB + (((2 * l.g) ^ swz<RB>(l.i)) << 4); }
-  __device__ static frag row(const char* tile, int base, int k) {
-    return frag{{lds_get<f32x4>(tile, base ^ (k << 7)), lds_get<f32x4>(tile, base ^ (k << 7) ^ 16)}};
+  __device__ static frag row(int tile, int base, int k) {
+    return frag{{lds_get<f32x4>(tile + (base ^ (k << 7))), lds_get<f32x4>(tile + (base ^ (k << 7) ^ 16))}};
   }
   template <int RB>
   __device__ static int col_base(Lane l) { return 8 * l.g * RB + (((l.i >> 2) ^ swz<RB>(8 * l.g)) << 4) + 4 * (l.i & 3); }
   template <int RB>
-  __device__ static frag col(const char* tile, int base, int t) {
+  __device__ static frag col(int tile, int base, int t) {
     frag f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f.v[j >> 2][j & 3] = lds_get<float>(tile + j * RB, base ^ (t << 6) ^ (swz<RB>(j) << 4));
+    for (int j = 0; j < 8; ++j) f.v[j >> 2][j & 3] = lds_get<float>(tile + j * RB + (base ^ (t << 6) ^ (swz<RB>(j) << 4)));
     return f;
   }
   __device__ static frag state(f32x4 a, f32x4 b) {
@@ -154,7 +163,7 @@ struct Op<float> {
   }
   template <int RB>
   __device__ static int put_base(Lane l) { return l.i * RB + ((l.g ^ swz<RB>(l.i)) << 4); }
-  __device__ static void put4(char* tile, int base, int kt, f32x4 v) { *reinterpret_cast<f32x4*>(tile + (base ^ (kt << 6))) = v; }
+  __device__ static void put4(int tile, int base, int kt, f32x4 v) { lds_put(tile + (base ^ (kt << 6)), v); }
   __device__ static void store4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, b, at, 0, 0);
   }
@@ -223,11 +232,11 @@ struct Tile {
       }
     }
   }
-  __device__ void store(char* tile, int tid) const {
+  __device__ void store(int tile, int tid) const {
     const int row0 = tid / kPieces, base = row0 * RB + (((tid % kPieces) ^ swz<RB>(row0)) << 4);
     // kStep is a power of two and row0 below it: further rows are one xor with a constant away
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) *reinterpret_cast<u32x4*>(tile + i * kStep * RB + (base ^ (swz<RB>((i * kStep) & 15) << 4))) = r[i];
+    for (int i = 0; i < kEach; ++i) lds_put(tile + i * kStep * RB + (base ^ (swz<RB>((i * kStep) & 15) << 4)), r[i]);
   }
 };
 
@@ -272,8 +281,8 @@ __device__ static inline float power(float a2, int n) { return fast_exp2(a2 * (f
 
 // Weights su g^(nr-1-key+off) of the chunk's keys, 0 behind the last row: C floats in LDS.
 template <int C>
-__device__ static inline void put_weights(char* tw, float a2, int nr, int off, float su, int tid) {
-  if (tid < C) *reinterpret_cast<float*>(tw + 4 * tid) = tid < nr ? su * power(a2, max(nr - 1 - tid, 0) + off) : 0.f;
+__device__ static inline void put_weights(int tw, float a2, int nr, int off, float su, int tid) {
+  if (tid < C) lds_put(tw + 4 * tid, tid < nr ? su * power(a2, max(nr - 1 - tid, 0) + off) : 0.f);
 }
 
 // Nothing is moved across: what one step has read is used up before the next step reads, so that 128 registers are enough.
@@ -284,7 +293,7 @@ __device__ static inline void hold() {
 
 // U <- U + x2^T (f w x3): the 16 columns of U that the wave owns.
 template <typename T, int C, int D1, int D2, bool EXACT>
-__device__ static inline void update(f32x4 (&U)[D1 / 16], const char* t2, const char* t3, const char* tw, float f, int wave, Lane l) {
+__device__ static inline void update(f32x4 (&U)[D1 / 16], int t2, int t3, int tw, float f, int wave, Lane l) {
   typedef Op<T> O;
   constexpr int kUsed = O::kPlanes == 3 && !EXACT ? 2 : O::kPlanes;
   constexpr int RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T);
@@ -292,7 +301,7 @@ __device__ static inline void update(f32x4 (&U)[D1 / 16], const char* t2, const 
 #pragma unroll
   for (int ks = 0; ks < C / 32; ++ks) {
     typename O::frag x[O::kPlanes];
-    const f32x4 w0 = f * lds_get<f32x4>(tw, 128 * ks + 32 * l.g), w1 = f * lds_get<f32x4>(tw, 128 * ks + 32 * l.g + 16);
+    const f32x4 w0 = f * lds_get<f32x4>(tw + 128 * ks + 32 * l.g), w1 = f * lds_get<f32x4>(tw + 128 * ks + 32 * l.g + 16);
     O::weighted(O::template col<RB2>(t3 + 32 * ks * RB2, b3, wave), w0, w1, x);
 #pragma unroll
     for (int k0 = 0; k0 < D1 / 16; k0 += 4) {   // four sums at a time: a product does not wait for the one before it
@@ -328,14 +337,9 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
   typedef Op<T> O;
   constexpr int C = O::kChunk, QT = C / 16, KS = C / 32, KT = D1 / 16, K1 = D1 / 32, W = D2 / 16, NTH = 64 * W;
   constexpr int RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T), RBP = C * (int)sizeof(T);
-  extern __shared__ __attribute__((aligned(256))) char smem[];
-  char* const t1 = smem;
-  char* const t2 = t1 + C * RB1;
-  char* const t3 = t2 + C * RB1;
-  char* const tp = t3 + C * RB2;
-  char* const tw = tp + C * RBP;
-  char* const tl = tw + 4 * C;   // sr g^(r+1-off) of the chunk's rows
-  char* const td = tl + 4 * C;   // sp g^(n - 15), n = 0 ... C + 14 (what stands before g^0 is not used)
+  constexpr int t1 = 0, t2 = t1 + C * RB1, t3 = t2 + C * RB1, tp = t3 + C * RB2, tw = tp + C * RBP;
+  constexpr int tl = tw + 4 * C;   // sr g^(r+1-off) of the chunk's rows
+  constexpr int td = tl + 4 * C;   // sp g^(n - 15), n = 0 ... C + 14 (what stands before g^0 is not used)
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   Scan a = A.s[0];
   if (blockIdx.z == 1) a = A.s[1];
@@ -374,10 +378,10 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
     for (int kt = 0; kt < KT; ++kt) U[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   // Tiles of P above the diagonal that a product over 32 keys reads: zero from here on, never written again.
-  for (int e = tid; e < C * RBP / 16; e += NTH) *reinterpret_cast<u32x4*>(tp + 16 * e) = u32x4{0, 0, 0, 0};
+  for (int e = tid; e < C * RBP / 16; e += NTH) lds_put(tp + 16 * e, u32x4{0, 0, 0, 0});
   put_weights<C>(tw, a2, C, a.off, a.su, tid);
-  if (tid < C + 15) *reinterpret_cast<float*>(td + 4 * tid) = a.sp * power(a2, max(tid - 15, 0));
-  if (tid < C) *reinterpret_cast<float*>(tl + 4 * tid) = a.sr * power(a2, tid + 1 - a.off);
+  if (tid < C + 15) lds_put(td + 4 * tid, a.sp * power(a2, max(tid - 15, 0)));
+  if (tid < C) lds_put(tl + 4 * tid, a.sr * power(a2, tid + 1 - a.off));
   const float gC = power(a2, C);
 
   for (int r0 = begin; r0 < last; r0 += C) {
@@ -406,7 +410,7 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
 #pragma unroll
         for (int k = 0; k < K1; ++k) s = O::mma(O::row(t2 + kt * 16 * RB1, b1, k), O::row(t1 + qt * 16 * RB1, b1, k), k > 0 ? s : f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] *= lds_get<float>(td + 64 * (qt - kt) + 4 * (3 - j), 4 * (l.i - 4 * l.g + 12));
+        for (int j = 0; j < 4; ++j) s[j] *= lds_get<float>(td + 64 * (qt - kt) + 4 * (3 - j) + 4 * (l.i - 4 * l.g + 12));
         if (qt == kt) {
 #pragma unroll
           for (int j = 0; j < 4; ++j) s[j] = l.i - 4 * l.g - j >= 0 ? s[j] : 0.f;
@@ -425,7 +429,7 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
       hold();
     }
 #pragma unroll
-    for (int qt = 0; qt < QT; ++qt) out[qt] *= lds_get<float>(tl + 64 * qt, 4 * l.i);
+    for (int qt = 0; qt < QT; ++qt) out[qt] *= lds_get<float>(tl + 64 * qt + 4 * l.i);
     lds_barrier();   // P is there
     {
       const int b3 = O::template col_base<RB2>(l), bp = O::template row_base<RBP>(l);
@@ -465,10 +469,7 @@ template <typename T, int D1, int D2, bool VEC, bool EXACT>
 __global__ __launch_bounds__(4 * D2, state_waves(D1)) void k_decay_state(States A) {
   typedef Op<T> O;
   constexpr int C = O::kChunk, KT = D1 / 16, NTH = 4 * D2;
-  extern __shared__ __attribute__((aligned(256))) char smem[];
-  char* const t2 = smem;
-  char* const t3 = t2 + C * D1 * (int)sizeof(T);
-  char* const tw = t3 + C * D2 * (int)sizeof(T);
+  constexpr int t2 = 0, t3 = t2 + C * D1 * (int)sizeof(T), tw = t3 + C * D2 * (int)sizeof(T);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   State a = A.s[0];
   if (blockIdx.z == 1) a = A.s[1];
