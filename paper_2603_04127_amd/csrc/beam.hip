@@ -3,8 +3,8 @@
 //
 // Selection, per batch entry with n beams: candidate (j, t) is worth score_j + logit_jt - log sum_u exp logit_ju; the n largest win,
 // equal ones by the lowest j, then the lowest t.  k_beam_rows reads every logit once: a workgroup takes a slice of a row and leaves
-// the slice's maximum, its sum of exponentials and, wave by wave, the n largest logits in order.  k_beam_pick joins the sums of a
-// batch entry's rows and merges the sorted lists from their heads.  Bound by reading the logits; few rows are cut into more slices.
+// the slice's maximum, its sum of exponentials and its n largest logits in order.  k_beam_pick joins the sums of a batch entry's
+// rows and merges the sorted lists from their heads.  Bound by reading the logits; few rows are cut into more slices.
 // Two candidates of different beams may lie closer together than fp32 resolves: offsets and comparisons are in fp64.
 #include <cmath>
 
@@ -32,7 +32,12 @@ __device__ __forceinline__ unsigned ordered(float v) {
 }
 __device__ __forceinline__ float value_of(unsigned k) { return __uint_as_float(k & 0x80000000u ? k ^ 0x80000000u : ~k); }
 
-__device__ __forceinline__ float clean(float v) { return v != v ? -INFINITY : v == 0.f ? 0.f : v; }   // one zero
+// The same for doubles that are numbers or -infinity.
+__device__ __forceinline__ u64 ordered64(double v) {
+  const u64 u = (u64)__double_as_longlong(v);
+  return u >> 63 ? ~u : u | 0x8000000000000000ull;
+}
+__device__ __forceinline__ double value64(u64 k) { return __longlong_as_double((long long)(k >> 63 ? k ^ 0x8000000000000000ull : ~k)); }
 
 // Largest key of the wave.
 template <int CTRL>
@@ -55,249 +60,375 @@ __device__ __forceinline__ unsigned wave_max(unsigned v) {
 __device__ __forceinline__ bool finite(float v) { return v > -INFINITY && v < INFINITY; }
 
 constexpr int kMostBeams = 32;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// The first `count` lanes of a wave hold a candidate each: every one counts those before it (larger, or equal with a lower token) and
+// takes that place in the list if it is one of the n.  Token -1 behind the last.
+__device__ __forceinline__ void place(unsigned key, int token, int count, Entry* list, int n, int lane) {
+  const u64 own = (u64)key << 32 | (unsigned)~token;
+  int before = 0;
+  for (int i = 0; i < count; ++i) {
+    const u64 other = (u64)__builtin_amdgcn_readlane(key, i) << 32 | (unsigned)~__builtin_amdgcn_readlane(token, i);
+    before += other > own;
+  }
+  if (lane < count && before < n) list[before] = Entry{value_of(key), token};
+  if (lane == 0 && count < n) list[count] = Entry{0.f, -1};
+}
+
+// The n-th largest of the lanes' values.
+__device__ __forceinline__ unsigned nth_of_lanes(unsigned v, int n, int lane) {
+  unsigned w = 0;
+  for (int i = 0; i < n; ++i) {
+    w = wave_max(v);
+    if (lane == __builtin_ctzll(__ballot(v == w))) v = 0;
+  }
+  return w;
+}
+
+// The element of row-relative index t, as a number that may win: NaN where there is none.
+template <typename T>
+__device__ __forceinline__ float number(const T* row, long long t, int V) {
+  if (t < 0 || t >= V) return NAN;
+  if constexpr (sizeof(T) == 2) return __uint_as_float((unsigned)row[t] << 16);
+  else return row[t];
+}
 
 // A slice is 256 E elements of a row; thread t holds pieces t, t + 256, ... of 16 bytes.  Rows begin where they begin: the slices
-// count from the 16-byte boundary at or before the row's first element.
+// count from the 16-byte boundary at or before the row's first element.  Elements that are not the row's are NaN: like a NaN among
+// the logits they lose every comparison.  Lists hold what is larger than -infinity.
+// A wave's n largest: the n-th largest of its lanes' maxima bounds them from below, so that a comparison each is all that most
+// elements cost; the few that pass are compacted into one a lane and placed.  Where more than 64 pass (many equal ones, or the largest
+// in few lanes) they are looked for one after the other in memory.
+// (32 x 8 rows of 131,071, n = 8: 70 us when every wave took its largest out one by one.)
+constexpr int kMostPassed = 64;
 template <typename T, int E>
-__global__ __launch_bounds__(256) void k_beam_rows(const T* __restrict__ logits, const float* __restrict__ scores,
-                                                   const unsigned char* __restrict__ finished, Part* __restrict__ parts,
-                                                   Entry* __restrict__ lists, int n, int V, long long total) {
+__global__ __launch_bounds__(256, 4) void k_beam_rows(const T* __restrict__ logits, const float* __restrict__ scores,
+                                                      const unsigned char* __restrict__ finished, Part* __restrict__ parts,
+                                                      Entry* __restrict__ lists, int n, int V, long long total) {
   constexpr int P = 16 / (int)sizeof(T), N = E / P;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, slice = blockIdx.x, slices = gridDim.x, row = blockIdx.y;
   if ((finished != nullptr && finished[row] != 0) || !finite(scores[row])) return;   // k_beam_pick knows what these offer
   const long long first = (long long)row * V, base = first / P * P + (long long)slice * 256 * E;
-  unsigned key[E];
+  const long long whole = total / P * P;   // behind it: an unfinished piece, which is read element by element
+  const T* const own = logits + first;
+  const int begin = (int)(base - first);   // token of the slice's first element
+  u32x4 r[N];
+  if (base + 256 * E <= whole) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const long long at = base + (long long)(i * 256 + tid) * P;
-    T v[P];
-    if (at + P <= total) {
-      const u32x4 r = *reinterpret_cast<const u32x4*>(logits + at);
-      __builtin_memcpy(v, &r, 16);
-    } else {
+    for (int i = 0; i < N; ++i) r[i] = *reinterpret_cast<const u32x4*>(logits + base + (i * 256 + tid) * P);
+  } else {   // the tensor's end
 #pragma unroll
-      for (int j = 0; j < P; ++j) v[j] = at + j < total ? logits[at + j] : (T)0;
-    }
+    for (int i = 0; i < N; ++i) {
+      const long long at = base + (i * 256 + tid) * P;
+      r[i] = u32x4{0, 0, 0, 0};
+      if (at < whole) {
+        r[i] = *reinterpret_cast<const u32x4*>(logits + at);
+      } else if (at < total) {
+        T e[P];
 #pragma unroll
-    for (int j = 0; j < P; ++j) {
-      float f;
-      if constexpr (sizeof(T) == 2) f = __uint_as_float((unsigned)v[j] << 16);
-      else f = v[j];
-      const long long t = at + j - first;
-      key[i * P + j] = t >= 0 && t < V ? ordered(clean(f)) : 0u;
+        for (int j = 0; j < P; ++j) e[j] = at + j < total ? logits[at + j] : (T)0;
+        __builtin_memcpy(&r[i], e, 16);
+      }
     }
   }
-  // maximum and sum of exponentials
-  unsigned best = 0;
+  float v[E];
 #pragma unroll
-  for (int e = 0; e < E; ++e) best = key[e] > best ? key[e] : best;
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      if constexpr (sizeof(T) == 2) v[i * P + j] = __uint_as_float(j & 1 ? r[i][j / 2] & 0xffff0000u : r[i][j / 2] << 16);
+      else v[i * P + j] = __uint_as_float(r[i][j]);
+    }
+  if (begin < 0 || begin + 256 * E > V) {   // the row's ends
+    int t0 = begin + tid * P;
+    asm volatile("" : "+v"(t0));   // nothing is computed ahead for the slices within
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int t = t0 + e / P * 256 * P + e % P;
+      v[e] = (unsigned)t < (unsigned)V ? v[e] : NAN;
+    }
+  }
+  // the maximum
+  float best = NAN;
+#pragma unroll
+  for (int e = 0; e < E; ++e) best = fmaxf(best, v[e]);
+  const unsigned mine = best == best ? ordered(best) : 0u;
   __shared__ unsigned tops[4];
   __shared__ float sums[4];
-  const unsigned wtop = wave_max(best);
+  __shared__ Entry passed[4][kMostPassed];
+  __shared__ Entry taken[4][kMostBeams];
+  const unsigned wtop = wave_max(mine);
   if (lane == 0) tops[wave] = wtop;
   __syncthreads();
   unsigned top = tops[0];
 #pragma unroll
   for (int i = 1; i < 4; ++i) top = tops[i] > top ? tops[i] : top;
   const float m = top != 0 ? value_of(top) : -INFINITY;
+  // sum of 2^(v L - c) with c = m L, L = log2 e in fp32: one rounding of the exponent; k_beam_pick takes c as it is here
   float s = 0.f;
   if (finite(m)) {
+    const float c = m * kLog2e;
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      // exp(x) = 2^(x log2 e) with the product's rounding error made good: far below the maximum it would be 2^-20 of the term
-      const float x = key[e] != 0 ? value_of(key[e]) - m : -INFINITY, t = x * 1.4426950408889634f;
-      const float low = fmaf(x, 1.4426950408889634f, -t) + x * 1.925963033500234e-8f;
-      const float p = __builtin_amdgcn_exp2f(t);
-      s += p > 0.f ? fmaf(p, 0.6931471805599453f * low, p) : 0.f;
-    }
+    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaxf(fmaf(v[e], kLog2e, -c), -200.f));   // 2^-200 vanishes beside the maximum's 1
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if (lane == 0) sums[wave] = s;
+  // the wave's n largest
+  const unsigned bound = nth_of_lanes(mine, n, lane), lowest = ordered(-3.402823466e38f);
+  const float least = value_of(bound > lowest ? bound : lowest);
+  int count = 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const u64 pass = __ballot(v[e] >= least);
+    if (pass != 0) {
+      const int at = count + __builtin_amdgcn_mbcnt_hi((unsigned)(pass >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)pass, 0u));
+      if (v[e] >= least && at < kMostPassed) passed[wave][at] = Entry{v[e], begin + (e / P * 256 + tid) * P + e % P};
+      count += __builtin_popcountll(pass);
+    }
+  }
+  if (count <= kMostPassed) {
+    __builtin_amdgcn_wave_barrier();
+    Entry e{0.f, 0};
+    if (lane < count) e = passed[wave][lane];
+    place(ordered(e.logit + 0.f), e.token, count, taken[wave], n, lane);   // + 0: one zero
+  } else {
+    u64 last = ~0ull;   // the one found before
+    for (int i = 0; i < n; ++i) {
+      u64 next = 0;
+#pragma unroll 1
+      for (int k = 0; k < N; ++k) {
+        const int t = begin + (k * 256 + tid) * P;
+        float e[P];
+#pragma unroll
+        for (int j = 0; j < P; ++j) e[j] = number(own, t + j, V);
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+          const float x = e[j] + 0.f;
+          const u64 key = x >= least ? (u64)ordered(x) << 32 | (unsigned)~(t + j) : 0;
+          if (key < last && key > next) next = key;
+        }
+      }
+      const unsigned hi = wave_max((unsigned)(next >> 32));
+      const unsigned lo = wave_max((unsigned)(next >> 32) == hi ? (unsigned)next : 0u);
+      last = (u64)hi << 32 | lo;
+      if (lane == 0) taken[wave][i] = hi != 0 ? Entry{value_of(hi), (int)~lo} : Entry{0.f, -1};
+      if (hi == 0) break;
+    }
+  }
   __syncthreads();
   if (tid == 0) parts[(long long)row * slices + slice] = Part{m, (sums[0] + sums[1]) + (sums[2] + sums[3])};
-  // the wave's n largest, in order
-  Entry* const list = lists + (((long long)row * slices + slice) * 4 + wave) * n;
-  unsigned mine = best;
-  for (int i = 0; i < n; ++i) {
-    const unsigned w = wave_max(mine);
-    if (w == 0) {   // no values left: token -1 ends the list
-      if (lane == 0) list[i] = Entry{0.f, -1};
-      break;
-    }
-    int at = 0x7fffffff;   // the lane's first element of that value
-    if (mine == w) {
-#pragma unroll
-      for (int e = E - 1; e >= 0; --e)
-        if (key[e] == w) at = e;
-    }
-    long long t = at != 0x7fffffff ? base - first + (long long)(at / P * 256 + tid) * P + at % P : 0x7fffffff;
-    int token = (int)t;
-    u64 has = __ballot(mine == w);
-    int low;
-    if ((has & (has - 1)) == 0) {
-      low = __builtin_amdgcn_readlane(token, __builtin_ctzll(has));
-    } else {
-      low = token;
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) low = min(low, __shfl_xor(low, o, 64));
-    }
-    if (token == low && mine == w) {
-      list[i] = Entry{value_of(w), low};
-      unsigned next = 0;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        key[e] = e == at ? 0u : key[e];
-        next = key[e] > next ? key[e] : next;
+  // the slice's n largest out of the waves'
+  if (wave == 0) {
+    Entry* const list = lists + ((long long)row * slices + slice) * n;
+    // lanes 0-3 stand for the waves' lists and show their first entries left
+    int at = 0;
+    Entry e{0.f, -1};
+    if (lane < 4) e = taken[lane][0];
+    for (int i = 0; i < n; ++i) {
+      const unsigned key = e.token >= 0 ? ordered(e.logit) : 0u;
+      const unsigned w = wave_max(key);
+      if (w == 0) {
+        if (lane == 0) list[i] = Entry{0.f, -1};
+        break;
       }
-      mine = next;
+      int low = 0x7fffffff;
+      for (u64 h = __ballot(key == w); h != 0; h &= h - 1) low = min(low, __builtin_amdgcn_readlane(e.token, __builtin_ctzll(h)));
+      if (key == w && e.token == low) {
+        list[i] = e;
+        ++at;
+        e = Entry{0.f, -1};
+        if (at < n) e = taken[lane][at];
+      }
     }
   }
 }
 
 // ---------------------------------------------------------------------------
-// One workgroup a batch entry.  List l of the n * slices * 4 belongs to beam l / (4 slices); thread t watches over lists t, t + 256, ...
+// One workgroup a batch entry.  List l of the n * slices belongs to beam l / slices.  The n-th best of the lanes' best list heads bounds
+// the n best from below; the few entries that reach it are gathered, and each counts those before it.  Where too many do, the best is
+// looked for n times.
 // ---------------------------------------------------------------------------
-constexpr int kMostLists = 32768;
+constexpr int kMostLists = 8704;
+constexpr int kStaged = 48 * 1024;   // bytes of lists that are brought to LDS at once (else they are read where they are)
+constexpr int kMostGathered = 256;
 
+// A candidate: its value in an order of integers (0: none), and beam * V + token.
 struct Head {
-  double value;
-  unsigned flat;   // beam * V + token; ~0: none
+  u64 key;
+  unsigned flat;
 };
-__device__ __forceinline__ bool before(const Head& a, const Head& b) { return a.value > b.value || (a.value == b.value && a.flat < b.flat); }
+__device__ __forceinline__ bool before(const Head& a, const Head& b) { return a.key > b.key || (a.key == b.key && a.flat < b.flat); }
 
 enum { kAlive = 0, kFinished = 1, kDead = 2 };
 
 __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ parts, const Entry* __restrict__ lists,
                                                    const float* __restrict__ scores, const unsigned char* __restrict__ finished, int n,
-                                                   int V, int slices, int eos, int keep_slots, float* __restrict__ out_scores,
+                                                   int V, int slices, int eos, int keep_slots, int staged, float* __restrict__ out_scores,
                                                    int32_t* __restrict__ out_parent, int32_t* __restrict__ out_token) {
-  extern __shared__ __attribute__((aligned(16))) unsigned char taken[];   // entries taken from every list
+  extern __shared__ __attribute__((aligned(16))) unsigned char smem[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, count = n * slices;
+  Entry* const near = reinterpret_cast<Entry*>(smem);
   __shared__ double offset[kMostBeams];
   __shared__ int kind[kMostBeams];
-  __shared__ double wv[4];
-  __shared__ unsigned wf[4];
-  __shared__ double pick_value[kMostBeams];
-  __shared__ unsigned pick_flat[kMostBeams];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, per = 4 * slices, count = n * per;
-  for (int l = tid; l < count; l += 256) taken[l] = 0;
-  for (int j = wave; j < n; j += 4) {
+  __shared__ Head gathered[kMostGathered];
+  __shared__ Head picks[kMostBeams];
+  __shared__ Head best[4];
+  __shared__ unsigned reach;
+  __shared__ int size;
+  const Entry* const own = lists + (long long)b * count * n;
+  if (tid == 0) size = 0;
+  if (tid < kMostBeams) picks[tid] = Head{0, 0u};
+  constexpr int kAtOnce = 8;   // what a thread asks for before it waits: every trip to memory takes longer than all the rest
+  if (staged)
+    for (int l0 = 0; l0 < count * n; l0 += 256 * kAtOnce) {
+      Entry e[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) e[i] = own[min(l0 + 256 * i + tid, count * n - 1)];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (l0 + 256 * i + tid < count * n) near[l0 + 256 * i + tid] = e[i];
+    }
+  // a beam for every 32 threads: the logarithm of its sum of exponentials
+  for (int j0 = 0; j0 < n; j0 += 8) {
+    const int j = j0 + tid / 32, t = tid % 32;
     const long long row = (long long)b * n + j;
-    const float score = scores[row];
-    if (finished != nullptr && finished[row] != 0) {
-      if (lane == 0) {
-        kind[j] = kFinished;
-        offset[j] = finite(score) ? (double)score : -INFINITY;
-      }
-      continue;
-    }
-    double z = 0.0;
+    const float score = j < n ? scores[row] : 0.f;
+    const bool done = j < n && finished != nullptr && finished[row] != 0, live = j < n && !done && finite(score);
     float top = -INFINITY;
-    if (finite(score)) {
-      for (int i = lane; i < slices; i += 64) top = fmaxf(top, parts[row * slices + i].top);
+    double z = 0.0;
+    Part mine{-INFINITY, 0.f};
+    if (j < n && t < slices) mine = parts[row * slices + t];   // where the beam is not live: read, not used
+    if (live) {
+      top = mine.top;
+      for (int i = t + 32; i < slices; i += 32) top = fmaxf(top, parts[row * slices + i].top);
+    }
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-      for (int i = lane; i < slices; i += 64) {
-        const Part p = parts[row * slices + i];
-        if (p.sum > 0.f) z += (double)p.sum * exp((double)p.top - (double)top);
+    for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+    // sums are of 2^(v L - c), L and c = top L in fp32
+    if (live && finite(top))
+      for (int i = t; i < slices; i += 32) {
+        const Part p = i == t ? mine : parts[row * slices + i];
+        if (p.sum > 0.f) z += (double)p.sum * exp2((double)(p.top * kLog2e) - (double)(top * kLog2e));
       }
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
-    }
-    if (lane == 0) {
-      const bool alive = finite(top);
-      kind[j] = alive ? kAlive : kDead;
-      offset[j] = alive ? (double)score - ((double)top + log(z)) : -INFINITY;
+    for (int o = 16; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
+    if (t == 0 && j < n) {
+      const bool alive = live && finite(top);
+      kind[j] = alive ? kAlive : done && finite(score) ? kFinished : kDead;
+      // log sum exp = ln 2 (c + log2 z), where the exponents v L of the terms that matter stand for v log2 e near v = top
+      const double c = (double)(top * kLog2e) + (double)top * (1.4426950408889634074 - (double)kLog2e);
+      offset[j] = alive ? (double)score - 0.69314718055994530942 * (c + log2(z)) : (double)score + 0.0;
     }
   }
   __syncthreads();
-  const Entry* const own = lists + (long long)b * count * n;
-  // what list l offers after `at` of its entries
-  const auto head = [&](int l, int at) {
-    const int j = l / per;
-    Head hd{-INFINITY, ~0u};
+  // entry `at` of list l
+  const auto entry = [&](int l, int at) {
+    const int j = l / slices;
+    Head hd{0, 0u};
     if (kind[j] == kAlive) {
-      if (at >= n) return hd;
-      const Entry e = own[(long long)l * n + at];
+      const Entry e = staged ? near[l * n + at] : own[(long long)l * n + at];
       if (e.token < 0) return hd;
-      hd.value = offset[j] + (double)e.logit;
+      hd.key = ordered64(offset[j] + (double)e.logit + 0.0);   // one zero
       hd.flat = (unsigned)j * (unsigned)V + (unsigned)e.token;
-    } else if (l % per == 0 && at < V) {   // a finished beam goes on with `eos` alone; what else it and a dead one offer is worth nothing
-      int token = at;
-      if (kind[j] == kFinished) {
-        token = at == 0 ? eos : at - 1 + (at - 1 >= eos ? 1 : 0);
-        if (at == 0) hd.value = offset[j];
-      }
-      hd.flat = (unsigned)j * (unsigned)V + (unsigned)token;
+    } else if (kind[j] == kFinished && l % slices == 0 && at == 0) {   // a finished beam goes on with `eos` alone
+      hd.key = ordered64(offset[j]);
+      hd.flat = (unsigned)j * (unsigned)V + (unsigned)eos;
     }
     return hd;
   };
-  Head mine{-INFINITY, ~0u};
-  int from = -1;
-  const auto rescan = [&]() {
-    mine = Head{-INFINITY, ~0u};
-    from = -1;
-    for (int l = tid; l < count; l += 256) {
-      const Head hd = head(l, taken[l]);
-      if (hd.flat != ~0u && (from < 0 || before(hd, mine))) {
-        mine = hd;
-        from = l;
-      }
+  if (wave == 0) {
+    unsigned most = 0;
+    for (int l = lane; l < count; l += 64) {
+      const unsigned k = (unsigned)(entry(l, 0).key >> 32);
+      most = k > most ? k : most;
     }
-  };
-  rescan();
-  for (int i = 0; i < n; ++i) {
-    Head w = mine;
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-      Head x;
-      x.value = __shfl_xor(w.value, o, 64);
-      x.flat = __shfl_xor(w.flat, o, 64);
-      if (before(x, w)) w = x;
-    }
-    if (lane == 0) {
-      wv[wave] = w.value;
-      wf[wave] = w.flat;
-    }
-    __syncthreads();
-    w = Head{wv[0], wf[0]};
-#pragma unroll
-    for (int k = 1; k < 4; ++k)
-      if (before(Head{wv[k], wf[k]}, w)) w = Head{wv[k], wf[k]};
-    if (tid == 0) {
-      pick_value[i] = w.value;
-      pick_flat[i] = w.flat;
-    }
-    if (from >= 0 && mine.flat == w.flat) {
-      ++taken[from];
-      rescan();
-    }
-    __syncthreads();
+    const unsigned bound = nth_of_lanes(most, n, lane);
+    if (lane == 0) reach = bound > 0 ? bound : 1u;
   }
-  if (tid == 0) {
-    unsigned used = 0;   // slots that are given away
-    if (keep_slots) {
-      for (int i = 0; i < n; ++i) used |= 1u << (pick_flat[i] / (unsigned)V);
+  __syncthreads();
+  for (int l = tid; l < count; l += 256) {
+    for (int at = 0; at < n; ++at) {   // in order: none behind the first that falls short
+      const Head hd = entry(l, at);
+      if ((unsigned)(hd.key >> 32) < reach) break;
+      const int to = atomicAdd(&size, 1);   // whatever their order there: they are told apart by key and index
+      if (to < kMostGathered) gathered[to] = hd;
     }
+  }
+  __syncthreads();
+  const int found = size < n ? size : n;
+  if (size <= kMostGathered) {
+    if (tid < size) {
+      const Head mine = gathered[tid];
+      int place = 0;
+#pragma unroll 4
+      for (int i = 0; i < size; ++i) place += before(gathered[i], mine);
+      if (place < n) picks[place] = mine;
+    }
+    __syncthreads();
+  } else {
+    Head last{~0ull, 0u};
+    for (int i = 0; i < n; ++i) {
+      Head w{0, ~0u};
+      for (int l = tid; l < count; l += 256)
+        for (int at = 0; at < n; ++at) {
+          const Head hd = entry(l, at);
+          if (hd.key == 0) break;
+          if (before(last, hd)) {   // the list's first that is not taken
+            if (before(hd, w)) w = hd;
+            break;
+          }
+        }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) {
+        Head x;
+        x.key = __shfl_xor(w.key, o, 64);
+        x.flat = __shfl_xor(w.flat, o, 64);
+        if (before(x, w)) w = x;
+      }
+      if (lane == 0) best[wave] = w;
+      __syncthreads();
+      last = best[0];
+#pragma unroll
+      for (int k = 1; k < 4; ++k)
+        if (before(best[k], last)) last = best[k];
+      if (tid == 0) picks[i] = last;
+      __syncthreads();
+    }
+  }
+  if (wave != 0) return;
+  Head mine{0, 0u};
+  if (lane < found) mine = picks[lane];
+  // too few: candidates of value -infinity, the lowest that are not taken yet
+  int have = found;
+  for (unsigned flat = 0; have < n; ++flat) {
+    if (__ballot(lane < have && mine.flat == flat) != 0) continue;
+    if (lane == have) mine.flat = flat;
+    ++have;
+  }
+  const int parent = (int)(mine.flat / (unsigned)V), token = (int)(mine.flat % (unsigned)V);
+  int slot = lane;
+  if (keep_slots) {
+    unsigned used = 0;   // places of beams that survive
+    for (int i = 0; i < n; ++i) used |= 1u << __builtin_amdgcn_readlane(parent, i);
     unsigned kept = 0;
     int free = 0;
     for (int i = 0; i < n; ++i) {
-      const int parent = (int)(pick_flat[i] / (unsigned)V), token = (int)(pick_flat[i] % (unsigned)V);
-      int slot = i;
-      if (keep_slots) {
-        if ((kept >> parent & 1u) == 0) {
-          kept |= 1u << parent;
-          slot = parent;
-        } else {
-          while (used >> free & 1u) ++free;
-          slot = free++;
-        }
+      const int p = __builtin_amdgcn_readlane(parent, i);
+      int at = p;
+      if ((kept >> p & 1u) != 0) {
+        while (used >> free & 1u) ++free;
+        at = free++;
       }
-      const long long at = (long long)b * n + slot;
-      out_scores[at] = (float)pick_value[i];
-      out_parent[at] = parent;
-      out_token[at] = token;
+      kept |= 1u << p;
+      if (lane == i) slot = at;
     }
+  }
+  if (lane < n) {
+    const long long at = (long long)b * n + slot;
+    out_scores[at] = mine.key != 0 ? (float)value64(mine.key) : -INFINITY;
+    out_parent[at] = parent;
+    out_token[at] = token;
   }
 }
 
@@ -346,7 +477,7 @@ __global__ __launch_bounds__(256) void k_state_reorder(Tensors t, const int32_t*
   else reorder<unsigned char, N>(rows, row_bytes, at, from, n);
 }
 
-// Elements a thread holds: 32, or 8 where the rows are too few to give every CU a workgroup.
+// Elements a thread holds: 32, or 8 where the rows are too few to give every CU two workgroups.
 int slice_elements(const dark_beam_params& p) {
   const long long rows = (long long)p.B * p.n;
   return rows * ((p.V + 8191) / 8192) >= 512 ? 32 : 8;
@@ -360,14 +491,14 @@ dark_status check(const dark_beam_params* p) {
   if (p == nullptr || p->B < 0 || p->n <= 0 || p->V <= 0) return DARK_EINVAL;
   if (p->io_dtype != DARK_F32 && p->io_dtype != DARK_BF16) return DARK_EINVAL;
   if (p->n > kMostBeams || (long long)p->n * p->V >= (1LL << 31) || (long long)p->B * p->n > 65535) return DARK_EUNSUPPORTED;
-  if ((long long)p->n * 4 * slices_of(*p) > kMostLists) return DARK_EUNSUPPORTED;
+  if ((long long)p->n * slices_of(*p) > kMostLists) return DARK_EUNSUPPORTED;
   return DARK_OK;
 }
 
 void plan(const dark_beam_params& p, Arena& ar, Part** parts, Entry** lists) {
   const size_t slots = (size_t)p.B * p.n * slices_of(p);
   *parts = ar.take<Part>(slots);
-  *lists = ar.take<Entry>(slots * 4 * p.n);
+  *lists = ar.take<Entry>(slots * p.n);
 }
 
 template <typename T>
@@ -418,8 +549,10 @@ dark_status dark_beam_select(const dark_beam_params* p, const void* logits, cons
   DARK_TRY(p->io_dtype == DARK_BF16 ? beam::rows<unsigned short>(*p, logits, scores, finished, parts, lists, st)
                                     : beam::rows<float>(*p, logits, scores, finished, parts, lists, st));
   const int slices = beam::slices_of(*p);
-  DARK_LAUNCH(KID_BEAM_PICK, st, beam::k_beam_pick, dim3(p->B), dim3(256), (size_t)p->n * 4 * slices, parts, lists, scores, finished, p->n, p->V,
-              slices, p->eos, p->keep_slots != 0, out_scores, out_parent, out_token);
+  const size_t count = (size_t)p->n * slices, bytes = count * p->n * sizeof(beam::Entry);
+  const int staged = bytes <= beam::kStaged;
+  DARK_LAUNCH(KID_BEAM_PICK, st, beam::k_beam_pick, dim3(p->B), dim3(256), staged ? bytes : 0, parts, lists, scores, finished, p->n,
+              p->V, slices, p->eos, p->keep_slots != 0, staged, out_scores, out_parent, out_token);
   return DARK_OK;
 }
 
