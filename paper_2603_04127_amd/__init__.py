@@ -7,7 +7,6 @@ missing the import of this binding's functions raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import math
 import os
@@ -438,42 +437,31 @@ def dark_attn_bwd(Q, K, V, M, W, dOut, causal: bool, *, chunk=0, scale=0.0, path
 # ----------------------------------------------------------------------------
 # linear attention with a decay for each head; beam search over recurrent states
 # ----------------------------------------------------------------------------
-def _on_device(*tensors):
-    """The device that all given tensors (None: not given) are on; refuses host tensors and mixed devices."""
-    index = None
-    for t in tensors:
-        if t is None:
-            continue
-        i = t.get_device()
-        if i < 0 or (index is not None and i != index):
-            raise ValueError("tensors must be on one GPU")
-        index = i
-    return index
-
-
-def _on(index):
-    """Calls are enqueued on the current stream of the tensors' device, whichever is current."""
-    torch = _torch()
-    return _HERE_ALREADY if torch._C._cuda_getDevice() == index else torch.cuda.device(index)
-
-
-_HERE_ALREADY = contextlib.nullcontext()
 _LAYOUTS = {"bhld": BHLD, "blhd": BLHD}
 
 
-def _f32(t, shape, what):
-    if t is not None and (t.dtype != _torch().float32 or tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{what} must be float32 of shape {tuple(shape)}")
+def _pointers(*tensors):
+    """(The device that all given tensors are on, their addresses; None: not given).  In one pass over them: this is a third of the
+    host time of a short call."""
+    index, out = None, []
+    for t in tensors:
+        if t is None:
+            out.append(None)
+            continue
+        i = t.get_device()
+        if i != index:
+            if i < 0 or index is not None:
+                raise ValueError("tensors must be on one GPU")
+            index = i
+        if not t.is_contiguous():
+            raise ValueError("tensors must be contiguous device tensors")
+        out.append(t.data_ptr())
+    return index, out
 
 
-def _i32(t, shape, what):
-    if t is not None and (t.dtype != _torch().int32 or tuple(t.shape) != tuple(shape)):
-        raise ValueError(f"{what} must be int32 of shape {tuple(shape)}")
-
-
-def _like(t, x, what):
-    if t is not None and (t.dtype != x.dtype or t.shape != x.shape):
-        raise ValueError(f"{what} must have the shape and type of what it belongs to")
+def _require(t, dtype, shape, what):
+    if t is not None and (t.dtype != dtype or t.shape != shape):
+        raise ValueError(f"{what} must be {dtype} of shape {tuple(shape)}")
 
 
 def _decay_plan(Q, K, V, layout, scale, segments, backward):
@@ -494,11 +482,6 @@ def _decay_plan(Q, K, V, layout, scale, segments, backward):
     return plan
 
 
-def _decay_checks(p, log_decay, lengths):
-    _f32(log_decay, (p.H,), "log_decay")
-    _i32(lengths, (p.B,), "lengths")
-
-
 def dark_decay_fwd(Q, K, V, log_decay, *, lengths=None, state=None, out=None, state_out=None, want_state=False, scale=0.0,
                    layout="bhld", segments=0):
     """Linear attention with the decay exp(log_decay[h]) of each head, from `state` [B,H,dk,dv] (None: empty):
@@ -507,21 +490,25 @@ def dark_decay_fwd(Q, K, V, log_decay, *, lengths=None, state=None, out=None, st
     `lengths` [B] int32: rows of each sequence; out is 0 behind them.  `segments`: a schedule override (0: none)."""
     torch = _torch()
     p, nb = _decay_plan(Q, K, V, layout, float(scale), segments, False)
-    _decay_checks(p, log_decay, lengths)
-    shape = (p.B, p.H, p.dk, p.dv)
-    _f32(state, shape, "state")
-    _f32(state_out, shape, "state_out")
-    _like(out, V, "out")
-    index = _on_device(Q, K, V, log_decay, lengths, state, out, state_out)
-    with _on(index):
-        if out is None:
-            out = _result(V, V.dtype, Q)
-        if want_state and state_out is None:
-            state_out = torch.empty(shape, dtype=torch.float32, device=Q.device)
-        ws, stream = _workspace(nb, Q.device) if nb else (None, _stream())
-        _check(lib().dark_decay_fwd(ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(lengths), _ptr(state), _ptr(out),
-                                    _ptr(state_out), None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream),
-               "dark_decay_fwd")
+    f32, shape = torch.float32, (p.B, p.H, p.dk, p.dv)
+    _require(log_decay, f32, (p.H,), "log_decay")
+    _require(lengths, torch.int32, (p.B,), "lengths")
+    _require(state, f32, shape, "state")
+    _require(state_out, f32, shape, "state_out")
+    _require(out, V.dtype, V.shape, "out")
+    index, (q, k, v, a, n, s, o, so) = _pointers(Q, K, V, log_decay, lengths, state, out, state_out)
+    if index != torch._C._cuda_getDevice():   # enqueued on the current stream of the tensors' device
+        with torch.cuda.device(index):
+            return dark_decay_fwd(Q, K, V, log_decay, lengths=lengths, state=state, out=out, state_out=state_out, want_state=want_state,
+                                  scale=scale, layout=layout, segments=segments)
+    if o is None:
+        out = _result(V, V.dtype, Q)
+        o = out.data_ptr()
+    if want_state and so is None:
+        state_out = torch.empty(shape, dtype=f32, device=Q.device)
+        so = state_out.data_ptr()
+    ws, stream = _workspace(nb, Q.device) if nb else (None, torch._C._cuda_getCurrentRawStream(index))
+    _check(lib().dark_decay_fwd(ctypes.byref(p), q, k, v, a, n, s, o, so, None if ws is None else ws.data_ptr(), nb, stream), "dark_decay_fwd")
     return out if state_out is None else (out, state_out)
 
 
@@ -532,30 +519,33 @@ def dark_decay_bwd(Q, K, V, log_decay, dOut, *, lengths=None, state=None, dstate
     `grads`: a dict of preallocated tensors to write into instead."""
     torch = _torch()
     p, nb = _decay_plan(Q, K, V, layout, float(scale), segments, True)
-    _decay_checks(p, log_decay, lengths)
-    shape = (p.B, p.H, p.dk, p.dv)
-    _f32(state, shape, "state")
-    _f32(dstate, shape, "dstate")
-    if dOut.dtype != V.dtype or dOut.shape != V.shape:
-        raise ValueError("dOut must have the shape and type of V")
+    f32, shape = torch.float32, (p.B, p.H, p.dk, p.dv)
+    _require(log_decay, f32, (p.H,), "log_decay")
+    _require(lengths, torch.int32, (p.B,), "lengths")
+    _require(state, f32, shape, "state")
+    _require(dstate, f32, shape, "dstate")
+    _require(dOut, V.dtype, V.shape, "dOut")
     like = {"dQ": Q, "dK": K, "dV": V}
     unknown = set(need if grads is None else grads) - {"dQ", "dK", "dV", "dstate"}
     if unknown:
         raise ValueError(f"unknown gradient(s) {sorted(unknown)}")
-    if grads is not None:
-        g = {k: t for k, t in grads.items() if t is not None}
-        for k, t in g.items():
-            _f32(t, shape, k) if k == "dstate" else _like(t, like[k], k)
-    index = _on_device(Q, K, V, log_decay, dOut, lengths, state, dstate, *(g.values() if grads is not None else ()))
-    with _on(index):
-        if grads is None:
-            g = {k: _result(x, x.dtype, Q) for k, x in like.items() if k in need}
-            if "dstate" in need and state is not None:
-                g["dstate"] = torch.empty(shape, dtype=torch.float32, device=Q.device)
-        ws, stream = _workspace(nb, Q.device) if nb else (None, _stream())
-        _check(lib().dark_decay_bwd(ctypes.byref(p), _ptr(Q), _ptr(K), _ptr(V), _ptr(log_decay), _ptr(lengths), _ptr(state), _ptr(dOut),
-                                    _ptr(dstate), _ptr(g.get("dQ")), _ptr(g.get("dK")), _ptr(g.get("dV")), _ptr(g.get("dstate")),
-                                    None if ws is None else ws.data_ptr(), 0 if ws is None else ws.numel(), stream), "dark_decay_bwd")
+    g = {} if grads is None else {name: t for name, t in grads.items() if t is not None}
+    for name, t in g.items():
+        _require(t, *((f32, shape) if name == "dstate" else (like[name].dtype, like[name].shape)), name)
+    index, (q, k, v, a, do, n, s, ds, gq, gk, gv, gs) = _pointers(Q, K, V, log_decay, dOut, lengths, state, dstate, g.get("dQ"), g.get("dK"),
+                                                                  g.get("dV"), g.get("dstate"))
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return dark_decay_bwd(Q, K, V, log_decay, dOut, lengths=lengths, state=state, dstate=dstate, need=need, grads=grads, scale=scale,
+                                  layout=layout, segments=segments)
+    if grads is None:
+        g = {name: _result(x, x.dtype, Q) for name, x in like.items() if name in need}
+        if "dstate" in need and state is not None:
+            g["dstate"] = torch.empty(shape, dtype=f32, device=Q.device)
+        gq, gk, gv, gs = (g[name].data_ptr() if name in g else None for name in ("dQ", "dK", "dV", "dstate"))
+    ws, stream = _workspace(nb, Q.device) if nb else (None, torch._C._cuda_getCurrentRawStream(index))
+    _check(lib().dark_decay_bwd(ctypes.byref(p), q, k, v, a, n, s, do, ds, gq, gk, gv, gs, None if ws is None else ws.data_ptr(), nb, stream),
+           "dark_decay_bwd")
     return g
 
 
@@ -563,6 +553,7 @@ def dark_decay_step(q, k, v, log_decay, state, *, parent=None, state_out=None, o
     """One token of dark_decay_fwd: q, k [B,H,dk], v [B,H,dv]; returns out [B,H,dv].  `state` [B,H,dk,dv] is updated in place,
     or left alone and the new one written to `state_out`.  With `parent` [B] int32 (and a `state_out`) row b continues row
     parent[b] of `state` [any number of rows,H,dk,dv]; a parent that is no row of it stands for an empty state."""
+    torch = _torch()
     scale = float(scale)
     key = ("decay_step", q.shape, q.dtype, k.shape, k.dtype, v.shape, v.dtype, scale)
     plan = _plans.get(key)
@@ -571,25 +562,28 @@ def dark_decay_step(q, k, v, log_decay, state, *, parent=None, state_out=None, o
             raise ValueError("q and k must be [B, H, dk], v [B, H, dv]")
         if k.dtype != q.dtype or v.dtype != q.dtype:
             raise TypeError("q, k and v must have one type")
-        plan = (DecayParams(q.shape[0], q.shape[1], 1, q.shape[2], v.shape[2], _dtype_code(q), BHLD, scale, 0), 0)
+        p = DecayParams(q.shape[0], q.shape[1], 1, q.shape[2], v.shape[2], _dtype_code(q), BHLD, scale, 0)
+        plan = (p, (p.B, p.H, p.dk, p.dv))
         _keep_plan(key, plan)
-    p = plan[0]
-    shape = (p.B, p.H, p.dk, p.dv)
-    _f32(log_decay, (p.H,), "log_decay")
-    _i32(parent, (p.B,), "parent")
+    p, shape = plan
     if state_out is None:
         if parent is not None:
             raise ValueError("a step that reads its states through `parent` needs a state_out")
         state_out = state
-    rows = state.shape[0]
-    _f32(state, (rows,) + shape[1:], "state")
-    _f32(state_out, shape, "state_out")
-    _like(out, v, "out")
-    with _on(_on_device(q, k, v, log_decay, state, parent, state_out, out)):
-        if out is None:
-            out = _result(v, v.dtype, q)
-        _check(lib().dark_decay_step(ctypes.byref(p), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(parent), rows, _ptr(state),
-                                     _ptr(state_out), _ptr(out), _stream()), "dark_decay_step")
+    f32, rows = torch.float32, state.shape[0]
+    _require(log_decay, f32, shape[1:2], "log_decay")
+    _require(parent, torch.int32, shape[:1], "parent")
+    _require(state, f32, (rows,) + shape[1:], "state")
+    _require(state_out, f32, shape, "state_out")
+    _require(out, v.dtype, v.shape, "out")
+    index, (pq, pk, pv, a, s, pp, so, o) = _pointers(q, k, v, log_decay, state, parent, state_out, out)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return dark_decay_step(q, k, v, log_decay, state, parent=parent, state_out=state_out, out=out, scale=scale)
+    if o is None:
+        out = _result(v, v.dtype, q)
+        o = out.data_ptr()
+    _check(lib().dark_decay_step(ctypes.byref(p), pq, pk, pv, a, pp, rows, s, so, o, torch._C._cuda_getCurrentRawStream(index)), "dark_decay_step")
     return out
 
 
@@ -607,40 +601,46 @@ def dark_beam_select(logits, scores, *, finished=None, eos=0, keep_slots=False, 
         plan = (p, int(lib().dark_beam_workspace_bytes(ctypes.byref(p))))
         _keep_plan(key, plan)
     p, nb = plan
-    shape = (p.B, p.n)
-    _f32(scores, shape, "scores")
-    if finished is not None and (finished.dtype not in (torch.uint8, torch.bool) or tuple(finished.shape) != shape):
+    f32, i32, shape = torch.float32, torch.int32, (p.B, p.n)
+    _require(scores, f32, shape, "scores")
+    if finished is not None and (finished.dtype not in (torch.uint8, torch.bool) or finished.shape != shape):
         raise ValueError(f"finished must be uint8 or bool of shape {shape}")
-    if out is not None:
-        _f32(out[0], shape, "the scores of out")
-        _i32(out[1], shape, "the parents of out")
-        _i32(out[2], shape, "the tokens of out")
-    with _on(_on_device(logits, scores, finished, *(out or ()))):
-        if out is None:
-            out = (torch.empty(shape, dtype=torch.float32, device=logits.device), torch.empty(shape, dtype=torch.int32, device=logits.device),
-                   torch.empty(shape, dtype=torch.int32, device=logits.device))
-        ws, stream = _workspace(nb, logits.device)
-        _check(lib().dark_beam_select(ctypes.byref(p), _ptr(logits), _ptr(scores), _ptr(finished), _ptr(out[0]), _ptr(out[1]), _ptr(out[2]),
-                                      ws.data_ptr(), ws.numel(), stream), "dark_beam_select")
-    return tuple(out)
+    s, parent, token = (None, None, None) if out is None else out
+    _require(s, f32, shape, "the scores of out")
+    _require(parent, i32, shape, "the parents of out")
+    _require(token, i32, shape, "the tokens of out")
+    index, (x, c, f, ps, pp, pt) = _pointers(logits, scores, finished, s, parent, token)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return dark_beam_select(logits, scores, finished=finished, eos=eos, keep_slots=keep_slots, out=out)
+    if out is None:
+        s, parent, token = _result(scores, f32, logits), torch.empty_like(scores, dtype=i32), torch.empty_like(scores, dtype=i32)
+        ps, pp, pt = s.data_ptr(), parent.data_ptr(), token.data_ptr()
+    ws, stream = _workspace(nb, logits.device)
+    _check(lib().dark_beam_select(ctypes.byref(p), x, c, f, ps, pp, pt, ws.data_ptr(), ws.numel(), stream), "dark_beam_select")
+    return s, parent, token
 
 
 def dark_state_reorder(states, parent):
     """States of beams follow their parents, in place: row (b, j) of every tensor [B*n, ...] (or [B, n, ...]) becomes row
     (b, parent[b, j]) of before.  parent [B, n] int32; an entry outside 0 ... n - 1 leaves its row as it is.  The tensors may not overlap."""
+    torch = _torch()
     if parent.dim() != 2:
         raise ValueError("parent must be [B, n]")
     B, n = parent.shape
-    _i32(parent, (B, n), "parent")
+    _require(parent, torch.int32, parent.shape, "parent")
     count = len(states)
-    ptrs, sizes = (ctypes.c_void_p * count)(), (ctypes.c_size_t * count)()
+    index, ptrs = _pointers(parent, *states)
+    sizes = (ctypes.c_size_t * count)()
     for i, t in enumerate(states):
-        if t.shape[0] != B * n and tuple(t.shape[:2]) != (B, n):
+        if t.shape[0] != B * n and t.shape[:2] != (B, n):
             raise ValueError("a state must have a row for each beam")
-        ptrs[i] = _ptr(t)
         sizes[i] = t.numel() * t.element_size() // (B * n) if B else 0
-    with _on(_on_device(parent, *states)):
-        _check(lib().dark_state_reorder(B, n, _ptr(parent), count, ptrs, sizes, _stream()), "dark_state_reorder")
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return dark_state_reorder(states, parent)
+    _check(lib().dark_state_reorder(B, n, ptrs[0], count, (ctypes.c_void_p * count)(*ptrs[1:]), sizes,
+                                    torch._C._cuda_getCurrentRawStream(index)), "dark_state_reorder")
 
 
 # ----------------------------------------------------------------------------
