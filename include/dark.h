@@ -332,7 +332,7 @@ typedef struct {
 } dark_decay_params;
 
 /* Bytes of scratch of dark_decay_fwd (backward == 0) or dark_decay_bwd; 0 on invalid parameters, and where none is needed
- * (ws may then be NULL). */
+ * (ws may then be NULL).  Short bf16 sequences need some only for a state that is updated in place (S_out == S_in). */
 size_t dark_decay_workspace_bytes(const dark_decay_params* p, int backward);
 
 dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,

@@ -70,6 +70,8 @@ dark_status launch_scan_bf16(const Scans& a, int n, hipStream_t st);
 dark_status launch_scan_f32(const Scans& a, int n, hipStream_t st);
 dark_status launch_state_bf16(const States& a, int n, hipStream_t st);
 dark_status launch_state_f32(const States& a, int n, hipStream_t st);
+// decay_short.hip: the same scans, one segment, without a state where nobody asks for it.
+dark_status launch_short_bf16(const Scans& a, int n, hipStream_t st);
 
 dark_status check_params(const dark_decay_params* p, Problem* out);
 dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, const void* V, const float* log_decay,

@@ -37,6 +37,11 @@ __global__ __launch_bounds__(256) void k_decay_prefix(States A) {
   *reinterpret_cast<vec*>(s + (long long)(used - 1) * size) = U;
 }
 
+// A state that is updated in place while other workgroups still read it is read from a copy.
+__global__ __launch_bounds__(256) void k_decay_copy(const float* __restrict__ from, float* __restrict__ to, long long n) {
+  for (long long i = (long long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long long)gridDim.x * 256) to[i] = from[i];
+}
+
 // ---------------------------------------------------------------------------
 // One token: S <- g S + k v^T, out = scale S^T q, for the columns of a workgroup.  Bound by reading and writing the state once.
 // 256 threads as `tx` units of W columns by 256 / tx rows; every thread sums its rows' share of the output, LDS joins the shares.
@@ -135,24 +140,75 @@ dark_status check_params(const dark_decay_params* p, Problem* out) {
 
 namespace {
 
-int blocks_of(int d1, int d2) { return d1 > 128 || d2 <= 64 ? (d2 + 63) / 64 : (d2 + 127) / 128; }
+// How a call is laid out: one segment or several, or bf16 sequences of some chunks without states (decay_short.h).
+struct Plan {
+  int nseg = 1, seg_len = 0;
+  bool direct = false;
+};
 
-// Segments of a sequence: about two workgroups a CU over all (b,h), column blocks and scans, of at least four chunks.
-void segments(const Problem& pb, int scans, int d1, int d2, int* nseg, int* seg_len) {
-  const int C = pb.p.io_dtype == DARK_BF16 ? kChunkBf16 : kChunkF32;
-  const long long have = pb.BH() * blocks_of(d1, d2) * scans;
-  const int chunks = pb.p.L > 0 ? (pb.p.L + C - 1) / C : 1;
-  long long want = pb.p.sched_segments > 0 ? pb.p.sched_segments : 512 / (have > 0 ? have : 1);
-  if (pb.p.sched_segments == 0 && want > (chunks + 3) / 4) want = (chunks + 3) / 4;
-  if (want > chunks) want = chunks;
-  if (want > 64) want = 64;
-  if (want < 1) want = 1;
-  const int each = (int)((chunks + want - 1) / want);
-  *seg_len = each * C;
-  *nseg = (chunks + each - 1) / each;
+// What the kernels take, in us, by the widths of their instances (d1, d2): a chunk of the scan while a CU has nothing else to do (the
+// segment states take 0.45 of it), a step of the direct kernel, and how many (block, chunk) pairs a us that kernel gets through when
+// the chip is full.  Measured on 8 heads of 1024 (fp32) and 2048 rows, and on 16 to 128 heads of 256 to 1024.
+struct Cost {
+  float bf16, f32, step, pairs;
+};
+Cost cost_of(int d1, int d2) {
+  if (d1 > 128) return {5.2f, 8.2f, 2.9f, 120.f};
+  if (d1 > 64) return d2 <= 64 ? Cost{2.6f, 4.5f, 1.8f, 250.f} : Cost{3.2f, 6.4f, 2.0f, 172.f};
+  return d2 <= 64 ? Cost{1.9f, 2.8f, 1.4f, 335.f} : Cost{2.4f, 4.0f, 1.8f, 250.f};
 }
 
-dark_status run_scan(const Problem& pb, const Scans& a, int n) {
+// A launch costs 4 us and, on the CUs, its workgroups' chunks one after the other: workgroups beyond one a CU wait for it or share it,
+// which comes to the same.  More segments shorten the chains until the chip is full; their states are written, and read and written
+// once more by the prefix over them, and cost two launches.
+Plan plan_of(const Problem& pb, int scans, int states) {
+  const dark_decay_params& p = pb.p;
+  const int C = p.io_dtype == DARK_BF16 ? kChunkBf16 : kChunkF32;
+  const int chunks = p.L > 0 ? (p.L + C - 1) / C : 1;
+  // scans of both orientations: the larger width counts
+  const int d1 = scans > 1 && p.dv > p.dk ? p.dv : p.dk, d2 = scans > 1 && p.dk > p.dv ? p.dk : p.dv;
+  const Cost cost = cost_of(d1, d2);
+  const float c = p.io_dtype == DARK_BF16 ? cost.bf16 : cost.f32;
+  const float heads = (float)pb.BH() * (float)(d1 > 128 || d2 <= 64 ? (d2 + 63) / 64 : (d2 + 127) / 128);
+  Plan best;
+  if (p.sched_segments > 0) {
+    best.nseg = p.sched_segments < chunks ? p.sched_segments : chunks;
+    if (best.nseg > 64) best.nseg = 64;
+  } else {
+    float least = 0.f;
+    for (int s = 1; s <= chunks && s <= 64; ++s) {
+      const int each = (chunks + s - 1) / s;
+      if (s > 1 && (chunks + each - 1) / each != s) continue;   // the same chunks a segment as with fewer
+      float rounds = std::ceil(scans * heads * s / 256.f);
+      if (rounds == 1.f && scans * heads * s > 192.f && d1 <= 128) rounds = 1.12f;   // with one a CU everywhere, none hides another's waits
+      float us = 4.f + each * c * rounds;
+      if (s > 1) {
+        us += 8.f + each * 0.45f * c * std::ceil(states * heads * (s - 1) / 256.f);
+        us += 0.2f * s + 2.f * 4.f * states * (float)pb.BH() * s * p.dk * p.dv / 5.5e6f;
+      }
+      if (s == 1 || us < least) {
+        least = us;
+        best.nseg = s;
+      }
+    }
+    if (p.io_dtype == DARK_BF16 && chunks >= 2 && chunks <= 16) {
+      const float pairs = scans * heads * (float)(chunks * (chunks + 1) / 2) / cost.pairs, steps = (float)((chunks + 1) / 2) * cost.step;
+      if (6.f + (pairs > steps ? pairs : steps) < least) {
+        best.direct = true;
+        best.nseg = 1;
+      }
+    }
+  }
+  const int each = (chunks + best.nseg - 1) / best.nseg;
+  best.seg_len = each * C;
+  best.nseg = (chunks + each - 1) / each;
+  return best;
+}
+Plan forward_plan(const Problem& pb) { return plan_of(pb, 1, 1); }
+Plan backward_plan(const Problem& pb) { return plan_of(pb, 3, 2); }
+
+dark_status run_scan(const Problem& pb, const Plan& plan, const Scans& a, int n) {
+  if (plan.direct) return launch_short_bf16(a, n, pb.st);
   return pb.p.io_dtype == DARK_BF16 ? launch_scan_bf16(a, n, pb.st) : launch_scan_f32(a, n, pb.st);
 }
 
@@ -188,10 +244,17 @@ void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* length
 dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, const void* V, const float* log_decay,
                     const int32_t* lengths, const float* S_in, void* out, float* S_out) {
   const int dk = pb.p.dk, dv = pb.p.dv;
-  int nseg, seg_len;
-  segments(pb, 1, dk, dv, &nseg, &seg_len);
+  const Plan plan = forward_plan(pb);
+  const int nseg = plan.nseg, seg_len = plan.seg_len;
   float* const seg = nseg > 1 ? ar.take<float>((size_t)pb.BH() * nseg * dk * dv) : nullptr;
-  if (ar.base == nullptr && nseg > 1) return DARK_OK;   // measuring
+  if (plan.direct && S_in != nullptr && S_in == S_out) {
+    const long long size = pb.BH() * dk * dv;
+    float* const copy = ar.take<float>((size_t)size);
+    if (ar.overflow) return DARK_EWORKSPACE;
+    const long long blocks = (size + 1023) / 1024;
+    DARK_LAUNCH(KID_DECAY_PREFIX, pb.st, k_decay_copy, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, S_in, copy, size);
+    S_in = copy;
+  }
   if (ar.overflow) return DARK_EWORKSPACE;
   if (nseg > 1) {
     States st;
@@ -202,19 +265,18 @@ dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, 
   Scans a;
   fill(pb, a, log_decay, lengths, nseg, seg_len, S_out != nullptr);
   a.s[0] = a.s[1] = a.s[2] = Scan{Q, K, V, out, nseg > 1 ? seg : S_in, S_out, dk, dv, 0, 0, 0, pb.scale, pb.scale, 1.f};
-  return run_scan(pb, a, 1);
+  return run_scan(pb, plan, a, 1);
 }
 
 dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K, const void* V, const float* log_decay,
                      const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out, void* dQ, void* dK,
                      void* dV, float* dS_in) {
   const int dk = pb.p.dk, dv = pb.p.dv;
-  int nseg, seg_len;
-  segments(pb, 3, dk > dv ? dk : dv, dk > dv ? dk : dv, &nseg, &seg_len);
+  const Plan plan = backward_plan(pb);
+  const int nseg = plan.nseg, seg_len = plan.seg_len;
   const size_t states = (size_t)pb.BH() * nseg * dk * dv;
   float* const sseg = nseg > 1 ? ar.take<float>(states) : nullptr;
   float* const gseg = nseg > 1 ? ar.take<float>(states) : nullptr;
-  if (ar.base == nullptr && nseg > 1) return DARK_OK;
   if (ar.overflow) return DARK_EWORKSPACE;
   const float s = pb.scale;
   const bool rev = dK != nullptr || dV != nullptr || dS_in != nullptr;
@@ -239,13 +301,13 @@ dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K,
   if (dK != nullptr) a.s[n++] = k;
   if (dk != dv && n > 0) {   // dV has other widths: a launch of its own
     for (int i = n; i < kMostScans; ++i) a.s[i] = a.s[0];
-    DARK_TRY(run_scan(pb, a, n));
+    DARK_TRY(run_scan(pb, plan, a, n));
     n = 0;
   }
   if (dV != nullptr || dS_in != nullptr) a.s[n++] = v;
   if (n == 0) return DARK_OK;
   for (int i = n; i < kMostScans; ++i) a.s[i] = a.s[0];
-  return run_scan(pb, a, n);
+  return run_scan(pb, plan, a, n);
 }
 
 dark_status step(const Problem& pb, const void* q, const void* k, const void* v, const float* log_decay, const int32_t* parent,
@@ -290,18 +352,13 @@ dark_status check_workspace(const void* ws, size_t ws_bytes, size_t need) {
   if (ws == nullptr || ws_bytes < need) return DARK_EWORKSPACE;
   return aligned(ws, 256) ? DARK_OK : DARK_EALIGN;
 }
-size_t measure(const decay::Problem& pb, bool bwd) {
-  int nseg, seg_len;
-  if (bwd) {
-    const int w = pb.p.dk > pb.p.dv ? pb.p.dk : pb.p.dv;
-    decay::segments(pb, 3, w, w, &nseg, &seg_len);
-  } else {
-    decay::segments(pb, 1, pb.p.dk, pb.p.dv, &nseg, &seg_len);
-  }
-  if (nseg == 1) return 0;
+// `in_place`: the forward call updates a state in place, or may.
+size_t measure(const decay::Problem& pb, bool bwd, bool in_place) {
+  const decay::Plan plan = bwd ? decay::backward_plan(pb) : decay::forward_plan(pb);
   Arena ar(nullptr, 0);
-  const size_t states = (size_t)pb.BH() * nseg * pb.p.dk * pb.p.dv;
-  for (int i = 0; i < (bwd ? 2 : 1); ++i) (void)ar.take<float>(states);
+  const size_t state = (size_t)pb.BH() * pb.p.dk * pb.p.dv;
+  if (plan.direct && !bwd && in_place) (void)ar.take<float>(state);
+  for (int i = 0; plan.nseg > 1 && i < (bwd ? 2 : 1); ++i) (void)ar.take<float>(state * plan.nseg);
   return ar.off;
 }
 }  // namespace
@@ -311,7 +368,7 @@ extern "C" {
 size_t dark_decay_workspace_bytes(const dark_decay_params* p, int backward) {
   decay::Problem pb;
   if (decay::check_params(p, &pb) != DARK_OK || pb.p.B == 0) return 0;
-  return measure(pb, backward != 0);
+  return measure(pb, backward != 0, true);
 }
 
 dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,
@@ -327,7 +384,7 @@ dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void
     return DARK_EALIGN;
   const size_t state = (size_t)pb.BH() * pb.p.dk * pb.p.dv * sizeof(float);
   if (S_in != S_out && overlap(S_in, state, S_out, state)) return DARK_EINVAL;
-  const size_t need = measure(pb, false);
+  const size_t need = measure(pb, false, S_in != nullptr && S_in == S_out);
   DARK_TRY(check_workspace(ws, ws_bytes, need));
   pb.st = static_cast<hipStream_t>(hip_stream);
   Arena ar(ws, ws_bytes);
@@ -347,7 +404,7 @@ dark_status dark_decay_bwd(const dark_decay_params* p, const void* Q, const void
     return DARK_EALIGN;
   const size_t state = (size_t)pb.BH() * pb.p.dk * pb.p.dv * sizeof(float);
   if (overlap(dS_in, state, dS_out, state) || overlap(dS_in, state, S_in, state)) return DARK_EINVAL;
-  const size_t need = measure(pb, true);
+  const size_t need = measure(pb, true, false);
   DARK_TRY(check_workspace(ws, ws_bytes, need));
   pb.st = static_cast<hipStream_t>(hip_stream);
   Arena ar(ws, ws_bytes);

@@ -174,8 +174,10 @@ struct Op<float> {
 // reads as zero and is not written, so that rows behind a sequence, columns behind the last and parts of a tile need no branches:
 // they are given offsets that are too large.
 typedef __amdgpu_buffer_rsrc_t Buffer;
+// (Extents of a chunk are wave-uniform; said so here, as the compiler loops over the lanes' values where it has computed one in a
+// vector register.)
 __device__ static inline Buffer buffer(const void* p, unsigned bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, (int)bytes, 0x00027000);
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, __builtin_amdgcn_readfirstlane((int)bytes), 0x00027000);
 }
 constexpr unsigned kNowhere = 0x80000000u;   // every extent is smaller (check_params)
 

@@ -41,20 +41,22 @@ def _run(p, layout="bhld", segments=0, scale=0.0, backward=True):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("L", [1, 2, 31, 33, 64, 65, 200])
+@pytest.mark.parametrize("L", [1, 2, 31, 33, 64, 65, 200, 515])
 def test_lengths(L, dtype):
-    _run(U.problem(L, 2, 3, L, 64, 64, dtype, state=True, dstate=True))
+    for segments in (0, 1):
+        _run(U.problem(L, 2, 3, L, 64, 64, dtype, state=True, dstate=True), segments=segments)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("widths", [(1, 1), (64, 128), (128, 64), (128, 128), (96, 80), (33, 65), (7, 200), (256, 64), (64, 256), (256, 256), (250, 131)])
 def test_widths(widths, dtype):
-    _run(U.problem(3, 1, 2, 150, *widths, dtype, state=True, dstate=True))
+    for segments in (0, 2):
+        _run(U.problem(3, 1, 2, 150, *widths, dtype, state=True, dstate=True), segments=segments)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("layout", ["bhld", "blhd"])
-@pytest.mark.parametrize("segments", [1, 2, 3, 100])
+@pytest.mark.parametrize("segments", [0, 1, 2, 3, 100])
 def test_segments_and_layouts(segments, layout, dtype):
     _run(U.problem(4, 2, 3, 333, 64, 64, dtype, lengths=[333, 191], state=True, dstate=True), layout, segments)
     _run(U.problem(5, 1, 2, 260, 40, 72, dtype), layout, segments)
@@ -63,7 +65,8 @@ def test_segments_and_layouts(segments, layout, dtype):
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("decay", [0.0, -1e-4, -1.0, -30.0, -1e5, -np.inf])
 def test_decays(decay, dtype):
-    _run(U.problem(6, 1, 2, 170, 64, 64, dtype, decay=[decay], state=True, dstate=True), segments=2)
+    for segments in (0, 2):
+        _run(U.problem(6, 1, 2, 170, 64, 64, dtype, decay=[decay], state=True, dstate=True), segments=segments)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -81,7 +84,7 @@ def test_ragged_batches_read_nothing_behind_a_sequence(lengths, dtype):
         for k, bad in zip(NAMES, (float("nan"), float("inf"), float("-inf"), float("nan"))):
             d[k][b, :, n:] = bad
     ref, size = U.oracle(p), U.oracle(p, magnitude=True)
-    for segments in (1, 3):
+    for segments in (0, 1, 3):
         out, last = _forward(d, segments=segments)
         g = _backward(d, segments=segments)
         torch.cuda.synchronize()
@@ -117,16 +120,18 @@ def test_long_sequences_by_the_library_s_own_segments(dtype):
 def test_state_in_place_and_continued_prompts():
     p = U.problem(10, 2, 2, 300, 64, 64, "bf16", state=True)
     d = _device(p)
-    out, last = _forward(d)
-    for segments in (1, 3):
+    want, size = U.oracle(p), U.oracle(p, magnitude=True)
+    # Against the oracle, not against another schedule: where the terms of an element nearly cancel, two schedules differ by the roundings
+    # of both, 2 * 2^-8 of the sum of its terms' magnitudes each, which no multiple of the element itself bounds.
+    for segments in (0, 1, 3):
         S = d["state"].clone()
         got, same = dk.dark_decay_fwd(d["Q"], d["K"], d["V"], d["a"], state=S, state_out=S, segments=segments)
         assert same is S
-        assert torch.allclose(got.float(), out.float(), rtol=2.0 ** -6, atol=2e-2) and torch.allclose(S, last, rtol=1e-4, atol=1e-4)
+        U.check(got, want["out"], size["out"], "bf16", "in place")
+        U.check(S, want["last"], size["last"], "f32", "state in place")
     # the same prompt in two calls
     first, S = dk.dark_decay_fwd(*(d[k][:, :, :111].contiguous() for k in "QKV"), d["a"], state=d["state"], want_state=True)
     second, S = dk.dark_decay_fwd(*(d[k][:, :, 111:].contiguous() for k in "QKV"), d["a"], state=S, want_state=True)
-    want, size = U.oracle(p), U.oracle(p, magnitude=True)
     U.check(torch.cat([first, second], 2), want["out"], size["out"], "bf16", "two calls")
     U.check(S, want["last"], size["last"], "f32", "state of two calls")
 
