@@ -153,7 +153,7 @@ struct Cost {
   float bf16, f32, step, pairs;
 };
 Cost cost_of(int d1, int d2) {
-  if (d1 > 128) return {5.2f, 8.2f, 2.9f, 120.f};
+  if (d1 > 128) return {3.9f, 7.2f, 2.9f, 120.f};
   if (d1 > 64) return d2 <= 64 ? Cost{2.6f, 4.5f, 1.8f, 250.f} : Cost{3.2f, 6.4f, 2.0f, 172.f};
   return d2 <= 64 ? Cost{1.9f, 2.8f, 1.4f, 335.f} : Cost{2.4f, 4.0f, 1.8f, 250.f};
 }

@@ -4,6 +4,8 @@
 // The state U [D1, D2] stays in the accumulators of the products that update it: each wave owns 16 of its columns, and what it
 // owns serves the next chunk's readout as an operand without a way through LDS: an accumulator tile holds rows 4 g ... + 3 of a column in
 // lane group g, an operand of two such tiles wants rows 8 g ... + 7, and two exchanges between the lane groups make one of the other.
+// With 256 rows a wave owns half of them, and the halves' readouts are joined through LDS: twice the waves on a CU whose LDS holds no
+// second workgroup (24 heads of 2048 x 256, values 64 wide: 48.6 -> 43 us).
 // Per chunk: P = x1 x2^T, decayed and masked, by all waves together through LDS; y^T = U^T x1^T + x3^T P^T; U' = g^C U + x2^T (w x3).
 // The next chunk's rows are on their way into registers meanwhile.
 #pragma once
@@ -242,21 +244,21 @@ struct Tile {
   }
 };
 
-// A wave's columns of a state [d1, d2] in memory (or of its transpose): rows 16 kt + 4 g ... + 3 of column c (behind the last: c >= d2).
+// A wave's columns of a state [d1, d2] in memory (or of its transpose): rows r0 + 16 kt + 4 g ... + 3 of column c (behind the last: c >= d2).
 template <int KT, bool VEC>
-__device__ static inline void load_state(f32x4 (&U)[KT], const float* p, int d1, int d2, int transposed, int c, int g) {
+__device__ static inline void load_state(f32x4 (&U)[KT], const float* p, int d1, int d2, int transposed, int c, int g, int r0 = 0) {
   const Buffer b = buffer(p, (unsigned)(d1 * d2) * 4u);
   if (!transposed) {
-    const unsigned off = c < d2 ? (unsigned)(4 * g * d2 + c) * 4u : kNowhere;
+    const unsigned off = c < d2 ? (unsigned)((r0 + 4 * g) * d2 + c) * 4u : kNowhere;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
       for (int j = 0; j < 4; ++j) U[kt][j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off + (unsigned)((16 * kt + j) * d2) * 4u, 0, 0));
   } else {
-    const unsigned off = c < d2 ? (unsigned)(c * d1 + 4 * g) * 4u : kNowhere;
+    const unsigned off = c < d2 ? (unsigned)(c * d1 + r0 + 4 * g) * 4u : kNowhere;
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) {
-      const int row = 16 * kt + 4 * g;   // rows behind the last would be the next column
+      const int row = r0 + 16 * kt + 4 * g;   // rows behind the last would be the next column
       if (VEC) {
         const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(b, row < d1 ? off + 64u * kt : kNowhere, 0, 0);
         __builtin_memcpy(&U[kt], &v, 16);
@@ -268,9 +270,9 @@ __device__ static inline void load_state(f32x4 (&U)[KT], const float* p, int d1,
   }
 }
 template <int KT>
-__device__ static inline void store_state(const f32x4 (&U)[KT], float* p, int d1, int d2, int c, int g) {
+__device__ static inline void store_state(const f32x4 (&U)[KT], float* p, int d1, int d2, int c, int g, int r0 = 0) {
   const Buffer b = buffer(p, (unsigned)(d1 * d2) * 4u);
-  const unsigned off = c < d2 ? (unsigned)(4 * g * d2 + c) * 4u : kNowhere;
+  const unsigned off = c < d2 ? (unsigned)((r0 + 4 * g) * d2 + c) * 4u : kNowhere;
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
@@ -293,20 +295,20 @@ __device__ static inline void hold() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// U <- U + x2^T (f w x3): the 16 columns of U that the wave owns.
-template <typename T, int C, int D1, int D2, bool EXACT>
-__device__ static inline void update(f32x4 (&U)[D1 / 16], int t2, int t3, int tw, float f, int wave, Lane l) {
+// U <- U + x2^T (f w x3): the 16 columns of U that the wave owns, of its half of the rows.
+template <typename T, int C, int D1, int D2, bool EXACT, int H = 1>
+__device__ static inline void update(f32x4 (&U)[D1 / 16 / H], int t2, int t3, int tw, float f, int wave, Lane l, int half = 0) {
   typedef Op<T> O;
   constexpr int kUsed = O::kPlanes == 3 && !EXACT ? 2 : O::kPlanes;
   constexpr int RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T);
-  const int b2 = O::template col_base<RB1>(l), b3 = O::template col_base<RB2>(l);
+  const int b2 = O::template col_base<RB1>(l) ^ (half * (RB1 / H)), b3 = O::template col_base<RB2>(l);
 #pragma unroll
   for (int ks = 0; ks < C / 32; ++ks) {
     typename O::frag x[O::kPlanes];
     const f32x4 w0 = f * lds_get<f32x4>(tw + 128 * ks + 32 * l.g), w1 = f * lds_get<f32x4>(tw + 128 * ks + 32 * l.g + 16);
     O::weighted(O::template col<RB2>(t3 + 32 * ks * RB2, b3, wave), w0, w1, x);
 #pragma unroll
-    for (int k0 = 0; k0 < D1 / 16; k0 += 4) {   // four sums at a time: a product does not wait for the one before it
+    for (int k0 = 0; k0 < D1 / 16 / H; k0 += 4) {   // four sums at a time: a product does not wait for the one before it
       typename O::frag k[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) k[i] = O::template col<RB1>(t2 + 32 * ks * RB1, b2, k0 + i);
@@ -319,8 +321,11 @@ __device__ static inline void update(f32x4 (&U)[D1 / 16], int t2, int t3, int tw
   }
 }
 
+constexpr int halves(int d1) { return d1 == 256 ? 2 : 1; }
 template <typename T, int D1, int D2>
-constexpr int scan_lds() { return Op<T>::kChunk * ((2 * D1 + D2 + Op<T>::kChunk) * (int)sizeof(T) + 12) + 64; }
+constexpr int scan_lds() {
+  return Op<T>::kChunk * ((2 * D1 + D2 + Op<T>::kChunk) * (int)sizeof(T) + 12) + 64 + (halves(D1) == 2 ? Op<T>::kChunk * D2 * 4 : 0);
+}
 template <typename T, int D1, int D2>
 constexpr int state_lds() { return Op<T>::kChunk * ((D1 + D2) * (int)sizeof(T) + 4); }
 
@@ -335,14 +340,16 @@ __device__ static inline Lane fresh(int lane) {
 }
 
 template <typename T, int D1, int D2, bool VEC, bool EXACT>
-__global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans A) {
+__global__ __launch_bounds__(4 * D2 * halves(D1), scan_waves(D1, D2)) void k_decay_scan(Scans A) {
   typedef Op<T> O;
-  constexpr int C = O::kChunk, QT = C / 16, KS = C / 32, KT = D1 / 16, K1 = D1 / 32, W = D2 / 16, NTH = 64 * W;
+  constexpr int H = halves(D1), C = O::kChunk, QT = C / 16, KS = C / 32, KT = D1 / 16 / H, K1 = D1 / 32, W = H * D2 / 16, NTH = 64 * W;
   constexpr int RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T), RBP = C * (int)sizeof(T);
   constexpr int t1 = 0, t2 = t1 + C * RB1, t3 = t2 + C * RB1, tp = t3 + C * RB2, tw = tp + C * RBP;
   constexpr int tl = tw + 4 * C;   // sr g^(r+1-off) of the chunk's rows
   constexpr int td = tl + 4 * C;   // sp g^(n - 15), n = 0 ... C + 14 (what stands before g^0 is not used)
+  constexpr int te = td + 4 * C + 64;   // readouts of the other half
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int part = wave % (D2 / 16), half = H == 2 ? wave / (D2 / 16) : 0;   // the wave's columns and rows of the state
   Scan a = A.s[0];
   if (blockIdx.z == 1) a = A.s[1];
   if (blockIdx.z == 2) a = A.s[2];
@@ -369,12 +376,12 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
   p2.load(x2, begin, min(C, last - begin), tid);
   p3.load(x3, begin, min(C, last - begin), tid);
 
-  // the state: rows 16 kt + 4 g ... + 3 of column col0 + 16 wave + lane % 16
+  // the state: rows 16 kt + 4 g ... + 3 of the wave's half, column col0 + 16 part + lane % 16
   f32x4 U[KT];
   const long long uat = (A.nseg > 1 ? (long long)bh * A.nseg + seg : bh) * a.d1 * a.d2;
-  const int uc = col0 + 16 * wave + (lane & 15);
+  const int uc = col0 + 16 * part + (lane & 15), ur = half * (D1 / H);
   if (a.u_in != nullptr) {
-    load_state<KT, VEC>(U, a.u_in + uat, a.d1, a.d2, a.transposed, uc, lane >> 4);
+    load_state<KT, VEC>(U, a.u_in + uat, a.d1, a.d2, a.transposed, uc, lane >> 4, ur);
   } else {
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) U[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -386,9 +393,36 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
   if (tid < C) lds_put(tl + 4 * tid, a.sr * power(a2, tid + 1 - a.off));
   const float gC = power(a2, C);
 
+  f32x4 out[QT];
+  // rows 16 qt + lane % 16 of the chunk at r0
+  const auto put_rows = [&](int r0, int nr, Lane l, int qt0, int step) {
+    const Buffer yb = y.rows(r0, nr);
+    const unsigned c = (unsigned)((16 * part + 4 * l.g) * (int)sizeof(T)), row = y.offset(l.i, nr);
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt) {
+      if (qt % step != qt0) continue;
+      const unsigned at = row + (unsigned)y.step(16 * qt);
+      if (VEC) {
+        O::store4(yb, c < y.width ? at + c : kNowhere, out[qt]);
+      } else {
+#pragma unroll
+        for (unsigned j = 0; j < 4; ++j) O::store1(yb, c + j * (unsigned)sizeof(T) < y.width ? at + c + j * (unsigned)sizeof(T) : kNowhere, out[qt][j]);
+      }
+    }
+  };
+  // Halves: each stores every second row tile, with what the other half has left of it in LDS.
+  const auto join_rows = [&](int r0, int nr) {
+    const Lane l = fresh(lane);
+#pragma unroll
+    for (int qt = 0; qt < QT; ++qt)
+      if (qt % 2 == half) out[qt] += lds_get<f32x4>(te + (part * QT + qt) * 1024 + 16 * (16 * l.g + l.i));
+    if (a.y != nullptr) put_rows(r0, nr, l, half, 2);
+  };
+
   for (int r0 = begin; r0 < last; r0 += C) {
     const int nr = min(C, last - r0);
     lds_barrier();   // the tiles' readers are done
+    if (H == 2 && r0 > begin) join_rows(r0 - C, C);
     p1.store(t1, tid);
     p2.store(t2, tid);
     p3.store(t3, tid);
@@ -421,13 +455,13 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
         hold();
       }
     }
-    f32x4 out[QT];
+    const int bu = b1 ^ (half * (RB1 / H));
 #pragma unroll
-    for (int k = 0; k < K1; ++k) {
+    for (int k = 0; k < K1 / H; ++k) {
       const typename O::frag u = O::state(U[2 * k], U[2 * k + 1]);
 #pragma unroll
       for (int qt = 0; qt < QT; ++qt)
-        out[qt] = O::mma(u, O::row(t1 + qt * 16 * RB1, b1, k), k > 0 ? out[qt] : f32x4{0.f, 0.f, 0.f, 0.f});
+        out[qt] = O::mma(u, O::row(t1 + qt * 16 * RB1, bu, k), k > 0 ? out[qt] : f32x4{0.f, 0.f, 0.f, 0.f});
       hold();
     }
 #pragma unroll
@@ -437,42 +471,42 @@ __global__ __launch_bounds__(4 * D2, scan_waves(D1, D2)) void k_decay_scan(Scans
       const int b3 = O::template col_base<RB2>(l), bp = O::template row_base<RBP>(l);
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const typename O::frag v = O::template col<RB2>(t3 + 32 * ks * RB2, b3, wave);
+        if (H == 2 && half != ks) continue;
+        const typename O::frag v = O::template col<RB2>(t3 + 32 * ks * RB2, b3, part);
 #pragma unroll
         for (int qt = 2 * ks; qt < QT; ++qt) out[qt] = O::mma(v, O::row(tp + qt * 16 * RBP, bp, ks), out[qt]);
         hold();
       }
     }
-    if (a.y != nullptr) {
-      const Buffer yb = y.rows(r0, nr);
-      const unsigned c = (unsigned)((16 * wave + 4 * l.g) * (int)sizeof(T)), row = y.offset(l.i, nr);
+    if (H == 2) {
 #pragma unroll
-      for (int qt = 0; qt < QT; ++qt) {
-        const unsigned at = row + (unsigned)y.step(16 * qt);
-        if (VEC) {
-          O::store4(yb, c < y.width ? at + c : kNowhere, out[qt]);
-        } else {
-#pragma unroll
-          for (unsigned j = 0; j < 4; ++j) O::store1(yb, c + j * (unsigned)sizeof(T) < y.width ? at + c + j * (unsigned)sizeof(T) : kNowhere, out[qt][j]);
-        }
-      }
+      for (int qt = 0; qt < QT; ++qt)
+        if (qt % 2 != half) lds_put(te + (part * QT + qt) * 1024 + 16 * (16 * l.g + l.i), out[qt]);
+    } else if (a.y != nullptr) {
+      put_rows(r0, nr, l, 0, 1);
     }
     if (r0 + C < last || (last == n && a.u_out != nullptr)) {
       const float gn = nr < C ? power(a2, nr) : gC;
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) U[kt] *= gn;
-      update<T, C, D1, D2, EXACT>(U, t2, t3, tw, 1.f, wave, l);
+      update<T, C, D1, D2, EXACT, H>(U, t2, t3, tw, 1.f, part, l, half);
     }
   }
-  if (last == n && a.u_out != nullptr) store_state<KT>(U, a.u_out + (long long)bh * a.d1 * a.d2, a.d1, a.d2, uc, lane >> 4);
+  if (H == 2 && last > begin) {
+    lds_barrier();
+    const int r0 = begin + (last - begin - 1) / C * C;
+    join_rows(r0, last - r0);
+  }
+  if (last == n && a.u_out != nullptr) store_state<KT>(U, a.u_out + (long long)bh * a.d1 * a.d2, a.d1, a.d2, uc, lane >> 4, ur);
 }
 
 template <typename T, int D1, int D2, bool VEC, bool EXACT>
-__global__ __launch_bounds__(4 * D2, state_waves(D1)) void k_decay_state(States A) {
+__global__ __launch_bounds__(4 * D2 * halves(D1), state_waves(D1)) void k_decay_state(States A) {
   typedef Op<T> O;
-  constexpr int C = O::kChunk, KT = D1 / 16, NTH = 4 * D2;
+  constexpr int H = halves(D1), C = O::kChunk, KT = D1 / 16 / H, NTH = 4 * D2 * H;
   constexpr int t2 = 0, t3 = t2 + C * D1 * (int)sizeof(T), tw = t3 + C * D2 * (int)sizeof(T);
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int part = wave % (D2 / 16), half = H == 2 ? wave / (D2 / 16) : 0;
   State a = A.s[0];
   if (blockIdx.z == 1) a = A.s[1];
   const int segs = A.nseg - 1, bh = blockIdx.x / segs, seg = blockIdx.x % segs, b = bh / A.H, h = bh % A.H, col0 = blockIdx.y * D2;
@@ -500,9 +534,9 @@ __global__ __launch_bounds__(4 * D2, state_waves(D1)) void k_decay_state(States 
       p2.load(x2, r0 - C, C, tid);
       p3.load(x3, r0 - C, C, tid);
     }
-    update<T, C, D1, D2, EXACT>(U, t2, t3, tw, power(a2, end - C - r0), wave, fresh(lane));
+    update<T, C, D1, D2, EXACT, H>(U, t2, t3, tw, power(a2, end - C - r0), part, fresh(lane), half);
   }
-  store_state<KT>(U, a.seg + ((long long)bh * A.nseg + seg) * a.d1 * a.d2, a.d1, a.d2, col0 + 16 * wave + (lane & 15), lane >> 4);
+  store_state<KT>(U, a.seg + ((long long)bh * A.nseg + seg) * a.d1 * a.d2, a.d1, a.d2, col0 + 16 * part + (lane & 15), lane >> 4, half * (D1 / H));
 }
 
 template <typename T, int D1, int D2, bool VEC, bool EXACT>
@@ -510,7 +544,7 @@ static dark_status launch(const Scans& a, int n, hipStream_t st) {
   constexpr int lds = scan_lds<T, D1, D2>();
   DARK_TRY(allow_lds(k_decay_scan<T, D1, D2, VEC, EXACT>, lds));
   const dim3 grid((unsigned)((long long)a.B * a.H * a.nseg), (unsigned)((a.s[0].d2 + D2 - 1) / D2), (unsigned)n);
-  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_scan<T, D1, D2, VEC, EXACT>), grid, dim3(4 * D2), lds, a);
+  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_scan<T, D1, D2, VEC, EXACT>), grid, dim3(4 * D2 * halves(D1)), lds, a);
   return DARK_OK;
 }
 template <typename T, int D1, int D2, bool VEC, bool EXACT>
@@ -518,7 +552,7 @@ static dark_status launch(const States& a, int n, hipStream_t st) {
   constexpr int lds = state_lds<T, D1, D2>();
   DARK_TRY(allow_lds(k_decay_state<T, D1, D2, VEC, EXACT>, lds));
   const dim3 grid((unsigned)((long long)a.B * a.H * (a.nseg - 1)), (unsigned)((a.s[0].d2 + D2 - 1) / D2), (unsigned)n);
-  DARK_LAUNCH(KID_DECAY_STATE, st, (k_decay_state<T, D1, D2, VEC, EXACT>), grid, dim3(4 * D2), lds, a);
+  DARK_LAUNCH(KID_DECAY_STATE, st, (k_decay_state<T, D1, D2, VEC, EXACT>), grid, dim3(4 * D2 * halves(D1)), lds, a);
   return DARK_OK;
 }
 
