@@ -307,12 +307,14 @@ dark_status dark_decode_step(const dark_params* p, const void* q, const void* k,
  *   Q, K: [B, H, L, dk], V, out: [B, H, L, dv] in io_dtype with layout DARK_BHLD, or [B, L, H, dk] and [B, L, H, dv] with
  *   DARK_BLHD (as a projection lays them out); all of them in the same layout.
  *   log_decay: [H] float32, the natural logarithm of the decay: 0 keeps everything, -infinity nothing but the token itself.
- *   A decay is a constant of the model: there is no gradient with respect to it.  Values above 0 are computed as they are.
+ *   A decay is a constant of the model: there is no gradient with respect to it.  Values above 0 are computed as
+ *   they are; it must not be NaN or +infinity.
  *   lengths: [B] int32 or NULL (every sequence has L tokens).  Sequence b has its first lengths[b] rows, values outside
  *   0 ... L count as the nearer of the two.  What lies behind a sequence in Q, K, V and dOut is not read; out and the
  *   gradients are 0 there.
  *   States are float32, [B, H, dk, dv].  S_in NULL: zero.  S_out NULL: not wanted.  S_out is the state behind the last
- *   token; S_out == S_in updates a state in place, any other overlap is DARK_EINVAL.
+ *   token; S_out == S_in updates a state in place.  Any other overlap of a result with an operand or another result is
+ *   DARK_EINVAL, here and in the calls below.
  * dk and dv up to 256 (else DARK_EUNSUPPORTED), of any size; rows of whole 16 bytes are faster.  L == 0: the state is passed on.
  *
  * Arithmetic: fp32 operands are multiplied and summed in fp32.  bf16 operands go through the matrix units with fp32 sums; the
@@ -342,14 +344,14 @@ dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void
 /*
  * Gradients of sum(out dOut) + sum(S_out dS_out).  dS_out NULL: zero.  dQ, dK, dV have the element type and layout of what
  * they belong to (a product of bf16 operands has no more than its precision); dS_in: float32.  All are overwritten; each may be
- * NULL (skipped).  dS_in may not overlap dS_out or S_in (DARK_EINVAL).  Nothing is needed from the forward call.
+ * NULL (skipped).  Nothing is needed from the forward call.
  */
 dark_status dark_decay_bwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,
                            const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out,
                            void* dQ, void* dK, void* dV, float* dS_in, void* ws, size_t ws_bytes, void* hip_stream);
 
 /*
- * One token: q, k [B, H, dk], v, out [B, H, dv] in io_dtype; p->L and p->layout are ignored; q, k, v and out need
+ * One token: q, k [B, H, dk], v, out [B, H, dv] in io_dtype; p->L and p->layout, of the model's other calls, do not matter; q, k, v and out need
  * the alignment of their elements only.  No workspace.  fp32 arithmetic.
  * parent NULL: row b of S_out is the next state of row b of S_in (state_rows == B; S_out == S_in updates in place).
  * parent [B] int32: row b continues row parent[b] of S_in [state_rows, H, dk, dv], so that beams change places, and one
@@ -366,7 +368,7 @@ dark_status dark_decay_step(const dark_decay_params* p, const void* q, const voi
  *   logits [B, n, V] in io_dtype, scores [B, n] float32 (log-probabilities so far), finished [B, n] bytes or NULL.
  *   out_scores [B, n] float32, out_parent and out_token [B, n] int32, best first; with keep_slots != 0 instead so that a beam's best
  *   successor has the beam's own place (then out_parent[j] == j wherever beam j survives, and dark_state_reorder moves
- *   the other places only), the further ones, best first, the places left over, lowest first.  out_scores may be scores.
+ *   the other places only), the further ones, best first, the places left over, lowest first.  out_scores may be scores (no other overlap: DARK_EINVAL).
  *   A finished beam has the one candidate (j, eos) of value scores[j]; its logits are not read.  Logits that are -infinity or
  *   NaN, a score that is not finite (a beam not in use: -infinity), and rows whose logits are all -infinity or
  *   hold +infinity make candidates of value -infinity: such ones are taken, in the order of j and t, only where there are too few others.
@@ -387,7 +389,8 @@ dark_status dark_beam_select(const dark_beam_params* p, const void* logits, cons
  * The states of the beams follow their parents, in place: of each of the `count` tensors [B, n, ...] of row_bytes[i] bytes for one beam
  * (the recurrent states of dark_decode_step and dark_decay_step, or anything else kept for a beam) row (b, j) becomes what row
  * (b, parent[b][j]) was before the call.  A parent outside 0 ... n - 1 leaves its row as it is.
- *   parent: [B, n] int32 in device memory; states and row_bytes: host arrays, read before the call returns; tensors must not overlap.
+ *   parent: [B, n] int32 in device memory; states and row_bytes: host arrays, read before the call returns.  Tensors that overlap each
+ *   other or parent are DARK_EINVAL.
  * n <= 32, B <= 65535 (else DARK_EUNSUPPORTED).  Sixteen tensors a launch.
  */
 dark_status dark_state_reorder(int B, int n, const int32_t* parent, int count, void* const* states, const size_t* row_bytes,

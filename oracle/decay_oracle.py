@@ -60,7 +60,7 @@ def beam_select(logits, scores, finished=None, eos=0, keep_slots=False):
             value = np.full(V, -np.inf)
         else:
             top = row.max()
-            value = score - (top + np.log(np.exp(row - top).sum())) + row
+            value = score - np.log(np.exp(row - top).sum()) + (row - top)
         cand.append(value)
     cand = np.concatenate(cand)
     best = np.lexsort((np.arange(cand.size), -cand))[:n]

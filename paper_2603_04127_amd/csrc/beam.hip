@@ -62,6 +62,12 @@ __device__ __forceinline__ bool finite(float v) { return v > -INFINITY && v < IN
 constexpr int kMostBeams = 32;
 constexpr float kLog2e = 1.4426950408889634f;
 
+// A maximum m so large that the rounding of c = m L (below) would be more than an eighth of an exponent, or c infinite (a row masked
+// by the type's lowest value): exponents are (v - m) L instead, two roundings and an instruction more.
+__device__ __forceinline__ bool large(float m) { return fabsf(m) > 1048576.f; }
+// c of a sum of 2^(v L - c)
+__device__ __forceinline__ double origin(float m) { return large(m) ? (double)m * (double)kLog2e : (double)(m * kLog2e); }
+
 // The first `count` lanes of a wave hold a candidate each: every one counts those before it (larger, or equal with a lower token) and
 // takes that place in the list if it is one of the n.  Token -1 behind the last.
 __device__ __forceinline__ void place(unsigned key, int token, int count, Entry* list, int n, int lane) {
@@ -166,7 +172,10 @@ __global__ __launch_bounds__(256, 4) void k_beam_rows(const T* __restrict__ logi
   const float m = top != 0 ? value_of(top) : -INFINITY;
   // sum of 2^(v L - c) with c = m L, L = log2 e in fp32: one rounding of the exponent; k_beam_pick takes c as it is here
   float s = 0.f;
-  if (finite(m)) {
+  if (finite(m) && large(m)) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaxf((v[e] - m) * kLog2e, -200.f));
+  } else if (finite(m)) {
     const float c = m * kLog2e;
 #pragma unroll
     for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaxf(fmaf(v[e], kLog2e, -c), -200.f));   // 2^-200 vanishes beside the maximum's 1
@@ -270,6 +279,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = blockIdx.x, count = n * slices;
   Entry* const near = reinterpret_cast<Entry*>(smem);
   __shared__ double offset[kMostBeams];
+  __shared__ float tops[kMostBeams];
   __shared__ int kind[kMostBeams];
   __shared__ Head gathered[kMostGathered];
   __shared__ Head picks[kMostBeams];
@@ -309,16 +319,17 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
     if (live && finite(top))
       for (int i = t; i < slices; i += 32) {
         const Part p = i == t ? mine : parts[row * slices + i];
-        if (p.sum > 0.f) z += (double)p.sum * exp2((double)(p.top * kLog2e) - (double)(top * kLog2e));
+        if (p.sum > 0.f) z += (double)p.sum * exp2(origin(p.top) - origin(top));
       }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) z += __shfl_xor(z, o, 64);
     if (t == 0 && j < n) {
       const bool alive = live && finite(top);
       kind[j] = alive ? kAlive : done && finite(score) ? kFinished : kDead;
-      // log sum exp = ln 2 (c + log2 z), where the exponents v L of the terms that matter stand for v log2 e near v = top
-      const double c = (double)(top * kLog2e) + (double)top * (1.4426950408889634074 - (double)kLog2e);
+      // log sum exp(v - top) = ln 2 (c - top L + log2 z), where the exponents v L of the terms that matter stand for v log2 e near v = top
+      const double c = origin(top) - (double)top * (double)kLog2e;
       offset[j] = alive ? (double)score - 0.69314718055994530942 * (c + log2(z)) : (double)score + 0.0;
+      tops[j] = top;
     }
   }
   __syncthreads();
@@ -329,7 +340,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
     if (kind[j] == kAlive) {
       const Entry e = staged ? near[l * n + at] : own[(long long)l * n + at];
       if (e.token < 0) return hd;
-      hd.key = ordered64(offset[j] + (double)e.logit + 0.0);   // one zero
+      hd.key = ordered64(offset[j] + ((double)e.logit - (double)tops[j]) + 0.0);   // one zero
       hd.flat = (unsigned)j * (unsigned)V + (unsigned)e.token;
     } else if (kind[j] == kFinished && l % slices == 0 && at == 0) {   // a finished beam goes on with `eos` alone
       hd.key = ordered64(offset[j]);
@@ -542,6 +553,11 @@ dark_status dark_beam_select(const dark_beam_params* p, const void* logits, cons
   Arena ar(ws, ws_bytes);
   if (ws == nullptr || ws_bytes < dark_beam_workspace_bytes(p)) return DARK_EWORKSPACE;
   if (!aligned(ws, 256)) return DARK_EALIGN;
+  const size_t beams = (size_t)p->B * p->n;
+  const Span next{out_scores, 4 * beams}, past{scores, 4 * beams};
+  if (overlap({next, {out_parent, 4 * beams}, {out_token, 4 * beams}}, {{logits, beams * p->V * (p->io_dtype == DARK_BF16 ? 2 : 4)}, {finished, beams}}) ||
+      overlap({{out_parent, 4 * beams}, {out_token, 4 * beams}}, {past}) || (out_scores != scores && overlap(next, past)))
+    return DARK_EINVAL;
   beam::Part* parts;
   beam::Entry* lists;
   beam::plan(*p, ar, &parts, &lists);
@@ -568,6 +584,13 @@ dark_status dark_state_reorder(int B, int n, const int32_t* parent, int count, v
     if (states[i] == nullptr) return DARK_EINVAL;
     if (row_bytes[i] > ((size_t)1 << 38)) return DARK_EUNSUPPORTED;
     if (!aligned(states[i], 16)) return DARK_EALIGN;
+  }
+  const size_t beams = (size_t)B * n;
+  for (int i = 0; i < count; ++i) {
+    const Span own{states[i], row_bytes[i] * beams};
+    if (overlap(own, {parent, 4 * beams})) return DARK_EINVAL;
+    for (int j = 0; j < i; ++j)
+      if (overlap(own, {states[j], row_bytes[j] * beams})) return DARK_EINVAL;
   }
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   for (int i = 0; i < count;) {

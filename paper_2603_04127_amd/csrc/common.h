@@ -120,6 +120,26 @@ struct Problem {
 // Parameter validation shared by all entry points (no HIP call).
 dark_status check_params(const dark_params* p, Problem* out);
 inline bool aligned(const void* q, size_t a) { return (reinterpret_cast<uintptr_t>(q) & (a - 1)) == 0; }
+// Memory of an argument; none: null, or no bytes.
+struct Span {
+  const void* at;
+  size_t bytes;
+};
+inline bool overlap(const Span& a, const Span& b) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.at), y = reinterpret_cast<uintptr_t>(b.at);
+  return a.at != nullptr && b.at != nullptr && a.bytes > 0 && b.bytes > 0 && x < y + b.bytes && y < x + a.bytes;
+}
+// Whether one of the results lies on another, or on an operand.
+template <int R, int N>
+inline bool overlap(const Span (&results)[R], const Span (&operands)[N]) {
+  for (int i = 0; i < R; ++i) {
+    for (int j = 0; j < i; ++j)
+      if (overlap(results[i], results[j])) return true;
+    for (int j = 0; j < N; ++j)
+      if (overlap(results[i], operands[j])) return true;
+  }
+  return false;
+}
 
 // M[h] = I for every head, into a [H, d, d] fp32 buffer (generic.hip).
 dark_status fill_identity(const Problem& pb, float* Mid);

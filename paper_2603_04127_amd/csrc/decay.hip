@@ -1,5 +1,6 @@
 // Linear attention with a decay for each head: argument checks, the plan of a call, the prefix over segment states and the
 // one-token recurrence.  The scan itself is in decay_scan.h.
+#include <algorithm>
 #include <cmath>
 
 #include "decay.h"
@@ -56,6 +57,7 @@ __device__ __forceinline__ void st(float* p, float v) { *p = v; }
 __device__ __forceinline__ void st(unsigned short* p, float v) { *p = (unsigned short)fz::pack_bf16(v, 0.f); }
 
 constexpr int kMostWidth = 256;
+constexpr long long kMostGroups = 1 << 22;   // along a grid's x: of 512 threads each they stay under the 2^32 that a launch can have
 constexpr int kAhead = 8;   // rows in flight a thread
 
 template <typename T, int W>
@@ -129,7 +131,7 @@ dark_status check_params(const dark_decay_params* p, Problem* out) {
   if (p->io_dtype != DARK_F32 && p->io_dtype != DARK_BF16) return DARK_EINVAL;
   if (p->layout != DARK_BHLD && p->layout != DARK_BLHD) return DARK_EINVAL;
   if (!(p->scale >= 0.f) || std::isinf(p->scale) || p->sched_segments < 0) return DARK_EINVAL;
-  if (p->dk > kMostWidth || p->dv > kMostWidth || (long long)p->B * p->H > (1 << 22) || p->L > (1 << 30)) return DARK_EUNSUPPORTED;
+  if (p->dk > kMostWidth || p->dv > kMostWidth || (long long)p->B * p->H > kMostGroups || p->L > (1 << 30)) return DARK_EUNSUPPORTED;
   // a chunk's rows are addressed by 32-bit offsets: 64 rows of all heads stay under 2^31 bytes
   if (p->layout == DARK_BLHD && (long long)p->H * (p->dk > p->dv ? p->dk : p->dv) > (1 << 22)) return DARK_EUNSUPPORTED;
   out->p = *p;
@@ -171,12 +173,13 @@ Plan plan_of(const Problem& pb, int scans, int states) {
   const float c = p.io_dtype == DARK_BF16 ? cost.bf16 : cost.f32;
   const float heads = (float)pb.BH() * (float)(d1 > 128 || d2 <= 64 ? (d2 + 63) / 64 : (d2 + 127) / 128);
   Plan best;
+  const int most = (int)std::min(64LL, std::max(1LL, kMostGroups / pb.BH()));
   if (p.sched_segments > 0) {
     best.nseg = p.sched_segments < chunks ? p.sched_segments : chunks;
-    if (best.nseg > 64) best.nseg = 64;
+    best.nseg = best.nseg < most ? best.nseg : most;
   } else {
     float least = 0.f;
-    for (int s = 1; s <= chunks && s <= 64; ++s) {
+    for (int s = 1; s <= chunks && s <= most; ++s) {
       const int each = (chunks + s - 1) / s;
       if (s > 1 && (chunks + each - 1) / each != s) continue;   // the same chunks a segment as with fewer
       float rounds = std::ceil(scans * heads * s / 256.f);
@@ -191,7 +194,7 @@ Plan plan_of(const Problem& pb, int scans, int states) {
         best.nseg = s;
       }
     }
-    if (p.io_dtype == DARK_BF16 && chunks >= 2 && chunks <= 16) {
+    if (p.io_dtype == DARK_BF16 && chunks >= 2 && chunks <= 16 && pb.BH() * (chunks + 4) <= kMostGroups) {
       const float pairs = scans * heads * (float)(chunks * (chunks + 1) / 2) / cost.pairs, steps = (float)((chunks + 1) / 2) * cost.step;
       if (6.f + (pairs > steps ? pairs : steps) < least) {
         best.direct = true;
@@ -343,10 +346,19 @@ dark_status step(const Problem& pb, const void* q, const void* k, const void* v,
 using namespace dark;
 
 namespace {
-bool overlap(const void* a, size_t na, const void* b, size_t nb) {
-  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
-  return a != nullptr && b != nullptr && x < y + nb && y < x + na;
-}
+size_t size_of(const dark_decay_params& p) { return p.io_dtype == DARK_BF16 ? 2 : 4; }
+// Bytes of Q or K, of V, of a state.
+struct Sizes {
+  size_t k, v, state, decay, lengths;
+  explicit Sizes(const decay::Problem& pb) {
+    const size_t rows = (size_t)pb.BH() * pb.p.L * size_of(pb.p);
+    k = rows * pb.p.dk;
+    v = rows * pb.p.dv;
+    state = (size_t)pb.BH() * pb.p.dk * pb.p.dv * sizeof(float);
+    decay = (size_t)pb.p.H * sizeof(float);
+    lengths = (size_t)pb.p.B * sizeof(int32_t);
+  }
+};
 dark_status check_workspace(const void* ws, size_t ws_bytes, size_t need) {
   if (need == 0) return DARK_OK;
   if (ws == nullptr || ws_bytes < need) return DARK_EWORKSPACE;
@@ -382,10 +394,13 @@ dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void
   if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(out, 16) || !aligned(S_in, 16) || !aligned(S_out, 16) ||
       !aligned(log_decay, 4) || !aligned(lengths, 4))
     return DARK_EALIGN;
-  const size_t state = (size_t)pb.BH() * pb.p.dk * pb.p.dv * sizeof(float);
-  if (S_in != S_out && overlap(S_in, state, S_out, state)) return DARK_EINVAL;
+  const Sizes n(pb);
+  if (S_in != S_out && overlap({S_in, n.state}, {S_out, n.state})) return DARK_EINVAL;
   const size_t need = measure(pb, false, S_in != nullptr && S_in == S_out);
   DARK_TRY(check_workspace(ws, ws_bytes, need));
+  if (overlap({{out, n.v}, {S_out, n.state}}, {{Q, n.k}, {K, n.k}, {V, n.v}, {log_decay, n.decay}, {lengths, n.lengths}}) ||
+      overlap({out, n.v}, {S_in, n.state}))
+    return DARK_EINVAL;
   pb.st = static_cast<hipStream_t>(hip_stream);
   Arena ar(ws, ws_bytes);
   return decay::forward(pb, ar, Q, K, V, log_decay, lengths, S_in, out, S_out);
@@ -402,10 +417,13 @@ dark_status dark_decay_bwd(const dark_decay_params* p, const void* Q, const void
   if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(dOut, 16) || !aligned(S_in, 16) || !aligned(dS_out, 16) ||
       !aligned(dQ, 16) || !aligned(dK, 16) || !aligned(dV, 16) || !aligned(dS_in, 16) || !aligned(log_decay, 4) || !aligned(lengths, 4))
     return DARK_EALIGN;
-  const size_t state = (size_t)pb.BH() * pb.p.dk * pb.p.dv * sizeof(float);
-  if (overlap(dS_in, state, dS_out, state) || overlap(dS_in, state, S_in, state)) return DARK_EINVAL;
+  const Sizes n(pb);
+  if (overlap({dS_in, n.state}, {dS_out, n.state}) || overlap({dS_in, n.state}, {S_in, n.state})) return DARK_EINVAL;
   const size_t need = measure(pb, true, false);
   DARK_TRY(check_workspace(ws, ws_bytes, need));
+  if (overlap({{dQ, n.k}, {dK, n.k}, {dV, n.v}, {dS_in, n.state}}, {{Q, n.k}, {K, n.k}, {V, n.v}, {dOut, n.v}, {S_in, n.state}, {dS_out, n.state},
+                                                                    {log_decay, n.decay}, {lengths, n.lengths}}))
+    return DARK_EINVAL;
   pb.st = static_cast<hipStream_t>(hip_stream);
   Arena ar(ws, ws_bytes);
   return decay::backward(pb, ar, Q, K, V, log_decay, lengths, S_in, dOut, dS_out, dQ, dK, dV, dS_in);
@@ -415,15 +433,20 @@ dark_status dark_decay_step(const dark_decay_params* p, const void* q, const voi
                             const int32_t* parent, int state_rows, const float* S_in, float* S_out, void* out, void* hip_stream) {
   decay::Problem pb;
   DARK_TRY(decay::check_params(p, &pb));
+  pb.p.L = 1;
   if (pb.p.B == 0) return DARK_OK;
   if (!q || !k || !v || !log_decay || !S_in || !S_out || !out) return DARK_EINVAL;
   if (parent == nullptr ? state_rows != pb.p.B : state_rows <= 0) return DARK_EINVAL;
-  const size_t elem = pb.p.io_dtype == DARK_BF16 ? 2 : 4;   // rows of one tensor, slices of a longer one: no more is asked of them
+  const size_t elem = size_of(pb.p);   // rows of one tensor, slices of a longer one: no more is asked of them
   if (!aligned(q, elem) || !aligned(k, elem) || !aligned(v, elem) || !aligned(out, elem) || !aligned(S_in, 16) || !aligned(S_out, 16) ||
       !aligned(log_decay, 4) || !aligned(parent, 4))
     return DARK_EALIGN;
-  const size_t row = (size_t)pb.p.H * pb.p.dk * pb.p.dv * sizeof(float);
-  if ((parent != nullptr || S_in != S_out) && overlap(S_in, row * state_rows, S_out, row * pb.p.B)) return DARK_EINVAL;
+  const Sizes n(pb);
+  const size_t past = n.state / pb.p.B * state_rows;
+  if ((parent != nullptr || S_in != S_out) && overlap({S_in, past}, {S_out, n.state})) return DARK_EINVAL;
+  if (overlap({{out, n.v}, {S_out, n.state}}, {{q, n.k}, {k, n.k}, {v, n.v}, {log_decay, n.decay}, {parent, n.lengths}}) ||
+      overlap({out, n.v}, {S_in, past}))
+    return DARK_EINVAL;
   pb.st = static_cast<hipStream_t>(hip_stream);
   return decay::step(pb, q, k, v, log_decay, parent, state_rows, S_in, S_out, out);
 }

@@ -124,6 +124,29 @@ def test_reorder_refusals():
     assert f(0, 4, A, 2, ptrs, sizes, None) == dk.DARK_OK and f(1, 4, A, 0, None, None, None) == dk.DARK_OK
 
 
+def test_results_lie_on_nothing_else():
+    far = [A + (i << 20) for i in range(16)]   # every argument a place of its own, then one result on another argument
+    fwd, bwd, step, select, reorder = (getattr(dk.lib(), "dark_" + name) for name in ("decay_fwd", "decay_bwd", "decay_step", "beam_select", "state_reorder"))
+    args = far[:6] + far[6:8] + [None, 0, None]   # Q, K, V, log_decay, lengths, S_in; out, S_out
+    for result, other in [(6, j) for j in range(6)] + [(7, j) for j in (0, 1, 2, 3, 4, 6)]:
+        assert fwd(_p(), *(far[other] if i == result else x for i, x in enumerate(args))) == dk.DARK_EINVAL, (result, other)
+    assert fwd(_p(), *(far[2] + 64 * 8 * 4 - 16 if i == 6 else x for i, x in enumerate(args))) == dk.DARK_EINVAL   # out begins in V's last row
+    args = far[:12] + [None, 0, None]   # Q, K, V, log_decay, lengths, S_in, dOut, dS_out; dQ, dK, dV, dS_in
+    for result in range(8, 12):
+        for other in range(result):
+            assert bwd(_p(), *(far[other] if i == result else x for i, x in enumerate(args))) == dk.DARK_EINVAL, (result, other)
+    args = far[:5] + [1] + far[6:9] + [None]   # q, k, v, log_decay, parent, rows, S_in; S_out, out
+    for result, other in [(7, j) for j in (0, 1, 2, 3, 4, 6)] + [(8, j) for j in (0, 1, 2, 3, 4, 6, 7)]:
+        assert step(_p(), *(far[other] if i == result else x for i, x in enumerate(args))) == dk.DARK_EINVAL, (result, other)
+    args = far[:6] + [WS, BIG, None]   # logits, scores, finished; scores, parents, tokens
+    for result, other in ((3, 0), (3, 2), (4, 0), (4, 1), (4, 2), (4, 3), (5, 0), (5, 1), (5, 2), (5, 3), (5, 4)):
+        assert select(_b(), *(far[other] if i == result else x for i, x in enumerate(args))) == dk.DARK_EINVAL, (result, other)
+    assert select(_b(), far[0], far[1], None, far[1] + 4, far[4], far[5], WS, BIG, None) == dk.DARK_EINVAL   # scores, shifted
+    sizes = (ctypes.c_size_t * 3)(64, 64, 64)
+    for places in ((A, A, far[1]), (A, far[1], A + 3 * 64), (far[1], far[2], far[3] - 16)):   # twice the same, the last row, the parents
+        assert reorder(1, 4, far[3], 3, (ctypes.c_void_p * 3)(*places), sizes, None) == dk.DARK_EINVAL
+
+
 def test_binding_refusals():
     x, a = torch.zeros(2, 3, 10, 16), torch.zeros(3)
     with pytest.raises(ValueError, match="layout"):

@@ -65,6 +65,19 @@ def test_masked_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [300, 20000])
+def test_logits_near_the_end_of_the_type(V, dtype):
+    logits, scores = _problem(9, 4, 4, V, dtype)
+    low, high = torch.finfo(logits.dtype).min, torch.finfo(logits.dtype).max
+    logits[0, 1] = low               # a row masked as a whole: every token has the same share
+    logits[1] = low
+    logits[1, 2, 17] = low / 2
+    logits[2, 0, [3, V - 1]] = high  # two tokens share everything, the others end below the range: -infinity, or nearly
+    logits[3] *= 2.0 ** 20           # large, but not so large that log2 e is too much
+    _check(logits, scores)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("kind", [torch.uint8, torch.bool])
 def test_finished_beams(kind, dtype):
     logits, scores = _problem(4, 4, 4, 1500, dtype)
