@@ -129,6 +129,26 @@ def test_reorder_many_tensors_and_none():
     dk.dark_state_reorder([torch.empty(2, 0, device="cuda")], parent)
 
 
+def test_offsets_beyond_32_bits():
+    B, n, V = 1081, 8, 249999
+    g = torch.Generator(device="cuda").manual_seed(7)
+    logits = torch.zeros(B, n, V, dtype=torch.bfloat16, device="cuda")
+    assert logits.numel() > 1 << 31
+    logits[-1] = torch.randn(n, V, generator=g, device="cuda")
+    scores = -torch.rand(B, n, generator=g, device="cuda")
+    s, p, t = dk.dark_beam_select(logits, scores)
+    ws, wp, wt = dk.dark_beam_select(logits[-1:].clone(), scores[-1:].clone())   # smaller slices: sums of 2^-22 in another order
+    assert torch.equal(p[-1:], wp) and torch.equal(t[-1:], wt) and ((s[-1:] - ws).abs() <= 2 * 2.0 ** -21 + 2.0 ** -23 * ws.abs()).all()
+    assert (t[0] == torch.arange(n, device="cuda")).all() and (p[0] == scores[0].argmax()).all()   # equal logits: the best beam's first tokens
+    states = torch.zeros(40, 4, 1 << 23, device="cuda")
+    states[-1] = torch.randn(4, 1 << 23, generator=g, device="cuda")
+    want = states[-1].clone()
+    parent = torch.arange(4, dtype=torch.int32, device="cuda").repeat(40, 1)
+    parent[-1] = torch.tensor([2, 2, 0, 1])
+    dk.dark_state_reorder([states], parent)
+    assert torch.equal(states[-1], want[parent[-1].long()]) and not states[0].any()
+
+
 def _search(step, reorder, logits_of, B, n, V, steps, keep_slots):
     """Beam search with `step` (token features in, outputs back) and `reorder` (parents)."""
     scores = torch.full((B, n), float("-inf"))

@@ -257,3 +257,45 @@ def test_captured_calls_replay():
         got = [t.clone() for t in held]
         _forward(other)   # eager work between the replays
         assert all(torch.equal(x, y) for x, y in zip(got, work()))
+
+
+# ---------------------------------------------------------------------------
+# tensors of more than 2^32 bytes: the last sequence against a call of its own, by the same schedule
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("layout", ["bhld", "blhd"])
+@pytest.mark.parametrize("dtype,L,segments", [("bf16", 66000, 5), ("bf16", 520, 0), ("f32", 33000, 5)])
+def test_offsets_beyond_32_bits(dtype, L, segments, layout):
+    H, d = 16, 128
+    B = (1 << 32) // (H * L * d * (2 if dtype == "bf16" else 4)) + 2
+    shape = (B, H, L, d) if layout == "bhld" else (B, L, H, d)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    x = [torch.zeros(shape, dtype=U.TORCH[dtype], device="cuda") for _ in range(4)]
+    for t in x:
+        t[-1] = torch.randn(shape[1:], generator=g, device="cuda")
+    a = -0.01 * torch.arange(H, device="cuda")
+    kw = dict(layout=layout, segments=segments or 1)
+    out, state = dk.dark_decay_fwd(*x[:3], a, want_state=True, **kw)
+    grads = dk.dark_decay_bwd(*x[:3], a, x[3], state=state, **kw)
+    alone = [t[-1:].clone() for t in x]
+    want, last = dk.dark_decay_fwd(*alone[:3], a, want_state=True, **kw)
+    assert torch.equal(out[-1:], want) and torch.equal(state[-1:], last) and not out[0].any()
+    for name, t in dk.dark_decay_bwd(*alone[:3], a, alone[3], state=last, **kw).items():
+        assert torch.equal(grads[name][-1:], t), name
+    if not segments:   # the library's own choice: another order of sums, within the bounds of both (1.01: the magnitudes are rounded themselves)
+        size = dk.dark_decay_fwd(*(t.abs() for t in alone[:3]), a, **kw).float()
+        assert ((dk.dark_decay_fwd(*x[:3], a, layout=layout)[-1:].float() - want.float()).abs() <= 2 * 1.01 * U.ABS["bf16"] * size).all()
+
+
+def test_step_offsets_beyond_32_bits():
+    B, H, d = 1026, 16, 256
+    g = torch.Generator(device="cuda").manual_seed(6)
+    past, S = (torch.zeros(B, H, d, d, device="cuda") for _ in range(2))
+    past[-1] = torch.randn(H, d, d, generator=g, device="cuda")
+    q, k, v = (torch.randn(B, H, d, generator=g, device="cuda") for _ in range(3))
+    a = -0.01 * torch.arange(H, device="cuda")
+    parent = torch.zeros(B, dtype=torch.int32, device="cuda")
+    parent[-1] = B - 1
+    out = dk.dark_decay_step(q, k, v, a, past, parent=parent, state_out=S)
+    want = torch.exp(a)[:, None, None].double() * past[-1].double() + k[-1].double()[:, :, None] * v[-1].double()[:, None]
+    assert torch.allclose(S[-1].double(), want, rtol=1e-6, atol=1e-6)
+    assert torch.allclose(out[-1].double(), (want * q[-1].double()[:, :, None]).sum(1) / 16, rtol=1e-5, atol=1e-4)
