@@ -633,9 +633,9 @@ def dark_state_reorder(states, parent):
     index, ptrs = _pointers(parent, *states)
     sizes = (ctypes.c_size_t * count)()
     for i, t in enumerate(states):
-        if t.shape[0] != B * n and t.shape[:2] != (B, n):
+        if t.shape[:1] != (B * n,) and t.shape[:2] != (B, n):
             raise ValueError("a state must have a row for each beam")
-        sizes[i] = t.numel() * t.element_size() // (B * n) if B else 0
+        sizes[i] = t.numel() * t.element_size() // (B * n) if B * n else 0
     if index != torch._C._cuda_getDevice():
         with torch.cuda.device(index):
             return dark_state_reorder(states, parent)

@@ -29,11 +29,18 @@ __global__ __launch_bounds__(256) void k_decay_prefix(States A) {
   vec U = 0.f;
   if (a.u_in != nullptr) U = *reinterpret_cast<const vec*>(a.u_in + bh * size + e);
   float* const s = a.seg + (long long)bh * A.nseg * size + e;
-#pragma unroll 4
-  for (int i = 0; i < used - 1; ++i) {
-    const vec own = *reinterpret_cast<const vec*>(s + i * size);
-    *reinterpret_cast<vec*>(s + i * size) = U;
-    U = gl * U + own;
+  constexpr int kAtOnce = 8;
+  for (int i0 = 0; i0 < used - 1; i0 += kAtOnce) {
+    vec own[kAtOnce];
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) own[i] = *reinterpret_cast<const vec*>(s + min(i0 + i, used - 2) * size);
+#pragma unroll
+    for (int i = 0; i < kAtOnce; ++i) {
+      if (i0 + i < used - 1) {
+        *reinterpret_cast<vec*>(s + (i0 + i) * size) = U;
+        U = gl * U + own[i];
+      }
+    }
   }
   *reinterpret_cast<vec*>(s + (long long)(used - 1) * size) = U;
 }
