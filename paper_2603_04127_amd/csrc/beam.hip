@@ -100,20 +100,27 @@ __device__ __forceinline__ float number(const T* row, long long t, int V) {
 }
 
 // A slice is 256 E elements of a row; thread t holds pieces t, t + 256, ... of 16 bytes.  Rows begin where they begin: the slices
-// count from the 16-byte boundary at or before the row's first element.  Elements that are not the row's are NaN: like a NaN among
-// the logits they lose every comparison.  Lists hold what is larger than -infinity.
-// A wave's n largest: the n-th largest of its lanes' maxima bounds them from below, so that a comparison each is all that most
-// elements cost; the few that pass are compacted into one a lane and placed.  Where more than 64 pass (many equal ones, or the largest
-// in few lanes) they are looked for one after the other in memory.
-// (32 x 8 rows of 131,071, n = 8: 70 us when every wave took its largest out one by one.)
+// count from the 16-byte boundary at or before the row's first element.  Elements that are not the row's are -infinity, which like a NaN
+// among the logits loses every comparison: lists hold what is larger than -infinity.
+// The slice's n largest: the n-th largest of 64 groups' maxima (a lane of each of the four waves) bounds them from below, so that a
+// comparison each is all that most elements cost; the few that pass are collected and each counts those before it.  Where more than 64
+// pass (many equal ones, or the largest in few lanes) they are looked for one after the other in memory.
+// Vector instructions bound it for bf16, memory for fp32.  Hence: 16-bit elements stay packed, and in two passes of three the upper one
+// of a pair is taken with the lower one's bits behind it, which no comparison between such numbers minds; a NaN costs the sum a
+// second pass instead of every element an instruction.
+// (32 x 8 rows of 131,071, n = 8: 70 us when every wave took its largest out one by one, 25 with a list for every wave.)
 constexpr int kMostPassed = 64;
 template <typename T, int E>
-__global__ __launch_bounds__(256, 4) void k_beam_rows(const T* __restrict__ logits, const float* __restrict__ scores,
+__global__ __launch_bounds__(256, 8) void k_beam_rows(const T* __restrict__ logits, const float* __restrict__ scores,
                                                       const unsigned char* __restrict__ finished, Part* __restrict__ parts,
                                                       Entry* __restrict__ lists, int n, int V, long long total) {
   constexpr int P = 16 / (int)sizeof(T), N = E / P;
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, slice = blockIdx.x, slices = gridDim.x, row = blockIdx.y;
+  constexpr bool k16 = sizeof(T) == 2;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slice = blockIdx.x, slices = gridDim.x, row = blockIdx.y;
   if ((finished != nullptr && finished[row] != 0) || !finite(scores[row])) return;   // k_beam_pick knows what these offer
+  // Bit 9 of MODE, IEEE, off: a maximum of a signalling NaN (which an infinity with another element's bits behind it is, too) and a
+  // number is the number.
+  __builtin_amdgcn_s_setreg(1 | 9 << 6, 0);
   const long long first = (long long)row * V, base = first / P * P + (long long)slice * 256 * E;
   const long long whole = total / P * P;   // behind it: an unfinished piece, which is read element by element
   const T* const own = logits + first;
@@ -137,32 +144,35 @@ __global__ __launch_bounds__(256, 4) void k_beam_rows(const T* __restrict__ logi
       }
     }
   }
-  float v[E];
+  const auto word = [&](int e) -> unsigned { return r[e / P][e % P * (int)sizeof(T) / 4]; };
+  const auto number_of = [](unsigned w, int e) { return __uint_as_float(!k16 ? w : e & 1 ? w & 0xffff0000u : w << 16); };
+  const auto rough = [](unsigned w, int e) { return __uint_as_float(!k16 || (e & 1) ? w : w << 16); };   // the lower one's bits behind the upper
+  const auto anew = [&]() {   // 16-bit elements are unpacked where they are used, not held unpacked from one pass to the next
 #pragma unroll
-  for (int i = 0; i < N; ++i)
-#pragma unroll
-    for (int j = 0; j < P; ++j) {
-      if constexpr (sizeof(T) == 2) v[i * P + j] = __uint_as_float(j & 1 ? r[i][j / 2] & 0xffff0000u : r[i][j / 2] << 16);
-      else v[i * P + j] = __uint_as_float(r[i][j]);
-    }
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(r[i]));
+  };
   if (begin < 0 || begin + 256 * E > V) {   // the row's ends
     int t0 = begin + tid * P;
     asm volatile("" : "+v"(t0));   // nothing is computed ahead for the slices within
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int t = t0 + e / P * 256 * P + e % P;
-      v[e] = (unsigned)t < (unsigned)V ? v[e] : NAN;
+      const unsigned w = word(e), out = !k16 ? 0xff800000u : e & 1 ? (w & 0xffffu) | 0xff800000u : (w & 0xffff0000u) | 0xff80u;
+      r[e / P][e % P * (int)sizeof(T) / 4] = (unsigned)t < (unsigned)V ? w : out;
     }
   }
+  __shared__ unsigned tops[4], maxima[4][64], least_key;
+  __shared__ float sums[4];
+  __shared__ int counts[4];
+  __shared__ Entry passed[4][kMostPassed];
+  __shared__ u64 best_of[4];
   // the maximum
   float best = NAN;
 #pragma unroll
-  for (int e = 0; e < E; ++e) best = fmaxf(best, v[e]);
+  for (int e = 0; e < E; e += 2) best = fmaxf(fmaxf(best, rough(word(e), e)), rough(word(e + 1), e + 1));
+  if (k16) best = __uint_as_float(__float_as_uint(best) & 0xffff0000u);
   const unsigned mine = best == best ? ordered(best) : 0u;
-  __shared__ unsigned tops[4];
-  __shared__ float sums[4];
-  __shared__ Entry passed[4][kMostPassed];
-  __shared__ Entry taken[4][kMostBeams];
+  maxima[wave][lane] = mine;
   const unsigned wtop = wave_max(mine);
   if (lane == 0) tops[wave] = wtop;
   __syncthreads();
@@ -170,86 +180,103 @@ __global__ __launch_bounds__(256, 4) void k_beam_rows(const T* __restrict__ logi
 #pragma unroll
   for (int i = 1; i < 4; ++i) top = tops[i] > top ? tops[i] : top;
   const float m = top != 0 ? value_of(top) : -INFINITY;
+  const bool chooses = wave == (slice & 3);   // one wave of the four, on every SIMD in turn
+  if (chooses) {
+    unsigned group = maxima[0][lane];
+#pragma unroll
+    for (int i = 1; i < 4; ++i) group = maxima[i][lane] > group ? maxima[i][lane] : group;
+    const unsigned bound = nth_of_lanes(group, n, lane), lowest = ordered(-3.402823466e38f);
+    if (lane == 0) least_key = bound > lowest ? bound : lowest;
+  }
+  anew();
   // sum of 2^(v L - c) with c = m L, L = log2 e in fp32: one rounding of the exponent; k_beam_pick takes c as it is here
   float s = 0.f;
-  if (finite(m) && large(m)) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaxf((v[e] - m) * kLog2e, -200.f));
-  } else if (finite(m)) {
+  if (finite(m)) {
+    const bool far = large(m);
     const float c = m * kLog2e;
+    if (far) {
 #pragma unroll
-    for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaxf(fmaf(v[e], kLog2e, -c), -200.f));   // 2^-200 vanishes beside the maximum's 1
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((number_of(word(e), e) - m) * kLog2e);
+    } else {
+#pragma unroll
+      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(number_of(word(e), e), kLog2e, -c));
+    }
+    if (__ballot(s != s) != 0) {   // a NaN counts for nothing
+      s = 0.f;
+#pragma unroll 1
+      for (int k = 0; k < N; ++k)
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+          const float v = number(own, begin + (k * 256 + tid) * P + j, V);
+          s += v == v ? __builtin_amdgcn_exp2f(far ? (v - m) * kLog2e : fmaf(v, kLog2e, -c)) : 0.f;
+        }
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < E; ++e) s += number_of(word(e), e) == INFINITY ? INFINITY : 0.f;
   }
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
   if (lane == 0) sums[wave] = s;
-  // the wave's n largest
-  const unsigned bound = nth_of_lanes(mine, n, lane), lowest = ordered(-3.402823466e38f);
-  const float least = value_of(bound > lowest ? bound : lowest);
+  __syncthreads();
+  anew();
+  const float least = value_of(least_key);
+  // for an upper element with other bits behind it: those that equal the bound lie up to 2^16 below its bits if it is negative
+  const float least_rough = !k16 || least > 0.f ? least : __uint_as_float(__float_as_uint(least) | 0x8000ffffu);
   int count = 0;
 #pragma unroll
   for (int e = 0; e < E; ++e) {
-    const u64 pass = __ballot(v[e] >= least);
+    const bool in = rough(word(e), e) >= (e & 1 ? least_rough : least);
+    const u64 pass = __ballot(in);
     if (pass != 0) {
       const int at = count + __builtin_amdgcn_mbcnt_hi((unsigned)(pass >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)pass, 0u));
-      if (v[e] >= least && at < kMostPassed) passed[wave][at] = Entry{v[e], begin + (e / P * 256 + tid) * P + e % P};
+      if (in && at < kMostPassed) passed[wave][at] = Entry{number_of(word(e), e), begin + (e / P * 256 + tid) * P + e % P};
       count += __builtin_popcountll(pass);
     }
   }
-  if (count <= kMostPassed) {
-    __builtin_amdgcn_wave_barrier();
-    Entry e{0.f, 0};
-    if (lane < count) e = passed[wave][lane];
-    place(ordered(e.logit + 0.f), e.token, count, taken[wave], n, lane);   // + 0: one zero
-  } else {
-    u64 last = ~0ull;   // the one found before
-    for (int i = 0; i < n; ++i) {
-      u64 next = 0;
-#pragma unroll 1
-      for (int k = 0; k < N; ++k) {
-        const int t = begin + (k * 256 + tid) * P;
-        float e[P];
-#pragma unroll
-        for (int j = 0; j < P; ++j) e[j] = number(own, t + j, V);
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-          const float x = e[j] + 0.f;
-          const u64 key = x >= least ? (u64)ordered(x) << 32 | (unsigned)~(t + j) : 0;
-          if (key < last && key > next) next = key;
-        }
-      }
-      const unsigned hi = wave_max((unsigned)(next >> 32));
-      const unsigned lo = wave_max((unsigned)(next >> 32) == hi ? (unsigned)next : 0u);
-      last = (u64)hi << 32 | lo;
-      if (lane == 0) taken[wave][i] = hi != 0 ? Entry{value_of(hi), (int)~lo} : Entry{0.f, -1};
-      if (hi == 0) break;
-    }
-  }
+  if (lane == 0) counts[wave] = count;
   __syncthreads();
-  if (tid == 0) parts[(long long)row * slices + slice] = Part{m, (sums[0] + sums[1]) + (sums[2] + sums[3])};
-  // the slice's n largest out of the waves'
-  if (wave == 0) {
-    Entry* const list = lists + ((long long)row * slices + slice) * n;
-    // lanes 0-3 stand for the waves' lists and show their first entries left
-    int at = 0;
-    Entry e{0.f, -1};
-    if (lane < 4) e = taken[lane][0];
-    for (int i = 0; i < n; ++i) {
-      const unsigned key = e.token >= 0 ? ordered(e.logit) : 0u;
-      const unsigned w = wave_max(key);
-      if (w == 0) {
-        if (lane == 0) list[i] = Entry{0.f, -1};
-        break;
-      }
-      int low = 0x7fffffff;
-      for (u64 h = __ballot(key == w); h != 0; h &= h - 1) low = min(low, __builtin_amdgcn_readlane(e.token, __builtin_ctzll(h)));
-      if (key == w && e.token == low) {
-        list[i] = e;
-        ++at;
-        e = Entry{0.f, -1};
-        if (at < n) e = taken[lane][at];
+  if (tid == 0) {
+    const float sum = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    parts[(long long)row * slices + slice] = Part{sum < INFINITY ? m : INFINITY, sum};   // an infinite logit
+  }
+  Entry* const list = lists + ((long long)row * slices + slice) * n;
+  const int c0 = counts[0], c1 = c0 + counts[1], c2 = c1 + counts[2], all = c2 + counts[3];
+  if (all <= kMostPassed) {
+    if (chooses) {
+      const int of = (lane >= c0) + (lane >= c1) + (lane >= c2), at = lane - (of == 0 ? 0 : of == 1 ? c0 : of == 2 ? c1 : c2);
+      Entry e{0.f, 0};
+      if (lane < all) e = passed[of][at];
+      place(ordered(e.logit + 0.f), e.token, all, list, n, lane);   // + 0: one zero
+    }
+    return;
+  }
+  u64 last = ~0ull;   // the one found before
+  for (int i = 0; i < n; ++i) {
+    u64 next = 0;
+#pragma unroll 1
+    for (int k = 0; k < N; ++k) {
+      const int t = begin + (k * 256 + tid) * P;
+      float e[P];
+#pragma unroll
+      for (int j = 0; j < P; ++j) e[j] = number(own, t + j, V);
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const float x = e[j] + 0.f;
+        const u64 key = x >= least ? (u64)ordered(x) << 32 | (unsigned)~(t + j) : 0;
+        if (key < last && key > next) next = key;
       }
     }
+    const unsigned hi = wave_max((unsigned)(next >> 32));
+    const unsigned lo = wave_max((unsigned)(next >> 32) == hi ? (unsigned)next : 0u);
+    if (lane == 0) best_of[wave] = (u64)hi << 32 | lo;
+    __syncthreads();
+    last = best_of[0];
+#pragma unroll
+    for (int k = 1; k < 4; ++k) last = best_of[k] > last ? best_of[k] : last;
+    if (tid == 0) list[i] = last != 0 ? Entry{value_of((unsigned)(last >> 32)), (int)~(unsigned)last} : Entry{0.f, -1};
+    if (last == 0) break;
+    __syncthreads();
   }
 }
 

@@ -65,6 +65,24 @@ def test_masked_rows(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [301, 20001])
+def test_infinities_and_nan_beside_numbers(V, dtype):
+    logits, scores = _problem(10, 6, 4, V, dtype)
+    inf = float("inf")
+    bits = logits.view(torch.int16 if dtype == "bf16" else torch.int32)
+    bits[0, :, 1::3] = 0x7F81 if dtype == "bf16" else 0x7F800001   # signalling NaN in each half of a word, at every lane
+    logits[1, :, 0::2] = -inf
+    logits[2, :, 1::2] = -inf
+    logits[3] = -3.0 + 0.01 * logits[3]              # below zero, and close together
+    logits[4, 0, 5], logits[4, 1, 6], logits[4, 2] = inf, inf, -inf
+    logits[4, 2, [8, 9]] = torch.tensor([inf, 1.0], dtype=logits.dtype)
+    logits[4, 3, :] = -inf
+    logits[4, 3, V - 1] = -0.0
+    logits[5] = torch.where(logits[5] > 0, 0.0, -0.0)   # both zeros
+    _check(logits, scores)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("V", [300, 20000])
 def test_logits_near_the_end_of_the_type(V, dtype):
     logits, scores = _problem(9, 4, 4, V, dtype)
