@@ -4,7 +4,7 @@
 // Selection, per batch entry with n beams: candidate (j, t) is worth score_j + logit_jt - log sum_u exp logit_ju; the n largest win,
 // equal ones by the lowest j, then the lowest t.  k_beam_rows reads every logit once: a workgroup takes a slice of a row and leaves
 // the slice's maximum, its sum of exponentials and its n largest logits in order.  k_beam_pick joins the sums of a batch entry's
-// rows and merges the sorted lists from their heads.  Bound by reading the logits; few rows are cut into more slices.
+// rows and takes the best of the sorted lists.
 // Two candidates of different beams may lie closer together than fp32 resolves: offsets and comparisons are in fp64.
 #include <cmath>
 
@@ -99,7 +99,7 @@ __device__ __forceinline__ float number(const T* row, long long t, int V) {
   else return row[t];
 }
 
-// A slice is 256 E elements of a row; thread t holds pieces t, t + 256, ... of 16 bytes.  Rows begin where they begin: the slices
+// A slice is 8192 elements of a row; thread t holds pieces t, t + 256, ... of 16 bytes.  Rows begin where they begin: the slices
 // count from the 16-byte boundary at or before the row's first element.  Elements that are not the row's are -infinity, which like a NaN
 // among the logits loses every comparison: lists hold what is larger than -infinity.
 // The slice's n largest: the n-th largest of 64 groups' maxima (a lane of each of the four waves) bounds them from below, so that a
@@ -108,25 +108,27 @@ __device__ __forceinline__ float number(const T* row, long long t, int V) {
 // Vector instructions bound it for bf16, memory for fp32.  Hence: 16-bit elements stay packed, and in two passes of three the upper one
 // of a pair is taken with the lower one's bits behind it, which no comparison between such numbers minds; a NaN costs the sum a
 // second pass instead of every element an instruction.
-// (32 x 8 rows of 131,071, n = 8: 70 us when every wave took its largest out one by one, 25 with a list for every wave.)
-constexpr int kMostPassed = 64;
-template <typename T, int E>
+// (32 x 8 rows of 131,071, n = 8: 70 us when every wave took its largest out one by one, 25 with a list for every wave, 19.5 now.
+// Slices of 2048: as many lists more for k_beam_pick; 1 x 4 rows of 32,000 4.1 + 6.2 us against 4.6 + 5.4, 1 x 8 of 131,071 4.7 + 10.9
+// against 5.8 + 6.7, 16 x 8 of them 19 + 12 against 12.4 + 7.3.  Of 16,384: no faster, and more registers for fp32.)
+constexpr int kMostPassed = 64, kEach = 32, kSlice = 256 * kEach;
+template <typename T>
 __global__ __launch_bounds__(256, 8) void k_beam_rows(const T* __restrict__ logits, const float* __restrict__ scores,
                                                       const unsigned char* __restrict__ finished, Part* __restrict__ parts,
                                                       Entry* __restrict__ lists, int n, int V, long long total) {
-  constexpr int P = 16 / (int)sizeof(T), N = E / P;
+  constexpr int E = kEach, P = 16 / (int)sizeof(T), N = E / P;
   constexpr bool k16 = sizeof(T) == 2;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), slice = blockIdx.x, slices = gridDim.x, row = blockIdx.y;
   if ((finished != nullptr && finished[row] != 0) || !finite(scores[row])) return;   // k_beam_pick knows what these offer
   // Bit 9 of MODE, IEEE, off: a maximum of a signalling NaN (which an infinity with another element's bits behind it is, too) and a
   // number is the number.
   __builtin_amdgcn_s_setreg(1 | 9 << 6, 0);
-  const long long first = (long long)row * V, base = first / P * P + (long long)slice * 256 * E;
+  const long long first = (long long)row * V, base = first / P * P + (long long)slice * kSlice;
   const long long whole = total / P * P;   // behind it: an unfinished piece, which is read element by element
   const T* const own = logits + first;
   const int begin = (int)(base - first);   // token of the slice's first element
   u32x4 r[N];
-  if (base + 256 * E <= whole) {
+  if (base + kSlice <= whole) {
 #pragma unroll
     for (int i = 0; i < N; ++i) r[i] = *reinterpret_cast<const u32x4*>(logits + base + (i * 256 + tid) * P);
   } else {   // the tensor's end
@@ -151,7 +153,7 @@ __global__ __launch_bounds__(256, 8) void k_beam_rows(const T* __restrict__ logi
 #pragma unroll
     for (int i = 0; i < N; ++i) asm volatile("" : "+v"(r[i]));
   };
-  if (begin < 0 || begin + 256 * E > V) {   // the row's ends
+  if (begin < 0 || begin + kSlice > V) {   // the row's ends
     int t0 = begin + tid * P;
     asm volatile("" : "+v"(t0));   // nothing is computed ahead for the slices within
 #pragma unroll
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(256, 8) void k_beam_rows(const T* __restrict__ logi
 // ---------------------------------------------------------------------------
 // One workgroup a batch entry.  List l of the n * slices belongs to beam l / slices.  The n-th best of the lanes' best list heads bounds
 // the n best from below; the few entries that reach it are gathered, and each counts those before it.  Where too many do, the best is
-// looked for n times.
+// looked for n times.  Bound by latency: 5 us (one entry, 4 beams) to 11 (8 beams, 512 lists).
 // ---------------------------------------------------------------------------
 constexpr int kMostLists = 8704;
 constexpr int kStaged = 48 * 1024;   // bytes of lists that are brought to LDS at once (else they are read where they are)
@@ -472,7 +474,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
 
 // ---------------------------------------------------------------------------
 // States in place: a thread holds the same 16 (4, 1) bytes of every row that changes, so that all are read before any is written.
-// Bound by reading the parents of the rows that change and writing those rows.
+// Bound by reading the parents of the rows that change and writing those rows (8 x 4 beams, two layers of 16 x 256 x 128: 86 MB in 17 us).
 // ---------------------------------------------------------------------------
 constexpr int kMostTensors = 16;
 struct Tensors {
@@ -483,22 +485,32 @@ struct Tensors {
   int count;
 };
 
+// Rows by buffer instructions without branches: of a row that stays where it is nothing exists, so that no byte of it is moved.
+// (With a branch a row the eight's kernel took 226 registers: 4 x 8 rows of 2 MB twice 42 us.)
+__device__ __forceinline__ void get(u32x4& v, __amdgpu_buffer_rsrc_t b, unsigned at) { v = __builtin_amdgcn_raw_buffer_load_b128(b, at, 0, 0); }
+__device__ __forceinline__ void get(unsigned& v, __amdgpu_buffer_rsrc_t b, unsigned at) { v = __builtin_amdgcn_raw_buffer_load_b32(b, at, 0, 0); }
+__device__ __forceinline__ void get(unsigned char& v, __amdgpu_buffer_rsrc_t b, unsigned at) { v = __builtin_amdgcn_raw_buffer_load_b8(b, at, 0, 0); }
+__device__ __forceinline__ void put(u32x4 v, __amdgpu_buffer_rsrc_t b, unsigned at) { __builtin_amdgcn_raw_buffer_store_b128(v, b, at, 0, 0); }
+__device__ __forceinline__ void put(unsigned v, __amdgpu_buffer_rsrc_t b, unsigned at) { __builtin_amdgcn_raw_buffer_store_b32(v, b, at, 0, 0); }
+__device__ __forceinline__ void put(unsigned char v, __amdgpu_buffer_rsrc_t b, unsigned at) { __builtin_amdgcn_raw_buffer_store_b8(v, b, at, 0, 0); }
+
+// Bytes at ... of the rows, 256 units of them at most.
 template <typename U, int N>
 __device__ __forceinline__ void reorder(char* rows, long long row_bytes, long long at, const int32_t* from, int n) {
+  const int bytes = (int)min(row_bytes - at, 256LL * (long long)sizeof(U));
+  const unsigned own = threadIdx.x * (unsigned)sizeof(U);
   U v[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    if (j < n) {
-      const int p = from[j];
-      if (p != j && (unsigned)p < (unsigned)n) v[j] = *reinterpret_cast<const U*>(rows + p * row_bytes + at);
-    }
+    const int p = from[min(j, n - 1)];
+    const bool moves = j < n && p != j && (unsigned)p < (unsigned)n;
+    get(v[j], __builtin_amdgcn_make_buffer_rsrc(rows + (moves ? p : 0) * row_bytes + at, 0, moves ? bytes : 0, 0x00027000), own);
   }
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    if (j < n) {
-      const int p = from[j];
-      if (p != j && (unsigned)p < (unsigned)n) *reinterpret_cast<U*>(rows + j * row_bytes + at) = v[j];
-    }
+    const int p = from[min(j, n - 1)];
+    const bool moves = j < n && p != j && (unsigned)p < (unsigned)n;
+    put(v[j], __builtin_amdgcn_make_buffer_rsrc(rows + (moves ? j : 0) * row_bytes + at, 0, moves ? bytes : 0, 0x00027000), own);
   }
 }
 
@@ -506,8 +518,7 @@ template <int N>
 __global__ __launch_bounds__(256) void k_state_reorder(Tensors t, const int32_t* __restrict__ parent, int n) {
   int i = 0;
   while (i + 1 < t.count && (int)blockIdx.x >= t.first[i + 1]) ++i;
-  const long long at = ((long long)((int)blockIdx.x - t.first[i]) * 256 + threadIdx.x) * t.unit[i], row_bytes = t.row_bytes[i];
-  if (at >= row_bytes) return;
+  const long long at = (long long)((int)blockIdx.x - t.first[i]) * 256 * t.unit[i], row_bytes = t.row_bytes[i];
   char* const rows = t.data[i] + (long long)blockIdx.y * n * row_bytes;
   const int32_t* const from = parent + (long long)blockIdx.y * n;
   if (t.unit[i] == 16) reorder<u32x4, N>(rows, row_bytes, at, from, n);
@@ -515,14 +526,9 @@ __global__ __launch_bounds__(256) void k_state_reorder(Tensors t, const int32_t*
   else reorder<unsigned char, N>(rows, row_bytes, at, from, n);
 }
 
-// Elements a thread holds: 32, or 8 where the rows are too few to give every CU two workgroups.
-int slice_elements(const dark_beam_params& p) {
-  const long long rows = (long long)p.B * p.n;
-  return rows * ((p.V + 8191) / 8192) >= 512 ? 32 : 8;
-}
 int slices_of(const dark_beam_params& p) {
-  const int per = p.io_dtype == DARK_BF16 ? 8 : 4, len = 256 * slice_elements(p);
-  return (int)(((long long)p.V + per - 1 + len - 1) / len);   // a row begins up to per - 1 elements behind its first slice
+  const int per = p.io_dtype == DARK_BF16 ? 8 : 4;
+  return (int)(((long long)p.V + per - 1 + kSlice - 1) / kSlice);   // a row begins up to per - 1 elements behind its first slice
 }
 
 dark_status check(const dark_beam_params* p) {
@@ -544,11 +550,7 @@ dark_status rows(const dark_beam_params& p, const void* logits, const float* sco
                  Entry* lists, hipStream_t st) {
   const dim3 grid(slices_of(p), p.B * p.n);
   const long long total = (long long)p.B * p.n * p.V;
-  if (slice_elements(p) == 32) {
-    DARK_LAUNCH(KID_BEAM_ROWS, st, (k_beam_rows<T, 32>), grid, dim3(256), 0, static_cast<const T*>(logits), scores, finished, parts, lists, p.n, p.V, total);
-  } else {
-    DARK_LAUNCH(KID_BEAM_ROWS, st, (k_beam_rows<T, 8>), grid, dim3(256), 0, static_cast<const T*>(logits), scores, finished, parts, lists, p.n, p.V, total);
-  }
+  DARK_LAUNCH(KID_BEAM_ROWS, st, k_beam_rows<T>, grid, dim3(256), 0, static_cast<const T*>(logits), scores, finished, parts, lists, p.n, p.V, total);
   return DARK_OK;
 }
 

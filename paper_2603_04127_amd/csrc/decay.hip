@@ -14,7 +14,8 @@ using fz::fast_exp2;
 using fz::kLog2e;
 
 // The states before every segment, in place of the segments' own: U_0 = u_in, U_(s+1) = g^len U_s + seg_s.  One thread an element
-// (four where they divide), segment by segment; bound by reading and writing the states once.
+// (four where they divide), segment by segment, eight of them asked for at once; bound by reading and writing the states once (64 heads of
+// 128 x 128, 8 segments: 63 MB in 12 us, the rate of a copy), few states by a launch and two trips to memory (4 us).
 template <int W>
 __global__ __launch_bounds__(256) void k_decay_prefix(States A) {
   typedef float vec __attribute__((ext_vector_type(W)));
@@ -51,7 +52,8 @@ __global__ __launch_bounds__(256) void k_decay_copy(const float* __restrict__ fr
 }
 
 // ---------------------------------------------------------------------------
-// One token: S <- g S + k v^T, out = scale S^T q, for the columns of a workgroup.  Bound by reading and writing the state once.
+// One token: S <- g S + k v^T, out = scale S^T q, for the columns of a workgroup.  Bound by reading and writing the state once
+// (64 x 32 states of 128 x 128, beams that share parents: 271 MB in 45 us; 16 states 4.6 us, a launch).
 // 256 threads as `tx` units of W columns by 256 / tx rows; every thread sums its rows' share of the output, LDS joins the shares.
 // ---------------------------------------------------------------------------
 template <typename T>
