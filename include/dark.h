@@ -310,8 +310,8 @@ dark_status dark_decode_step(const dark_params* p, const void* q, const void* k,
  *   A decay is a constant of the model: there is no gradient with respect to it.  Values above 0 are computed as
  *   they are; it must not be NaN or +infinity.
  *   lengths: [B] int32 or NULL (every sequence has L tokens).  Sequence b has its first lengths[b] rows, values outside
- *   0 ... L count as the nearer of the two.  What lies behind a sequence in Q, K, V and dOut is not read; out and the
- *   gradients are 0 there.
+ *   0 ... L count as the nearer of the two.  What lies behind a sequence in Q, K, V and dOut does not matter; out and
+ *   the gradients are 0 there.
  *   States are float32, [B, H, dk, dv].  S_in NULL: zero.  S_out NULL: not wanted.  S_out is the state behind the last
  *   token; S_out == S_in updates a state in place.  Any other overlap of a result with an operand or another result is
  *   DARK_EINVAL, here and in the calls below.

@@ -121,8 +121,16 @@ struct Op<unsigned short> {
   __device__ static void store4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])}, b, at, 0, 0);
   }
-  __device__ static void store1(__amdgpu_buffer_rsrc_t b, unsigned at, float v) {
-    __builtin_amdgcn_raw_buffer_store_b16((unsigned short)pack_bf16(v, 0.f), b, at, 0, 0);
+  // to an address of any alignment; the first `left` bytes
+  __device__ static void store_loose(char* p, int left, f32x4 v) {
+    const u32x2 w = {pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+    if (left >= 8) {
+      __builtin_memcpy(p, &w, 8);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (left > 2 * j) reinterpret_cast<unsigned short*>(p)[j] = (unsigned short)(w[j / 2] >> 16 * (j & 1));
+    }
   }
 };
 
@@ -173,7 +181,15 @@ struct Op<float> {
   __device__ static void store4(__amdgpu_buffer_rsrc_t b, unsigned at, f32x4 v) {
     __builtin_amdgcn_raw_buffer_store_b128(u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}, b, at, 0, 0);
   }
-  __device__ static void store1(__amdgpu_buffer_rsrc_t b, unsigned at, float v) { __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v), b, at, 0, 0); }
+  __device__ static void store_loose(char* p, int left, f32x4 v) {
+    if (left >= 16) {
+      __builtin_memcpy(p, &v, 16);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 3; ++j)
+        if (left > 4 * j) reinterpret_cast<float*>(p)[j] = v[j];
+    }
+  }
 };
 
 // Memory by buffer instructions: a wave-uniform address and extent, 32-bit offsets of the lanes.  What lies at or behind the extent
@@ -197,6 +213,14 @@ struct Rows {
   __device__ Buffer rows(int r0, int nr) const {
     return buffer(head + (long long)(reverse ? n - r0 - nr : r0) * row, nr > 0 ? (unsigned)(nr - 1) * row + width : 0u);
   }
+  // the same from a multiple of 4 bytes on, `skew` before the first of them, to a multiple of 4
+  __device__ Buffer loose(int r0, int nr, unsigned& skew) const {
+    const char* const p = head + (long long)(reverse ? n - r0 - nr : r0) * row;
+    skew = (unsigned)reinterpret_cast<uintptr_t>(p) & 3u;
+    return buffer(p - skew, nr > 0 ? ((unsigned)(nr - 1) * row + width + skew + 3u) & ~3u : 0u);
+  }
+  // row r of the sequence
+  __device__ char* at(int r) const { return const_cast<char*>(head) + (long long)(reverse ? n - 1 - r : r) * row; }
   // offset of the chunk's row `row`, of nr; too large for a row that does not exist (negative, read as unsigned, where counted from the end)
   __device__ unsigned offset(int r, int nr) const { return (unsigned)(reverse ? nr - 1 - r : r) * row; }
   // from there to the row `by` rows further on
@@ -209,8 +233,31 @@ __device__ static inline Rows rows_of(const void* x, int b, int h, int H, int L,
           (unsigned)(cols * (int)sizeof(T)), n, reverse};
 }
 
+// 16 bytes of a row that begins anywhere, as they come: the whole words that hold them, and which of their bytes are the row's.
+// (Element by element, every load waited for where it was issued: the training step of 24 heads of 1534, 33 and 65 wide, took 113 us.)
+template <typename T>
+struct Piece {
+  u32x4 r;
+  unsigned behind;   // 16-bit elements: what follows
+  // at: where it begins in the buffer, or kNowhere
+  __device__ void load(Buffer b, unsigned at) {
+    r = __builtin_amdgcn_raw_buffer_load_b128(b, at & ~3u, 0, 0);
+    if (sizeof(T) == 2) behind = __builtin_amdgcn_raw_buffer_load_b32(b, (at & ~3u) + 16u, 0, 0);
+  }
+  // the piece: `shift` is 16 where it begins in the middle of a word, `have` its bytes that exist
+  __device__ u32x4 get(unsigned shift, int have) const {
+    u32x4 v = r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (sizeof(T) == 2) v[j] = __builtin_amdgcn_alignbit(j < 3 ? r[j < 3 ? j + 1 : 3] : behind, r[j], shift);
+      v[j] &= have >= 4 * j + 4 ? ~0u : have > 4 * j ? 0xffffu : 0u;
+    }
+    return v;
+  }
+};
+
 // A tile of C rows and D columns on its way to LDS: some pieces of 16 bytes for each of NTH threads, zeros behind the last
-// row and column (what lies there in memory is never read).  VEC: rows begin at multiples of 16 bytes and are whole pieces long.
+// row and column (whatever lies there in memory).  VEC: rows begin at multiples of 16 bytes and are whole pieces long.
 template <typename T, int C, int D, int NTH, bool VEC>
 struct Tile {
   static constexpr int kPieces = D * (int)sizeof(T) / 16;   // of a row
@@ -219,24 +266,29 @@ struct Tile {
   static constexpr int kPer = 16 / (int)sizeof(T);
   static constexpr int RB = D * (int)sizeof(T);
   static_assert(C * kPieces % NTH == 0 && NTH % kPieces == 0 && (kStep & (kStep - 1)) == 0, "whole pieces a thread");
-  u32x4 r[kEach];
+  u32x4 r[VEC ? kEach : 1];
+  Piece<T> p[VEC ? 1 : kEach];
+  unsigned odd;   // pieces that begin in the middle of a word, a bit each
+  int have;
   __device__ void load(const Rows& x, int r0, int nr, int tid) {
-    const Buffer b = x.rows(r0, nr);
     const unsigned c = (unsigned)(tid % kPieces) * 16u, row = x.offset(tid / kPieces, nr);
+    if (VEC) {
+      const Buffer b = x.rows(r0, nr);
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) {
-      const unsigned at = row + (unsigned)x.step(i * kStep);   // wraps around to far behind the extent where rows are counted from the end
-      if (VEC) {
+      for (int i = 0; i < kEach; ++i) {
+        const unsigned at = row + (unsigned)x.step(i * kStep);   // wraps around to far behind the extent where rows are counted from the end
         r[i] = __builtin_amdgcn_raw_buffer_load_b128(b, c < x.width ? at + c : kNowhere, 0, 0);
-      } else {
-        T v[kPer];
+      }
+    } else {
+      unsigned skew;
+      const Buffer b = x.loose(r0, nr, skew);
+      have = (int)x.width - (int)c;
+      odd = 0;
 #pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-          const unsigned cj = c + j * (unsigned)sizeof(T), off = cj < x.width ? at + cj : kNowhere;
-          if constexpr (sizeof(T) == 2) v[j] = __builtin_amdgcn_raw_buffer_load_b16(b, off, 0, 0);
-          else v[j] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(b, off, 0, 0));
-        }
-        __builtin_memcpy(&r[i], v, 16);
+      for (int i = 0; i < kEach; ++i) {
+        const unsigned at = row + (unsigned)x.step(i * kStep) + c + skew;
+        p[i].load(b, have > 0 && tid / kPieces + i * kStep < nr ? at : kNowhere);
+        odd |= (at >> 1 & 1u) << i;
       }
     }
   }
@@ -244,7 +296,8 @@ struct Tile {
     const int row0 = tid / kPieces, base = row0 * RB + (((tid % kPieces) ^ swz<RB>(row0)) << 4);
     // kStep is a power of two and row0 below it: further rows are one xor with a constant away
 #pragma unroll
-    for (int i = 0; i < kEach; ++i) lds_put(tile + i * kStep * RB + (base ^ (swz<RB>((i * kStep) & 15) << 4)), r[i]);
+    for (int i = 0; i < kEach; ++i)
+      lds_put(tile + i * kStep * RB + (base ^ (swz<RB>((i * kStep) & 15) << 4)), VEC ? r[VEC ? i : 0] : p[VEC ? 0 : i].get((odd >> i & 1u) * 16u, have));
   }
 };
 
@@ -405,12 +458,10 @@ __global__ __launch_bounds__(4 * D2 * halves(D1), scan_waves(D1, D2)) void k_dec
 #pragma unroll
     for (int qt = 0; qt < QT; ++qt) {
       if (qt % step != qt0) continue;
-      const unsigned at = row + (unsigned)y.step(16 * qt);
       if (VEC) {
-        O::store4(yb, c < y.width ? at + c : kNowhere, out[qt]);
-      } else {
-#pragma unroll
-        for (unsigned j = 0; j < 4; ++j) O::store1(yb, c + j * (unsigned)sizeof(T) < y.width ? at + c + j * (unsigned)sizeof(T) : kNowhere, out[qt][j]);
+        O::store4(yb, c < y.width ? row + (unsigned)y.step(16 * qt) + c : kNowhere, out[qt]);
+      } else if (16 * qt + l.i < nr && c < y.width) {
+        O::store_loose(y.at(r0 + 16 * qt + l.i) + c, (int)(y.width - c), out[qt]);
       }
     }
   };

@@ -19,19 +19,25 @@ namespace decay {
 template <typename T, int D1, bool VEC>
 __device__ static inline void load_rows(typename Op<T>::frag (&x)[D1 / 32], const Rows& rows, int r0, int nr, int r, int g) {
   static_assert(sizeof(T) == 2, "bf16");
-  const Buffer b = rows.rows(r0, nr);
   const unsigned at = rows.offset(r, nr);
+  if (VEC) {
+    const Buffer b = rows.rows(r0, nr);
 #pragma unroll
-  for (int k = 0; k < D1 / 32; ++k) {
-    const unsigned c = (unsigned)(32 * k + 8 * g) * 2u;
-    if (VEC) {
+    for (int k = 0; k < D1 / 32; ++k) {
+      const unsigned c = (unsigned)(32 * k + 8 * g) * 2u;
       x[k] = __builtin_amdgcn_raw_buffer_load_b128(b, c < rows.width ? at + c : kNowhere, 0, 0);
-    } else {
-      unsigned short v[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = __builtin_amdgcn_raw_buffer_load_b16(b, c + 2u * j < rows.width ? at + c + 2u * j : kNowhere, 0, 0);
-      __builtin_memcpy(&x[k], v, 16);
     }
+  } else {
+    unsigned skew;
+    const Buffer b = rows.loose(r0, nr, skew);
+    Piece<T> p[D1 / 32];
+#pragma unroll
+    for (int k = 0; k < D1 / 32; ++k) {
+      const unsigned c = (unsigned)(32 * k + 8 * g) * 2u;
+      p[k].load(b, c < rows.width && r < nr ? at + c + skew : kNowhere);
+    }
+#pragma unroll
+    for (int k = 0; k < D1 / 32; ++k) x[k] = p[k].get(((at + skew) >> 1 & 1u) * 16u, (int)rows.width - (32 * k + 8 * g) * 2);
   }
 }
 
@@ -224,9 +230,8 @@ __global__ __launch_bounds__(512, 2) void k_decay_short(Scans A, int blocks, int
     const unsigned c = (unsigned)((16 * ct + 4 * l.g) * (int)sizeof(T));
     if (VEC) {
       O::store4(yb, c < y.width ? row + c : kNowhere, v);
-    } else {
-#pragma unroll
-      for (unsigned j = 0; j < 4; ++j) O::store1(yb, c + j * (unsigned)sizeof(T) < y.width ? row + c + j * (unsigned)sizeof(T) : kNowhere, v[j]);
+    } else if (q < nr && c < y.width) {
+      O::store_loose(y.at(begin + q) + c, (int)(y.width - c), v);
     }
   }
 }
