@@ -65,7 +65,16 @@ struct States {
 // Rows of a chunk: what the scan takes at a time.
 constexpr int kChunkBf16 = 64, kChunkF32 = 32;
 
-// decay_bf16.hip, decay_f32.hip: all `n` scans (states) share d1 and d2.
+// The widths that hold all `n` scans (states).
+template <typename A>
+inline void widths_of(const A& a, int n, int* d1, int* d2) {
+  *d1 = *d2 = 0;
+  for (int i = 0; i < n; ++i) {
+    *d1 = a.s[i].d1 > *d1 ? a.s[i].d1 : *d1;
+    *d2 = a.s[i].d2 > *d2 ? a.s[i].d2 : *d2;
+  }
+}
+
 dark_status launch_scan_bf16(const Scans& a, int n, hipStream_t st);
 dark_status launch_scan_f32(const Scans& a, int n, hipStream_t st);
 dark_status launch_state_bf16(const States& a, int n, hipStream_t st);

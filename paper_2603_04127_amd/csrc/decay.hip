@@ -238,6 +238,16 @@ dark_status run_states(const Problem& pb, const States& a, int n) {
   return DARK_OK;
 }
 
+// Whether the scans of a backward pass, [dv, dk] wide two of them and [dk, dv] the third, are one launch: where the instances are the
+// same, and up to 128 wide also where one of them is wider than its scans (bf16, 64 and 128 wide: 4 heads of 500 22 -> 14 us, 96 of them
+// 45 -> 41, 32 of 2000 59 -> 58).  fp32 pays for products with zeros as soon as the chip is full: 3 heads of 223 22 -> 19 us, 96 of 82
+// 29 -> 35, so there with a workgroup a CU at most.
+bool together(const Problem& pb, const Plan& plan) {
+  const auto kind = [](int d) { return d > 128 ? 2 : d > 64 ? 1 : 0; };
+  const int dk = kind(pb.p.dk), dv = kind(pb.p.dv);
+  return dk == dv || (dk < 2 && dv < 2 && (pb.p.io_dtype == DARK_BF16 || 3 * pb.BH() * plan.nseg <= 256));
+}
+
 template <typename A>
 void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* lengths, int nseg, int seg_len, bool exact) {
   a.exact = exact;
@@ -311,7 +321,7 @@ dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K,
   int n = 0;
   if (dQ != nullptr) a.s[n++] = q;
   if (dK != nullptr) a.s[n++] = k;
-  if (dk != dv && n > 0) {   // dV has other widths: a launch of its own
+  if (n > 0 && !together(pb, plan)) {   // dV has other widths: a launch of its own
     for (int i = n; i < kMostScans; ++i) a.s[i] = a.s[0];
     DARK_TRY(run_scan(pb, plan, a, n));
     n = 0;

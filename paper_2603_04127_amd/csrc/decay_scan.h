@@ -414,6 +414,7 @@ __global__ __launch_bounds__(4 * D2 * halves(D1), scan_waves(D1, D2)) void k_dec
   const int n = A.lengths != nullptr ? min(max(A.lengths[b], 0), A.L) : A.L;
   const float a2 = decay_log2(A.log_decay, h);
   const int begin = seg * A.seg_len, end = min(begin + A.seg_len, A.L), cols = min(a.d2 - col0, D2);
+  if (cols <= 0) return;   // a narrower scan than another one of the launch
   // rows behind the sequence
   if (a.y != nullptr && end > n) {
     const Rows y = rows_of<T>(a.y, b, h, A.H, A.L, a.d2, A.layout, 0, n, col0, cols);
@@ -598,7 +599,9 @@ template <typename T, int D1, int D2, bool VEC, bool EXACT>
 static dark_status launch(const Scans& a, int n, hipStream_t st) {
   constexpr int lds = scan_lds<T, D1, D2>();
   DARK_TRY(allow_lds(k_decay_scan<T, D1, D2, VEC, EXACT>, lds));
-  const dim3 grid((unsigned)((long long)a.B * a.H * a.nseg), (unsigned)((a.s[0].d2 + D2 - 1) / D2), (unsigned)n);
+  int d1, d2;
+  widths_of(a, n, &d1, &d2);
+  const dim3 grid((unsigned)((long long)a.B * a.H * a.nseg), (unsigned)((d2 + D2 - 1) / D2), (unsigned)n);
   DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_scan<T, D1, D2, VEC, EXACT>), grid, dim3(4 * D2 * halves(D1)), lds, a);
   return DARK_OK;
 }
@@ -615,7 +618,7 @@ static dark_status launch(const States& a, int n, hipStream_t st) {
 // half of the registers), else 128.
 template <typename T, int D1, int D2, typename A>
 static dark_status pick(const A& a, int n, hipStream_t st) {
-  const bool vec = a.s[0].d1 * sizeof(T) % 16 == 0 && a.s[0].d2 * sizeof(T) % 16 == 0;
+  const bool vec = a.s[0].d1 * sizeof(T) % 16 == 0 && a.s[0].d2 * sizeof(T) % 16 == 0;   // the same two in every scan
   if constexpr (Op<T>::kPlanes == 3) {
     if (a.exact) return vec ? launch<T, D1, D2, true, true>(a, n, st) : launch<T, D1, D2, false, true>(a, n, st);
   }
@@ -623,7 +626,8 @@ static dark_status pick(const A& a, int n, hipStream_t st) {
 }
 template <typename T, typename A>
 static dark_status pick(const A& a, int n, hipStream_t st) {
-  const int d1 = a.s[0].d1, d2 = a.s[0].d2;
+  int d1, d2;
+  widths_of(a, n, &d1, &d2);
   if (d1 > 128) return pick<T, 256, 64>(a, n, st);
   if (d1 > 64) return d2 <= 64 ? pick<T, 128, 64>(a, n, st) : pick<T, 128, 128>(a, n, st);
   return d2 <= 64 ? pick<T, 64, 64>(a, n, st) : pick<T, 64, 128>(a, n, st);

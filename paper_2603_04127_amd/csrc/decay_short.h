@@ -117,6 +117,7 @@ __global__ __launch_bounds__(512, 2) void k_decay_short(Scans A, int blocks, int
 
   if (a.y == nullptr) return;
   const int qb = blocks - 1 - at / heads, begin = qb * C, end = min(begin + C, A.L), col0 = blockIdx.y * D2, cols = min(a.d2 - col0, D2);
+  if (cols <= 0) return;   // a narrower scan than another one of the launch
   if (end > n) {   // rows behind the sequence
     const Rows y = rows_of<T>(a.y, b, h, A.H, A.L, a.d2, A.layout, 0, n, col0, cols);
     for (int r = max(begin, n) + (tid >> 6); r < end; r += 8)
@@ -245,7 +246,9 @@ static dark_status launch_short(const Scans& a, int n, hipStream_t st) {
     out = out || a.s[i].u_out != nullptr;
     rows = rows || a.s[i].y != nullptr;
   }
-  const int d2 = a.s[0].d2, blocks = rows ? (a.L + 63) / 64 : 0, states = out ? ((d2 < D2 ? d2 : D2) + 63) / 64 : 0;
+  int d1, d2;
+  widths_of(a, n, &d1, &d2);
+  const int blocks = rows ? (a.L + 63) / 64 : 0, states = out ? ((d2 < D2 ? d2 : D2) + 63) / 64 : 0;
   const dim3 grid((unsigned)(a.B * a.H * (blocks + states)), (unsigned)((d2 + D2 - 1) / D2), (unsigned)n);
   if (grid.x == 0) return DARK_OK;
   DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_short<T, D1, D2, VEC, EXACT>), grid, dim3(512), lds, a, blocks, states);
@@ -259,7 +262,8 @@ static dark_status pick_short(const Scans& a, int n, hipStream_t st) {
 }
 template <typename T>
 static dark_status pick_short(const Scans& a, int n, hipStream_t st) {
-  const int d1 = a.s[0].d1, d2 = a.s[0].d2;
+  int d1, d2;
+  widths_of(a, n, &d1, &d2);
   if (d1 > 128) return pick_short<T, 256, 64>(a, n, st);
   if (d1 > 64) return d2 <= 64 ? pick_short<T, 128, 64>(a, n, st) : pick_short<T, 128, 128>(a, n, st);
   return d2 <= 64 ? pick_short<T, 64, 64>(a, n, st) : pick_short<T, 64, 128>(a, n, st);
