@@ -154,6 +154,7 @@ namespace {
 // How a call is laid out: one segment or several, or bf16 sequences of some chunks without states (decay_short.h).
 struct Plan {
   int nseg = 1, seg_len = 0;
+  bool narrow = false;   // 64 columns a workgroup
   bool direct = false;
 };
 
@@ -171,21 +172,24 @@ Cost cost_of(int d1, int d2) {
 
 // A launch costs 4 us and, on the CUs, its workgroups' chunks one after the other: workgroups beyond one a CU wait for it or share it,
 // which comes to the same.  More segments shorten the chains until the chip is full; their states are written, and read and written
-// once more by the prefix over them, and cost two launches.
+// once more by the prefix over them, and cost two launches.  Workgroups of 64 columns instead of 128 are another way to have more of
+// them, with shorter chunks, each computing P for itself: fp32, bound by its products, gains while there are few chunks a CU (12 heads of
+// 478 x 128 30 -> 26 us, 96 of 82 x 64 x 128 16 -> 12) and loses later (64 of 1000 x 128 100 -> 105); bf16 gains nothing.
 Plan plan_of(const Problem& pb, int scans, int states) {
   const dark_decay_params& p = pb.p;
   const int C = p.io_dtype == DARK_BF16 ? kChunkBf16 : kChunkF32;
   const int chunks = p.L > 0 ? (p.L + C - 1) / C : 1;
   // scans of both orientations: the larger width counts
   const int d1 = scans > 1 && p.dv > p.dk ? p.dv : p.dk, d2 = scans > 1 && p.dk > p.dv ? p.dk : p.dv;
-  const Cost cost = cost_of(d1, d2);
-  const float c = p.io_dtype == DARK_BF16 ? cost.bf16 : cost.f32;
-  const float heads = (float)pb.BH() * (float)(d1 > 128 || d2 <= 64 ? (d2 + 63) / 64 : (d2 + 127) / 128);
-  Plan best;
   const int most = (int)std::min(64LL, std::max(1LL, kMostGroups / pb.BH()));
+  Plan best;
+  const long long blocks = pb.BH() * ((d2 + 127) / 128);
+  best.narrow = d1 > 128 || d2 <= 64 || (p.io_dtype == DARK_F32 && scans * blocks * chunks <= 1280);
+  const Cost cost = cost_of(d1, best.narrow ? 64 : d2);
+  const float c = p.io_dtype == DARK_BF16 ? cost.bf16 : cost.f32;
+  const float heads = (float)(best.narrow ? pb.BH() * ((d2 + 63) / 64) : blocks);
   if (p.sched_segments > 0) {
-    best.nseg = p.sched_segments < chunks ? p.sched_segments : chunks;
-    best.nseg = best.nseg < most ? best.nseg : most;
+    best.nseg = std::min(p.sched_segments, std::min(chunks, most));
   } else {
     float least = 0.f;
     for (int s = 1; s <= chunks && s <= most; ++s) {
@@ -249,7 +253,8 @@ bool together(const Problem& pb, const Plan& plan) {
 }
 
 template <typename A>
-void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* lengths, int nseg, int seg_len, bool exact) {
+void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* lengths, const Plan& plan, bool exact) {
+  a.narrow = plan.narrow;
   a.exact = exact;
   a.log_decay = log_decay;
   a.lengths = lengths;
@@ -257,8 +262,8 @@ void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* length
   a.H = pb.p.H;
   a.L = pb.p.L;
   a.layout = pb.p.layout;
-  a.nseg = nseg;
-  a.seg_len = seg_len;
+  a.nseg = plan.nseg;
+  a.seg_len = plan.seg_len;
 }
 
 }  // namespace
@@ -267,7 +272,7 @@ dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, 
                     const int32_t* lengths, const float* S_in, void* out, float* S_out) {
   const int dk = pb.p.dk, dv = pb.p.dv;
   const Plan plan = forward_plan(pb);
-  const int nseg = plan.nseg, seg_len = plan.seg_len;
+  const int nseg = plan.nseg;
   float* const seg = nseg > 1 ? ar.take<float>((size_t)pb.BH() * nseg * dk * dv) : nullptr;
   if (plan.direct && S_in != nullptr && S_in == S_out) {
     const long long size = pb.BH() * dk * dv;
@@ -280,12 +285,12 @@ dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, 
   if (ar.overflow) return DARK_EWORKSPACE;
   if (nseg > 1) {
     States st;
-    fill(pb, st, log_decay, lengths, nseg, seg_len, S_out != nullptr);
+    fill(pb, st, log_decay, lengths, plan, S_out != nullptr);
     st.s[0] = st.s[1] = State{K, V, S_in, seg, dk, dv, 0, 0, 1.f};
     DARK_TRY(run_states(pb, st, 1));
   }
   Scans a;
-  fill(pb, a, log_decay, lengths, nseg, seg_len, S_out != nullptr);
+  fill(pb, a, log_decay, lengths, plan, S_out != nullptr);
   a.s[0] = a.s[1] = a.s[2] = Scan{Q, K, V, out, nseg > 1 ? seg : S_in, S_out, dk, dv, 0, 0, 0, pb.scale, pb.scale, 1.f};
   return run_scan(pb, plan, a, 1);
 }
@@ -295,7 +300,7 @@ dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K,
                      void* dV, float* dS_in) {
   const int dk = pb.p.dk, dv = pb.p.dv;
   const Plan plan = backward_plan(pb);
-  const int nseg = plan.nseg, seg_len = plan.seg_len;
+  const int nseg = plan.nseg;
   const size_t states = (size_t)pb.BH() * nseg * dk * dv;
   float* const sseg = nseg > 1 ? ar.take<float>(states) : nullptr;
   float* const gseg = nseg > 1 ? ar.take<float>(states) : nullptr;
@@ -304,7 +309,7 @@ dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K,
   const bool rev = dK != nullptr || dV != nullptr || dS_in != nullptr;
   if (nseg > 1) {
     States st;
-    fill(pb, st, log_decay, lengths, nseg, seg_len, S_in != nullptr || dS_in != nullptr);   // the same bits whichever gradients are wanted
+    fill(pb, st, log_decay, lengths, plan, S_in != nullptr || dS_in != nullptr);   // the same bits whichever gradients are wanted
     int n = 0;
     if (dQ != nullptr) st.s[n++] = State{K, V, S_in, sseg, dk, dv, 0, 0, 1.f};
     if (rev) st.s[n++] = State{Q, dOut, dS_out, gseg, dk, dv, 1, 1, s};
@@ -317,7 +322,7 @@ dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K,
   const Scan k{V, dOut, Q, dK, Gu, nullptr, dv, dk, 1, 1, 1, s, 1.f, s};
   const Scan v{K, Q, dOut, dV, Gu, dS_in, dk, dv, 0, 1, 1, s, 1.f, s};
   Scans a;
-  fill(pb, a, log_decay, lengths, nseg, seg_len, S_in != nullptr || dS_in != nullptr);   // the same bits whichever gradients are wanted
+  fill(pb, a, log_decay, lengths, plan, S_in != nullptr || dS_in != nullptr);   // the same bits whichever gradients are wanted
   int n = 0;
   if (dQ != nullptr) a.s[n++] = q;
   if (dK != nullptr) a.s[n++] = k;

@@ -615,7 +615,7 @@ static dark_status launch(const States& a, int n, hipStream_t st) {
 }
 
 // The instance that holds d1 inner values, with 64 columns a workgroup where x3 has no more (or the state of 256 x 128 would take
-// half of the registers), else 128.
+// half of the registers) or the plan wants them, else 128.
 template <typename T, int D1, int D2, typename A>
 static dark_status pick(const A& a, int n, hipStream_t st) {
   const bool vec = a.s[0].d1 * sizeof(T) % 16 == 0 && a.s[0].d2 * sizeof(T) % 16 == 0;   // the same two in every scan
@@ -628,6 +628,7 @@ template <typename T, typename A>
 static dark_status pick(const A& a, int n, hipStream_t st) {
   int d1, d2;
   widths_of(a, n, &d1, &d2);
+  if (a.narrow) d2 = 64;
   if (d1 > 128) return pick<T, 256, 64>(a, n, st);
   if (d1 > 64) return d2 <= 64 ? pick<T, 128, 64>(a, n, st) : pick<T, 128, 128>(a, n, st);
   return d2 <= 64 ? pick<T, 64, 64>(a, n, st) : pick<T, 64, 128>(a, n, st);
