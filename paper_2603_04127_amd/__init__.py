@@ -502,10 +502,10 @@ def dark_decay_fwd(Q, K, V, log_decay, *, lengths=None, state=None, out=None, st
             return dark_decay_fwd(Q, K, V, log_decay, lengths=lengths, state=state, out=out, state_out=state_out, want_state=want_state,
                                   scale=scale, layout=layout, segments=segments)
     if o is None:
-        out = _result(V, V.dtype, Q)
+        out = torch.empty_like(V)
         o = out.data_ptr()
     if want_state and so is None:
-        state_out = torch.empty(shape, dtype=f32, device=Q.device)
+        state_out = torch.empty(shape, dtype=f32, device=Q.device) if state is None else torch.empty_like(state)
         so = state_out.data_ptr()
     ws, stream = _workspace(nb, Q.device) if nb else (None, torch._C._cuda_getCurrentRawStream(index))
     _check(lib().dark_decay_fwd(ctypes.byref(p), q, k, v, a, n, s, o, so, None if ws is None else ws.data_ptr(), nb, stream), "dark_decay_fwd")
@@ -539,9 +539,9 @@ def dark_decay_bwd(Q, K, V, log_decay, dOut, *, lengths=None, state=None, dstate
             return dark_decay_bwd(Q, K, V, log_decay, dOut, lengths=lengths, state=state, dstate=dstate, need=need, grads=grads, scale=scale,
                                   layout=layout, segments=segments)
     if grads is None:
-        g = {name: _result(x, x.dtype, Q) for name, x in like.items() if name in need}
+        g = {name: torch.empty_like(x) for name, x in like.items() if name in need}
         if "dstate" in need and state is not None:
-            g["dstate"] = torch.empty(shape, dtype=f32, device=Q.device)
+            g["dstate"] = torch.empty_like(state)
         gq, gk, gv, gs = (g[name].data_ptr() if name in g else None for name in ("dQ", "dK", "dV", "dstate"))
     ws, stream = _workspace(nb, Q.device) if nb else (None, torch._C._cuda_getCurrentRawStream(index))
     _check(lib().dark_decay_bwd(ctypes.byref(p), q, k, v, a, n, s, do, ds, gq, gk, gv, gs, None if ws is None else ws.data_ptr(), nb, stream),
@@ -581,7 +581,7 @@ def dark_decay_step(q, k, v, log_decay, state, *, parent=None, state_out=None, o
         with torch.cuda.device(index):
             return dark_decay_step(q, k, v, log_decay, state, parent=parent, state_out=state_out, out=out, scale=scale)
     if o is None:
-        out = _result(v, v.dtype, q)
+        out = torch.empty_like(v)
         o = out.data_ptr()
     _check(lib().dark_decay_step(ctypes.byref(p), pq, pk, pv, a, pp, rows, s, so, o, torch._C._cuda_getCurrentRawStream(index)), "dark_decay_step")
     return out
@@ -614,7 +614,7 @@ def dark_beam_select(logits, scores, *, finished=None, eos=0, keep_slots=False, 
         with torch.cuda.device(index):
             return dark_beam_select(logits, scores, finished=finished, eos=eos, keep_slots=keep_slots, out=out)
     if out is None:
-        s, parent, token = _result(scores, f32, logits), torch.empty_like(scores, dtype=i32), torch.empty_like(scores, dtype=i32)
+        s, parent, token = torch.empty_like(scores), torch.empty_like(scores, dtype=i32), torch.empty_like(scores, dtype=i32)
         ps, pp, pt = s.data_ptr(), parent.data_ptr(), token.data_ptr()
     ws, stream = _workspace(nb, logits.device)
     _check(lib().dark_beam_select(ctypes.byref(p), x, c, f, ps, pp, pt, ws.data_ptr(), ws.numel(), stream), "dark_beam_select")
