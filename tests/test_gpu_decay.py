@@ -100,6 +100,41 @@ def test_ragged_batches_read_nothing_behind_a_sequence(lengths, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("layout", ["bhld", "blhd"])
+@pytest.mark.parametrize("widths", [(33, 65), (1, 3), (66, 31), (150, 7)])
+def test_odd_widths_touch_nothing_beside_them(widths, layout, dtype):
+    # rows that share a word with their neighbours: NaN behind every sequence, results inside larger tensors that stay as they are
+    lengths = [130, 67, 0, 129]
+    p = U.problem(14, 4, 3, 130, *widths, dtype, lengths=lengths, state=True, dstate=True)
+    for k in NAMES:
+        for b in range(4):
+            p[k][b, :, lengths[b]:] = 0.0
+    ref, size = U.oracle(p), U.oracle(p, magnitude=True)
+    d = _device(p, layout)
+    for k in NAMES:
+        for b in range(4):
+            _heads_first(d[k], layout)[b, :, lengths[b]:] = float("nan")
+    room = []
+
+    def inside(t):   # a tensor of t's kind, 256 elements into a larger one
+        room.append(torch.full((t.numel() + 512,), 7.0, dtype=t.dtype, device="cuda"))
+        return room[-1][256:256 + t.numel()].view(t.shape)
+
+    for segments in (0, 1, 2):
+        room.clear()
+        out, last = inside(d["V"]), inside(d["state"])
+        grads = {k: inside(d[x]) for k, x in (("dQ", "Q"), ("dK", "K"), ("dV", "V"), ("dstate", "state"))}
+        _forward(d, layout=layout, segments=segments, out=out, state_out=last)
+        _backward(d, layout=layout, segments=segments, grads=grads)
+        torch.cuda.synchronize()
+        U.check(_heads_first(out, layout), ref["out"], size["out"], dtype, "out")
+        U.check(last, ref["last"], size["last"], "f32", "last")
+        for k, t in grads.items():
+            U.check(t if k == "dstate" else _heads_first(t, layout), ref[k], size[k], "f32" if k == "dstate" else dtype, k)
+        assert all((r[:256] == 7).all() and (r[-256:] == 7).all() for r in room)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_no_rows_pass_the_state_on(dtype):
     p = U.problem(8, 2, 2, 0, 64, 48, dtype, state=True, dstate=True)
     d = _device(p)
@@ -257,6 +292,30 @@ def test_captured_calls_replay():
         got = [t.clone() for t in held]
         _forward(other)   # eager work between the replays
         assert all(torch.equal(x, y) for x, y in zip(got, work()))
+
+
+def test_two_graphs_and_states_in_place():
+    # two captured calls on one stream's workspaces, replayed in turn; short sequences in one launch and long ones in segments
+    ds = [_device(U.problem(42 + i, 1, 4, L, 64, 64, "bf16", state=True, dstate=True)) for i, L in enumerate((300, 1500))]
+
+    def work(d):   # the state is updated in place from a copy, so that a replay starts from the same one
+        S = d["state"].clone()
+        out, _ = dk.dark_decay_fwd(d["Q"], d["K"], d["V"], d["a"], state=S, state_out=S)
+        return (out, S, *_backward(d).values())
+
+    want = [work(d) for d in ds]
+    torch.cuda.synchronize()
+    graphs, held = [], []
+    for d in ds:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            held.append(work(d))
+    for i in range(4):
+        for j in ((0, 1), (1, 0))[i % 2]:
+            graphs[j].replay()
+        work(ds[i % 2])   # eager work behind them
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for h, w in zip(held, want) for x, y in zip(h, w))
 
 
 # ---------------------------------------------------------------------------
