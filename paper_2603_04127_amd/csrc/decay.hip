@@ -208,7 +208,10 @@ Plan plan_of(const Problem& pb, int scans, int states) {
       }
     }
     if (p.io_dtype == DARK_BF16 && chunks >= 2 && chunks <= 16 && pb.BH() * (chunks + 4) <= kMostGroups) {
-      const float pairs = scans * heads * (float)(chunks * (chunks + 1) / 2) / cost.pairs, steps = (float)((chunks + 1) / 2) * cost.step;
+      // rows that begin anywhere take registers: past 64 inner values there is room for one workgroup a CU instead of two (the backward pass of
+      // 96 heads of 264, 33 and 65 wide: 48 us, as one segment 31)
+      const float share = d1 <= 64 || (p.dk % 8 == 0 && p.dv % 8 == 0) ? 1.f : 0.5f;
+      const float pairs = scans * heads * (float)(chunks * (chunks + 1) / 2) / (share * cost.pairs), steps = (float)((chunks + 1) / 2) * cost.step;
       if (6.f + (pairs > steps ? pairs : steps) < least) {
         best.direct = true;
         best.nseg = 1;

@@ -90,7 +90,7 @@ __global__ __launch_bounds__(512, 2) void k_decay_short(Scans A, int blocks, int
       p3.store(t3, gtid);
       lds_barrier();
       load(c + 2);
-      if (c < chunks) update<T, C, D1, 64, EXACT>(U, t2, t3, c == chunks - 1 ? tl : tw, power(a2, max(n - (c + 1) * C, 0)), wave, fresh<D1>(lane));
+      if (c < chunks) update<T, C, D1, 64, EXACT>(U, t2, t3, c == chunks - 1 ? tl : tw, power(a2, max(n - (c + 1) * C, 0)), wave, fresh<VEC && D2 <= 64 ? D1 : 128>(lane));
     }
     lds_barrier();
     const int mine = (wave * KT * 64 + lane) * 16;
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(512, 2) void k_decay_short(Scans A, int blocks, int
     lds_barrier();
     load(s + 1 < steps ? kb - 2 : -1);
     if (kb < 0) continue;
-    const Lane f = fresh<D1>(lane);
+    const Lane f = fresh<VEC && D2 <= 64 ? D1 : 128>(lane);
     const int br = O::template row_base<RB1>(f);
     typename O::frag p[2];
     // g^(r-c) with r - c = 64 (qb - kb) - 63 + q + (63 - key): both factors have exponents >= 0 except on the diagonal

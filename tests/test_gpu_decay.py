@@ -63,7 +63,7 @@ def test_segments_and_layouts(segments, layout, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
-@pytest.mark.parametrize("decay", [0.0, -1e-4, -1.0, -30.0, -1e5, -np.inf])
+@pytest.mark.parametrize("decay", [0.02, 0.0, -1e-4, -1.0, -30.0, -1e5, -np.inf])
 def test_decays(decay, dtype):
     for segments in (0, 2):
         _run(U.problem(6, 1, 2, 170, 64, 64, dtype, decay=[decay], state=True, dstate=True), segments=segments)
