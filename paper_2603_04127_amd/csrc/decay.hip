@@ -14,7 +14,7 @@ using fz::fast_exp2;
 using fz::kLog2e;
 
 // The states before every segment, in place of the segments' own: U_0 = u_in, U_(s+1) = g^len U_s + seg_s.  One thread an element
-// (four where they divide), segment by segment, eight of them asked for at once; bound by reading and writing the states once (64 heads of
+// (four where they divide), segment by segment, sixteen of them asked for at once; bound by reading and writing the states once (64 heads of
 // 128 x 128, 8 segments: 63 MB in 12 us, the rate of a copy), few states by a launch and two trips to memory (4 us).
 template <int W>
 __global__ __launch_bounds__(256) void k_decay_prefix(States A) {
@@ -30,7 +30,7 @@ __global__ __launch_bounds__(256) void k_decay_prefix(States A) {
   vec U = 0.f;
   if (a.u_in != nullptr) U = *reinterpret_cast<const vec*>(a.u_in + bh * size + e);
   float* const s = a.seg + (long long)bh * A.nseg * size + e;
-  constexpr int kAtOnce = 8;
+  constexpr int kAtOnce = 16;
   for (int i0 = 0; i0 < used - 1; i0 += kAtOnce) {
     vec own[kAtOnce];
 #pragma unroll
