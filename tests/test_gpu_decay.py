@@ -270,6 +270,34 @@ def test_two_streams_at_once():
         assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))
 
 
+def test_two_threads_at_once():
+    import threading
+
+    ds = [_device(U.problem(32 + i, 1, 4, 1500, 64, 64, "bf16", state=True, dstate=True)) for i in range(2)]
+    logits = [torch.randn(2, 4, 30000, device="cuda") for _ in ds]
+    scores = [-torch.rand(2, 4, device="cuda") for _ in ds]
+
+    def work(i):
+        return (*_forward(ds[i]), *_backward(ds[i]).values(), *dk.dark_beam_select(logits[i], scores[i]))
+
+    want = [work(i) for i in range(2)]
+    torch.cuda.synchronize()
+    got = [None, None]
+
+    def run(i):
+        with torch.cuda.stream(torch.cuda.Stream()):
+            for _ in range(20):
+                got[i] = work(i)
+            torch.cuda.current_stream().synchronize()
+
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert all(torch.equal(x, y) for g, w in zip(got, want) for x, y in zip(g, w))
+
+
 def test_captured_calls_replay():
     d = _device(U.problem(40, 1, 4, 1500, 64, 64, "bf16", state=True, dstate=True))
     other = _device(U.problem(41, 1, 4, 1500, 64, 64, "bf16", state=True, dstate=True))
