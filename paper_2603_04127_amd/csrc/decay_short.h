@@ -7,7 +7,8 @@
 // as many steps one after the other.  In a group each wave holds 16 rows of x1 as operands in registers.  P^T comes out of the matrix
 // unit with the keys along a lane's registers and goes back in as an operand after two exchanges between lane groups.
 // Bound by the chain of a block's chunks, two of them in 1.4 to 2.9 us: 16 heads of 777 x 128 take 20 us (24 as segments), 24 of 512 x 64 11
-// (17).  Four groups of half the rows are no faster there and slower where the chip is full (128 heads of 1024 x 128: 103 -> 151 us).
+// (17).  More groups shorten the chain and take their turns on the same SIMDs: four are no faster there (four of half the rows 20 us, four
+// of all 20.4) and slower elsewhere.
 #pragma once
 
 #include "decay_scan.h"
