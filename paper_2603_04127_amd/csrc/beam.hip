@@ -5,7 +5,8 @@
 // equal ones by the lowest j, then the lowest t.  k_beam_rows reads every logit once: a workgroup takes a slice of a row and leaves
 // the slice's maximum, its sum of exponentials and its n largest logits in order.  k_beam_pick joins the sums of a batch entry's
 // rows and takes the best of the sorted lists.
-// Two candidates of different beams may lie closer together than fp32 resolves: offsets and comparisons are in fp64.
+// Two candidates of different beams may lie closer together than fp32 resolves beside a score: offsets and comparisons are in fp64, and
+// what tells them apart is then the sums, exact to 2^-22.
 #include <cmath>
 
 #include "common.h"
