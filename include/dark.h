@@ -364,7 +364,8 @@ dark_status dark_decay_step(const dark_decay_params* p, const void* q, const voi
 /*
  * Beam search: the next n beams of each batch entry.  Candidate (j, t), beam j going on with token t, is worth
  *   scores[j] + logits[j][t] - log sum_u exp logits[j][u];
- * the n largest are taken, of equal ones that with the lowest j, then the lowest t.
+ * the n largest are taken, of equal ones that with the lowest j, then the lowest t.  In one beam a larger logit is a larger candidate,
+ * however little it adds beside the score.
  *   logits [B, n, V] in io_dtype, scores [B, n] float32 (log-probabilities so far), finished [B, n] bytes or NULL.
  *   out_scores [B, n] float32, out_parent and out_token [B, n] int32, best first; with keep_slots != 0 instead so that a beam's best
  *   successor has the beam's own place (then out_parent[j] == j wherever beam j survives, and dark_state_reorder moves

@@ -7,6 +7,7 @@
 // rows and takes the best of the sorted lists.
 // Two candidates of different beams may lie closer together than fp32 resolves beside a score: offsets and comparisons are in fp64, and
 // what tells them apart is then the sums, exact to 2^-22.
+// Where fp64 resolves no more either (a score of -10^20, logits that differ by 10^-20) the logits themselves decide within a beam.
 #include <cmath>
 
 #include "common.h"
@@ -292,12 +293,20 @@ constexpr int kMostLists = 8704;
 constexpr int kStaged = 48 * 1024;   // bytes of lists that are brought to LDS at once (else they are read where they are)
 constexpr int kMostGathered = 256;
 
-// A candidate: its value in an order of integers (0: none), and beam * V + token.
+// A candidate: its value in an order of integers (0: none), and what decides where fp64 holds two values for one: the lower beam, in a beam
+// the larger logit, then the lower token.  A list is in that order as well (equal logits have equal values, and no smaller one a larger
+// value), so that its first entry behind any candidate is the best of those behind it.
 struct Head {
-  u64 key;
-  unsigned flat;
+  u64 key, rank;
 };
-__device__ __forceinline__ bool before(const Head& a, const Head& b) { return a.key > b.key || (a.key == b.key && a.flat < b.flat); }
+constexpr int kTokenBits = 27;
+static_assert((long long)kMostLists * kSlice <= 1LL << kTokenBits && kMostBeams <= 1 << (32 - kTokenBits), "a beam, a logit and a token are 64 bits");
+__device__ __forceinline__ u64 rank_of(int beam, unsigned logit, int token) {
+  return (u64)(kMostBeams - 1 - beam) << (32 + kTokenBits) | (u64)logit << kTokenBits | ((1u << kTokenBits) - 1u - (unsigned)token);
+}
+__device__ __forceinline__ int beam_of(u64 rank) { return kMostBeams - 1 - (int)(rank >> (32 + kTokenBits)); }
+__device__ __forceinline__ int token_of(u64 rank) { return (int)(~(unsigned)rank & ((1u << kTokenBits) - 1u)); }
+__device__ __forceinline__ bool before(const Head& a, const Head& b) { return a.key > b.key || (a.key == b.key && a.rank > b.rank); }
 
 enum { kAlive = 0, kFinished = 1, kDead = 2 };
 
@@ -318,7 +327,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
   __shared__ int size;
   const Entry* const own = lists + (long long)b * count * n;
   if (tid == 0) size = 0;
-  if (tid < kMostBeams) picks[tid] = Head{0, 0u};
+  if (tid < kMostBeams) picks[tid] = Head{0, 0};
   constexpr int kAtOnce = 8;   // what a thread asks for before it waits: every trip to memory takes longer than all the rest
   if (staged)
     for (int l0 = 0; l0 < count * n; l0 += 256 * kAtOnce) {
@@ -366,15 +375,15 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
   // entry `at` of list l
   const auto entry = [&](int l, int at) {
     const int j = l / slices;
-    Head hd{0, 0u};
+    Head hd{0, 0};
     if (kind[j] == kAlive) {
       const Entry e = staged ? near[l * n + at] : own[(long long)l * n + at];
       if (e.token < 0) return hd;
       hd.key = ordered64(offset[j] + ((double)e.logit - (double)tops[j]) + 0.0);   // one zero
-      hd.flat = (unsigned)j * (unsigned)V + (unsigned)e.token;
+      hd.rank = rank_of(j, ordered(e.logit), e.token);
     } else if (kind[j] == kFinished && l % slices == 0 && at == 0) {   // a finished beam goes on with `eos` alone
       hd.key = ordered64(offset[j]);
-      hd.flat = (unsigned)j * (unsigned)V + (unsigned)eos;
+      hd.rank = rank_of(j, 0u, eos);
     }
     return hd;
   };
@@ -397,7 +406,6 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
     }
   }
   __syncthreads();
-  const int found = size < n ? size : n;
   if (size <= kMostGathered) {
     if (tid < size) {
       const Head mine = gathered[tid];
@@ -408,9 +416,9 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
     }
     __syncthreads();
   } else {
-    Head last{~0ull, 0u};
+    Head last{~0ull, 0};
     for (int i = 0; i < n; ++i) {
-      Head w{0, ~0u};
+      Head w{0, 0};
       for (int l = tid; l < count; l += 256)
         for (int at = 0; at < n; ++at) {
           const Head hd = entry(l, at);
@@ -424,7 +432,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
       for (int o = 32; o > 0; o >>= 1) {
         Head x;
         x.key = __shfl_xor(w.key, o, 64);
-        x.flat = __shfl_xor(w.flat, o, 64);
+        x.rank = __shfl_xor(w.rank, o, 64);
         if (before(x, w)) w = x;
       }
       if (lane == 0) best[wave] = w;
@@ -438,16 +446,18 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
     }
   }
   if (wave != 0) return;
-  Head mine{0, 0u};
-  if (lane < found) mine = picks[lane];
+  Head mine{0, 0};
+  if (lane < n) mine = picks[lane];
+  const int found = __builtin_popcountll(__ballot(mine.key != 0));   // the first ones
+  int parent = beam_of(mine.rank), token = token_of(mine.rank);
   // too few: candidates of value -infinity, the lowest that are not taken yet
   int have = found;
-  for (unsigned flat = 0; have < n; ++flat) {
-    if (__ballot(lane < have && mine.flat == flat) != 0) continue;
-    if (lane == have) mine.flat = flat;
+  for (int j = 0, t = 0; have < n; ++t) {
+    if (t == V) ++j, t = 0;
+    if (__ballot(lane < have && parent == j && token == t) != 0) continue;
+    if (lane == have) parent = j, token = t;
     ++have;
   }
-  const int parent = (int)(mine.flat / (unsigned)V), token = (int)(mine.flat % (unsigned)V);
   int slot = lane;
   if (keep_slots) {
     unsigned used = 0;   // places of beams that survive

@@ -107,6 +107,36 @@ def test_finished_beams(kind, dtype):
         _check(logits, scores, finished, eos)
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape,kind", [((1, 17, 999), "tiny"), ((3, 17, 999), "tiny"), ((1, 4, 999), "tiny"), ((1, 32, 73000), "rising"), ((2, 32, 999), "same"),
+                                        ((1, 32, 73000), "huge"), ((2, 5, 20001), "huge")])
+def test_candidates_that_no_double_tells_apart(shape, kind, dtype):
+    # all winners are beam 0's largest logits, equal ones by the lowest token, though many values are one and the same double
+    B, n, V = shape
+    row = torch.linspace(-3, 3, V)[torch.randperm(V, generator=torch.Generator().manual_seed(V))]
+    if kind in ("tiny", "rising"):
+        row = 1e-20 * torch.arange(V) if kind == "tiny" else torch.linspace(-3, 3, V)
+    row = row.to(TORCH[dtype])
+    scores = torch.full((n,), float("-inf"))
+    scores[0] = -1e20
+    if kind == "tiny":
+        scores = -torch.arange(n, dtype=torch.float32)
+    elif kind == "same":
+        scores[:] = -1e20
+    elif kind == "huge":
+        scores[0], row[V // 2] = -2.0, 2.0 ** 100
+    want = np.lexsort((np.arange(V), -row.double().numpy()))[:n]
+    for keep in (False, True):
+        room = [torch.full((3, B, n), 7, dtype=t, device="cuda") for t in (torch.float32, torch.int32, torch.int32)]
+        s, p, t = dk.dark_beam_select(row.expand(B, n, V).contiguous().cuda(), scores.repeat(B, 1).cuda(), keep_slots=keep, out=[r[1] for r in room])
+        assert (p == 0).all() and (t.cpu().numpy() == want).all(), (keep, p, t, want)
+        x = row.double().numpy() - float(row.max())
+        value = float(scores[0]) - np.log(np.exp(x).sum()) + x[want]
+        # the score's rounding, and the sum's: at most 31 + 8 additions one after the other and an exponential off by 2^-23
+        assert np.all(np.abs(s.cpu().numpy() - value) <= 2.0 ** -24 * np.abs(value) + 2.0 ** -18)
+        assert all((r[0] == 7).all() and (r[2] == 7).all() for r in room)   # nothing beside the results
+
+
 def test_scores_in_place_and_given_outputs():
     logits, scores = _problem(5, 2, 4, 5000, "f32")
     logits, scores = logits.cuda(), scores.cuda()
