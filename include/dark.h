@@ -394,7 +394,8 @@ dark_status dark_beam_select(const dark_beam_params* p, const void* logits, cons
  * (b, parent[b][j]) was before the call.  A parent outside 0 ... n - 1 leaves its row as it is.
  *   parent: [B, n] int32 in device memory; states and row_bytes: host arrays, read before the call returns.  Tensors that overlap each
  *   other or parent are DARK_EINVAL.
- * n <= 32, B <= 65535 (else DARK_EUNSUPPORTED).  Sixteen tensors a launch.
+ * n <= 32, B <= 65535, row_bytes at most 2^31 units of 16 bytes, of 4 or of 1, the largest that divides it (else DARK_EUNSUPPORTED; a refused call has
+ * moved nothing).  Sixteen tensors a launch.
  */
 dark_status dark_state_reorder(int B, int n, const int32_t* parent, int count, void* const* states, const size_t* row_bytes,
                                void* hip_stream);

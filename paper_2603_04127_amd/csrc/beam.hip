@@ -537,6 +537,14 @@ __global__ __launch_bounds__(256) void k_state_reorder(Tensors t, const int32_t*
   else reorder<unsigned char, N>(rows, row_bytes, at, from, n);
 }
 
+// A row's unit, and the workgroups of 256 units each that move it; along a grid's x.
+constexpr size_t kMostBlocks = 1 << 23;
+int unit_of(size_t row_bytes) { return row_bytes % 16 == 0 ? 16 : row_bytes % 4 == 0 ? 4 : 1; }
+size_t blocks_of(size_t row_bytes) {
+  const size_t units = row_bytes / unit_of(row_bytes);
+  return units / 256 + (units % 256 != 0);
+}
+
 int slices_of(const dark_beam_params& p) {
   const int per = p.io_dtype == DARK_BF16 ? 8 : 4;
   return (int)(((long long)p.V + per - 1 + kSlice - 1) / kSlice);   // a row begins up to per - 1 elements behind its first slice
@@ -622,7 +630,7 @@ dark_status dark_state_reorder(int B, int n, const int32_t* parent, int count, v
   for (int i = 0; i < count; ++i) {
     if (row_bytes[i] == 0) continue;
     if (states[i] == nullptr) return DARK_EINVAL;
-    if (row_bytes[i] > ((size_t)1 << 38)) return DARK_EUNSUPPORTED;
+    if (beam::blocks_of(row_bytes[i]) > beam::kMostBlocks) return DARK_EUNSUPPORTED;   // here, before anything has moved
     if (!aligned(states[i], 16)) return DARK_EALIGN;
   }
   const size_t beams = (size_t)B * n;
@@ -639,15 +647,11 @@ dark_status dark_state_reorder(int B, int n, const int32_t* parent, int count, v
     long long blocks = 0;
     for (; i < count && t.count < beam::kMostTensors; ++i) {
       if (row_bytes[i] == 0) continue;
-      const int unit = row_bytes[i] % 16 == 0 ? 16 : row_bytes[i] % 4 == 0 ? 4 : 1;
-      const long long more = (long long)((row_bytes[i] / unit + 255) / 256);
-      if (blocks + more > (1 << 23)) {
-        if (t.count == 0) return DARK_EUNSUPPORTED;
-        break;
-      }
+      const long long more = (long long)beam::blocks_of(row_bytes[i]);
+      if (blocks + more > (long long)beam::kMostBlocks) break;   // never the first of a launch
       t.data[t.count] = static_cast<char*>(states[i]);
       t.row_bytes[t.count] = (long long)row_bytes[i];
-      t.unit[t.count] = unit;
+      t.unit[t.count] = beam::unit_of(row_bytes[i]);
       t.first[t.count] = (int)blocks;
       blocks += more;
       ++t.count;

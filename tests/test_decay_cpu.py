@@ -124,6 +124,18 @@ def test_reorder_refusals():
     assert f(0, 4, A, 2, ptrs, sizes, None) == dk.DARK_OK and f(1, 4, A, 0, None, None, None) == dk.DARK_OK
 
 
+def test_reorder_refuses_before_anything_has_moved():
+    # a row too long for a launch, behind more tensors than one launch takes: without a GPU a launch would be DARK_EHIP
+    f = dk.lib().dark_state_reorder
+    for unit in (1, 4, 16):
+        for where in (0, 1, 16, 39):
+            sizes = (ctypes.c_size_t * 40)(*([64] * 40))
+            sizes[where] = unit * ((1 << 31) + 1)
+            ptrs = (ctypes.c_void_p * 40)(*(A + 4096 * i if i != where else 1 << 40 for i in range(40)))
+            assert f(1, 4, A - 4096, 40, ptrs, sizes, None) == dk.DARK_EUNSUPPORTED, (unit, where)
+    assert f(1, 4, A - 4096, 1, (ctypes.c_void_p * 1)(1 << 40), (ctypes.c_size_t * 1)((1 << 64) - 16), None) == dk.DARK_EUNSUPPORTED
+
+
 def test_results_lie_on_nothing_else():
     far = [A + (i << 20) for i in range(16)]   # every argument a place of its own, then one result on another argument
     fwd, bwd, step, select, reorder = (getattr(dk.lib(), "dark_" + name) for name in ("decay_fwd", "decay_bwd", "decay_step", "beam_select", "state_reorder"))
