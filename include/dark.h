@@ -319,8 +319,10 @@ dark_status dark_decode_step(const dark_params* p, const void* q, const void* k,
  *
  * Arithmetic: fp32 operands are multiplied and summed in fp32.  bf16 operands go through the matrix units with fp32 sums; the
  * weights (q_t . k_l) g^(t-l), formed inside a chunk of 64 rows and in short sequences everywhere, and the state where it is read,
- * are rounded to bf16 (2^-8 relative) on their way into an output of that type; a state that is handed out keeps 24 bits.  An element of K or V that is not finite makes the outputs
- * from its row on not finite, in its column at least; one of V also those of up to 63 rows before it.
+ * are rounded to bf16 (2^-8 relative) on their way into an output of that type; the state itself keeps 24 bits.  To the last bit, out does
+ * not depend on whether S_out is wanted, nor a gradient on which others are, and no state is an empty state.
+ * An element of K or V that is not finite makes the outputs from its row on not finite, in its column at least; one of V also those of
+ * up to 63 rows before it.
  */
 typedef enum { DARK_BHLD = 0, DARK_BLHD = 1 } dark_layout;
 

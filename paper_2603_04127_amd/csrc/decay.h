@@ -44,7 +44,6 @@ struct Scans {
   const int32_t* lengths;
   int B, H, L, layout;
   int nseg, seg_len;          // segments of a sequence; seg_len is a multiple of the chunk
-  int exact;                  // a state is handed out: bf16 operands keep 24 bits of what enters it
   int narrow;                 // 64 columns a workgroup
 };
 
@@ -60,7 +59,7 @@ struct States {
   State s[2];
   const float* log_decay;
   const int32_t* lengths;
-  int B, H, L, layout, nseg, seg_len, exact, narrow;
+  int B, H, L, layout, nseg, seg_len, narrow;
 };
 
 // Rows of a chunk: what the scan takes at a time.

@@ -256,9 +256,8 @@ bool together(const Problem& pb, const Plan& plan) {
 }
 
 template <typename A>
-void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* lengths, const Plan& plan, bool exact) {
+void fill(const Problem& pb, A& a, const float* log_decay, const int32_t* lengths, const Plan& plan) {
   a.narrow = plan.narrow;
-  a.exact = exact;
   a.log_decay = log_decay;
   a.lengths = lengths;
   a.B = pb.p.B;
@@ -288,12 +287,12 @@ dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, 
   if (ar.overflow) return DARK_EWORKSPACE;
   if (nseg > 1) {
     States st;
-    fill(pb, st, log_decay, lengths, plan, S_out != nullptr);
+    fill(pb, st, log_decay, lengths, plan);
     st.s[0] = st.s[1] = State{K, V, S_in, seg, dk, dv, 0, 0, 1.f};
     DARK_TRY(run_states(pb, st, 1));
   }
   Scans a;
-  fill(pb, a, log_decay, lengths, plan, S_out != nullptr);
+  fill(pb, a, log_decay, lengths, plan);
   a.s[0] = a.s[1] = a.s[2] = Scan{Q, K, V, out, nseg > 1 ? seg : S_in, S_out, dk, dv, 0, 0, 0, pb.scale, pb.scale, 1.f};
   return run_scan(pb, plan, a, 1);
 }
@@ -312,7 +311,7 @@ dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K,
   const bool rev = dK != nullptr || dV != nullptr || dS_in != nullptr;
   if (nseg > 1) {
     States st;
-    fill(pb, st, log_decay, lengths, plan, S_in != nullptr || dS_in != nullptr);   // the same bits whichever gradients are wanted
+    fill(pb, st, log_decay, lengths, plan);
     int n = 0;
     if (dQ != nullptr) st.s[n++] = State{K, V, S_in, sseg, dk, dv, 0, 0, 1.f};
     if (rev) st.s[n++] = State{Q, dOut, dS_out, gseg, dk, dv, 1, 1, s};
@@ -325,7 +324,7 @@ dark_status backward(const Problem& pb, Arena& ar, const void* Q, const void* K,
   const Scan k{V, dOut, Q, dK, Gu, nullptr, dv, dk, 1, 1, 1, s, 1.f, s};
   const Scan v{K, Q, dOut, dV, Gu, dS_in, dk, dv, 0, 1, 1, s, 1.f, s};
   Scans a;
-  fill(pb, a, log_decay, lengths, plan, S_in != nullptr || dS_in != nullptr);   // the same bits whichever gradients are wanted
+  fill(pb, a, log_decay, lengths, plan);
   int n = 0;
   if (dQ != nullptr) a.s[n++] = q;
   if (dK != nullptr) a.s[n++] = k;

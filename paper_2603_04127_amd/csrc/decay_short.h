@@ -45,7 +45,7 @@ __device__ static inline void load_rows(typename Op<T>::frag (&x)[D1 / 32], cons
 template <typename T, int D1, int D2>
 constexpr int short_lds() { return 64 * 2 * (D1 + D2) * (int)sizeof(T) + 3 * 64 * 4; }
 
-template <typename T, int D1, int D2, bool VEC, bool EXACT>
+template <typename T, int D1, int D2, bool VEC>
 __global__ __launch_bounds__(512, 2) void k_decay_short(Scans A, int blocks, int state_blocks) {
   typedef Op<T> O;
   constexpr int C = 64, RB1 = D1 * (int)sizeof(T), RB2 = D2 * (int)sizeof(T), K1 = D1 / 32, CT = D2 / 16, KT = D1 / 16;
@@ -91,7 +91,7 @@ __global__ __launch_bounds__(512, 2) void k_decay_short(Scans A, int blocks, int
       p3.store(t3, gtid);
       lds_barrier();
       load(c + 2);
-      if (c < chunks) update<T, C, D1, 64, EXACT>(U, t2, t3, c == chunks - 1 ? tl : tw, power(a2, max(n - (c + 1) * C, 0)), wave, fresh<VEC && D2 <= 64 ? D1 : 128>(lane));
+      if (c < chunks) update<T, C, D1, 64>(U, t2, t3, c == chunks - 1 ? tl : tw, power(a2, max(n - (c + 1) * C, 0)), wave, fresh<VEC && D2 <= 64 ? D1 : 128>(lane));
     }
     lds_barrier();
     const int mine = (wave * KT * 64 + lane) * 16;
@@ -238,10 +238,10 @@ __global__ __launch_bounds__(512, 2) void k_decay_short(Scans A, int blocks, int
   }
 }
 
-template <typename T, int D1, int D2, bool VEC, bool EXACT>
+template <typename T, int D1, int D2, bool VEC>
 static dark_status launch_short(const Scans& a, int n, hipStream_t st) {
   constexpr int lds = short_lds<T, D1, D2>();
-  DARK_TRY(allow_lds(k_decay_short<T, D1, D2, VEC, EXACT>, lds));
+  DARK_TRY(allow_lds(k_decay_short<T, D1, D2, VEC>, lds));
   bool out = false, rows = false;
   for (int i = 0; i < n; ++i) {
     out = out || a.s[i].u_out != nullptr;
@@ -252,14 +252,13 @@ static dark_status launch_short(const Scans& a, int n, hipStream_t st) {
   const int blocks = rows ? (a.L + 63) / 64 : 0, states = out ? ((d2 < D2 ? d2 : D2) + 63) / 64 : 0;
   const dim3 grid((unsigned)(a.B * a.H * (blocks + states)), (unsigned)((d2 + D2 - 1) / D2), (unsigned)n);
   if (grid.x == 0) return DARK_OK;
-  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_short<T, D1, D2, VEC, EXACT>), grid, dim3(512), lds, a, blocks, states);
+  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_short<T, D1, D2, VEC>), grid, dim3(512), lds, a, blocks, states);
   return DARK_OK;
 }
 template <typename T, int D1, int D2>
 static dark_status pick_short(const Scans& a, int n, hipStream_t st) {
   const bool vec = a.s[0].d1 * sizeof(T) % 16 == 0 && a.s[0].d2 * sizeof(T) % 16 == 0;
-  if (a.exact) return vec ? launch_short<T, D1, D2, true, true>(a, n, st) : launch_short<T, D1, D2, false, true>(a, n, st);
-  return vec ? launch_short<T, D1, D2, true, false>(a, n, st) : launch_short<T, D1, D2, false, false>(a, n, st);
+  return vec ? launch_short<T, D1, D2, true>(a, n, st) : launch_short<T, D1, D2, false>(a, n, st);
 }
 template <typename T>
 static dark_status pick_short(const Scans& a, int n, hipStream_t st) {

@@ -181,6 +181,43 @@ def test_needed_gradients_only():
     assert _backward(d, grads=own)["dQ"] is own["dQ"] and torch.equal(own["dV"], whole["dV"])
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("segments", [0, 1, 3])
+@pytest.mark.parametrize("widths", [(64, 64), (128, 64), (256, 64), (33, 65)])
+def test_the_same_bits_whatever_is_handed_out(widths, segments, dtype):
+    d = _device(U.problem(15, 2, 3, 333, *widths, dtype, lengths=[333, 191]))
+    out, grads = _forward(d, segments=segments)[0], _backward(d, segments=segments)
+    assert torch.equal(dk.dark_decay_fwd(d["Q"], d["K"], d["V"], d["a"], lengths=d["lengths"], segments=segments), out)
+    d["state"] = d["dstate"] = torch.zeros(2, 3, *widths, device="cuda")   # an empty state is none
+    assert torch.equal(_forward(d, segments=segments)[0], out)
+    same = _backward(d, segments=segments)
+    assert "dstate" in same and all(torch.equal(same[k], t) for k, t in grads.items())
+
+
+def _run_without_states(p, **kw):
+    d = _device(p)
+    want, size = U.oracle(p), U.oracle(p, magnitude=True)
+    U.check(dk.dark_decay_fwd(d["Q"], d["K"], d["V"], d["a"], lengths=d["lengths"], **kw), want["out"], size["out"], p["dtype"], "out")
+    grads = _backward(d, **kw)
+    assert set(grads) == {"dQ", "dK", "dV"}
+    for k, t in grads.items():
+        U.check(t, want[k], size[k], p["dtype"], k)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [1, 2, 31, 33, 64, 65, 200, 515])
+def test_lengths_without_states(L, dtype):
+    for segments in (0, 1, 2):
+        _run_without_states(U.problem(L, 2, 3, L, 64, 64, dtype), segments=segments)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("segments", [0, 1, 2])
+@pytest.mark.parametrize("widths", [(64, 64), (64, 128), (128, 64), (128, 128), (256, 64), (33, 65), (250, 131)])
+def test_widths_without_states(widths, segments, dtype):
+    _run_without_states(U.problem(16, 2, 2, 333, *widths, dtype, lengths=[333, 191]), segments=segments)
+
+
 def test_scale_and_repeatability():
     p = U.problem(12, 2, 4, 500, 64, 64, "bf16", state=True, dstate=True)
     _run(p, scale=0.75)
