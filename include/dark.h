@@ -375,8 +375,8 @@ dark_status dark_decay_step(const dark_decay_params* p, const void* q, const voi
  *   A finished beam has the one candidate (j, eos) of value scores[j]; its logits are not read.  Logits that are -infinity or
  *   NaN, a score that is not finite (a beam not in use: -infinity), and rows whose logits are all -infinity or
  *   hold +infinity make candidates of value -infinity: such ones are taken, in the order of j and t, only where there are too few others.
- *   The sums of exponentials are in fp32, everything behind them in fp64: candidates of different beams that lie closer together than
- *   about 2^-21 may come in either order, the same one in every call.
+ *   The sums of exponentials are in fp32, within 2^-19 of their values, everything behind them in fp64: candidates of different beams
+ *   that lie closer together than 2^-18 may come in either order, the same one in every call.
  * n <= 32 and n V < 2^31, B n <= 65535 (else DARK_EUNSUPPORTED; V too, beyond some millions); eos in 0 ... V - 1 if finished is given.
  */
 typedef struct {

@@ -6,7 +6,9 @@
 // the slice's maximum, its sum of exponentials and its n largest logits in order.  k_beam_pick joins the sums of a batch entry's
 // rows and takes the best of the sorted lists.
 // Two candidates of different beams may lie closer together than fp32 resolves beside a score: offsets and comparisons are in fp64, and
-// what tells them apart is then the sums, exact to 2^-22.
+// what tells them apart is then the sums.  A sum of exponentials is within 2^-19 of its value: 5 + 6 + 2 additions one after the other (a
+// thread's 32 terms, the lanes, the waves; beside a NaN one more) are off by at most 14 2^-24, an exponential by 2^-23, and where the terms that matter lie x below the
+// maximum, x log2 e < 2^5 since there are less than 2^27 of them, by ln 2 2^-20 for the exponent's rounding and 18 2^-26 for that of log2 e.
 // Where fp64 resolves no more either (a score of -10^20, logits that differ by 10^-20) the logits themselves decide within a beam.
 #include <cmath>
 
@@ -91,6 +93,13 @@ __device__ __forceinline__ unsigned nth_of_lanes(unsigned v, int n, int lane) {
     if (lane == __builtin_ctzll(__ballot(v == w))) v = 0;
   }
   return w;
+}
+
+// f(FIRST) + ... + f(FIRST + COUNT - 1) by halves: log2 COUNT roundings one after the other, and none where all terms are equal.
+template <int FIRST, int COUNT, typename F>
+__device__ __forceinline__ float tree(const F& f) {
+  if constexpr (COUNT == 1) return f(FIRST);
+  else return tree<FIRST, COUNT / 2>(f) + tree<FIRST + COUNT / 2, COUNT - COUNT / 2>(f);
 }
 
 // The element of row-relative index t, as a number that may win: NaN where there is none.
@@ -198,22 +207,16 @@ __global__ __launch_bounds__(256, 8) void k_beam_rows(const T* __restrict__ logi
   if (finite(m)) {
     const bool far = large(m);
     const float c = m * kLog2e;
-    if (far) {
-#pragma unroll
-      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f((number_of(word(e), e) - m) * kLog2e);
-    } else {
-#pragma unroll
-      for (int e = 0; e < E; ++e) s += __builtin_amdgcn_exp2f(fmaf(number_of(word(e), e), kLog2e, -c));
-    }
+    if (far) s = tree<0, E>([&](int e) { return __builtin_amdgcn_exp2f((number_of(word(e), e) - m) * kLog2e); });
+    else s = tree<0, E>([&](int e) { return __builtin_amdgcn_exp2f(fmaf(number_of(word(e), e), kLog2e, -c)); });
     if (__ballot(s != s) != 0) {   // a NaN counts for nothing
       s = 0.f;
 #pragma unroll 1
-      for (int k = 0; k < N; ++k)
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-          const float v = number(own, begin + (k * 256 + tid) * P + j, V);
-          s += v == v ? __builtin_amdgcn_exp2f(far ? (v - m) * kLog2e : fmaf(v, kLog2e, -c)) : 0.f;
-        }
+      for (int k = 0; k < N; k += 2)
+        s += tree<0, 2 * P>([&](int e) {
+          const float v = number(own, begin + ((k + e / P) * 256 + tid) * P + e % P, V);
+          return v == v ? __builtin_amdgcn_exp2f(far ? (v - m) * kLog2e : fmaf(v, kLog2e, -c)) : 0.f;
+        });
     }
   } else {
 #pragma unroll

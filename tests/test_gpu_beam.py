@@ -137,6 +137,43 @@ def test_candidates_that_no_double_tells_apart(shape, kind, dtype):
         assert all((r[0] == 7).all() and (r[2] == 7).all() for r in room)   # nothing beside the results
 
 
+def _sums_error(rows):
+    """How far the logarithms of the rows' sums of exponentials are off: [B, V] rows, each with a score that leaves its best candidate near
+    zero, so that the rounding of the result hides nothing."""
+    x = rows.double().numpy()
+    top = x.max(1, keepdims=True)
+    total = np.log(np.exp(x - top).sum(1))
+    scores = torch.from_numpy(total).float()
+    s, _, t = dk.dark_beam_select(rows[:, None].contiguous().cuda(), scores[:, None].contiguous().cuda())
+    assert (x[np.arange(len(x)), t[:, 0].cpu().numpy()] == top[:, 0]).all()
+    return np.abs(s[:, 0].double().cpu().numpy() - (scores.double().numpy() - total))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [8192, 24576])
+def test_sums_of_equal_logits(V, dtype):
+    # whole slices of equal terms: every addition by halves is exact, and an exponential is off by at most 2^-23
+    value = torch.cat([torch.tensor([513.117, -0.5, 0.0, 1e-3, -1e5, 1e6]), 700 * torch.rand(250, generator=torch.Generator().manual_seed(V)) - 350])
+    worst = _sums_error(value[:, None].expand(-1, V).to(TORCH[dtype])).max()
+    assert worst <= 2.0 ** -23 * 1.01
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("bad", [False, True])
+def test_sums_within_their_bound(bad, dtype):
+    # the bound of dark.h: 14 additions, an exponential, and exponents of up to 2^5 whose roundings may all have one sign
+    V, g = 131071, torch.Generator().manual_seed(8)
+    rows = torch.stack([torch.zeros(V) - x for x in (2.1, 7.3, 9.77, 10.9, 11.3, 11.77)] + [s * torch.randn(V, generator=g) for s in (0.1, 1.0, 3.0, 10.0)])
+    rows[:6, 5] = 0.0   # one large logit, and as much in all the others together
+    rows = (rows + torch.linspace(-40, 40, 10)[:, None]).to(TORCH[dtype])
+    error = _sums_error(rows if not bad else torch.where(torch.arange(V) % 301 == 7, float("-inf"), rows))
+    if bad:   # NaN count for nothing, as -infinity does
+        assert torch.equal(*(torch.stack(dk.dark_beam_select(torch.where(torch.arange(V) % 301 == 7, b, rows)[:, None].contiguous().cuda(),
+                                                             torch.zeros(10, 1, device="cuda"))[:1]) for b in (float("-inf"), float("nan"))))
+    print(error)
+    assert error.max() <= 2.0 ** -19, error
+
+
 def test_scores_in_place_and_given_outputs():
     logits, scores = _problem(5, 2, 4, 5000, "f32")
     logits, scores = logits.cuda(), scores.cuda()
