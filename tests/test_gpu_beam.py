@@ -37,6 +37,19 @@ def test_selection(shape, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(2, 32, 50001), (1, 32, 131071)])
+def test_lists_too_long_to_be_staged(shape, dtype):
+    # n n entries a slice: more than the second kernel brings to LDS, so that it reads them where they are
+    logits, scores = _problem(sum(shape), *shape, dtype)
+    logits[:, 3, 100:] = float("-inf")   # slices without an entry
+    logits[:, 4, ::7] = float("nan")
+    finished = torch.arange(shape[1]).repeat(shape[0], 1) % 5 == 2
+    _check(logits, scores, finished, 7)
+    scores[:, 1:] = float("-inf")
+    _check(logits, scores)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_equal_candidates(dtype):
     logits, scores = _problem(1, 3, 4, 3000, dtype)
     logits = logits.round()          # many equal logits in a row
