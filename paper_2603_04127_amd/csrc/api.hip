@@ -39,7 +39,7 @@ const char* kernel_name(int k) {
       "f32_finish",   "f32_scan",   "f32_bwd_elem", "fused_prep",   "fused_kv_reduce", "fused_kv_merge",
       "fused_readout", "fused_key_norms", "fused_causal_state", "fused_causal_prefix", "fused_causal_scan", "fused_featurize",
       "fused_bwd_fwd", "fused_bwd_suffix", "fused_bwd_rev", "fused_bwd_dm", "whiten_moments", "whiten_eig", "decode_step",
-      "decay_state", "decay_prefix", "decay_scan", "decay_step", "beam_rows", "beam_pick", "state_reorder"};
+      "decay_state", "decay_prefix", "decay_scan", "decay_short", "decay_copy", "decay_step", "beam_rows", "beam_pick", "state_reorder"};
   return (k >= 0 && k < KID_COUNT) ? names[k] : "?";
 }
 bool timing_on() { return g_timing; }

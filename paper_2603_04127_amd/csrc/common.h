@@ -43,6 +43,8 @@ enum KernelId : int {
   KID_DECAY_STATE,     // decayed linear attention: states of the segments
   KID_DECAY_PREFIX,    // decayed linear attention: states before every segment
   KID_DECAY_SCAN,      // decayed linear attention: outputs, or gradients, of a segment chunk by chunk
+  KID_DECAY_SHORT,     // decayed linear attention: short sequences, in one launch
+  KID_DECAY_COPY,      // decayed linear attention: copy of a state that is updated in place
   KID_DECAY_STEP,      // decayed linear attention: one token
   KID_BEAM_ROWS,       // beam search: sums and largest logits of every slice of a row
   KID_BEAM_PICK,       // beam search: the next beams of a batch entry

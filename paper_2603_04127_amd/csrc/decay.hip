@@ -281,7 +281,7 @@ dark_status forward(const Problem& pb, Arena& ar, const void* Q, const void* K, 
     float* const copy = ar.take<float>((size_t)size);
     if (ar.overflow) return DARK_EWORKSPACE;
     const long long blocks = (size + 1023) / 1024;
-    DARK_LAUNCH(KID_DECAY_PREFIX, pb.st, k_decay_copy, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, S_in, copy, size);
+    DARK_LAUNCH(KID_DECAY_COPY, pb.st, k_decay_copy, dim3((unsigned)(blocks < 65536 ? blocks : 65536)), dim3(256), 0, S_in, copy, size);
     S_in = copy;
   }
   if (ar.overflow) return DARK_EWORKSPACE;

@@ -252,7 +252,7 @@ static dark_status launch_short(const Scans& a, int n, hipStream_t st) {
   const int blocks = rows ? (a.L + 63) / 64 : 0, states = out ? ((d2 < D2 ? d2 : D2) + 63) / 64 : 0;
   const dim3 grid((unsigned)(a.B * a.H * (blocks + states)), (unsigned)((d2 + D2 - 1) / D2), (unsigned)n);
   if (grid.x == 0) return DARK_OK;
-  DARK_LAUNCH(KID_DECAY_SCAN, st, (k_decay_short<T, D1, D2, VEC>), grid, dim3(512), lds, a, blocks, states);
+  DARK_LAUNCH(KID_DECAY_SHORT, st, (k_decay_short<T, D1, D2, VEC>), grid, dim3(512), lds, a, blocks, states);
   return DARK_OK;
 }
 template <typename T, int D1, int D2>

@@ -218,6 +218,24 @@ def test_widths_without_states(widths, segments, dtype):
     _run_without_states(U.problem(16, 2, 2, 333, *widths, dtype, lengths=[333, 191]), segments=segments)
 
 
+def test_every_form_is_timed_under_its_own_name():
+    def names(L, dtype, segments, in_place):
+        d = _device(U.problem(17, 1, 2, L, 64, 64, dtype, state=True))
+        dk.timing_reset()
+        dk.timing_enable(True)
+        try:
+            dk.dark_decay_fwd(d["Q"], d["K"], d["V"], d["a"], state=d["state"], state_out=d["state"] if in_place else None, segments=segments)
+            return {k: n for k, (n, _) in dk.timing_read().items()}
+        finally:
+            dk.timing_enable(False)
+            dk.timing_reset()
+
+    assert names(300, "bf16", 0, False) == {"decay_short": 1}
+    assert names(300, "bf16", 0, True) == {"decay_copy": 1, "decay_short": 1}
+    assert names(300, "bf16", 1, True) == names(20, "f32", 0, False) == {"decay_scan": 1}
+    assert names(300, "f32", 2, True) == {"decay_state": 1, "decay_prefix": 1, "decay_scan": 1}
+
+
 def test_scale_and_repeatability():
     p = U.problem(12, 2, 4, 500, 64, 64, "bf16", state=True, dstate=True)
     _run(p, scale=0.75)
