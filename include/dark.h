@@ -308,14 +308,15 @@ dark_status dark_decode_step(const dark_params* p, const void* q, const void* k,
  *   DARK_BLHD (as a projection lays them out); all of them in the same layout.
  *   log_decay: [H] float32, the natural logarithm of the decay: 0 keeps everything, -infinity nothing but the token itself.
  *   A decay is a constant of the model: there is no gradient with respect to it.  Values above 0 are computed as
- *   they are; it must not be NaN or +infinity.
+ *   they are, as long as exp(L log_decay) is a number in fp32 (beyond it results may be NaN); it must not be NaN or +infinity.
  *   lengths: [B] int32 or NULL (every sequence has L tokens).  Sequence b has its first lengths[b] rows, values outside
  *   0 ... L count as the nearer of the two.  What lies behind a sequence in Q, K, V and dOut does not matter; out and
  *   the gradients are 0 there.
  *   States are float32, [B, H, dk, dv].  S_in NULL: zero.  S_out NULL: not wanted.  S_out is the state behind the last
  *   token; S_out == S_in updates a state in place.  Any other overlap of a result with an operand or another result is
  *   DARK_EINVAL, here and in the calls below.
- * dk and dv up to 256 (else DARK_EUNSUPPORTED), of any size; rows of whole 16 bytes are faster.  L == 0: the state is passed on.
+ * dk and dv up to 256 (else DARK_EUNSUPPORTED), of any size; rows of whole 16 bytes are faster (V with a column of ones, for a normaliser:
+ * padded to a multiple of 8 columns).  L == 0: the state is passed on.
  *
  * Arithmetic: fp32 operands are multiplied and summed in fp32.  bf16 operands go through the matrix units with fp32 sums; the
  * weights (q_t . k_l) g^(t-l), formed inside a chunk of 64 rows and in short sequences everywhere, and the state where it is read,
@@ -347,6 +348,8 @@ dark_status dark_decay_fwd(const dark_decay_params* p, const void* Q, const void
  * Gradients of sum(out dOut) + sum(S_out dS_out).  dS_out NULL: zero.  dQ, dK, dV have the element type and layout of what
  * they belong to (a product of bf16 operands has no more than its precision); dS_in: float32.  All are overwritten; each may be
  * NULL (skipped).  Nothing is needed from the forward call.
+ * An element that is not finite makes the gradients of its own row not finite; one of K or V also dQ from its row on, one of Q or dOut dK and
+ * dV up to its row; one of K dQ of up to 63 rows before it, one of Q or dOut dK or dV of up to 63 rows behind it.
  */
 dark_status dark_decay_bwd(const dark_decay_params* p, const void* Q, const void* K, const void* V, const float* log_decay,
                            const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out,

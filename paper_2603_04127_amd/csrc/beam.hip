@@ -119,7 +119,8 @@ __device__ __forceinline__ float number(const T* row, long long t, int V) {
 // Vector instructions bound it for bf16, memory for fp32.  Hence: 16-bit elements stay packed, and in two passes of three the upper one
 // of a pair is taken with the lower one's bits behind it, which no comparison between such numbers minds; a NaN costs the sum a
 // second pass instead of every element an instruction.
-// (32 x 8 rows of 131,071, n = 8: 70 us when every wave took its largest out one by one, 25 with a list for every wave, 19.5 now.
+// (32 x 8 rows of 131,071, n = 8: 70 us when every wave took its largest out one by one, 25 with a list for every wave, 19.5 now; fp32 25.6,
+// 134 MB at 5.2 TB/s.
 // Slices of 2048: as many lists more for k_beam_pick; 1 x 4 rows of 32,000 4.1 + 6.2 us against 4.6 + 5.4, 1 x 8 of 131,071 4.7 + 10.9
 // against 5.8 + 6.7, 16 x 8 of them 19 + 12 against 12.4 + 7.3.  Of 16,384: no faster, and more registers for fp32.)
 constexpr int kMostPassed = 64, kEach = 32, kSlice = 256 * kEach;
@@ -488,7 +489,7 @@ __global__ __launch_bounds__(256) void k_beam_pick(const Part* __restrict__ part
 
 // ---------------------------------------------------------------------------
 // States in place: a thread holds the same 16 (4, 1) bytes of every row that changes, so that all are read before any is written.
-// Bound by reading the parents of the rows that change and writing those rows (8 x 4 beams, two layers of 16 x 256 x 128: 86 MB in 17 us).
+// Bound by reading the parents of the rows that change and writing those rows (8 x 4 beams, two layers of 16 x 256 x 128: 75 MB in 17.7 us).
 // ---------------------------------------------------------------------------
 constexpr int kMostTensors = 16;
 struct Tensors {

@@ -8,10 +8,10 @@
 // second workgroup (24 heads of 2048 x 256, values 64 wide: 48.6 -> 43 us).
 // Per chunk: P = x1 x2^T, decayed and masked, by all waves together through LDS; y^T = U^T x1^T + x3^T P^T; U' = g^C U + x2^T (w x3).
 // The next chunk's rows are on their way into registers meanwhile.
-// Long sequences are bound by memory: 64 heads of 8192 x 128 in 8 segments, the segment states 264 MB in 57 us, the scan 585 MB in 120 us, both
-// the rate of a copy.  With 64 wide heads (24 of 4096: states 10, scan 18 us; the three scans of the backward pass 31 us) vector
-// instructions and LDS take a third of the time each and the waits between a chunk's steps the rest; fp32 (36 heads of 509 x 64: 7 and
-// 12 us) waits for its products, 1.7 us of the 2.8 of a chunk.
+// Long sequences of many heads are bound by memory: 64 heads of 8192 x 128 in 8 segments, the segment states 264 MB in 70 us (59 at least), the
+// scan 575 MB in 143 us (118), 4 to 4.9 TB/s where a copy has 4.9.  With 64 wide heads (24 of 4096: states 10, scan 18 us for 28 and 55 MB; of
+// the backward pass 13 and 33 us for 47 and 130 MB) memory takes over half of the time, the waits between a chunk's steps the rest; fp32
+// (36 heads of 509 x 64: 7 and 12 us) waits for its products, 1.7 us of the 2.8 of a chunk.
 #pragma once
 
 #include "decay.h"
