@@ -7,8 +7,9 @@
 // rows and takes the best of the sorted lists.
 // Two candidates of different beams may lie closer together than fp32 resolves beside a score: offsets and comparisons are in fp64, and
 // what tells them apart is then the sums.  A sum of exponentials is within 2^-19 of its value: 5 + 6 + 2 additions one after the other (a
-// thread's 32 terms, the lanes, the waves; beside a NaN one more) are off by at most 14 2^-24, an exponential by 2^-23, and where the terms that matter lie x below the
-// maximum, x log2 e < 2^5 since there are less than 2^27 of them, by ln 2 2^-20 for the exponent's rounding and 18 2^-26 for that of log2 e.
+// thread's 32 terms, the lanes, the waves; beside a NaN one more) are off by at most 14 2^-24, an exponential by 2^-23, and where the terms
+// that matter lie x below the maximum, x < 19 since there are less than 2^27 of them, ln 2 2^-20 for the rounding of the exponent x log2 e < 2^5
+// and 19 2^-26 for that of log2 e.
 // Where fp64 resolves no more either (a score of -10^20, logits that differ by 10^-20) the logits themselves decide within a beam.
 #include <cmath>
 
