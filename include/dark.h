@@ -367,6 +367,63 @@ dark_status dark_decay_step(const dark_decay_params* p, const void* q, const voi
                             const int32_t* parent, int state_rows, const float* S_in, float* S_out, void* out, void* hip_stream);
 
 /*
+ * The gated delta rule: linear attention whose state forgets by a gate of each token, and corrects what it holds for a key before it
+ * adds to it.  Per (b, h), with a_t = exp(log_gate_t), from a state S_0 [dk, dv]:
+ *   u_t = beta_t (v_t - a_t S_(t-1)^T k_t),      S_t = a_t S_(t-1) + k_t u_t^T,      out_t = scale S_t^T q_t,      t = 1 ... n.
+ * Chunked form (prompts, training): dark_delta_fwd, dark_delta_bwd; recurrent form (single tokens): dark_delta_step.
+ *
+ *   Q, K: [B, H, L, dk], V, out: [B, H, L, dv] in io_dtype with layout DARK_BHLD, or [B, L, H, dk] and [B, L, H, dv] with DARK_BLHD; all of
+ *   them in the same layout.  Keys are taken as they are: a rule that is to stay bounded needs beta_t |k_t|^2 <= 2 (keys of length one).
+ *   log_gate, beta: [B, H, L] float32, [B, L, H] with DARK_BLHD.  log_gate, the natural logarithm of the gate: 0 keeps everything,
+ *   -infinity nothing of what was before; NULL: 0 everywhere.  Values above 0 are computed as they are, as long as the exponential of
+ *   the sum of 64 consecutive ones is a number in fp32.
+ *   lengths: [B] int32 or NULL (every sequence has L tokens).  Sequence b has its first lengths[b] rows, values outside 0 ... L count as the
+ *   nearer of the two.  What lies behind a sequence in the operands does not matter; out and the gradients are 0 there.
+ *   States are float32, [B, H, dk, dv].  S_in NULL: zero.  S_out NULL: not wanted.  S_out is the state behind the last token; S_out == S_in
+ *   updates a state in place.  Any other overlap of a result with an operand or another result is DARK_EINVAL, here and below.
+ * dk and dv up to 256, B H L up to 2^28 (else DARK_EUNSUPPORTED); rows of whole 16 bytes are faster.  L == 0: the state is passed on.
+ *
+ * Arithmetic: products on the matrix units, with fp32 sums, of operands that are sums of bf16 numbers: 24 bits of whatever has 32 (states,
+ * corrections, fp32 operands), the operands themselves where they are bf16.  What goes into a bf16 output alone keeps 16 bits.  Outputs and gradients do not depend on which others are wanted.
+ * An element of K, V, log_gate or beta that is not finite makes the outputs from its row on not finite, in its column at least for V, and may
+ * make those of up to 63 rows before it so.
+ */
+typedef struct {
+  int32_t B, H, L;        /* batch, heads, rows of a sequence */
+  int32_t dk, dv;         /* width of queries and keys, of values */
+  int32_t io_dtype;       /* dark_dtype of Q, K, V, out, dOut, dQ, dK, dV */
+  int32_t layout;         /* dark_layout */
+  float scale;            /* 0 = 1/sqrt(dk) */
+} dark_delta_params;
+
+/* Bytes of scratch of dark_delta_fwd (backward == 0) or dark_delta_bwd; 0 on invalid parameters, and where none is needed. */
+size_t dark_delta_workspace_bytes(const dark_delta_params* p, int backward);
+
+dark_status dark_delta_fwd(const dark_delta_params* p, const void* Q, const void* K, const void* V, const float* log_gate,
+                           const float* beta, const int32_t* lengths, const float* S_in, void* out, float* S_out,
+                           void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * Gradients of sum(out dOut) + sum(S_out dS_out).  dS_out NULL: zero.  dQ, dK, dV have the element type and layout of what they belong to;
+ * dlog_gate, dbeta and dS_in are float32.  All are overwritten; each may be NULL (skipped).  Nothing is needed from the forward
+ * call.  The gradient of a gate of exp(log_gate) == 0 is 0.  An element that is not finite makes the gradients of its sequence not finite
+ * from its chunk of 64 rows on, or up to it, or both.
+ */
+dark_status dark_delta_bwd(const dark_delta_params* p, const void* Q, const void* K, const void* V, const float* log_gate,
+                           const float* beta, const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out,
+                           void* dQ, void* dK, void* dV, float* dlog_gate, float* dbeta, float* dS_in,
+                           void* ws, size_t ws_bytes, void* hip_stream);
+
+/*
+ * One token: q, k [B, H, dk], v, out [B, H, dv] in io_dtype, log_gate (or NULL) and beta [B, H] float32; p->L and p->layout do not matter;
+ * q, k, v and out need the alignment of their elements only.  No workspace.  fp32 arithmetic.
+ * parent, state_rows, S_in and S_out as in dark_decay_step.
+ */
+dark_status dark_delta_step(const dark_delta_params* p, const void* q, const void* k, const void* v, const float* log_gate,
+                            const float* beta, const int32_t* parent, int state_rows, const float* S_in, float* S_out, void* out,
+                            void* hip_stream);
+
+/*
  * Beam search: the next n beams of each batch entry.  Candidate (j, t), beam j going on with token t, is worth
  *   scores[j] + logits[j][t] - log sum_u exp logits[j][u];
  * the n largest are taken, of equal ones that with the lowest j, then the lowest t.  In one beam a larger logit is a larger candidate,

@@ -41,6 +41,13 @@ class DecayParams(ctypes.Structure):
     ]
 
 
+class DeltaParams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("H", ctypes.c_int32), ("L", ctypes.c_int32), ("dk", ctypes.c_int32), ("dv", ctypes.c_int32),
+        ("io_dtype", ctypes.c_int32), ("layout", ctypes.c_int32), ("scale", ctypes.c_float),
+    ]
+
+
 class BeamParams(ctypes.Structure):
     _fields_ = [
         ("B", ctypes.c_int32), ("n", ctypes.c_int32), ("V", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("eos", ctypes.c_int32),
@@ -104,6 +111,15 @@ def lib() -> ctypes.CDLL:
     L.dark_decay_bwd.argtypes = [dp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     L.dark_decay_step.restype = i32
     L.dark_decay_step.argtypes = [dp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
+    ep = ctypes.POINTER(DeltaParams)
+    L.dark_delta_workspace_bytes.restype = sz
+    L.dark_delta_workspace_bytes.argtypes = [ep, i32]
+    L.dark_delta_fwd.restype = i32
+    L.dark_delta_fwd.argtypes = [ep, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.dark_delta_bwd.restype = i32
+    L.dark_delta_bwd.argtypes = [ep, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.dark_delta_step.restype = i32
+    L.dark_delta_step.argtypes = [ep, vp, vp, vp, vp, vp, vp, i32, vp, vp, vp, vp]
     L.dark_beam_workspace_bytes.restype = sz
     L.dark_beam_workspace_bytes.argtypes = [bp]
     L.dark_beam_select.restype = i32
@@ -435,7 +451,7 @@ def dark_attn_bwd(Q, K, V, M, W, dOut, causal: bool, *, chunk=0, scale=0.0, path
 
 
 # ----------------------------------------------------------------------------
-# linear attention with a decay for each head; beam search over recurrent states
+# linear attention with a decay for each head
 # ----------------------------------------------------------------------------
 _LAYOUTS = {"bhld": BHLD, "blhd": BLHD}
 
@@ -587,6 +603,142 @@ def dark_decay_step(q, k, v, log_decay, state, *, parent=None, state_out=None, o
     return out
 
 
+# ----------------------------------------------------------------------------
+# the gated delta rule
+# ----------------------------------------------------------------------------
+def _delta_plan(Q, K, V, layout, scale, backward):
+    """(DeltaParams, workspace bytes, shape of the gates) of a call."""
+    key = ("delta", Q.shape, Q.dtype, K.shape, K.dtype, V.shape, V.dtype, layout, scale, backward)
+    plan = _plans.get(key)
+    if plan is None:
+        if layout not in _LAYOUTS:
+            raise ValueError(f"layout must be one of {sorted(_LAYOUTS)}")
+        if Q.dim() != 4 or K.shape != Q.shape or V.dim() != 4 or V.shape[:3] != Q.shape[:3]:
+            raise ValueError("Q, K and V must have the same batch, heads and length, Q and K the same width")
+        if K.dtype != Q.dtype or V.dtype != Q.dtype:
+            raise TypeError("Q, K and V must have one type")
+        B, H, L, dk = Q.shape if layout == "bhld" else (Q.shape[0], Q.shape[2], Q.shape[1], Q.shape[3])
+        p = DeltaParams(B, H, L, dk, V.shape[3], _dtype_code(Q), _LAYOUTS[layout], scale)
+        plan = (p, int(lib().dark_delta_workspace_bytes(ctypes.byref(p), int(backward))), Q.shape[:3])
+        _keep_plan(key, plan)
+    return plan
+
+
+def dark_delta_fwd(Q, K, V, log_gate, beta, *, lengths=None, state=None, out=None, state_out=None, want_state=False, scale=0.0, layout="bhld"):
+    """Linear attention by the gated delta rule, from `state` [B,H,dk,dv] (None: empty): with a = exp(log_gate_t),
+    u_t = beta_t (v_t - a S_{t-1}^T k_t), S_t = a S_{t-1} + k_t u_t^T, out_t = scale S_t^T q_t.
+    Q, K [B,H,L,dk], V [B,H,L,dv], log_gate (None: no decay) and beta [B,H,L] float32 (layout "blhd": [B,L,H,..] and [B,L,H]).
+    Returns out, or (out, state after the last token) with want_state or a `state_out` (which may be `state`).
+    `lengths` [B] int32: rows of each sequence; out is 0 behind them."""
+    torch = _torch()
+    p, nb, gates = _delta_plan(Q, K, V, layout, float(scale), False)
+    f32, shape = torch.float32, (p.B, p.H, p.dk, p.dv)
+    _require(log_gate, f32, gates, "log_gate")
+    _require(beta, f32, gates, "beta")
+    _require(lengths, torch.int32, (p.B,), "lengths")
+    _require(state, f32, shape, "state")
+    _require(state_out, f32, shape, "state_out")
+    _require(out, V.dtype, V.shape, "out")
+    index, (q, k, v, a, be, n, s, o, so) = _pointers(Q, K, V, log_gate, beta, lengths, state, out, state_out)
+    if index != torch._C._cuda_getDevice():   # enqueued on the current stream of the tensors' device
+        with torch.cuda.device(index):
+            return dark_delta_fwd(Q, K, V, log_gate, beta, lengths=lengths, state=state, out=out, state_out=state_out, want_state=want_state,
+                                  scale=scale, layout=layout)
+    if o is None:
+        out = torch.empty_like(V)
+        o = out.data_ptr()
+    if want_state and so is None:
+        state_out = torch.empty(shape, dtype=f32, device=Q.device) if state is None else torch.empty_like(state)
+        so = state_out.data_ptr()
+    ws, stream = _workspace(nb, Q.device) if nb else (None, torch._C._cuda_getCurrentRawStream(index))
+    _check(lib().dark_delta_fwd(ctypes.byref(p), q, k, v, a, be, n, s, o, so, None if ws is None else ws.data_ptr(), nb, stream), "dark_delta_fwd")
+    return out if state_out is None else (out, state_out)
+
+
+_DELTA_GRADS = ("dQ", "dK", "dV", "dlog_gate", "dbeta", "dstate")
+
+
+def dark_delta_bwd(Q, K, V, log_gate, beta, dOut, *, lengths=None, state=None, dstate=None, need=_DELTA_GRADS, grads=None, scale=0.0,
+                   layout="bhld"):
+    """Gradients of sum(out dOut) + sum(state_out dstate) of dark_delta_fwd: a dict of those named in `need` ("dlog_gate" only where
+    `log_gate` is given, "dstate", the gradient of the incoming state, only where `state` is), in the types and layouts of what they belong to.
+    `grads`: a dict of preallocated tensors to write into instead."""
+    torch = _torch()
+    p, nb, gates = _delta_plan(Q, K, V, layout, float(scale), True)
+    f32, shape = torch.float32, (p.B, p.H, p.dk, p.dv)
+    _require(log_gate, f32, gates, "log_gate")
+    _require(beta, f32, gates, "beta")
+    _require(lengths, torch.int32, (p.B,), "lengths")
+    _require(state, f32, shape, "state")
+    _require(dstate, f32, shape, "dstate")
+    _require(dOut, V.dtype, V.shape, "dOut")
+    like = {"dQ": Q, "dK": K, "dV": V, "dbeta": beta}
+    if log_gate is not None:
+        like["dlog_gate"] = log_gate
+    if state is not None:
+        like["dstate"] = state
+    unknown = set(need if grads is None else grads) - set(_DELTA_GRADS)
+    if unknown:
+        raise ValueError(f"unknown gradient(s) {sorted(unknown)}")
+    g = {} if grads is None else {name: t for name, t in grads.items() if t is not None}
+    for name, t in g.items():
+        _require(t, *((f32, shape) if name == "dstate" else (f32, gates) if name in ("dlog_gate", "dbeta") else (like[name].dtype, like[name].shape)), name)
+    index, (q, k, v, a, be, do, n, s, ds, *gp) = _pointers(Q, K, V, log_gate, beta, dOut, lengths, state, dstate, *(g.get(x) for x in _DELTA_GRADS))
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return dark_delta_bwd(Q, K, V, log_gate, beta, dOut, lengths=lengths, state=state, dstate=dstate, need=need, grads=grads, scale=scale,
+                                  layout=layout)
+    if grads is None:
+        g = {name: torch.empty_like(x) for name, x in like.items() if name in need}
+        gp = [g[name].data_ptr() if name in g else None for name in _DELTA_GRADS]
+    ws, stream = _workspace(nb, Q.device) if nb else (None, torch._C._cuda_getCurrentRawStream(index))
+    _check(lib().dark_delta_bwd(ctypes.byref(p), q, k, v, a, be, n, s, do, ds, *gp, None if ws is None else ws.data_ptr(), nb, stream),
+           "dark_delta_bwd")
+    return g
+
+
+def dark_delta_step(q, k, v, log_gate, beta, state, *, parent=None, state_out=None, out=None, scale=0.0):
+    """One token of dark_delta_fwd: q, k [B,H,dk], v [B,H,dv], log_gate (None: no decay) and beta [B,H] float32; returns out [B,H,dv].
+    `state`, `state_out` and `parent` as in dark_decay_step."""
+    torch = _torch()
+    scale = float(scale)
+    key = ("delta_step", q.shape, q.dtype, k.shape, k.dtype, v.shape, v.dtype, scale)
+    plan = _plans.get(key)
+    if plan is None:
+        if q.dim() != 3 or k.shape != q.shape or v.dim() != 3 or v.shape[:2] != q.shape[:2]:
+            raise ValueError("q and k must be [B, H, dk], v [B, H, dv]")
+        if k.dtype != q.dtype or v.dtype != q.dtype:
+            raise TypeError("q, k and v must have one type")
+        p = DeltaParams(q.shape[0], q.shape[1], 1, q.shape[2], v.shape[2], _dtype_code(q), BHLD, scale)
+        plan = (p, (p.B, p.H, p.dk, p.dv))
+        _keep_plan(key, plan)
+    p, shape = plan
+    if state_out is None:
+        if parent is not None:
+            raise ValueError("a step that reads its states through `parent` needs a state_out")
+        state_out = state
+    f32, rows = torch.float32, state.shape[0]
+    _require(log_gate, f32, shape[:2], "log_gate")
+    _require(beta, f32, shape[:2], "beta")
+    _require(parent, torch.int32, shape[:1], "parent")
+    _require(state, f32, (rows,) + shape[1:], "state")
+    _require(state_out, f32, shape, "state_out")
+    _require(out, v.dtype, v.shape, "out")
+    index, (pq, pk, pv, a, be, s, pp, so, o) = _pointers(q, k, v, log_gate, beta, state, parent, state_out, out)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return dark_delta_step(q, k, v, log_gate, beta, state, parent=parent, state_out=state_out, out=out, scale=scale)
+    if o is None:
+        out = torch.empty_like(v)
+        o = out.data_ptr()
+    _check(lib().dark_delta_step(ctypes.byref(p), pq, pk, pv, a, be, pp, rows, s, so, o, torch._C._cuda_getCurrentRawStream(index)),
+           "dark_delta_step")
+    return out
+
+
+# ----------------------------------------------------------------------------
+# beam search over recurrent states
+# ----------------------------------------------------------------------------
 def dark_beam_select(logits, scores, *, finished=None, eos=0, keep_slots=False, out=None):
     """The next n beams of each batch entry from logits [B,n,V] and scores [B,n] (float32): (scores, parent, token), [B,n] each,
     parent and token int32.  Candidate (j, t) is worth scores[j] + log_softmax(logits[j])[t]; best first, equal ones by the lowest j, then

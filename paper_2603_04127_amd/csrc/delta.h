@@ -1,0 +1,77 @@
+// The gated delta rule: what its translation units share.
+//
+// Per (b,h), with a_t = exp(log_gate_t), from a state S_0 [dk, dv]:
+//   u_t = beta_t (v_t - a_t S_(t-1)^T k_t),   S_t = a_t S_(t-1) + k_t u_t^T,   o_t = scale S_t^T q_t.
+// A chunk of C rows from the state S before it, with G_t the sum of the chunk's log gates up to row t, gamma_t = exp(G_t),
+// left_t = exp(G_C - G_t), Gamma = exp(G_C), D_ti = exp(G_t - G_i) for i <= t, E_ti = D_ti (k_t . k_i) for i < t (zero elsewhere):
+//   T = (I + diag(beta) E)^-1,   P = D o (Q K^T),
+//   R = diag(beta) (V - diag(gamma) K S),   U = T R,   O = scale (diag(gamma) Q S + P U),   S' = Gamma S + K^T diag(left) U.
+// Every exponent that is formed is a sum of gates of consecutive tokens: with gates <= 0 nothing overflows.
+// Backward, from the gradient G' of the state behind the chunk (below: dS'):
+//   dU = scale P^T dO + diag(left) K dS',   dR = T^T dU,   dV = diag(beta) dR,
+//   dS = Gamma dS' + scale Q^T diag(gamma) dO - K^T diag(gamma beta) dR,
+//   N = scale D o (dO U^T),   M = -diag(beta) (D o (dR U^T)) below the diagonal,
+//   dQ = scale diag(gamma) dO S^T + N K,
+//   dK = -diag(gamma beta) dR S^T + diag(left) U dS'^T + M K + M^T K + N^T Q,
+//   dbeta_t = dR_t . v_t - gamma_t k_t . (S dR_t) - sum_(i<t) E_ti (dR_t . u_i),
+// and the gradient of log gate t sums, over all weights exp(G_r - G_i) with i < t <= r, the weight times its gradient.
+// Three kernels forward: k_delta_prep (T and P of every chunk, in parallel), k_delta_scan (chunk after chunk); backward k_delta_prep,
+// k_delta_scan (states and U), k_delta_rev (dS' and dR, from the last chunk to the first), k_delta_grad (the rest, in parallel).
+#pragma once
+
+#include "rows.h"
+
+namespace dark {
+namespace delta {
+
+struct Problem {
+  dark_delta_params p;
+  float scale;    // resolved (never 0)
+  hipStream_t st;
+  long long BH() const { return (long long)p.B * p.H; }
+};
+
+// Rows of a chunk, blocks of 16 rows and 32 inner values that a lower triangle of C x C consists of as an operand.
+constexpr int chunk_of(int io_dtype) { return io_dtype == DARK_BF16 ? 64 : 32; }
+constexpr int blocks_of(int C) { return C == 64 ? 6 : 2; }
+// Floats that k_delta_prep leaves for a chunk beside its operands: gamma, left, beta, and G as the sum of two floats.
+constexpr int kVecs = 5;
+
+struct Args {
+  const void *Q, *K, *V, *dOut;
+  const float *log_gate, *beta;
+  const int32_t* lengths;
+  void *out, *dQ, *dK, *dV;
+  float *dgate, *dbeta;
+  const float* s_in;      // state before the first row (scan), gradient of the state behind the last (rev); null: zero
+  float* s_out;           // state behind the last row (scan), gradient of that before the first (rev); null: not asked for
+  int B, H, L, dk, dv, layout, chunks;
+  int dvp;                // columns of scratch states and rows: dv, rounded up to 64
+  float scale;
+  // scratch, for every (b,h) and chunk
+  float* tri;             // T in operand order, blocks_of(C) x 64 lanes x 8
+  float* trit;            // T^T (backward)
+  void* pri;              // P in operand order (bf16: as two planes); backward: P^T scale
+  float* vec;             // kVecs x C
+  float* states;          // [D1, dvp], before the chunk
+  float* dstates;         // [D1, dvp], gradient of the state behind the chunk
+  float *u, *dr;          // [C, dvp]
+};
+
+// What the launches of a call share beside the arguments.
+enum Pass { kForward, kStates };
+
+dark_status launch_prep_bf16(const Args& a, bool backward, hipStream_t st);
+dark_status launch_prep_f32(const Args& a, bool backward, hipStream_t st);
+dark_status launch_scan_bf16(const Args& a, Pass pass, hipStream_t st);
+dark_status launch_scan_f32(const Args& a, Pass pass, hipStream_t st);
+dark_status launch_rev_bf16(const Args& a, hipStream_t st);
+dark_status launch_rev_f32(const Args& a, hipStream_t st);
+dark_status launch_grad_bf16(const Args& a, hipStream_t st);
+dark_status launch_grad_f32(const Args& a, hipStream_t st);
+
+// Rows of the state that the kernels hold.
+inline int inner_of(int dk) { return dk > 128 ? 256 : dk > 64 ? 128 : 64; }
+
+}  // namespace delta
+}  // namespace dark

@@ -1,0 +1,501 @@
+// The gated delta rule chunk by chunk: the chunks' triangles, and the scans over them (see delta.h for the mathematics).
+#pragma once
+
+#include "delta_tile.h"
+
+namespace dark {
+namespace delta {
+
+// ---------------------------------------------------------------------------
+// T = (I + diag(beta) E)^-1 and P = D o (Q K^T) of every chunk, in operand order; backward their transposes, P times scale.
+// The inverse: blocks of 16 x 16 on the diagonal by substitution, row after row; below it T_rc = -T_rr sum_m A_rm T_mc, by fp32 matrix
+// products, one diagonal of blocks after the other.  Substitution and products are backward stable for any beta and keys.
+// ---------------------------------------------------------------------------
+template <typename T, int D1>
+constexpr int prep_lds() {
+  constexpr int C = Kind<T>::kChunk;
+  return 2 * Mat<C, D1, Kind<T>::kIn>::kAll + 3 * C * (C + 4) * 4 + kVecs * C * 4;
+}
+
+template <typename T, int D1, bool VEC, bool BWD>
+__global__ __launch_bounds__(256) void k_delta_prep(Args A) {
+  constexpr int C = Kind<T>::kChunk, NT = C / 16, NI = Kind<T>::kIn, NB = blocks_of(C), NTH = 256, S = C + 4;
+  typedef Mat<C, D1, NI> M;
+  constexpr int tk = 0, tq = M::kAll, ta = 2 * M::kAll, tt = ta + 4 * C * S, tp = tt + 4 * C * S, tv = tp + 4 * C * S;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int bh = blockIdx.x / A.chunks, c = blockIdx.x % A.chunks, r0 = c * C, n = length_of(A, bh), nr = min(C, n - r0);
+  if (nr <= 0) return;
+  {
+    const Rows k = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), q = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk);
+    Load<T, C, D1, NTH, VEC> lk, lq;
+    lk.load(k, r0, nr, tid);
+    lq.load(q, r0, nr, tid);
+    if (wave == 0) {
+      // Sums of log gates in 64 bits, as two floats: their differences are as exact as the gates.  exp(-1e4) is 0; -infinity would
+      // leave infinity - infinity.
+      float g = 0.f, be = 0.f;
+      if (lane < nr) {
+        if (A.log_gate != nullptr) g = A.log_gate[gate_at(A, bh, r0 + lane)];
+        be = A.beta[gate_at(A, bh, r0 + lane)];
+        g = g < -1e4f ? -1e4f : g;
+      }
+      double G = (double)g;
+#pragma unroll
+      for (int o = 1; o < C; o <<= 1) {
+        const double x = __shfl_up(G, o, 64);
+        if (lane >= o) G += x;
+      }
+      const double end = __shfl(G, C - 1, 64);
+      const float hi = (float)G, lo = (float)(G - (double)hi);
+      if (lane < C) {
+        const float v[kVecs] = {expf((float)G), expf((float)(end - G)), be, hi, lo};
+        float* const to = A.vec + chunk_at(A, bh, c) * (kVecs * C);
+#pragma unroll
+        for (int i = 0; i < kVecs; ++i) {
+          lds_put(tv + 4 * (i * C + lane), v[i]);
+          to[i * C + lane] = v[i];
+        }
+      }
+    }
+    lk.template store<M>(tk, tid);
+    lq.template store<M>(tq, tid);
+  }
+  __syncthreads();
+  const Lane l{lane & 15, lane >> 4};
+  const int rb = M::row_base(l);
+  const auto elem = [&](int base, int r, int col) { return base + 4 * (r * S + col); };
+  // tiles on and below the diagonal; those right of it that operands of 32 inner values take in are zero
+#pragma unroll 1
+  for (int t = wave; t < NT * (NT + 1) / 2 + NT / 2; t += 4) {
+    const bool above = t >= NT * (NT + 1) / 2;
+    const int u = t - NT * (NT + 1) / 2;
+    const int qt = above ? 2 * u : t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, kt = above ? 2 * u + 1 : t - qt * (qt + 1) / 2;
+    f32x4 kk = zero4(), qk = zero4();
+    if (!above) {
+#pragma unroll
+      for (int s = 0; s < D1 / 32; ++s) {
+        const Planes<NI> b = M::row(tk, rb, kt, s);
+        kk = mma(M::row(tk, rb, qt, s), b, kk);
+        qk = mma(M::row(tq, rb, qt, s), b, qk);
+      }
+    }
+    const int i = 16 * kt + l.i;
+    const float hi = lds_get<float>(tv + 4 * (3 * C + i)), lo = lds_get<float>(tv + 4 * (4 * C + i));
+    const f32x4 be = lds_get<f32x4>(tv + 4 * (2 * C + 16 * qt + 4 * l.g)), hs = lds_get<f32x4>(tv + 4 * (3 * C + 16 * qt + 4 * l.g)),
+                ls = lds_get<f32x4>(tv + 4 * (4 * C + 16 * qt + 4 * l.g));
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const int r = 16 * qt + 4 * l.g + j;
+      const float d = expf((hs[j] - hi) + (ls[j] - lo));
+      lds_put(elem(ta, r, i), r > i ? be[j] * d * kk[j] : 0.f);
+      lds_put(elem(tp, r, i), r >= i ? (BWD ? A.scale : 1.f) * d * qk[j] : 0.f);
+      if (above) lds_put(elem(tt, r, i), 0.f);
+    }
+  }
+  __syncthreads();
+  if (wave < NT) {
+    // x: column l.i of the block's inverse, the same in every lane group
+    float x[16];
+    const int at = elem(ta, 16 * wave, 16 * wave);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      float v = r == l.i ? 1.f : 0.f;
+      f32x4 a = zero4();
+#pragma unroll
+      for (int i = 0; i < r; ++i) {
+        if (i % 4 == 0) a = lds_get<f32x4>(at + 4 * (r * S + i));
+        v -= a[i % 4] * x[i];
+      }
+      x[r] = v;
+    }
+#pragma unroll
+    for (int r = 0; r < 16; ++r)
+      if (r / 4 == l.g) lds_put(elem(tt, 16 * wave + r, 16 * wave + l.i), x[r]);
+  }
+#pragma unroll
+  for (int d = 1; d < NT; ++d) {
+    __syncthreads();
+    const int cc = wave, rr = wave + d;
+    if (rr < NT) {
+      f32x4 y = zero4();
+#pragma unroll
+      for (int m = 0; m < d; ++m) {
+        const f32x4 a = lds_get<f32x4>(elem(ta, 16 * rr + l.i, 16 * (cc + m) + 4 * l.g));
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+          y = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], lds_get<float>(elem(tt, 16 * (cc + m) + 4 * l.g + k, 16 * cc + l.i)), y, 0, 0, 0);
+      }
+      const f32x4 a = lds_get<f32x4>(elem(tt, 16 * rr + l.i, 16 * rr + 4 * l.g));
+      f32x4 z = zero4();
+#pragma unroll
+      for (int k = 0; k < 4; ++k) z = __builtin_amdgcn_mfma_f32_16x16x4f32(a[k], y[k], z, 0, 0, 0);
+#pragma unroll
+      for (int k = 0; k < 4; ++k) lds_put(elem(tt, 16 * rr + 4 * l.g + k, 16 * cc + l.i), -z[k]);
+    }
+  }
+  __syncthreads();
+  const long long own = chunk_at(A, bh, c);
+  for (int u = tid; u < NB * 64; u += NTH) {
+    const int blk = u >> 6, i = u & 15, g = u >> 4 & 3;
+    {
+      const int r = C == 32 || blk < 2 ? blk : blk < 4 ? 2 : 3, s = C == 32 || blk < 2 ? 0 : blk & 1;
+      const int at = elem(0, 16 * r + i, 32 * s + 4 * g);
+      f32x4* const T4 = reinterpret_cast<f32x4*>(A.tri + own * (NB * 512)) + 2 * u;
+      T4[0] = lds_get<f32x4>(tt + at);
+      T4[1] = lds_get<f32x4>(tt + at + 64);
+      if (!BWD) {
+        const f32x4 a = lds_get<f32x4>(tp + at), b = lds_get<f32x4>(tp + at + 64);
+        if constexpr (NI == 1) {
+          u32x4* const P4 = static_cast<u32x4*>(A.pri) + own * (NB * 128) + u;
+          const Planes<2> f = split<2>(a, b);
+          P4[0] = f.p[0];
+          P4[NB * 64] = f.p[1];
+        } else {
+          f32x4* const P4 = static_cast<f32x4*>(A.pri) + own * (NB * 128) + 2 * u;
+          P4[0] = a;
+          P4[1] = b;
+        }
+      }
+    }
+    if (BWD) {
+      const int r = C == 32 ? blk : blk < 4 ? blk >> 1 : blk - 2, s = C == 32 ? 0 : blk < 4 ? blk & 1 : 1;
+      f32x4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = elem(0, 32 * s + 4 * g + j, 16 * r + i);
+        v[0][j] = lds_get<float>(tt + at);
+        v[1][j] = lds_get<float>(tt + at + 64 * S);
+        v[2][j] = lds_get<float>(tp + at);
+        v[3][j] = lds_get<float>(tp + at + 64 * S);
+      }
+      f32x4* const T4 = reinterpret_cast<f32x4*>(A.trit + own * (NB * 512)) + 2 * u;
+      f32x4* const P4 = static_cast<f32x4*>(A.pri) + own * (NB * 128) + 2 * u;
+      T4[0] = v[0];
+      T4[1] = v[1];
+      P4[0] = v[2];
+      P4[1] = v[3];
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Chunk after chunk.  A wave owns 16 columns of the state, in the accumulators of the products that update it, and takes them through
+// all of a chunk's products by itself: its state is an operand of K S and Q S, R of T R, U of P U and of the update, all without a way
+// through LDS or another wave.
+// ---------------------------------------------------------------------------
+template <typename T, int D1, int NW, bool FWD>
+struct ScanLds {
+  static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C);
+  typedef Mat<C, D1, NI> MK;
+  typedef Mat<C, 16 * NW, NI> MV;
+  static constexpr int k = 0, v = k + MK::kAll, t = v + MV::kAll, w = t + 3 * NB * 1024, q = w + 3 * C * 4, p = q + (FWD ? MK::kAll : 0),
+                       all = p + (FWD ? Kind<T>::kOut * NB * 1024 : 0);
+};
+
+template <typename T, int D1, int NW, bool VEC, bool FWD>
+__global__ __launch_bounds__(64 * NW) void k_delta_scan(Args A) {
+  typedef ScanLds<T, D1, NW, FWD> L;
+  constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, NB = L::NB, NTH = 64 * NW, VC = 16 * NW;
+  constexpr int NO = Kind<T>::kOut;
+  typedef typename L::MK MK;
+  typedef typename L::MV MV;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int bh = blockIdx.x, col0 = blockIdx.y * VC, n = length_of(A, bh), c0 = col0 + 16 * wave;
+  const Lane l{lane & 15, lane >> 4};
+  const Rows xk = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), xq = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk),
+             xv = rows_at<T>(A.V, A, bh, A.dv, n, col0, min(A.dv - col0, VC)), xo = rows_at<T>(A.out, A, bh, A.dv, n, col0, min(A.dv - col0, VC));
+  if (FWD && n < A.L) zero_rows<T>(xo, n, A.L, tid, NTH);
+  f32x4 S[KT];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) S[kt] = zero4();
+  if (A.s_in != nullptr) load_state<KT, true>(S, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g);
+  Load<T, C, D1, NTH, VEC> lk, lq;
+  Load<T, C, VC, NTH, VEC> lv;
+  LoadTri<NB, 3, NTH> lt;
+  LoadTri<NB, NO, NTH, NI == 1> lp;
+  float lw[(3 * C + NTH - 1) / NTH];
+  const auto fetch = [&](int c) {
+    const int r0 = c * C, nr = min(C, n - r0);
+    lk.load(xk, r0, nr, tid);
+    lv.load(xv, r0, nr, tid);
+    lt.load(A.tri + chunk_at(A, bh, c) * (NB * 512), tid);
+    if (FWD) {
+      lq.load(xq, r0, nr, tid);
+      lp.load(static_cast<const float*>(A.pri) + chunk_at(A, bh, c) * (NB * 512), tid);
+    }
+#pragma unroll
+    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
+      if (tid + e * NTH < 3 * C) lw[e] = A.vec[chunk_at(A, bh, c) * (kVecs * C) + tid + e * NTH];
+  };
+  const int chunks = (n + C - 1) / C;
+  if (chunks > 0) fetch(0);
+  for (int c = 0; c < chunks; ++c) {
+    const int r0 = c * C, nr = min(C, n - r0);
+    __syncthreads();
+    lk.template store<MK>(L::k, tid);
+    lv.template store<MV>(L::v, tid);
+    lt.store(L::t, tid);
+    if (FWD) {
+      lq.template store<MK>(L::q, tid);
+      lp.store(L::p, tid);
+    }
+#pragma unroll
+    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
+      if (tid + e * NTH < 3 * C) lds_put(L::w + 4 * (tid + e * NTH), lw[e]);
+    __syncthreads();
+    if (c + 1 < chunks) fetch(c + 1);
+    if (!FWD) {
+      float* const to = A.states + chunk_at(A, bh, c) * ((long long)D1 * A.dvp) + c0 + l.i;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[(long long)(16 * kt + 4 * l.g + j) * A.dvp] = S[kt][j];
+    }
+    const int rb = MK::row_base(l), cb = MK::col_base(l), vb = MV::col_base(l);
+    f32x4 R[NT], O[NT];
+#pragma unroll
+    for (int r = 0; r < NT; ++r) R[r] = O[r] = zero4();
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const Planes<3> b = split<3>(S[2 * s], S[2 * s + 1]);
+#pragma unroll
+      for (int r = 0; r < NT; ++r) {
+        R[r] = mma(MK::row(L::k, rb, r, s), b, R[r]);
+        if (FWD) O[r] = mma_of<NO, NI>(b, MK::row(L::q, rb, r, s), O[r]);
+      }
+    }
+    f32x4 U[NT];
+#pragma unroll
+    for (int r = 0; r < NT; ++r) {
+      const f32x4 gamma = lds_get<f32x4>(L::w + 4 * (16 * r + 4 * l.g)), beta = lds_get<f32x4>(L::w + 4 * (2 * C + 16 * r + 4 * l.g));
+      R[r] = beta * (MV::quad(L::v, vb, wave, r) - gamma * R[r]);
+      U[r] = zero4();
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const Planes<3> b = split<3>(R[2 * s], R[2 * s + 1]);
+#pragma unroll
+      for (int r = 2 * s; r < NT; ++r) U[r] = mma(tri<NB, 3>(L::t, lower<C>(r, s), lane), b, U[r]);
+    }
+    if (FWD) {
+#pragma unroll
+      for (int r = 0; r < NT; ++r) O[r] *= lds_get<float>(L::w + 4 * (16 * r + l.i));
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const Planes<NO> b = split<NO>(U[2 * s], U[2 * s + 1]);
+#pragma unroll
+        for (int r = 2 * s; r < NT; ++r) O[r] = mma(b, tri<NB, NO>(L::p, lower<C>(r, s), lane), O[r]);
+      }
+      const unsigned col = (unsigned)((16 * wave + 4 * l.g) * (int)sizeof(T));
+      const Buffer ob = xo.rows(r0, nr);
+#pragma unroll
+      for (int r = 0; r < NT; ++r) {
+        const int row = 16 * r + l.i;
+        if (VEC) buffer_quad<T>(ob, col < xo.width && row < nr ? (unsigned)row * xo.row + col : kNowhere, A.scale * O[r]);
+        else if (row < nr && col < xo.width) store_quad<T>(xo.at(r0 + row) + col, (int)(xo.width - col), A.scale * O[r]);
+      }
+    } else {
+      float* const to = A.u + chunk_at(A, bh, c) * ((long long)C * A.dvp) + c0 + l.i;
+#pragma unroll
+      for (int r = 0; r < NT; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[(long long)(16 * r + 4 * l.g + j) * A.dvp] = U[r][j];
+    }
+    if (c + 1 < chunks || A.s_out != nullptr) {
+      const float Gamma = lds_get<float>(L::w + 4 * (C - 1));
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) S[kt] *= Gamma;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const f32x4 w0 = lds_get<f32x4>(L::w + 4 * (C + 32 * s + 4 * l.g)), w1 = lds_get<f32x4>(L::w + 4 * (C + 32 * s + 16 + 4 * l.g));
+        const Planes<3> b = split<3>(w0 * U[2 * s], w1 * U[2 * s + 1]);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) S[kt] = mma(MK::col(L::k, cb, kt, s), b, S[kt]);
+      }
+    }
+  }
+  if (A.s_out != nullptr) store_state<KT>(S, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g);
+}
+
+// ---------------------------------------------------------------------------
+// From the last chunk to the first: the gradient G of the state behind each chunk, and dR.
+// ---------------------------------------------------------------------------
+template <typename T, int D1, int NW>
+struct RevLds {
+  static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C);
+  typedef Mat<C, D1, NI> MK;
+  typedef Mat<C, 16 * NW, NI> MV;
+  static constexpr int k = 0, q = k + MK::kAll, v = q + MK::kAll, t = v + MV::kAll, p = t + 3 * NB * 1024, w = p + 3 * NB * 1024, all = w + 3 * C * 4;
+};
+
+template <typename T, int D1, int NW, bool VEC>
+__global__ __launch_bounds__(64 * NW) void k_delta_rev(Args A) {
+  typedef RevLds<T, D1, NW> L;
+  constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, NB = L::NB, NTH = 64 * NW, VC = 16 * NW;
+  typedef typename L::MK MK;
+  typedef typename L::MV MV;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const int bh = blockIdx.x, col0 = blockIdx.y * VC, n = length_of(A, bh), c0 = col0 + 16 * wave;
+  const Lane l{lane & 15, lane >> 4};
+  const Rows xk = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), xq = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk),
+             xo = rows_at<T>(A.dOut, A, bh, A.dv, n, col0, min(A.dv - col0, VC));
+  f32x4 G[KT];
+#pragma unroll
+  for (int kt = 0; kt < KT; ++kt) G[kt] = zero4();
+  if (A.s_in != nullptr) load_state<KT, true>(G, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g);
+  Load<T, C, D1, NTH, VEC> lk, lq;
+  Load<T, C, VC, NTH, VEC> lo;
+  LoadTri<NB, 3, NTH> lt, lp;
+  float lw[(3 * C + NTH - 1) / NTH];
+  const auto fetch = [&](int c) {
+    const int r0 = c * C, nr = min(C, n - r0);
+    lk.load(xk, r0, nr, tid);
+    lq.load(xq, r0, nr, tid);
+    lo.load(xo, r0, nr, tid);
+    lt.load(A.trit + chunk_at(A, bh, c) * (NB * 512), tid);
+    lp.load(static_cast<const float*>(A.pri) + chunk_at(A, bh, c) * (NB * 512), tid);
+#pragma unroll
+    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
+      if (tid + e * NTH < 3 * C) lw[e] = A.vec[chunk_at(A, bh, c) * (kVecs * C) + tid + e * NTH];
+  };
+  const int chunks = (n + C - 1) / C;
+  if (chunks > 0) fetch(chunks - 1);
+  for (int c = chunks - 1; c >= 0; --c) {
+    __syncthreads();
+    lk.template store<MK>(L::k, tid);
+    lq.template store<MK>(L::q, tid);
+    lo.template store<MV>(L::v, tid);
+    lt.store(L::t, tid);
+    lp.store(L::p, tid);
+#pragma unroll
+    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
+      if (tid + e * NTH < 3 * C) lds_put(L::w + 4 * (tid + e * NTH), lw[e]);
+    __syncthreads();
+    if (c > 0) fetch(c - 1);
+    {
+      float* const to = A.dstates + chunk_at(A, bh, c) * ((long long)D1 * A.dvp) + c0 + l.i;
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[(long long)(16 * kt + 4 * l.g + j) * A.dvp] = G[kt][j];
+    }
+    const int rb = MK::row_base(l), cb = MK::col_base(l), vb = MV::col_base(l);
+    f32x4 U[NT], R[NT];
+#pragma unroll
+    for (int r = 0; r < NT; ++r) U[r] = R[r] = zero4();
+#pragma unroll
+    for (int s = 0; s < KS; ++s) {
+      const Planes<3> b = split<3>(G[2 * s], G[2 * s + 1]);
+#pragma unroll
+      for (int r = 0; r < NT; ++r) U[r] = mma(MK::row(L::k, rb, r, s), b, U[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < NT; ++r) U[r] *= lds_get<f32x4>(L::w + 4 * (C + 16 * r + 4 * l.g));
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const Planes<NI> b = MV::col(L::v, vb, wave, s);
+#pragma unroll
+      for (int r = 0; r < (NS == 1 ? NT : 2 * s + 2); ++r) U[r] = mma(tri<NB, 3>(L::p, upper<C>(r, s), lane), b, U[r]);
+    }
+#pragma unroll
+    for (int s = 0; s < NS; ++s) {
+      const Planes<3> b = split<3>(U[2 * s], U[2 * s + 1]);
+#pragma unroll
+      for (int r = 0; r < (NS == 1 ? NT : 2 * s + 2); ++r) R[r] = mma(tri<NB, 3>(L::t, upper<C>(r, s), lane), b, R[r]);
+    }
+    {
+      float* const to = A.dr + chunk_at(A, bh, c) * ((long long)C * A.dvp) + c0 + l.i;
+#pragma unroll
+      for (int r = 0; r < NT; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) to[(long long)(16 * r + 4 * l.g + j) * A.dvp] = R[r][j];
+    }
+    if (c > 0 || A.s_out != nullptr) {
+      const float Gamma = lds_get<float>(L::w + 4 * (C - 1));
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) G[kt] *= Gamma;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const f32x4 w0 = lds_get<f32x4>(L::w + 4 * (32 * s + 4 * l.g)), w1 = lds_get<f32x4>(L::w + 4 * (32 * s + 16 + 4 * l.g));
+        const f32x4 b0 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 4 * l.g)), b1 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 16 + 4 * l.g));
+        const Planes<3> o = split<3>(A.scale * w0 * MV::quad(L::v, vb, wave, 2 * s), A.scale * w1 * MV::quad(L::v, vb, wave, 2 * s + 1));
+        const Planes<3> b = split<3>(-(w0 * b0) * R[2 * s], -(w1 * b1) * R[2 * s + 1]);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) {
+          G[kt] = mma(MK::col(L::q, cb, kt, s), o, G[kt]);
+          G[kt] = mma(MK::col(L::k, cb, kt, s), b, G[kt]);
+        }
+      }
+    }
+  }
+  if (A.s_out != nullptr) store_state<KT>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g);
+}
+
+// ---------------------------------------------------------------------------
+// Launches: the instance that holds dk inner values.
+// ---------------------------------------------------------------------------
+template <typename T>
+static bool vec_of(const Args& a) { return a.dk * sizeof(T) % 16 == 0 && a.dv * sizeof(T) % 16 == 0; }
+
+template <typename T, int D1, bool VEC, bool BWD>
+static dark_status go_prep(const Args& a, hipStream_t st) {
+  constexpr int lds = prep_lds<T, D1>();
+  DARK_TRY(allow_lds(k_delta_prep<T, D1, VEC, BWD>, lds));
+  DARK_LAUNCH(KID_DELTA_PREP, st, (k_delta_prep<T, D1, VEC, BWD>), dim3((unsigned)(a.B * a.H * a.chunks)), dim3(256), lds, a);
+  return DARK_OK;
+}
+template <typename T, int D1>
+static dark_status go_prep(const Args& a, bool backward, hipStream_t st) {
+  if (vec_of<T>(a)) return backward ? go_prep<T, D1, true, true>(a, st) : go_prep<T, D1, true, false>(a, st);
+  return backward ? go_prep<T, D1, false, true>(a, st) : go_prep<T, D1, false, false>(a, st);
+}
+template <typename T>
+static dark_status launch_prep(const Args& a, bool backward, hipStream_t st) {
+  switch (inner_of(a.dk)) {
+    case 64: return go_prep<T, 64>(a, backward, st);
+    case 128: return go_prep<T, 128>(a, backward, st);
+    default: return go_prep<T, 256>(a, backward, st);
+  }
+}
+
+template <typename T, int D1, int NW, bool VEC, bool FWD>
+static dark_status go_scan(const Args& a, hipStream_t st) {
+  constexpr int lds = ScanLds<T, D1, NW, FWD>::all;
+  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD>, lds));
+  const int cols = FWD ? a.dv : a.dvp;
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(64 * NW), lds, a);
+  return DARK_OK;
+}
+template <typename T, int D1>
+static dark_status go_scan(const Args& a, Pass pass, hipStream_t st) {
+  if (vec_of<T>(a)) return pass == kForward ? go_scan<T, D1, 4, true, true>(a, st) : go_scan<T, D1, 4, true, false>(a, st);
+  return pass == kForward ? go_scan<T, D1, 4, false, true>(a, st) : go_scan<T, D1, 4, false, false>(a, st);
+}
+template <typename T>
+static dark_status launch_scan(const Args& a, Pass pass, hipStream_t st) {
+  switch (inner_of(a.dk)) {
+    case 64: return go_scan<T, 64>(a, pass, st);
+    case 128: return go_scan<T, 128>(a, pass, st);
+    default: return go_scan<T, 256>(a, pass, st);
+  }
+}
+
+template <typename T, int D1, int NW, bool VEC>
+static dark_status go_rev(const Args& a, hipStream_t st) {
+  constexpr int lds = RevLds<T, D1, NW>::all;
+  DARK_TRY(allow_lds(k_delta_rev<T, D1, NW, VEC>, lds));
+  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_rev<T, D1, NW, VEC>), dim3(a.B * a.H, a.dvp / (16 * NW)), dim3(64 * NW), lds, a);
+  return DARK_OK;
+}
+template <typename T>
+static dark_status launch_rev(const Args& a, hipStream_t st) {
+  const bool vec = vec_of<T>(a);
+  switch (inner_of(a.dk)) {
+    case 64: return vec ? go_rev<T, 64, 4, true>(a, st) : go_rev<T, 64, 4, false>(a, st);
+    case 128: return vec ? go_rev<T, 128, 4, true>(a, st) : go_rev<T, 128, 4, false>(a, st);
+    default: return vec ? go_rev<T, 256, 4, true>(a, st) : go_rev<T, 256, 4, false>(a, st);
+  }
+}
+
+}  // namespace delta
+}  // namespace dark
