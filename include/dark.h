@@ -451,6 +451,33 @@ dark_status dark_beam_select(const dark_beam_params* p, const void* logits, cons
                              void* ws, size_t ws_bytes, void* hip_stream);
 
 /*
+ * The next token of each row, drawn from its logits by a given random number.  With w_t = exp((logits[t] - max logits) / temperature) and the
+ * tokens in order of their logits, the largest first, equal ones by their number, a row keeps
+ *   the first top_k of them (top_k <= 0: all),
+ *   of those the shortest beginning of the order that holds top_p of their sum of w, the first one at least (top_p >= 1: all),
+ *   of those the ones with w_t >= min_p (min_p <= 0: all; above 1 it counts as 1).
+ * out_token is the first token, in the order of the tokens' numbers, behind which the kept w add up to more than u times their sum, for
+ * the row's u in 0 ... 1 (outside: the nearer of the two; 1: the last that is kept), so that equal numbers draw equal tokens.  out_logprob is
+ * the logarithm of the probability with which it was drawn, w / sum of the kept w.
+ * temperature 0 (in an array, whatever is not above 0): the largest logit, the lowest token of equal ones; out_logprob 0.
+ *   logits [B, V] in io_dtype; uniform [B] float32, NULL only if p->temperature is 0 and no array says otherwise.
+ *   temperature, top_p, min_p [B] float32, top_k [B] int32: settings of every row, each NULL: the call's own in p.  NaN in an array: top_p, min_p: no limit.
+ *   out_token [B] int32, out_logprob [B] float32 or NULL.
+ *   Logits that are -infinity or NaN are never drawn, nor counted; if a row has no others, its token is -1, its logarithm -infinity.  Where
+ *   logits are +infinity, those share everything.
+ * w is in fp32, to a few units of its last place, sums in 64 bits.  No workspace.  V <= 2^27, B <= 2^22 (else DARK_EUNSUPPORTED).
+ */
+typedef struct {
+  int32_t B, V;        /* rows, vocabulary */
+  int32_t io_dtype;    /* dark_dtype of logits */
+  int32_t top_k;
+  float temperature, top_p, min_p;
+} dark_sample_params;
+dark_status dark_sample(const dark_sample_params* p, const void* logits, const float* uniform, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p, int32_t* out_token, float* out_logprob,
+                        void* hip_stream);
+
+/*
  * The states of the beams follow their parents, in place: of each of the `count` tensors [B, n, ...] of row_bytes[i] bytes for one beam
  * (the recurrent states of dark_decode_step and dark_decay_step, or anything else kept for a beam) row (b, j) becomes what row
  * (b, parent[b][j]) was before the call.  A parent outside 0 ... n - 1 leaves its row as it is.

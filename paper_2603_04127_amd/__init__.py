@@ -55,6 +55,13 @@ class BeamParams(ctypes.Structure):
     ]
 
 
+class SampleParams(ctypes.Structure):
+    _fields_ = [
+        ("B", ctypes.c_int32), ("V", ctypes.c_int32), ("io_dtype", ctypes.c_int32), ("top_k", ctypes.c_int32), ("temperature", ctypes.c_float),
+        ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+    ]
+
+
 class DarkError(RuntimeError):
     def __init__(self, status: int, where: str):
         self.status = status
@@ -124,6 +131,8 @@ def lib() -> ctypes.CDLL:
     L.dark_beam_workspace_bytes.argtypes = [bp]
     L.dark_beam_select.restype = i32
     L.dark_beam_select.argtypes = [bp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    L.dark_sample.restype = i32
+    L.dark_sample.argtypes = [ctypes.POINTER(SampleParams), vp, vp, vp, vp, vp, vp, vp, vp, vp]
     L.dark_state_reorder.restype = i32
     L.dark_state_reorder.argtypes = [i32, i32, vp, i32, ctypes.POINTER(vp), ctypes.POINTER(sz), vp]
     L.dark_timing_enable.argtypes = [i32]
@@ -737,7 +746,7 @@ def dark_delta_step(q, k, v, log_gate, beta, state, *, parent=None, state_out=No
 
 
 # ----------------------------------------------------------------------------
-# beam search over recurrent states
+# beam search over recurrent states, tokens drawn from logits
 # ----------------------------------------------------------------------------
 def dark_beam_select(logits, scores, *, finished=None, eos=0, keep_slots=False, out=None):
     """The next n beams of each batch entry from logits [B,n,V] and scores [B,n] (float32): (scores, parent, token), [B,n] each,
@@ -771,6 +780,41 @@ def dark_beam_select(logits, scores, *, finished=None, eos=0, keep_slots=False, 
     ws, stream = _workspace(nb, logits.device)
     _check(lib().dark_beam_select(ctypes.byref(p), x, c, f, ps, pp, pt, ws.data_ptr(), ws.numel(), stream), "dark_beam_select")
     return s, parent, token
+
+
+def dark_sample(logits, uniform=None, *, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, want_logprob=False, out=None):
+    """The next token of each row of logits [B,V], drawn by uniform [B] (float32, 0 ... 1): int32 [B]; with want_logprob also the logarithm of the
+    probability with which it was drawn.  Of softmax(logits / temperature) are kept the top_k likeliest (0: all), of those the likeliest that
+    hold top_p of their sum (1: all), of those the ones of min_p times the largest (0: all); the token is where the sum of the kept, in the order
+    of their numbers, exceeds the share `uniform` of it.  temperature 0: the largest logit (`uniform` may then be None).  -1: a row without a token.
+    The settings are numbers, or tensors [B] with one for each row (float32; top_k int32).  `out`: the token tensor to write into."""
+    torch = _torch()
+    f32, i32 = torch.float32, torch.int32
+    settings = (temperature, top_k, top_p, min_p)
+    tensor = [x if isinstance(x, torch.Tensor) and x.dim() > 0 else None for x in settings]
+    t, k, p, q = (0 if y is not None else x for x, y in zip(settings, tensor))
+    key = ("sample", logits.shape, logits.dtype, float(t), int(k), float(p), float(q))
+    plan = _plans.get(key)
+    if plan is None:
+        B, V = logits.shape
+        plan = (SampleParams(B, V, _dtype_code(logits), int(k), float(t), float(p), float(q)), 0)
+        _keep_plan(key, plan)
+    params, shape = plan[0], logits.shape[:1]
+    _require(uniform, f32, shape, "uniform")
+    for x, dtype, name in zip(tensor, (f32, i32, f32, f32), ("temperature", "top_k", "top_p", "min_p")):
+        _require(x, dtype, shape, name)
+    _require(out, i32, shape, "out")
+    index, (x, u, *ptrs, o) = _pointers(logits, uniform, *tensor, out)
+    if index != torch._C._cuda_getDevice():
+        with torch.cuda.device(index):
+            return dark_sample(logits, uniform, temperature=temperature, top_k=top_k, top_p=top_p, min_p=min_p, want_logprob=want_logprob, out=out)
+    if out is None:
+        out = torch.empty(shape, dtype=i32, device=logits.device)
+        o = out.data_ptr()
+    log = torch.empty(shape, dtype=f32, device=logits.device) if want_logprob else None
+    _check(lib().dark_sample(ctypes.byref(params), x, u, *ptrs, o, None if log is None else log.data_ptr(),
+                             torch._C._cuda_getCurrentRawStream(index)), "dark_sample")
+    return (out, log) if want_logprob else out
 
 
 def dark_state_reorder(states, parent):

@@ -53,6 +53,7 @@ enum KernelId : int {
   KID_DELTA_STEP,      // gated delta rule: one token
   KID_BEAM_ROWS,       // beam search: sums and largest logits of every slice of a row
   KID_BEAM_PICK,       // beam search: the next beams of a batch entry
+  KID_SAMPLE,          // tokens drawn from logits
   KID_STATE_REORDER,   // recurrent states follow their beams
   KID_COUNT
 };
