@@ -34,8 +34,9 @@ struct Problem {
 // Rows of a chunk, blocks of 16 rows and 32 inner values that a lower triangle of C x C consists of as an operand.
 constexpr int chunk_of(int io_dtype) { return io_dtype == DARK_BF16 ? 64 : 32; }
 constexpr int blocks_of(int C) { return C == 64 ? 6 : 2; }
-// Floats that k_delta_prep leaves for a chunk beside its operands: gamma, left, beta, and G as the sum of two floats.
-constexpr int kVecs = 5;
+// Rows of C floats that k_delta_prep leaves for a chunk beside its operands: gamma, left, beta, Gamma (throughout), which the scans take, and G as
+// the sum of two floats.
+constexpr int kVecs = 6, kScanVecs = 4;
 
 struct Args {
   const void *Q, *K, *V, *dOut;
@@ -49,10 +50,10 @@ struct Args {
   int dvp;                // columns of scratch states and rows: dv, rounded up to 64
   float scale;
   // scratch, for every (b,h) and chunk
-  float* tri;             // T in operand order, blocks_of(C) x 64 lanes x 8
-  float* trit;            // T^T (backward)
-  void* pri;              // P in operand order (bf16: as two planes); backward: P^T scale
-  float* vec;             // kVecs x C
+  fz::u32x4* tri;         // T in operand order: 3 planes of blocks_of(C) x 64 lanes x 8 values
+  fz::u32x4* trit;        // T^T (backward)
+  fz::u32x4* pri;         // P, as many planes as an output takes; backward: P^T scale, 3 planes
+  float* vec;             // kVecs x C floats
   float* states;          // [D1, dvp], before the chunk
   float* dstates;         // [D1, dvp], gradient of the state behind the chunk
   float *u, *dr;          // [C, dvp]

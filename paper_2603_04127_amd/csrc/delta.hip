@@ -142,11 +142,11 @@ static Args args_of(const Problem& pb) {
 static void plan(const Problem& pb, Arena& ar, bool backward, Args* a) {
   const int C = chunk_of(pb.p.io_dtype), NB = blocks_of(C);
   const size_t chunks = (size_t)pb.BH() * a->chunks, inner = inner_of(pb.p.dk);
-  a->tri = ar.take<float>(chunks * NB * 512);
-  a->pri = ar.take<float>(chunks * NB * 512);
+  a->tri = ar.take<fz::u32x4>(chunks * NB * 192);
+  a->pri = ar.take<fz::u32x4>(chunks * NB * (pb.p.io_dtype == DARK_BF16 && !backward ? 128 : 192));
   a->vec = ar.take<float>(chunks * kVecs * C);
   if (!backward) return;
-  a->trit = ar.take<float>(chunks * NB * 512);
+  a->trit = ar.take<fz::u32x4>(chunks * NB * 192);
   a->states = ar.take<float>(chunks * inner * a->dvp);
   a->dstates = ar.take<float>(chunks * inner * a->dvp);
   a->u = ar.take<float>(chunks * C * a->dvp);

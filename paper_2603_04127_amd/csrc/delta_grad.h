@@ -189,8 +189,8 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
 
   const int rb = MK::row_base(l), cb = MK::col_base(l), xb = MX::row_base(l), xc = MX::col_base(l);
   if (wave < NT) {
-    const f32x4 be = lds_get<f32x4>(L::w + 4 * (2 * C + 16 * wave + 4 * l.g)), hs = lds_get<f32x4>(L::w + 4 * (3 * C + 16 * wave + 4 * l.g)),
-                ls = lds_get<f32x4>(L::w + 4 * (4 * C + 16 * wave + 4 * l.g));
+    const f32x4 be = lds_get<f32x4>(L::w + 4 * (2 * C + 16 * wave + 4 * l.g)), hs = lds_get<f32x4>(L::w + 4 * (4 * C + 16 * wave + 4 * l.g)),
+                ls = lds_get<f32x4>(L::w + 4 * (5 * C + 16 * wave + 4 * l.g));
     f32x4 before = zero4(), third = zero4();   // before: Z over the key tiles that are done
     // Z_ri: the weight exp(G_r - G_i) times its gradient.  The gate of row t has those with i < t <= r: sums over the keys up to each, and over
     // the rows behind it (never differences of longer sums, whose rounding a small gradient would not survive).
@@ -212,7 +212,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
         qk = mma(MK::row(L::q, rb, wave, s), b, qk);
       }
       const int i = 16 * r + l.i;
-      const float hi = lds_get<float>(L::w + 4 * (3 * C + i)), lo = lds_get<float>(L::w + 4 * (4 * C + i));
+      const float hi = lds_get<float>(L::w + 4 * (4 * C + i)), lo = lds_get<float>(L::w + 4 * (5 * C + i));
       f32x4 nn, mm;
       float cz = 0.f;
 #pragma unroll
@@ -330,7 +330,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
     if (lane == 0) left = 0.0;
     double total = 0.0;
     for (int w = 0; w < 4; ++w) total += lds_get<float>(L::total + 4 * w);
-    const double gate = reads + left + cross + total * (double)lds_get<float>(L::w + 4 * (C - 1));
+    const double gate = reads + left + cross + total * (double)lds_get<float>(L::w + 4 * (3 * C));
     if (lane < nr) {
       if (A.dgate != nullptr) A.dgate[gate_at(A, bh, r0 + lane)] = (float)gate;
       if (A.dbeta != nullptr) A.dbeta[gate_at(A, bh, r0 + lane)] = lds_get<float>(L::vdot + 4 * t) - (float)d1 - lds_get<float>(L::third + 4 * t);

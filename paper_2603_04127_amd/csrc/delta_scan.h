@@ -48,7 +48,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
       const double end = __shfl(G, C - 1, 64);
       const float hi = (float)G, lo = (float)(G - (double)hi);
       if (lane < C) {
-        const float v[kVecs] = {expf((float)G), expf((float)(end - G)), be, hi, lo};
+        const bool there = lane < nr;   // rows behind the last weigh nothing, whatever stands there
+        const float v[kVecs] = {there ? expf((float)G) : 0.f, there ? expf((float)(end - G)) : 0.f, be, expf((float)end), hi, lo};
         float* const to = A.vec + chunk_at(A, bh, c) * (kVecs * C);
 #pragma unroll
         for (int i = 0; i < kVecs; ++i) {
@@ -80,9 +81,9 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
       }
     }
     const int i = 16 * kt + l.i;
-    const float hi = lds_get<float>(tv + 4 * (3 * C + i)), lo = lds_get<float>(tv + 4 * (4 * C + i));
-    const f32x4 be = lds_get<f32x4>(tv + 4 * (2 * C + 16 * qt + 4 * l.g)), hs = lds_get<f32x4>(tv + 4 * (3 * C + 16 * qt + 4 * l.g)),
-                ls = lds_get<f32x4>(tv + 4 * (4 * C + 16 * qt + 4 * l.g));
+    const float hi = lds_get<float>(tv + 4 * (4 * C + i)), lo = lds_get<float>(tv + 4 * (5 * C + i));
+    const f32x4 be = lds_get<f32x4>(tv + 4 * (2 * C + 16 * qt + 4 * l.g)), hs = lds_get<f32x4>(tv + 4 * (4 * C + 16 * qt + 4 * l.g)),
+                ls = lds_get<f32x4>(tv + 4 * (5 * C + 16 * qt + 4 * l.g));
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const int r = 16 * qt + 4 * l.g + j;
@@ -135,26 +136,19 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
   }
   __syncthreads();
   const long long own = chunk_at(A, bh, c);
+  constexpr int NP = BWD ? 3 : Kind<T>::kOut;
   for (int u = tid; u < NB * 64; u += NTH) {
     const int blk = u >> 6, i = u & 15, g = u >> 4 & 3;
     {
       const int r = C == 32 || blk < 2 ? blk : blk < 4 ? 2 : 3, s = C == 32 || blk < 2 ? 0 : blk & 1;
       const int at = elem(0, 16 * r + i, 32 * s + 4 * g);
-      f32x4* const T4 = reinterpret_cast<f32x4*>(A.tri + own * (NB * 512)) + 2 * u;
-      T4[0] = lds_get<f32x4>(tt + at);
-      T4[1] = lds_get<f32x4>(tt + at + 64);
+      const Planes<3> t = split<3>(lds_get<f32x4>(tt + at), lds_get<f32x4>(tt + at + 64));
+#pragma unroll
+      for (int k = 0; k < 3; ++k) A.tri[(own * 3 + k) * (NB * 64) + u] = t.p[k];
       if (!BWD) {
-        const f32x4 a = lds_get<f32x4>(tp + at), b = lds_get<f32x4>(tp + at + 64);
-        if constexpr (NI == 1) {
-          u32x4* const P4 = static_cast<u32x4*>(A.pri) + own * (NB * 128) + u;
-          const Planes<2> f = split<2>(a, b);
-          P4[0] = f.p[0];
-          P4[NB * 64] = f.p[1];
-        } else {
-          f32x4* const P4 = static_cast<f32x4*>(A.pri) + own * (NB * 128) + 2 * u;
-          P4[0] = a;
-          P4[1] = b;
-        }
+        const Planes<NP> f = split<NP>(lds_get<f32x4>(tp + at), lds_get<f32x4>(tp + at + 64));
+#pragma unroll
+        for (int k = 0; k < NP; ++k) A.pri[(own * NP + k) * (NB * 64) + u] = f.p[k];
       }
     }
     if (BWD) {
@@ -168,12 +162,12 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
         v[2][j] = lds_get<float>(tp + at);
         v[3][j] = lds_get<float>(tp + at + 64 * S);
       }
-      f32x4* const T4 = reinterpret_cast<f32x4*>(A.trit + own * (NB * 512)) + 2 * u;
-      f32x4* const P4 = static_cast<f32x4*>(A.pri) + own * (NB * 128) + 2 * u;
-      T4[0] = v[0];
-      T4[1] = v[1];
-      P4[0] = v[2];
-      P4[1] = v[3];
+      const Planes<3> t = split<3>(v[0], v[1]), f = split<3>(v[2], v[3]);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) {
+        A.trit[(own * 3 + k) * (NB * 64) + u] = t.p[k];
+        A.pri[(own * 3 + k) * (NB * 64) + u] = f.p[k];
+      }
     }
   }
 }
@@ -183,18 +177,22 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
 // all of a chunk's products by itself: its state is an operand of K S and Q S, R of T R, U of P U and of the update, all without a way
 // through LDS or another wave.
 // ---------------------------------------------------------------------------
-template <typename T, int D1, int NW, bool FWD>
+// Where a chunk's operands lie in LDS; DIRECT: two chunks', one being read and one on its way there.
+template <typename T, int D1, int NW, bool FWD, bool DIRECT>
 struct ScanLds {
   static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C);
   typedef Mat<C, D1, NI> MK;
   typedef Mat<C, 16 * NW, NI> MV;
-  static constexpr int k = 0, v = k + MK::kAll, t = v + MV::kAll, w = t + 3 * NB * 1024, q = w + 3 * C * 4, p = q + (FWD ? MK::kAll : 0),
-                       all = p + (FWD ? Kind<T>::kOut * NB * 1024 : 0);
+  static constexpr int k = 0, v = k + MK::kAll, t = v + MV::kAll, w = t + 3 * NB * 1024, q = w + kScanVecs * C * 4, p = q + (FWD ? MK::kAll : 0),
+                       one = p + (FWD ? Kind<T>::kOut * NB * 1024 : 0), all = DIRECT ? 2 * one : one;
 };
+// Instances that take their operands straight to LDS: bf16 whose rows fill the tiles.
+template <typename T>
+constexpr bool direct_of(int D1) { return sizeof(T) == 2 && D1 <= 128; }
 
-template <typename T, int D1, int NW, bool VEC, bool FWD>
-__global__ __launch_bounds__(64 * NW) void k_delta_scan(Args A) {
-  typedef ScanLds<T, D1, NW, FWD> L;
+template <typename T, int D1, int NW, bool VEC, bool FWD, bool DIRECT>
+__global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args A) {
+  typedef ScanLds<T, D1, NW, FWD, DIRECT> L;
   constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, NB = L::NB, NTH = 64 * NW, VC = 16 * NW;
   constexpr int NO = Kind<T>::kOut;
   typedef typename L::MK MK;
@@ -212,80 +210,172 @@ __global__ __launch_bounds__(64 * NW) void k_delta_scan(Args A) {
   Load<T, C, D1, NTH, VEC> lk, lq;
   Load<T, C, VC, NTH, VEC> lv;
   LoadTri<NB, 3, NTH> lt;
-  LoadTri<NB, NO, NTH, NI == 1> lp;
-  float lw[(3 * C + NTH - 1) / NTH];
-  const auto fetch = [&](int c) {
+  LoadTri<NB, NO, NTH> lp;
+  f32x4 lw;
+  // A chunk's operands are asked for piece by piece between the products of the one before it: all at once they would stop the wave until
+  // the memory pipe has taken them (1200 of a chunk's 13,000 cycles).
+  const auto fetch_rows = [&](int c, int to) {
     const int r0 = c * C, nr = min(C, n - r0);
-    lk.load(xk, r0, nr, tid);
-    lv.load(xv, r0, nr, tid);
-    lt.load(A.tri + chunk_at(A, bh, c) * (NB * 512), tid);
-    if (FWD) {
-      lq.load(xq, r0, nr, tid);
-      lp.load(static_cast<const float*>(A.pri) + chunk_at(A, bh, c) * (NB * 512), tid);
+    if constexpr (DIRECT) {
+      Direct<C, D1, NTH>::load(to + L::k, xk, r0, nr, wave, lane);
+      if (FWD) Direct<C, D1, NTH>::load(to + L::q, xq, r0, nr, wave, lane);
+    } else {
+      lk.load(xk, r0, nr, tid);
+      if (FWD) lq.load(xq, r0, nr, tid);
     }
-#pragma unroll
-    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
-      if (tid + e * NTH < 3 * C) lw[e] = A.vec[chunk_at(A, bh, c) * (kVecs * C) + tid + e * NTH];
+  };
+  const auto fetch_rest = [&](int c, int to) {
+    const long long own = chunk_at(A, bh, c);
+    const int r0 = c * C, nr = min(C, n - r0);
+    const u32x4 *const tri = A.tri + own * (3 * NB * 64), *const pri = A.pri + own * (NO * NB * 64);
+    const float* const vec = A.vec + own * (kVecs * C);
+    if constexpr (DIRECT) {
+      Direct<C, VC, NTH>::load(to + L::v, xv, r0, nr, wave, lane);
+      direct_copy<3 * NB, NTH>(to + L::t, tri, wave, lane);
+      if (FWD) direct_copy<NO * NB, NTH>(to + L::p, pri, wave, lane);
+      direct_copy<kScanVecs * C / 256, NTH>(to + L::w, vec, wave, lane);
+    } else {
+      lv.load(xv, r0, nr, tid);
+      lt.load(tri, tid);
+      if (FWD) lp.load(pri, tid);
+      if (tid < C) lw = reinterpret_cast<const f32x4*>(vec)[tid];
+    }
   };
   const int chunks = (n + C - 1) / C;
-  if (chunks > 0) fetch(0);
+  if (chunks > 0) {
+    fetch_rows(0, 0);
+    fetch_rest(0, 0);
+  }
+  if (DIRECT) wait_loads<0>();
   for (int c = 0; c < chunks; ++c) {
     const int r0 = c * C, nr = min(C, n - r0);
-    __syncthreads();
-    lk.template store<MK>(L::k, tid);
-    lv.template store<MV>(L::v, tid);
-    lt.store(L::t, tid);
-    if (FWD) {
-      lq.template store<MK>(L::q, tid);
-      lp.store(L::p, tid);
+    const int next = min(c + 1, chunks - 1);   // behind the last: it again, without a branch that would part the products
+    const int here = DIRECT ? (c & 1) * L::one : 0, there = DIRECT ? L::one - here : 0;
+    if (DIRECT) {
+      if (c > 0) wait_loads<FWD ? NT : 4 * NT>();   // behind the loads came the last chunk's results, that many stores
+      lds_barrier();
+    } else {
+      lds_barrier();
+      lk.template store<MK>(L::k, tid);
+      lv.template store<MV>(L::v, tid);
+      lt.store(L::t, tid);
+      if (FWD) {
+        lq.template store<MK>(L::q, tid);
+        lp.store(L::p, tid);
+      }
+      if (tid < C) lds_put(L::w + 16 * tid, lw);
+      lds_barrier();
     }
-#pragma unroll
-    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
-      if (tid + e * NTH < 3 * C) lds_put(L::w + 4 * (tid + e * NTH), lw[e]);
-    __syncthreads();
-    if (c + 1 < chunks) fetch(c + 1);
     if (!FWD) {
-      float* const to = A.states + chunk_at(A, bh, c) * ((long long)D1 * A.dvp) + c0 + l.i;
+      const Buffer to = buffer(A.states + chunk_at(A, bh, c) * ((long long)D1 * A.dvp), (unsigned)(D1 * A.dvp) * 4u);
+      const unsigned at = (unsigned)(4 * l.g * A.dvp + c0 + l.i) * 4u;
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) to[(long long)(16 * kt + 4 * l.g + j) * A.dvp] = S[kt][j];
+        for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][j]), to, at, (unsigned)(16 * kt + j) * A.dvp * 4u, 0);
     }
     const int rb = MK::row_base(l), cb = MK::col_base(l), vb = MV::col_base(l);
-    f32x4 R[NT], O[NT];
+    // Steps: the products of one run while the next one's operands are read and split.
+    f32x4 R[NT], O[NT], U[NT], V[NT], gamma[NT], beta[NT];
 #pragma unroll
-    for (int r = 0; r < NT; ++r) R[r] = O[r] = zero4();
+    for (int r = 0; r < NT; ++r) R[r] = O[r] = U[r] = zero4();
+    u32x4 t0[3][NT];
+    {
+      Planes<NI> k[2][NT], q[2][NT];
+      Planes<3> b[2];
+      const auto ask = [&](int s) {
 #pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const Planes<3> b = split<3>(S[2 * s], S[2 * s + 1]);
+        for (int r = 0; r < NT; ++r) {
+          k[s & 1][r] = MK::row(here + L::k, rb, r, s);
+          if (FWD) q[s & 1][r] = MK::row(here + L::q, rb, r, s);
+        }
+      };
+      ask(0);
+      b[0] = split<3>(S[0], S[1]);
+      step_end();
 #pragma unroll
-      for (int r = 0; r < NT; ++r) {
-        R[r] = mma(MK::row(L::k, rb, r, s), b, R[r]);
-        if (FWD) O[r] = mma_of<NO, NI>(b, MK::row(L::q, rb, r, s), O[r]);
+      for (int s = 0; s < KS; ++s) {
+        if (s + 1 < KS) {
+          ask(s + 1);
+          b[(s + 1) & 1] = split<3>(S[2 * s + 2], S[2 * s + 3]);
+        } else {
+#pragma unroll
+          for (int r = 0; r < NT; ++r) {
+            V[r] = MV::quad(here + L::v, vb, wave, r);
+            gamma[r] = lds_get<f32x4>(here + L::w + 4 * (16 * r + 4 * l.g));
+            beta[r] = lds_get<f32x4>(here + L::w + 4 * (2 * C + 16 * r + 4 * l.g));
+          }
+#pragma unroll
+          for (int i = 0; i < 3; ++i) tri_plane<C, true>(here + L::t, lane, 0, i, t0[i]);
+        }
+        mma_rows<NI, 3>(k[s & 1], b[s & 1], R);
+        if (FWD) mma_cols<NO, NI>(b[s & 1], q[s & 1], O);
+        interleave<NI == 1 ? NT * (3 + (FWD ? NO : 0)) : 0, 3, NI == 1 ? (FWD ? 2 : 1) * NT : 0>();
       }
     }
-    f32x4 U[NT];
+    fetch_rows(next, there);
+    step_end();
+    const auto correct = [&](int r) { R[r] = beta[r] * (V[r] - gamma[r] * R[r]); };
+    const float Gamma = lds_get<float>(here + L::w + 4 * (3 * C));
+    Planes<NI> k0[KT];
+    Planes<3> bu[NS];
+    f32x4 left[NT];
+    {
+      Planes<3> b[NS];
+      correct(0);
+      correct(1);
+      b[0] = split<3>(R[0], R[1]);
+      step_end();
+      u32x4 t1[3][NT];
+      if constexpr (NS == 2) {
 #pragma unroll
-    for (int r = 0; r < NT; ++r) {
-      const f32x4 gamma = lds_get<f32x4>(L::w + 4 * (16 * r + 4 * l.g)), beta = lds_get<f32x4>(L::w + 4 * (2 * C + 16 * r + 4 * l.g));
-      R[r] = beta * (MV::quad(L::v, vb, wave, r) - gamma * R[r]);
-      U[r] = zero4();
+        for (int i = 0; i < 3; ++i) tri_plane<C, true>(here + L::t, lane, 1, i, t1[i]);
+        correct(2);
+        correct(3);
+        b[1] = split<3>(R[2], R[3]);
+      }
+      mma_step<C, true, false, 3, 3>(t0, 0, b[0], U);
+      interleave<NI == 1 ? 24 : 0, 4, NI == 1 ? 6 : 0>();
+#pragma unroll
+      for (int r = 0; r < NT; ++r) left[r] = lds_get<f32x4>(here + L::w + 4 * (C + 16 * r + 4 * l.g));
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) k0[kt] = MK::col(here + L::k, cb, kt, 0);
+      bu[0] = split<3>(left[0] * U[0], left[1] * U[1]);
+      if constexpr (NS == 2) {
+        mma_step<C, true, false, 3, 3>(t1, 1, b[1], U);
+        interleave<NI == 1 ? 12 : 0, 5, NI == 1 ? 2 * KT : 0>();
+      } else {
+        step_end();
+      }
     }
+    fetch_rest(next, there);
+    step_end();
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const Planes<3> b = split<3>(R[2 * s], R[2 * s + 1]);
+    for (int kt = 0; kt < KT; ++kt) S[kt] *= Gamma;
+    Planes<NO> po[NS];
+    Planes<NI> k1[KT];
+    if constexpr (NS == 2) {
 #pragma unroll
-      for (int r = 2 * s; r < NT; ++r) U[r] = mma(tri<NB, 3>(L::t, lower<C>(r, s), lane), b, U[r]);
+      for (int kt = 0; kt < KT; ++kt) k1[kt] = MK::col(here + L::k, cb, kt, 1);
+      bu[NS - 1] = split<3>(left[2] * U[2], left[3] * U[3]);
+    }
+    mma_rows<NI, 3>(k0, bu[0], S);
+    if constexpr (NS == 2) {
+      interleave<NI == 1 ? 3 * KT : 0, 2, NI == 1 ? 2 * KT : 0>();
+      mma_rows<NI, 3>(k1, bu[NS - 1], S);
     }
     if (FWD) {
 #pragma unroll
-      for (int r = 0; r < NT; ++r) O[r] *= lds_get<float>(L::w + 4 * (16 * r + l.i));
+      for (int r = 0; r < NT; ++r) O[r] *= lds_get<float>(here + L::w + 4 * (16 * r + l.i));
+      u32x4 t[NS][NO][NT];
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
-        const Planes<NO> b = split<NO>(U[2 * s], U[2 * s + 1]);
+        po[s] = split<NO>(U[2 * s], U[2 * s + 1]);
 #pragma unroll
-        for (int r = 2 * s; r < NT; ++r) O[r] = mma(b, tri<NB, NO>(L::p, lower<C>(r, s), lane), O[r]);
+        for (int i = 0; i < NO; ++i) tri_plane<C, true>(here + L::p, lane, s, i, t[s][i]);
       }
+#pragma unroll
+      for (int s = 0; s < NS; ++s) mma_step<C, true, true, NO, NO>(t[s], s, po[s], O);
       const unsigned col = (unsigned)((16 * wave + 4 * l.g) * (int)sizeof(T));
       const Buffer ob = xo.rows(r0, nr);
 #pragma unroll
@@ -295,25 +385,15 @@ __global__ __launch_bounds__(64 * NW) void k_delta_scan(Args A) {
         else if (row < nr && col < xo.width) store_quad<T>(xo.at(r0 + row) + col, (int)(xo.width - col), A.scale * O[r]);
       }
     } else {
-      float* const to = A.u + chunk_at(A, bh, c) * ((long long)C * A.dvp) + c0 + l.i;
+      const Buffer to = buffer(A.u + chunk_at(A, bh, c) * ((long long)C * A.dvp), (unsigned)(C * A.dvp) * 4u);
+      const unsigned at = (unsigned)(4 * l.g * A.dvp + c0 + l.i) * 4u;
 #pragma unroll
       for (int r = 0; r < NT; ++r)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) to[(long long)(16 * r + 4 * l.g + j) * A.dvp] = U[r][j];
-    }
-    if (c + 1 < chunks || A.s_out != nullptr) {
-      const float Gamma = lds_get<float>(L::w + 4 * (C - 1));
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) S[kt] *= Gamma;
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const f32x4 w0 = lds_get<f32x4>(L::w + 4 * (C + 32 * s + 4 * l.g)), w1 = lds_get<f32x4>(L::w + 4 * (C + 32 * s + 16 + 4 * l.g));
-        const Planes<3> b = split<3>(w0 * U[2 * s], w1 * U[2 * s + 1]);
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) S[kt] = mma(MK::col(L::k, cb, kt, s), b, S[kt]);
-      }
+        for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(U[r][j]), to, at, (unsigned)(16 * r + j) * A.dvp * 4u, 0);
     }
   }
+  if (DIRECT) wait_loads<0>();   // the loads of the chunk behind the last: LDS is handed on when the wave ends
   if (A.s_out != nullptr) store_state<KT>(S, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g);
 }
 
@@ -325,7 +405,7 @@ struct RevLds {
   static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C);
   typedef Mat<C, D1, NI> MK;
   typedef Mat<C, 16 * NW, NI> MV;
-  static constexpr int k = 0, q = k + MK::kAll, v = q + MK::kAll, t = v + MV::kAll, p = t + 3 * NB * 1024, w = p + 3 * NB * 1024, all = w + 3 * C * 4;
+  static constexpr int k = 0, q = k + MK::kAll, v = q + MK::kAll, t = v + MV::kAll, p = t + 3 * NB * 1024, w = p + 3 * NB * 1024, all = w + kScanVecs * C * 4;
 };
 
 template <typename T, int D1, int NW, bool VEC>
@@ -346,32 +426,33 @@ __global__ __launch_bounds__(64 * NW) void k_delta_rev(Args A) {
   Load<T, C, D1, NTH, VEC> lk, lq;
   Load<T, C, VC, NTH, VEC> lo;
   LoadTri<NB, 3, NTH> lt, lp;
-  float lw[(3 * C + NTH - 1) / NTH];
-  const auto fetch = [&](int c) {
+  f32x4 lw;
+  const auto fetch_rows = [&](int c) {
     const int r0 = c * C, nr = min(C, n - r0);
     lk.load(xk, r0, nr, tid);
     lq.load(xq, r0, nr, tid);
-    lo.load(xo, r0, nr, tid);
-    lt.load(A.trit + chunk_at(A, bh, c) * (NB * 512), tid);
-    lp.load(static_cast<const float*>(A.pri) + chunk_at(A, bh, c) * (NB * 512), tid);
-#pragma unroll
-    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
-      if (tid + e * NTH < 3 * C) lw[e] = A.vec[chunk_at(A, bh, c) * (kVecs * C) + tid + e * NTH];
+  };
+  const auto fetch_rest = [&](int c) {
+    const long long own = chunk_at(A, bh, c);
+    lo.load(xo, c * C, min(C, n - c * C), tid);
+    lt.load(A.trit + own * (3 * NB * 64), tid);
+    lp.load(A.pri + own * (3 * NB * 64), tid);
+    if (tid < C) lw = reinterpret_cast<const f32x4*>(A.vec + own * (kVecs * C))[tid];
   };
   const int chunks = (n + C - 1) / C;
-  if (chunks > 0) fetch(chunks - 1);
+  if (chunks > 0) {
+    fetch_rows(chunks - 1);
+    fetch_rest(chunks - 1);
+  }
   for (int c = chunks - 1; c >= 0; --c) {
-    __syncthreads();
+    lds_barrier();
     lk.template store<MK>(L::k, tid);
     lq.template store<MK>(L::q, tid);
     lo.template store<MV>(L::v, tid);
     lt.store(L::t, tid);
     lp.store(L::p, tid);
-#pragma unroll
-    for (int e = 0; e < (3 * C + NTH - 1) / NTH; ++e)
-      if (tid + e * NTH < 3 * C) lds_put(L::w + 4 * (tid + e * NTH), lw[e]);
-    __syncthreads();
-    if (c > 0) fetch(c - 1);
+    if (tid < C) lds_put(L::w + 16 * tid, lw);
+    lds_barrier();
     {
       float* const to = A.dstates + chunk_at(A, bh, c) * ((long long)D1 * A.dvp) + c0 + l.i;
 #pragma unroll
@@ -385,23 +466,47 @@ __global__ __launch_bounds__(64 * NW) void k_delta_rev(Args A) {
     for (int r = 0; r < NT; ++r) U[r] = R[r] = zero4();
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      const Planes<3> b = split<3>(G[2 * s], G[2 * s + 1]);
+      Planes<NI> k[NT];
 #pragma unroll
-      for (int r = 0; r < NT; ++r) U[r] = mma(MK::row(L::k, rb, r, s), b, U[r]);
+      for (int r = 0; r < NT; ++r) k[r] = MK::row(L::k, rb, r, s);
+      mma_rows<NI, 3>(k, split<3>(G[2 * s], G[2 * s + 1]), U);
     }
+    fetch_rows(max(c - 1, 0));
 #pragma unroll
     for (int r = 0; r < NT; ++r) U[r] *= lds_get<f32x4>(L::w + 4 * (C + 16 * r + 4 * l.g));
+    {
+      Planes<NI> b[NS];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const Planes<NI> b = MV::col(L::v, vb, wave, s);
-#pragma unroll
-      for (int r = 0; r < (NS == 1 ? NT : 2 * s + 2); ++r) U[r] = mma(tri<NB, 3>(L::p, upper<C>(r, s), lane), b, U[r]);
+      for (int s = 0; s < NS; ++s) b[s] = MV::col(L::v, vb, wave, s);
+      mma_tri<C, false, false, 3, NI, 3>(L::p, lane, b, U);
     }
+    {
+      Planes<3> b[NS];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const Planes<3> b = split<3>(U[2 * s], U[2 * s + 1]);
+      for (int s = 0; s < NS; ++s) b[s] = split<3>(U[2 * s], U[2 * s + 1]);
+      mma_tri<C, false, false, 3, 3, 3>(L::t, lane, b, R);
+    }
+    fetch_rest(max(c - 1, 0));
+    {
+      const float Gamma = lds_get<float>(L::w + 4 * (3 * C));
 #pragma unroll
-      for (int r = 0; r < (NS == 1 ? NT : 2 * s + 2); ++r) R[r] = mma(tri<NB, 3>(L::t, upper<C>(r, s), lane), b, R[r]);
+      for (int kt = 0; kt < KT; ++kt) G[kt] *= Gamma;
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const f32x4 w0 = lds_get<f32x4>(L::w + 4 * (32 * s + 4 * l.g)), w1 = lds_get<f32x4>(L::w + 4 * (32 * s + 16 + 4 * l.g));
+        const f32x4 b0 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 4 * l.g)), b1 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 16 + 4 * l.g));
+        Planes<NI> x[KT];
+        {
+          const Planes<3> o = split<3>(A.scale * w0 * MV::quad(L::v, vb, wave, 2 * s), A.scale * w1 * MV::quad(L::v, vb, wave, 2 * s + 1));
+#pragma unroll
+          for (int kt = 0; kt < KT; ++kt) x[kt] = MK::col(L::q, cb, kt, s);
+          mma_rows<NI, 3>(x, o, G);
+        }
+        const Planes<3> b = split<3>(-(w0 * b0) * R[2 * s], -(w1 * b1) * R[2 * s + 1]);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt) x[kt] = MK::col(L::k, cb, kt, s);
+        mma_rows<NI, 3>(x, b, G);
+      }
     }
     {
       float* const to = A.dr + chunk_at(A, bh, c) * ((long long)C * A.dvp) + c0 + l.i;
@@ -409,23 +514,6 @@ __global__ __launch_bounds__(64 * NW) void k_delta_rev(Args A) {
       for (int r = 0; r < NT; ++r)
 #pragma unroll
         for (int j = 0; j < 4; ++j) to[(long long)(16 * r + 4 * l.g + j) * A.dvp] = R[r][j];
-    }
-    if (c > 0 || A.s_out != nullptr) {
-      const float Gamma = lds_get<float>(L::w + 4 * (C - 1));
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) G[kt] *= Gamma;
-#pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        const f32x4 w0 = lds_get<f32x4>(L::w + 4 * (32 * s + 4 * l.g)), w1 = lds_get<f32x4>(L::w + 4 * (32 * s + 16 + 4 * l.g));
-        const f32x4 b0 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 4 * l.g)), b1 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 16 + 4 * l.g));
-        const Planes<3> o = split<3>(A.scale * w0 * MV::quad(L::v, vb, wave, 2 * s), A.scale * w1 * MV::quad(L::v, vb, wave, 2 * s + 1));
-        const Planes<3> b = split<3>(-(w0 * b0) * R[2 * s], -(w1 * b1) * R[2 * s + 1]);
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt) {
-          G[kt] = mma(MK::col(L::q, cb, kt, s), o, G[kt]);
-          G[kt] = mma(MK::col(L::k, cb, kt, s), b, G[kt]);
-        }
-      }
     }
   }
   if (A.s_out != nullptr) store_state<KT>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g);
@@ -458,18 +546,20 @@ static dark_status launch_prep(const Args& a, bool backward, hipStream_t st) {
   }
 }
 
-template <typename T, int D1, int NW, bool VEC, bool FWD>
+template <typename T, int D1, int NW, bool VEC, bool FWD, bool DIRECT>
 static dark_status go_scan(const Args& a, hipStream_t st) {
-  constexpr int lds = ScanLds<T, D1, NW, FWD>::all;
-  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD>, lds));
+  constexpr int lds = ScanLds<T, D1, NW, FWD, DIRECT>::all;
+  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>, lds));
   const int cols = FWD ? a.dv : a.dvp;
-  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(64 * NW), lds, a);
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(64 * NW), lds, a);
   return DARK_OK;
 }
 template <typename T, int D1>
 static dark_status go_scan(const Args& a, Pass pass, hipStream_t st) {
-  if (vec_of<T>(a)) return pass == kForward ? go_scan<T, D1, 4, true, true>(a, st) : go_scan<T, D1, 4, true, false>(a, st);
-  return pass == kForward ? go_scan<T, D1, 4, false, true>(a, st) : go_scan<T, D1, 4, false, false>(a, st);
+  if constexpr (direct_of<T>(D1))
+    if (a.dk == D1 && a.dv % 64 == 0) return pass == kForward ? go_scan<T, D1, 4, true, true, true>(a, st) : go_scan<T, D1, 4, true, false, true>(a, st);
+  if (vec_of<T>(a)) return pass == kForward ? go_scan<T, D1, 4, true, true, false>(a, st) : go_scan<T, D1, 4, true, false, false>(a, st);
+  return pass == kForward ? go_scan<T, D1, 4, false, true, false>(a, st) : go_scan<T, D1, 4, false, false, false>(a, st);
 }
 template <typename T>
 static dark_status launch_scan(const Args& a, Pass pass, hipStream_t st) {

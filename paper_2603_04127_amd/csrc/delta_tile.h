@@ -52,6 +52,47 @@ __device__ static inline f32x4 mma(const Planes<NA>& a, const Planes<NB>& b, f32
   return mma_of<NA, NB>(a, b, c);
 }
 
+// c_r + a_r b for some tiles at once, plane by plane: a product of 16 x 16 x 32 can follow another one into the same sums only after 8 of
+// its cycles more than it takes, and products of other tiles fill them.
+template <int MA, int MB, int R, int NA, int NB>
+__device__ static inline void mma_rows(const Planes<NA> (&a)[R], const Planes<NB>& b, f32x4 (&c)[R]) {
+  constexpr int W = MA > MB ? MA : MB;
+#pragma unroll
+  for (int w = W - 1; w >= 0; --w)
+#pragma unroll
+    for (int i = 0; i < MA; ++i)
+      if (w - i >= 0 && w - i < MB)
+#pragma unroll
+        for (int r = 0; r < R; ++r) c[r] = mma1(a[r].p[i], b.p[w - i], c[r]);
+}
+// c_r + a b_r
+template <int MA, int MB, int R, int NA, int NB>
+__device__ static inline void mma_cols(const Planes<NA>& a, const Planes<NB> (&b)[R], f32x4 (&c)[R]) {
+  constexpr int W = MA > MB ? MA : MB;
+#pragma unroll
+  for (int w = W - 1; w >= 0; --w)
+#pragma unroll
+    for (int i = 0; i < MA; ++i)
+      if (w - i >= 0 && w - i < MB)
+#pragma unroll
+        for (int r = 0; r < R; ++r) c[r] = mma1(a.p[i], b[r].p[w - i], c[r]);
+}
+
+// What follows stays behind what came before, for the compiler's scheduler.
+__device__ static inline void step_end() { __builtin_amdgcn_sched_barrier(0); }
+// Of the step that ends here: first `D` reads of LDS (the next step's operands), then products with `V` vector instructions behind each
+// (those make the next step's operands): a wave that has its SIMD to itself overlaps them in no other way.
+template <int M, int V, int D>
+__device__ static inline void interleave() {
+  if constexpr (D > 0) __builtin_amdgcn_sched_group_barrier(0x100, D, 0);
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x002, V, 0);
+  }
+  step_end();
+}
+
 // x as N truncated planes.
 template <int N>
 __device__ static inline Planes<N> split(f32x4 a, f32x4 b) {
@@ -195,51 +236,119 @@ struct Load {
   }
 };
 
-// A triangle in operand order on its way from scratch memory to LDS as planes: blocks of 64 lanes x 8 values.
-// N planes of fp32 values, or (RAW) N planes that were split before.
-template <int NB, int N, int NTH, bool RAW = false>
+// A triangle in operand order on its way from scratch memory to LDS: N planes of blocks of 64 lanes x 8 values.
+template <int NB, int N, int NTH>
 struct LoadTri {
-  static constexpr int kUnits = NB * 64, kEach = (kUnits + NTH - 1) / NTH, kP = RAW ? N : 2;
-  static constexpr int kBytes = NB * 1024;   // a plane
-  u32x4 r[kEach][kP];
-  __device__ void load(const void* from, int tid) {
+  static constexpr int kUnits = N * NB * 64, kEach = (kUnits + NTH - 1) / NTH;
+  u32x4 r[kEach];
+  __device__ void load(const u32x4* from, int tid) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int u = tid + e * NTH;
-      if (kUnits % NTH == 0 || u < kUnits)
-#pragma unroll
-        for (int k = 0; k < kP; ++k) r[e][k] = static_cast<const u32x4*>(from)[RAW ? k * kUnits + u : u * kP + k];
+      if (kUnits % NTH == 0 || u < kUnits) r[e] = from[u];
     }
   }
   __device__ void store(int tile, int tid) const {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int u = tid + e * NTH;
-      if (kUnits % NTH == 0 || u < kUnits) {
-        if constexpr (RAW) {
-#pragma unroll
-          for (int p = 0; p < N; ++p) lds_put(tile + p * kBytes + 16 * u, r[e][p]);
-        } else {
-          const Planes<N> f = split<N>(as_float(r[e][0]), as_float(r[e][kP - 1]));
-#pragma unroll
-          for (int p = 0; p < N; ++p) lds_put(tile + p * kBytes + 16 * u, f.p[p]);
-        }
-      }
+      if (kUnits % NTH == 0 || u < kUnits) lds_put(tile + 16 * u, r[e]);
     }
   }
 };
-template <int NB, int N>
-__device__ static inline Planes<N> tri(int tile, int block, int lane) {
-  Planes<N> f;
+// The same ways from memory to LDS without registers, 1 KB an instruction of a wave: for bf16 tiles whose rows fill them.  Rows behind the last
+// are copies of it (their weights are 0: k_delta_prep).  A wave's lanes write where they lie, so that a lane asks for the 16 bytes that
+// the swizzle puts there.  The caller waits for them (wait_loads) before the barrier that hands them out.
+template <int C, int D, int NTH>
+struct Direct {
+  typedef Mat<C, D, 1> M;
+  static constexpr int kLanes = M::RB / 16, kRows = 64 / kLanes, kAll = C / kRows, kEach = kAll / (NTH / 64);   // rows an instruction, instructions
+  static_assert(kAll % (NTH / 64) == 0, "whole instructions a wave");
+  __device__ static void load(int tile, const Rows& x, int r0, int nr, int wave, int lane) {
+    const char* const first = x.head + (long long)r0 * x.row;
 #pragma unroll
-  for (int p = 0; p < N; ++p) f.p[p] = lds_get<u32x4>(tile + p * NB * 1024 + block * 1024 + 16 * lane);
-  return f;
+    for (int e = 0; e < kEach; ++e) {
+      const int i = e * (NTH / 64) + wave, row = i * kRows + lane / kLanes;
+      const unsigned off = (unsigned)min(row, nr - 1) * x.row + (unsigned)(((lane % kLanes) ^ swz<M::RB>(row & 15)) << 4);
+      dma16_to_lds(first, off, reinterpret_cast<void*>((uintptr_t)(tile + i * 1024)));
+    }
+  }
+};
+// `bytes` (whole KB) as they are.
+template <int KB, int NTH>
+__device__ static inline void direct_copy(int tile, const void* from, int wave, int lane) {
+#pragma unroll
+  for (int e = 0; e < (KB + NTH / 64 - 1) / (NTH / 64); ++e) {
+    const int i = e * (NTH / 64) + wave;
+    if (KB % (NTH / 64) == 0 || i < KB) dma16_to_lds(static_cast<const char*>(from) + i * 1024, (unsigned)lane * 16u, reinterpret_cast<void*>((uintptr_t)(tile + i * 1024)));
+  }
 }
-// The block of row tile r and inner step s: of a lower triangle (s <= r / 2), of an upper one (s >= r / 2).
-template <int C>
-__device__ constexpr int lower(int r, int s) { return C == 32 || r < 2 ? r : 2 * (r - 1) + s; }
-template <int C>
-__device__ constexpr int upper(int r, int s) { return C == 32 ? r : r < 2 ? 2 * r + s : r + 2; }
+// Waits for all memory operations of the wave but the last `N`.
+template <int N>
+__device__ static inline void wait_loads() {
+  static_assert(N < 64, "what vmcnt counts");
+  __builtin_amdgcn_s_waitcnt(0x0F70 | (N & 15) | (N >> 4) << 14);
+}
+
+// The blocks of a triangle of one inner step: row tiles of a lower one from 2 s on, of an upper one up to 2 s + 1.
+template <int C, bool LOWER>
+struct Tri {
+  static constexpr int NT = C / 16;
+  __device__ static constexpr int first(int s) { return LOWER ? 2 * s : 0; }
+  __device__ static constexpr int last(int s) { return LOWER ? NT - 1 : C == 32 ? 1 : 2 * s + 1; }
+  __device__ static constexpr int block(int r, int s) { return C == 32 ? r : LOWER ? (r < 2 ? r : 2 * (r - 1) + s) : (r < 2 ? 2 * r + s : r + 2); }
+};
+// One plane of the blocks of step s.
+template <int C, bool LOWER>
+__device__ static inline void tri_plane(int tile, int lane, int s, int plane, u32x4 (&t)[C / 16]) {
+  typedef Tri<C, LOWER> X;
+#pragma unroll
+  for (int r = 0; r < C / 16; ++r)
+    if (r >= X::first(s) && r <= X::last(s)) t[r] = lds_get<u32x4>(tile + (plane * blocks_of(C) + X::block(r, s)) * 1024 + 16 * lane);
+}
+// x_r + the blocks' products with b, plane by plane of the triangle, the smallest first (TRANS: b on the left).
+template <int C, bool LOWER, bool TRANS, int MA, int MB, int N>
+__device__ static inline void mma_step(const u32x4 (&t)[MA][C / 16], int s, const Planes<N>& b, f32x4 (&x)[C / 16]) {
+  typedef Tri<C, LOWER> X;
+#pragma unroll
+  for (int i = MA - 1; i >= 0; --i)
+#pragma unroll
+    for (int j = (MA > MB ? MA : MB) - 1 - i; j >= 0; --j)
+      if (j < MB)
+#pragma unroll
+        for (int r = 0; r < C / 16; ++r)
+          if (r >= X::first(s) && r <= X::last(s)) x[r] = TRANS ? mma1(b.p[j], t[i][r], x[r]) : mma1(t[i][r], b.p[j], x[r]);
+}
+
+// x_r + triangle . b (or b . triangle, TRANS): plane by plane of the triangle, the smallest first; a row's two blocks into sums of their own.
+template <int C, bool LOWER, bool TRANS, int MA, int MB, int NA, int NB_>
+__device__ static inline void mma_tri(int tile, int lane, const Planes<NB_> (&b)[C / 32], f32x4 (&x)[C / 16]) {
+  constexpr int NB = blocks_of(C);
+  f32x4 more[2] = {zero4(), zero4()};
+#pragma unroll
+  for (int i = MA - 1; i >= 0; --i) {
+    u32x4 t[NB];
+#pragma unroll
+    for (int k = 0; k < NB; ++k) t[k] = lds_get<u32x4>(tile + i * NB * 1024 + k * 1024 + 16 * lane);
+#pragma unroll
+    for (int j = (MA > MB ? MA : MB) - 1 - i; j >= 0; --j) {
+      if (j >= MB) continue;
+#pragma unroll
+      for (int k = 0; k < NB; ++k) {
+        // block k: row tile r, inner step s
+        const int r = C == 32 ? k : LOWER ? (k < 2 ? k : k < 4 ? 2 : 3) : (k < 4 ? k >> 1 : k - 2);
+        const int s = C == 32 ? 0 : LOWER ? (k < 2 ? 0 : k & 1) : (k < 4 ? k & 1 : 1);
+        const bool second = C == 64 && (LOWER ? k == 3 || k == 5 : k == 1 || k == 3);
+        f32x4& y = second ? more[LOWER ? (k == 5) : (k == 3)] : x[r];
+        y = TRANS ? mma1(b[s].p[j], t[k], y) : mma1(t[k], b[s].p[j], y);
+      }
+    }
+  }
+  if constexpr (C == 64) {
+    x[LOWER ? 2 : 0] += more[0];
+    x[LOWER ? 3 : 1] += more[1];
+  }
+}
 
 // Rows of a (b,h), from column col0 on.
 template <typename T>
