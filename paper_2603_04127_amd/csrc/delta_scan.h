@@ -1,6 +1,8 @@
 // The gated delta rule chunk by chunk: the chunks' triangles, and the scans over them (see delta.h for the mathematics).
 #pragma once
 
+#include <type_traits>
+
 #include "delta_tile.h"
 
 namespace dark {
@@ -175,119 +177,180 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
 // ---------------------------------------------------------------------------
 // Chunk after chunk.  A wave owns 16 columns of the state, in the accumulators of the products that update it, and takes them through
 // all of a chunk's products by itself: its state is an operand of K S and Q S, R of T R, U of P U and of the update, all without a way
-// through LDS or another wave.
+// through LDS or another wave.  Further waves bring the next chunk's operands to LDS meanwhile: a wave that has its SIMD to itself issues an
+// instruction in five or six cycles, whatever it is, so that the chain from state to state is as long as it has instructions.
 // ---------------------------------------------------------------------------
-// Where a chunk's operands lie in LDS; DIRECT: two chunks', one being read and one on its way there.
-template <typename T, int D1, int NW, bool FWD, bool DIRECT>
-struct ScanLds {
-  static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C);
+// A chunk's operands in LDS (NP: planes of P, 0: neither Q nor P), in one buffer or two.  An instruction's own offset reaches 64 KB: a lane has a
+// base for each operand, and the buffers lie beside each other.
+// DIRECT: bf16 rows that fill the tiles, by loads that end in LDS, issued by one wave; else four waves take them through registers.
+template <typename T, int D1, int NW, int NP, bool DIRECT>
+struct Chunks {
+  static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C), VC = 16 * NW;
   typedef Mat<C, D1, NI> MK;
-  typedef Mat<C, 16 * NW, NI> MV;
-  static constexpr int k = 0, v = k + MK::kAll, t = v + MV::kAll, w = t + 3 * NB * 1024, q = w + kScanVecs * C * 4, p = q + (FWD ? MK::kAll : 0),
-                       one = p + (FWD ? Kind<T>::kOut * NB * 1024 : 0), all = DIRECT ? 2 * one : one;
+  typedef Mat<C, VC, NI> MV;
+  static constexpr int kV = MV::kAll, kW = kScanVecs * C * 4, kT = 3 * NB * 1024, kP = NP * NB * 1024, kQ = NP > 0 ? MK::kAll : 0;   // bytes of each
+  static constexpr int kBufs = 2 * (MK::kAll + kQ + kV + kW + kT + kP) <= 160 * 1024 ? 2 : 1;
+  static constexpr int k = 0, q = k + kBufs * MK::kAll, v = q + kBufs * kQ, w = v + kBufs * kV, t = w + kBufs * kW, p = t + kBufs * kT, all = p + kBufs * kP;
+  static constexpr int kLoaders = DIRECT ? 1 : D1 > 128 ? 2 : 4, kThreads = 64 * (NW + kLoaders), NTH = 64 * kLoaders;
+  static_assert(!DIRECT || kBufs == 2, "loads that end in LDS go to the other buffer");
 };
-// Instances that take their operands straight to LDS: bf16 whose rows fill the tiles.
-template <typename T>
-constexpr bool direct_of(int D1) { return sizeof(T) == 2 && D1 <= 128; }
+
+// A lane's bases.  The compiler is not to take them apart: it would hold one for every read behind the first 64 KB.
+template <typename L>
+struct Bases {
+  static constexpr bool kFar = L::q + L::kBufs * L::kQ > 65536;   // K and Q do not share bases
+  int rows, query, cols, query_cols, value, tri, weights, vec, vec_row;
+  __device__ Bases(Lane l, int lane, int wave)
+      : rows(L::MK::row_base(l)), query(rows + (kFar ? L::q : 0)), cols(L::MK::col_base(l)), query_cols(cols + (kFar ? L::q : 0)),
+        value((L::MV::col_base(l) ^ (wave << 5)) + L::v), tri(16 * lane + L::t), weights(16 * lane + L::p), vec(16 * l.g + L::w), vec_row(4 * l.i + L::w) {
+    if (kFar) {
+      asm("" : "+v"(query));
+      asm("" : "+v"(query_cols));
+    }
+    asm("" : "+v"(value));
+    asm("" : "+v"(tri));
+    asm("" : "+v"(weights));
+    asm("" : "+v"(vec));
+    asm("" : "+v"(vec_row));
+  }
+};
+
+// The loading waves: chunk after chunk (REV: from the last to the first), one ahead.
+template <typename L, typename T, int D1, int NP, bool VEC, bool DIRECT, bool REV>
+__device__ static inline void load_chunks(const Args& A, int bh, const Rows& xk, const Rows& xq, const Rows& xv, int n, int tid) {
+  constexpr int C = L::C, NB = L::NB, NTH = L::NTH;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, chunks = (n + C - 1) / C;
+  const auto chunk = [&](int i) { return REV ? chunks - 1 - i : i; };
+  const u32x4* const tri = REV ? A.trit : A.tri;
+  if constexpr (DIRECT) {
+    const auto load = [&](int i, int buf) {
+      const int c = chunk(i), r0 = c * C, nr = min(C, n - r0);
+      const long long own = chunk_at(A, bh, c);
+      Direct<C, D1, NTH>::load(L::k + buf * L::MK::kAll, xk, r0, nr, wave, lane);
+      if (NP > 0) Direct<C, D1, NTH>::load(L::q + buf * L::kQ, xq, r0, nr, wave, lane);
+      Direct<C, L::VC, NTH>::load(L::v + buf * L::kV, xv, r0, nr, wave, lane);
+      direct_copy<3 * NB, NTH>(L::t + buf * L::kT, tri + own * (3 * NB * 64), wave, lane);
+      if (NP > 0) direct_copy<NP * NB, NTH>(L::p + buf * L::kP, A.pri + own * (NP * NB * 64), wave, lane);
+      direct_copy<kScanVecs * C / 256, NTH>(L::w + buf * L::kW, A.vec + own * (kVecs * C), wave, lane);
+    };
+    load(0, 0);
+    wait_vmcnt0();
+    lds_barrier();
+    for (int i = 0; i < chunks; ++i) {
+      if (i + 1 < chunks) load(i + 1, (i + 1) % 2);
+      wait_vmcnt0();
+      lds_barrier();
+    }
+  } else {
+    Load<T, C, D1, NTH, VEC> lk, lq;
+    Load<T, C, L::VC, NTH, VEC> lv;
+    LoadTri<NB, 3, NTH> lt;
+    LoadTri<NB, (NP > 0 ? NP : 1), NTH> lp;
+    f32x4 lw;
+    const auto load = [&](int i) {
+      const int c = chunk(i), r0 = c * C, nr = min(C, n - r0);
+      const long long own = chunk_at(A, bh, c);
+      lk.load(xk, r0, nr, tid);
+      if (NP > 0) lq.load(xq, r0, nr, tid);
+      lv.load(xv, r0, nr, tid);
+      lt.load(tri + own * (3 * NB * 64), tid);
+      if (NP > 0) lp.load(A.pri + own * (NP * NB * 64), tid);
+      if (tid < C) lw = reinterpret_cast<const f32x4*>(A.vec + own * (kVecs * C))[tid];
+    };
+    const auto store = [&](int buf) {
+      lk.template store<typename L::MK>(L::k + buf * L::MK::kAll, tid);
+      if (NP > 0) lq.template store<typename L::MK>(L::q + buf * L::kQ, tid);
+      lv.template store<typename L::MV>(L::v + buf * L::kV, tid);
+      lt.store(L::t + buf * L::kT, tid);
+      if (NP > 0) lp.store(L::p + buf * L::kP, tid);
+      if (tid < C) lds_put(L::w + buf * L::kW + 16 * tid, lw);
+    };
+    load(0);
+    store(0);
+    if (chunks > 1) load(1);
+    lds_barrier();
+    for (int i = 0; i < chunks; ++i) {
+      if (L::kBufs == 1) lds_barrier();   // the chunk's readers are done
+      if (i + 1 < chunks) {
+        store((i + 1) % L::kBufs);
+        if (i + 2 < chunks) load(i + 2);
+      }
+      lds_barrier();
+    }
+  }
+}
+// The computing waves: f(chunk, the buffer of its operands, a constant) for every chunk.
+template <typename L, bool REV, typename F>
+__device__ static inline void each_chunk(int chunks, const F& f) {
+  lds_barrier();
+  for (int i = 0; i < chunks;) {
+    f(REV ? chunks - 1 - i : i, std::integral_constant<int, 0>());
+    if (L::kBufs == 1) lds_barrier();
+    lds_barrier();
+    ++i;
+    if (L::kBufs == 1 || i == chunks) continue;
+    f(REV ? chunks - 1 - i : i, std::integral_constant<int, 1>());
+    lds_barrier();
+    ++i;
+  }
+}
+
+// A wave's 16 columns from c0 on of rows (and columns) of scratch.
+template <int N>
+__device__ static inline void put_columns(const f32x4 (&x)[N], float* to, int rows, int stride, int c0, Lane l) {
+  const Buffer b = buffer(to, (unsigned)(rows * stride) * 4u);
+  const unsigned own = (unsigned)(4 * l.g * stride + c0 + l.i) * 4u;
+#pragma unroll
+  for (int r = 0; r < N; ++r)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[r][j]), b, own, (unsigned)((16 * r + j) * stride) * 4u, 0);
+}
 
 template <typename T, int D1, int NW, bool VEC, bool FWD, bool DIRECT>
-__global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args A) {
-  typedef ScanLds<T, D1, NW, FWD, DIRECT> L;
-  constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, NB = L::NB, NTH = 64 * NW, VC = 16 * NW;
+__global__ __launch_bounds__((Chunks<T, D1, NW, 1, DIRECT>::kThreads)) void k_delta_scan(Args A) {
   constexpr int NO = Kind<T>::kOut;
+  typedef Chunks<T, D1, NW, (FWD ? NO : 0), DIRECT> L;
+  constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, VC = 16 * NW;
   typedef typename L::MK MK;
   typedef typename L::MV MV;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int bh = blockIdx.x, col0 = blockIdx.y * VC, n = length_of(A, bh), c0 = col0 + 16 * wave;
+  const int bh = blockIdx.x, col0 = blockIdx.y * VC, n = length_of(A, bh), c0 = col0 + 16 * wave, chunks = (n + C - 1) / C;
   const Lane l{lane & 15, lane >> 4};
   const Rows xk = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), xq = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk),
              xv = rows_at<T>(A.V, A, bh, A.dv, n, col0, min(A.dv - col0, VC)), xo = rows_at<T>(A.out, A, bh, A.dv, n, col0, min(A.dv - col0, VC));
-  if (FWD && n < A.L) zero_rows<T>(xo, n, A.L, tid, NTH);
+  if (FWD && n < A.L) zero_rows<T>(xo, n, A.L, tid, L::kThreads);
+  if (wave >= NW) {
+    if (chunks > 0) load_chunks<L, T, D1, (FWD ? NO : 0), VEC, DIRECT, false>(A, bh, xk, xq, xv, n, tid - 64 * NW);
+    return;
+  }
   f32x4 S[KT];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) S[kt] = zero4();
   if (A.s_in != nullptr) load_state<KT, true>(S, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g);
-  Load<T, C, D1, NTH, VEC> lk, lq;
-  Load<T, C, VC, NTH, VEC> lv;
-  LoadTri<NB, 3, NTH> lt;
-  LoadTri<NB, NO, NTH> lp;
-  f32x4 lw;
-  // A chunk's operands are asked for piece by piece between the products of the one before it: all at once they would stop the wave until
-  // the memory pipe has taken them (1200 of a chunk's 13,000 cycles).
-  const auto fetch_rows = [&](int c, int to) {
+  const Bases<L> base(l, lane, wave);
+  const auto step = [&](int c, auto buffer_of) {
+    constexpr int buf = decltype(buffer_of)::value, tk = buf * MK::kAll, tq = base.kFar ? buf * MK::kAll : L::q + buf * MK::kAll, tv = buf * L::kV, tt = buf * L::kT, tp = buf * L::kP, tw = buf * L::kW;
+    const int rb = base.rows, rq = base.query, cb = base.cols, vb = base.value, tb = base.tri, pb = base.weights, wb = base.vec, wi = base.vec_row;
     const int r0 = c * C, nr = min(C, n - r0);
-    if constexpr (DIRECT) {
-      Direct<C, D1, NTH>::load(to + L::k, xk, r0, nr, wave, lane);
-      if (FWD) Direct<C, D1, NTH>::load(to + L::q, xq, r0, nr, wave, lane);
-    } else {
-      lk.load(xk, r0, nr, tid);
-      if (FWD) lq.load(xq, r0, nr, tid);
-    }
-  };
-  const auto fetch_rest = [&](int c, int to) {
-    const long long own = chunk_at(A, bh, c);
-    const int r0 = c * C, nr = min(C, n - r0);
-    const u32x4 *const tri = A.tri + own * (3 * NB * 64), *const pri = A.pri + own * (NO * NB * 64);
-    const float* const vec = A.vec + own * (kVecs * C);
-    if constexpr (DIRECT) {
-      Direct<C, VC, NTH>::load(to + L::v, xv, r0, nr, wave, lane);
-      direct_copy<3 * NB, NTH>(to + L::t, tri, wave, lane);
-      if (FWD) direct_copy<NO * NB, NTH>(to + L::p, pri, wave, lane);
-      direct_copy<kScanVecs * C / 256, NTH>(to + L::w, vec, wave, lane);
-    } else {
-      lv.load(xv, r0, nr, tid);
-      lt.load(tri, tid);
-      if (FWD) lp.load(pri, tid);
-      if (tid < C) lw = reinterpret_cast<const f32x4*>(vec)[tid];
-    }
-  };
-  const int chunks = (n + C - 1) / C;
-  if (chunks > 0) {
-    fetch_rows(0, 0);
-    fetch_rest(0, 0);
-  }
-  if (DIRECT) wait_loads<0>();
-  for (int c = 0; c < chunks; ++c) {
-    const int r0 = c * C, nr = min(C, n - r0);
-    const int next = min(c + 1, chunks - 1);   // behind the last: it again, without a branch that would part the products
-    const int here = DIRECT ? (c & 1) * L::one : 0, there = DIRECT ? L::one - here : 0;
-    if (DIRECT) {
-      if (c > 0) wait_loads<FWD ? NT : 4 * NT>();   // behind the loads came the last chunk's results, that many stores
-      lds_barrier();
-    } else {
-      lds_barrier();
-      lk.template store<MK>(L::k, tid);
-      lv.template store<MV>(L::v, tid);
-      lt.store(L::t, tid);
-      if (FWD) {
-        lq.template store<MK>(L::q, tid);
-        lp.store(L::p, tid);
-      }
-      if (tid < C) lds_put(L::w + 16 * tid, lw);
-      lds_barrier();
-    }
-    if (!FWD) {
-      const Buffer to = buffer(A.states + chunk_at(A, bh, c) * ((long long)D1 * A.dvp), (unsigned)(D1 * A.dvp) * 4u);
-      const unsigned at = (unsigned)(4 * l.g * A.dvp + c0 + l.i) * 4u;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[kt][j]), to, at, (unsigned)(16 * kt + j) * A.dvp * 4u, 0);
-    }
-    const int rb = MK::row_base(l), cb = MK::col_base(l), vb = MV::col_base(l);
+    if (!FWD) put_columns<KT>(S, A.states + chunk_at(A, bh, c) * ((long long)D1 * A.dvp), D1, A.dvp, c0, l);
     // Steps: the products of one run while the next one's operands are read and split.
     f32x4 R[NT], O[NT], U[NT], V[NT], gamma[NT], beta[NT];
 #pragma unroll
     for (int r = 0; r < NT; ++r) R[r] = O[r] = U[r] = zero4();
     u32x4 t0[3][NT];
+    const auto ask_row = [&](int r) {
+      V[r] = MV::quad(tv, vb, 0, r);
+      gamma[r] = lds_get<f32x4>(wb + tw + 4 * (16 * r));
+      beta[r] = lds_get<f32x4>(wb + tw + 4 * (2 * C + 16 * r));
+    };
     {
       Planes<NI> k[2][NT], q[2][NT];
       Planes<3> b[2];
       const auto ask = [&](int s) {
 #pragma unroll
         for (int r = 0; r < NT; ++r) {
-          k[s & 1][r] = MK::row(here + L::k, rb, r, s);
-          if (FWD) q[s & 1][r] = MK::row(here + L::q, rb, r, s);
+          k[s & 1][r] = MK::row(tk, rb, r, s);
+          if (FWD) q[s & 1][r] = MK::row(tq, rq, r, s);
         }
       };
       ask(0);
@@ -300,28 +363,25 @@ __global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args 
           b[(s + 1) & 1] = split<3>(S[2 * s + 2], S[2 * s + 3]);
         } else {
 #pragma unroll
-          for (int r = 0; r < NT; ++r) {
-            V[r] = MV::quad(here + L::v, vb, wave, r);
-            gamma[r] = lds_get<f32x4>(here + L::w + 4 * (16 * r + 4 * l.g));
-            beta[r] = lds_get<f32x4>(here + L::w + 4 * (2 * C + 16 * r + 4 * l.g));
-          }
-#pragma unroll
-          for (int i = 0; i < 3; ++i) tri_plane<C, true>(here + L::t, lane, 0, i, t0[i]);
+          for (int r = 0; r < 2; ++r) ask_row(r);
         }
         mma_rows<NI, 3>(k[s & 1], b[s & 1], R);
         if (FWD) mma_cols<NO, NI>(b[s & 1], q[s & 1], O);
         interleave<NI == 1 ? NT * (3 + (FWD ? NO : 0)) : 0, 3, NI == 1 ? (FWD ? 2 : 1) * NT : 0>();
       }
     }
-    fetch_rows(next, there);
     step_end();
     const auto correct = [&](int r) { R[r] = beta[r] * (V[r] - gamma[r] * R[r]); };
-    const float Gamma = lds_get<float>(here + L::w + 4 * (3 * C));
+    const float Gamma = lds_get<float>(wb + tw + 4 * (3 * C));
     Planes<NI> k0[KT];
     Planes<3> bu[NS];
     f32x4 left[NT];
     {
       Planes<3> b[NS];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) tri_plane<C, true>(tt, tb, 0, i, t0[i]);
+#pragma unroll
+      for (int r = 2; r < NT; ++r) ask_row(r);
       correct(0);
       correct(1);
       b[0] = split<3>(R[0], R[1]);
@@ -329,7 +389,7 @@ __global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args 
       u32x4 t1[3][NT];
       if constexpr (NS == 2) {
 #pragma unroll
-        for (int i = 0; i < 3; ++i) tri_plane<C, true>(here + L::t, lane, 1, i, t1[i]);
+        for (int i = 0; i < 3; ++i) tri_plane<C, true>(tt, tb, 1, i, t1[i]);
         correct(2);
         correct(3);
         b[1] = split<3>(R[2], R[3]);
@@ -337,9 +397,9 @@ __global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args 
       mma_step<C, true, false, 3, 3>(t0, 0, b[0], U);
       interleave<NI == 1 ? 24 : 0, 4, NI == 1 ? 6 : 0>();
 #pragma unroll
-      for (int r = 0; r < NT; ++r) left[r] = lds_get<f32x4>(here + L::w + 4 * (C + 16 * r + 4 * l.g));
+      for (int r = 0; r < NT; ++r) left[r] = lds_get<f32x4>(wb + tw + 4 * (C + 16 * r));
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) k0[kt] = MK::col(here + L::k, cb, kt, 0);
+      for (int kt = 0; kt < KT; ++kt) k0[kt] = MK::col(tk, cb, kt, 0);
       bu[0] = split<3>(left[0] * U[0], left[1] * U[1]);
       if constexpr (NS == 2) {
         mma_step<C, true, false, 3, 3>(t1, 1, b[1], U);
@@ -348,7 +408,6 @@ __global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args 
         step_end();
       }
     }
-    fetch_rest(next, there);
     step_end();
 #pragma unroll
     for (int kt = 0; kt < KT; ++kt) S[kt] *= Gamma;
@@ -356,7 +415,7 @@ __global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args 
     Planes<NI> k1[KT];
     if constexpr (NS == 2) {
 #pragma unroll
-      for (int kt = 0; kt < KT; ++kt) k1[kt] = MK::col(here + L::k, cb, kt, 1);
+      for (int kt = 0; kt < KT; ++kt) k1[kt] = MK::col(tk, cb, kt, 1);
       bu[NS - 1] = split<3>(left[2] * U[2], left[3] * U[3]);
     }
     mma_rows<NI, 3>(k0, bu[0], S);
@@ -365,17 +424,21 @@ __global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args 
       mma_rows<NI, 3>(k1, bu[NS - 1], S);
     }
     if (FWD) {
+      u32x4 t[NO][NT];
 #pragma unroll
-      for (int r = 0; r < NT; ++r) O[r] *= lds_get<float>(here + L::w + 4 * (16 * r + l.i));
-      u32x4 t[NS][NO][NT];
+      for (int i = 0; i < NO; ++i) tri_plane<C, true>(tp, pb, 0, i, t[i]);
 #pragma unroll
-      for (int s = 0; s < NS; ++s) {
-        po[s] = split<NO>(U[2 * s], U[2 * s + 1]);
+      for (int r = 0; r < NT; ++r) O[r] *= lds_get<float>(wi + tw + 4 * (16 * r));
+      po[0] = split<NO>(U[0], U[1]);
+      interleave<NI == 1 ? 3 * KT : 0, 2, 0>();
+      mma_step<C, true, true, NO, NO>(t, 0, po[0], O);
+      if constexpr (NS == 2) {
+        step_end();
 #pragma unroll
-        for (int i = 0; i < NO; ++i) tri_plane<C, true>(here + L::p, lane, s, i, t[s][i]);
+        for (int i = 0; i < NO; ++i) tri_plane<C, true>(tp, pb, 1, i, t[i]);
+        po[1] = split<NO>(U[2], U[3]);
+        mma_step<C, true, true, NO, NO>(t, 1, po[NS - 1], O);
       }
-#pragma unroll
-      for (int s = 0; s < NS; ++s) mma_step<C, true, true, NO, NO>(t[s], s, po[s], O);
       const unsigned col = (unsigned)((16 * wave + 4 * l.g) * (int)sizeof(T));
       const Buffer ob = xo.rows(r0, nr);
 #pragma unroll
@@ -385,82 +448,40 @@ __global__ __launch_bounds__(64 * NW, D1 <= 128 ? 2 : 1) void k_delta_scan(Args 
         else if (row < nr && col < xo.width) store_quad<T>(xo.at(r0 + row) + col, (int)(xo.width - col), A.scale * O[r]);
       }
     } else {
-      const Buffer to = buffer(A.u + chunk_at(A, bh, c) * ((long long)C * A.dvp), (unsigned)(C * A.dvp) * 4u);
-      const unsigned at = (unsigned)(4 * l.g * A.dvp + c0 + l.i) * 4u;
-#pragma unroll
-      for (int r = 0; r < NT; ++r)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(U[r][j]), to, at, (unsigned)(16 * r + j) * A.dvp * 4u, 0);
+      put_columns<NT>(U, A.u + chunk_at(A, bh, c) * ((long long)C * A.dvp), C, A.dvp, c0, l);
     }
-  }
-  if (DIRECT) wait_loads<0>();   // the loads of the chunk behind the last: LDS is handed on when the wave ends
+  };
+  if (chunks > 0) each_chunk<L, false>(chunks, step);
   if (A.s_out != nullptr) store_state<KT>(S, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g);
 }
 
 // ---------------------------------------------------------------------------
 // From the last chunk to the first: the gradient G of the state behind each chunk, and dR.
 // ---------------------------------------------------------------------------
-template <typename T, int D1, int NW>
-struct RevLds {
-  static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C);
-  typedef Mat<C, D1, NI> MK;
-  typedef Mat<C, 16 * NW, NI> MV;
-  static constexpr int k = 0, q = k + MK::kAll, v = q + MK::kAll, t = v + MV::kAll, p = t + 3 * NB * 1024, w = p + 3 * NB * 1024, all = w + kScanVecs * C * 4;
-};
-
-template <typename T, int D1, int NW, bool VEC>
-__global__ __launch_bounds__(64 * NW) void k_delta_rev(Args A) {
-  typedef RevLds<T, D1, NW> L;
-  constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, NB = L::NB, NTH = 64 * NW, VC = 16 * NW;
+template <typename T, int D1, int NW, bool VEC, bool DIRECT>
+__global__ __launch_bounds__((Chunks<T, D1, NW, 3, DIRECT>::kThreads)) void k_delta_rev(Args A) {
+  typedef Chunks<T, D1, NW, 3, DIRECT> L;
+  constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, VC = 16 * NW;
   typedef typename L::MK MK;
   typedef typename L::MV MV;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const int bh = blockIdx.x, col0 = blockIdx.y * VC, n = length_of(A, bh), c0 = col0 + 16 * wave;
+  const int bh = blockIdx.x, col0 = blockIdx.y * VC, n = length_of(A, bh), c0 = col0 + 16 * wave, chunks = (n + C - 1) / C;
   const Lane l{lane & 15, lane >> 4};
-  const Rows xk = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), xq = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk),
-             xo = rows_at<T>(A.dOut, A, bh, A.dv, n, col0, min(A.dv - col0, VC));
+  if (wave >= NW) {
+    const Rows xk = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), xq = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk),
+               xo = rows_at<T>(A.dOut, A, bh, A.dv, n, col0, min(A.dv - col0, VC));
+    if (chunks > 0) load_chunks<L, T, D1, 3, VEC, DIRECT, true>(A, bh, xk, xq, xo, n, tid - 64 * NW);
+    return;
+  }
   f32x4 G[KT];
 #pragma unroll
   for (int kt = 0; kt < KT; ++kt) G[kt] = zero4();
   if (A.s_in != nullptr) load_state<KT, true>(G, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g);
-  Load<T, C, D1, NTH, VEC> lk, lq;
-  Load<T, C, VC, NTH, VEC> lo;
-  LoadTri<NB, 3, NTH> lt, lp;
-  f32x4 lw;
-  const auto fetch_rows = [&](int c) {
-    const int r0 = c * C, nr = min(C, n - r0);
-    lk.load(xk, r0, nr, tid);
-    lq.load(xq, r0, nr, tid);
-  };
-  const auto fetch_rest = [&](int c) {
-    const long long own = chunk_at(A, bh, c);
-    lo.load(xo, c * C, min(C, n - c * C), tid);
-    lt.load(A.trit + own * (3 * NB * 64), tid);
-    lp.load(A.pri + own * (3 * NB * 64), tid);
-    if (tid < C) lw = reinterpret_cast<const f32x4*>(A.vec + own * (kVecs * C))[tid];
-  };
-  const int chunks = (n + C - 1) / C;
-  if (chunks > 0) {
-    fetch_rows(chunks - 1);
-    fetch_rest(chunks - 1);
-  }
-  for (int c = chunks - 1; c >= 0; --c) {
-    lds_barrier();
-    lk.template store<MK>(L::k, tid);
-    lq.template store<MK>(L::q, tid);
-    lo.template store<MV>(L::v, tid);
-    lt.store(L::t, tid);
-    lp.store(L::p, tid);
-    if (tid < C) lds_put(L::w + 16 * tid, lw);
-    lds_barrier();
-    {
-      float* const to = A.dstates + chunk_at(A, bh, c) * ((long long)D1 * A.dvp) + c0 + l.i;
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) to[(long long)(16 * kt + 4 * l.g + j) * A.dvp] = G[kt][j];
-    }
-    const int rb = MK::row_base(l), cb = MK::col_base(l), vb = MV::col_base(l);
+  const Bases<L> base(l, lane, wave);
+  const auto step = [&](int c, auto buffer_of) {
+    constexpr int buf = decltype(buffer_of)::value, tk = buf * MK::kAll, tq = base.kFar ? buf * MK::kAll : L::q + buf * MK::kAll, tv = buf * L::kV, tt = buf * L::kT, tp = buf * L::kP, tw = buf * L::kW;
+    const int rb = base.rows, cb = base.cols, qb = base.query_cols, vb = base.value, tb = base.tri, pb = base.weights, wb = base.vec;
+    put_columns<KT>(G, A.dstates + chunk_at(A, bh, c) * ((long long)D1 * A.dvp), D1, A.dvp, c0, l);
     f32x4 U[NT], R[NT];
 #pragma unroll
     for (int r = 0; r < NT; ++r) U[r] = R[r] = zero4();
@@ -468,54 +489,49 @@ __global__ __launch_bounds__(64 * NW) void k_delta_rev(Args A) {
     for (int s = 0; s < KS; ++s) {
       Planes<NI> k[NT];
 #pragma unroll
-      for (int r = 0; r < NT; ++r) k[r] = MK::row(L::k, rb, r, s);
+      for (int r = 0; r < NT; ++r) k[r] = MK::row(tk, rb, r, s);
       mma_rows<NI, 3>(k, split<3>(G[2 * s], G[2 * s + 1]), U);
     }
-    fetch_rows(max(c - 1, 0));
 #pragma unroll
-    for (int r = 0; r < NT; ++r) U[r] *= lds_get<f32x4>(L::w + 4 * (C + 16 * r + 4 * l.g));
+    for (int r = 0; r < NT; ++r) U[r] *= lds_get<f32x4>(wb + tw + 4 * (C + 16 * r));
     {
       Planes<NI> b[NS];
 #pragma unroll
-      for (int s = 0; s < NS; ++s) b[s] = MV::col(L::v, vb, wave, s);
-      mma_tri<C, false, false, 3, NI, 3>(L::p, lane, b, U);
+      for (int s = 0; s < NS; ++s) b[s] = MV::col(tv, vb, 0, s);
+      mma_tri<C, false, false, 3, NI, 3>(tp, pb, b, U);
     }
     {
       Planes<3> b[NS];
 #pragma unroll
       for (int s = 0; s < NS; ++s) b[s] = split<3>(U[2 * s], U[2 * s + 1]);
-      mma_tri<C, false, false, 3, 3, 3>(L::t, lane, b, R);
+      mma_tri<C, false, false, 3, 3, 3>(tt, tb, b, R);
     }
-    fetch_rest(max(c - 1, 0));
     {
-      const float Gamma = lds_get<float>(L::w + 4 * (3 * C));
+      const float Gamma = lds_get<float>(wb + tw + 4 * (3 * C));
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) G[kt] *= Gamma;
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
-        const f32x4 w0 = lds_get<f32x4>(L::w + 4 * (32 * s + 4 * l.g)), w1 = lds_get<f32x4>(L::w + 4 * (32 * s + 16 + 4 * l.g));
-        const f32x4 b0 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 4 * l.g)), b1 = lds_get<f32x4>(L::w + 4 * (2 * C + 32 * s + 16 + 4 * l.g));
+        const f32x4 w0 = lds_get<f32x4>(wb + tw + 4 * (32 * s)), w1 = lds_get<f32x4>(wb + tw + 4 * (32 * s + 16));
+        const f32x4 b0 = lds_get<f32x4>(wb + tw + 4 * (2 * C + 32 * s)), b1 = lds_get<f32x4>(wb + tw + 4 * (2 * C + 32 * s + 16));
         Planes<NI> x[KT];
         {
-          const Planes<3> o = split<3>(A.scale * w0 * MV::quad(L::v, vb, wave, 2 * s), A.scale * w1 * MV::quad(L::v, vb, wave, 2 * s + 1));
+          const Planes<3> o = split<3>(A.scale * w0 * MV::quad(tv, vb, 0, 2 * s), A.scale * w1 * MV::quad(tv, vb, 0, 2 * s + 1));
 #pragma unroll
-          for (int kt = 0; kt < KT; ++kt) x[kt] = MK::col(L::q, cb, kt, s);
+          for (int kt = 0; kt < KT; ++kt) x[kt] = MK::col(tq, qb, kt, s);
           mma_rows<NI, 3>(x, o, G);
         }
         const Planes<3> b = split<3>(-(w0 * b0) * R[2 * s], -(w1 * b1) * R[2 * s + 1]);
 #pragma unroll
-        for (int kt = 0; kt < KT; ++kt) x[kt] = MK::col(L::k, cb, kt, s);
+        for (int kt = 0; kt < KT; ++kt) x[kt] = MK::col(tk, cb, kt, s);
         mma_rows<NI, 3>(x, b, G);
       }
     }
     {
-      float* const to = A.dr + chunk_at(A, bh, c) * ((long long)C * A.dvp) + c0 + l.i;
-#pragma unroll
-      for (int r = 0; r < NT; ++r)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) to[(long long)(16 * r + 4 * l.g + j) * A.dvp] = R[r][j];
+      put_columns<NT>(R, A.dr + chunk_at(A, bh, c) * ((long long)C * A.dvp), C, A.dvp, c0, l);
     }
-  }
+  };
+  if (chunks > 0) each_chunk<L, true>(chunks, step);
   if (A.s_out != nullptr) store_state<KT>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g);
 }
 
@@ -546,44 +562,54 @@ static dark_status launch_prep(const Args& a, bool backward, hipStream_t st) {
   }
 }
 
+// Whether a call's rows fill the tiles of instances that take them straight to LDS.
+template <typename T, int D1>
+static bool direct_of(const Args& a) { return sizeof(T) == 2 && D1 <= 128 && a.dk == D1 && a.dv % 64 == 0; }
+
 template <typename T, int D1, int NW, bool VEC, bool FWD, bool DIRECT>
 static dark_status go_scan(const Args& a, hipStream_t st) {
-  constexpr int lds = ScanLds<T, D1, NW, FWD, DIRECT>::all;
-  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>, lds));
+  typedef Chunks<T, D1, NW, (FWD ? Kind<T>::kOut : 0), DIRECT> L;
+  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>, L::all));
   const int cols = FWD ? a.dv : a.dvp;
-  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(64 * NW), lds, a);
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(L::kThreads), L::all, a);
   return DARK_OK;
 }
-template <typename T, int D1>
-static dark_status go_scan(const Args& a, Pass pass, hipStream_t st) {
-  if constexpr (direct_of<T>(D1))
-    if (a.dk == D1 && a.dv % 64 == 0) return pass == kForward ? go_scan<T, D1, 4, true, true, true>(a, st) : go_scan<T, D1, 4, true, false, true>(a, st);
-  if (vec_of<T>(a)) return pass == kForward ? go_scan<T, D1, 4, true, true, false>(a, st) : go_scan<T, D1, 4, true, false, false>(a, st);
-  return pass == kForward ? go_scan<T, D1, 4, false, true, false>(a, st) : go_scan<T, D1, 4, false, false, false>(a, st);
+template <typename T, int D1, bool FWD>
+static dark_status go_scan(const Args& a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2 && D1 <= 128)
+    if (direct_of<T, D1>(a)) return go_scan<T, D1, 4, true, FWD, true>(a, st);
+  constexpr int NW = D1 > 128 ? 2 : 4;   // 256 rows of a state leave room for one wave a SIMD
+  return vec_of<T>(a) ? go_scan<T, D1, NW, true, FWD, false>(a, st) : go_scan<T, D1, NW, false, FWD, false>(a, st);
 }
 template <typename T>
 static dark_status launch_scan(const Args& a, Pass pass, hipStream_t st) {
   switch (inner_of(a.dk)) {
-    case 64: return go_scan<T, 64>(a, pass, st);
-    case 128: return go_scan<T, 128>(a, pass, st);
-    default: return go_scan<T, 256>(a, pass, st);
+    case 64: return pass == kForward ? go_scan<T, 64, true>(a, st) : go_scan<T, 64, false>(a, st);
+    case 128: return pass == kForward ? go_scan<T, 128, true>(a, st) : go_scan<T, 128, false>(a, st);
+    default: return pass == kForward ? go_scan<T, 256, true>(a, st) : go_scan<T, 256, false>(a, st);
   }
 }
 
-template <typename T, int D1, int NW, bool VEC>
+template <typename T, int D1, int NW, bool VEC, bool DIRECT>
 static dark_status go_rev(const Args& a, hipStream_t st) {
-  constexpr int lds = RevLds<T, D1, NW>::all;
-  DARK_TRY(allow_lds(k_delta_rev<T, D1, NW, VEC>, lds));
-  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_rev<T, D1, NW, VEC>), dim3(a.B * a.H, a.dvp / (16 * NW)), dim3(64 * NW), lds, a);
+  typedef Chunks<T, D1, NW, 3, DIRECT> L;
+  DARK_TRY(allow_lds(k_delta_rev<T, D1, NW, VEC, DIRECT>, L::all));
+  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_rev<T, D1, NW, VEC, DIRECT>), dim3(a.B * a.H, a.dvp / (16 * NW)), dim3(L::kThreads), L::all, a);
   return DARK_OK;
+}
+template <typename T, int D1>
+static dark_status go_rev(const Args& a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2 && D1 <= 128)
+    if (direct_of<T, D1>(a)) return go_rev<T, D1, 4, true, true>(a, st);
+  constexpr int NW = D1 > 128 ? 2 : 4;
+  return vec_of<T>(a) ? go_rev<T, D1, NW, true, false>(a, st) : go_rev<T, D1, NW, false, false>(a, st);
 }
 template <typename T>
 static dark_status launch_rev(const Args& a, hipStream_t st) {
-  const bool vec = vec_of<T>(a);
   switch (inner_of(a.dk)) {
-    case 64: return vec ? go_rev<T, 64, 4, true>(a, st) : go_rev<T, 64, 4, false>(a, st);
-    case 128: return vec ? go_rev<T, 128, 4, true>(a, st) : go_rev<T, 128, 4, false>(a, st);
-    default: return vec ? go_rev<T, 256, 4, true>(a, st) : go_rev<T, 256, 4, false>(a, st);
+    case 64: return go_rev<T, 64>(a, st);
+    case 128: return go_rev<T, 128>(a, st);
+    default: return go_rev<T, 256>(a, st);
   }
 }
 

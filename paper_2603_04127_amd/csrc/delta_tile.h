@@ -300,11 +300,11 @@ struct Tri {
 };
 // One plane of the blocks of step s.
 template <int C, bool LOWER>
-__device__ static inline void tri_plane(int tile, int lane, int s, int plane, u32x4 (&t)[C / 16]) {
+__device__ static inline void tri_plane(int tile, int base, int s, int plane, u32x4 (&t)[C / 16]) {
   typedef Tri<C, LOWER> X;
 #pragma unroll
   for (int r = 0; r < C / 16; ++r)
-    if (r >= X::first(s) && r <= X::last(s)) t[r] = lds_get<u32x4>(tile + (plane * blocks_of(C) + X::block(r, s)) * 1024 + 16 * lane);
+    if (r >= X::first(s) && r <= X::last(s)) t[r] = lds_get<u32x4>(base + tile + (plane * blocks_of(C) + X::block(r, s)) * 1024);
 }
 // x_r + the blocks' products with b, plane by plane of the triangle, the smallest first (TRANS: b on the left).
 template <int C, bool LOWER, bool TRANS, int MA, int MB, int N>
@@ -322,14 +322,14 @@ __device__ static inline void mma_step(const u32x4 (&t)[MA][C / 16], int s, cons
 
 // x_r + triangle . b (or b . triangle, TRANS): plane by plane of the triangle, the smallest first; a row's two blocks into sums of their own.
 template <int C, bool LOWER, bool TRANS, int MA, int MB, int NA, int NB_>
-__device__ static inline void mma_tri(int tile, int lane, const Planes<NB_> (&b)[C / 32], f32x4 (&x)[C / 16]) {
+__device__ static inline void mma_tri(int tile, int base, const Planes<NB_> (&b)[C / 32], f32x4 (&x)[C / 16]) {
   constexpr int NB = blocks_of(C);
   f32x4 more[2] = {zero4(), zero4()};
 #pragma unroll
   for (int i = MA - 1; i >= 0; --i) {
     u32x4 t[NB];
 #pragma unroll
-    for (int k = 0; k < NB; ++k) t[k] = lds_get<u32x4>(tile + i * NB * 1024 + k * 1024 + 16 * lane);
+    for (int k = 0; k < NB; ++k) t[k] = lds_get<u32x4>(base + tile + i * NB * 1024 + k * 1024);
 #pragma unroll
     for (int j = (MA > MB ? MA : MB) - 1 - i; j >= 0; --j) {
       if (j >= MB) continue;
