@@ -16,14 +16,16 @@ namespace delta {
 template <typename T, int D1>
 constexpr int prep_lds() {
   constexpr int C = Kind<T>::kChunk;
-  return 2 * Mat<C, D1, Kind<T>::kIn>::kAll + 3 * C * (C + 4) * 4 + kVecs * C * 4;
+  constexpr int tiles = 2 * Mat<C, D1, Kind<T>::kIn>::kAll, square = 4 * C * (C + 4);
+  return (tiles >= square ? tiles : tiles + square) + square + kVecs * C * 4;   // T in the place of K and Q where it fits
 }
 
 template <typename T, int D1, bool VEC, bool BWD>
 __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
   constexpr int C = Kind<T>::kChunk, NT = C / 16, NI = Kind<T>::kIn, NB = blocks_of(C), NTH = 256, S = C + 4;
   typedef Mat<C, D1, NI> M;
-  constexpr int tk = 0, tq = M::kAll, ta = 2 * M::kAll, tt = ta + 4 * C * S, tp = tt + 4 * C * S, tv = tp + 4 * C * S;
+  constexpr int tk = 0, tq = M::kAll, ta = 2 * M::kAll, tt = ta >= 4 * C * S ? 0 : ta + 4 * C * S, tv = tt == 0 ? ta + 4 * C * S : tt + 4 * C * S;
+  constexpr int NP = BWD ? 3 : Kind<T>::kOut;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const int bh = blockIdx.x / A.chunks, c = blockIdx.x % A.chunks, r0 = c * C, n = length_of(A, bh), nr = min(C, n - r0);
   if (nr <= 0) return;
@@ -67,33 +69,54 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
   const Lane l{lane & 15, lane >> 4};
   const int rb = M::row_base(l);
   const auto elem = [&](int base, int r, int col) { return base + 4 * (r * S + col); };
-  // tiles on and below the diagonal; those right of it that operands of 32 inner values take in are zero
-#pragma unroll 1
-  for (int t = wave; t < NT * (NT + 1) / 2 + NT / 2; t += 4) {
-    const bool above = t >= NT * (NT + 1) / 2;
-    const int u = t - NT * (NT + 1) / 2;
-    const int qt = above ? 2 * u : t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, kt = above ? 2 * u + 1 : t - qt * (qt + 1) / 2;
-    f32x4 kk = zero4(), qk = zero4();
-    if (!above) {
+  const long long own = chunk_at(A, bh, c);
+  // A block of P (P^T) as an operand takes two tiles, next to each other in its inner index: with that index along a lane's accumulators, they are
+  // the operand as they come.  Lane index i of tile `row`, accumulators of the tiles of step s; forward rows are tokens t, backward keys i.
+  const auto block = [&](int blk) {
+    const int row = C == 32 ? blk : !BWD ? (blk < 2 ? blk : blk < 4 ? 2 : 3) : blk < 4 ? blk >> 1 : blk - 2;
+    const int s = C == 32 ? 0 : !BWD ? (blk < 2 ? 0 : blk & 1) : blk < 4 ? blk & 1 : 1;
+    const int own_at = 16 * row + l.i;
+    const float hi = lds_get<float>(tv + 4 * (4 * C + own_at)), lo = lds_get<float>(tv + 4 * (5 * C + own_at));
+    f32x4 P[2];
 #pragma unroll
-      for (int s = 0; s < D1 / 32; ++s) {
-        const Planes<NI> b = M::row(tk, rb, kt, s);
-        kk = mma(M::row(tk, rb, qt, s), b, kk);
-        qk = mma(M::row(tq, rb, qt, s), b, qk);
+    for (int h = 0; h < 2; ++h) {
+      const int in = 2 * s + h, qt = BWD ? in : row, kt = BWD ? row : in;
+      P[h] = zero4();
+      if (kt > qt) continue;
+      f32x4 kk = zero4(), qk = zero4();
+#pragma unroll
+      for (int e = 0; e < D1 / 32; ++e) {
+        const Planes<NI> k = M::row(tk, rb, kt, e), kq = M::row(tk, rb, qt, e), q = M::row(tq, rb, qt, e);
+        kk = BWD ? mma(kq, k, kk) : mma(k, kq, kk);
+        qk = BWD ? mma(q, k, qk) : mma(k, q, qk);
       }
-    }
-    const int i = 16 * kt + l.i;
-    const float hi = lds_get<float>(tv + 4 * (4 * C + i)), lo = lds_get<float>(tv + 4 * (5 * C + i));
-    const f32x4 be = lds_get<f32x4>(tv + 4 * (2 * C + 16 * qt + 4 * l.g)), hs = lds_get<f32x4>(tv + 4 * (4 * C + 16 * qt + 4 * l.g)),
-                ls = lds_get<f32x4>(tv + 4 * (5 * C + 16 * qt + 4 * l.g));
+      const f32x4 his = lds_get<f32x4>(tv + 4 * (4 * C + 16 * in + 4 * l.g)), los = lds_get<f32x4>(tv + 4 * (5 * C + 16 * in + 4 * l.g));
+      const f32x4 bes = lds_get<f32x4>(tv + 4 * (2 * C + 16 * in + 4 * l.g));
+      const float be = lds_get<float>(tv + 4 * (2 * C + own_at));
+      f32x4 E;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int r = 16 * qt + 4 * l.g + j;
-      const float d = expf((hs[j] - hi) + (ls[j] - lo));
-      lds_put(elem(ta, r, i), r > i ? be[j] * d * kk[j] : 0.f);
-      lds_put(elem(tp, r, i), r >= i ? (BWD ? A.scale : 1.f) * d * qk[j] : 0.f);
-      if (above) lds_put(elem(tt, r, i), 0.f);
+      for (int j = 0; j < 4; ++j) {
+        const int in_at = 16 * in + 4 * l.g + j, t = BWD ? in_at : own_at, i = BWD ? own_at : in_at;
+        const float d = expf(BWD ? (his[j] - hi) + (los[j] - lo) : (hi - his[j]) + (lo - los[j]));
+        P[h][j] = t >= i ? (BWD ? A.scale : 1.f) * d * qk[j] : 0.f;
+        E[j] = t > i ? (BWD ? bes[j] : be) * d * kk[j] : 0.f;
+        if (BWD) lds_put(elem(ta, t, i), E[j]);
+      }
+      if (!BWD) lds_put(elem(ta, own_at, 16 * in + 4 * l.g), E);
     }
+    const Planes<NP> f = split<NP>(P[0], P[1]);
+#pragma unroll
+    for (int k = 0; k < NP; ++k) A.pri[(own * NP + k) * (NB * 64) + 64 * blk + lane] = f.p[k];
+  };
+  // blocks of one tile and of two: each wave two or three tiles
+  if (C == 32) {
+    if (wave < 2) block(wave);
+  } else if (BWD) {
+    block(wave == 0 ? 0 : wave == 1 ? 1 : wave == 2 ? 3 : 4);
+    if (wave >= 2) block(wave == 2 ? 2 : 5);
+  } else {
+    block(wave == 0 ? 4 : wave == 1 ? 5 : wave == 2 ? 2 : 1);
+    if (wave >= 2) block(wave == 2 ? 0 : 3);
   }
   __syncthreads();
   if (wave < NT) {
@@ -137,39 +160,27 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
     }
   }
   __syncthreads();
-  const long long own = chunk_at(A, bh, c);
-  constexpr int NP = BWD ? 3 : Kind<T>::kOut;
   for (int u = tid; u < NB * 64; u += NTH) {
     const int blk = u >> 6, i = u & 15, g = u >> 4 & 3;
     {
       const int r = C == 32 || blk < 2 ? blk : blk < 4 ? 2 : 3, s = C == 32 || blk < 2 ? 0 : blk & 1;
-      const int at = elem(0, 16 * r + i, 32 * s + 4 * g);
-      const Planes<3> t = split<3>(lds_get<f32x4>(tt + at), lds_get<f32x4>(tt + at + 64));
+      const int at = elem(tt, 16 * r + i, 32 * s + 4 * g);
+      const Planes<3> t = split<3>(lds_get<f32x4>(at), 2 * s + 1 <= r ? lds_get<f32x4>(at + 64) : zero4());   // nothing stands above the diagonal
 #pragma unroll
       for (int k = 0; k < 3; ++k) A.tri[(own * 3 + k) * (NB * 64) + u] = t.p[k];
-      if (!BWD) {
-        const Planes<NP> f = split<NP>(lds_get<f32x4>(tp + at), lds_get<f32x4>(tp + at + 64));
-#pragma unroll
-        for (int k = 0; k < NP; ++k) A.pri[(own * NP + k) * (NB * 64) + u] = f.p[k];
-      }
     }
     if (BWD) {
       const int r = C == 32 ? blk : blk < 4 ? blk >> 1 : blk - 2, s = C == 32 ? 0 : blk < 4 ? blk & 1 : 1;
-      f32x4 v[4];
+      f32x4 v[2] = {zero4(), zero4()};
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int at = elem(0, 32 * s + 4 * g + j, 16 * r + i);
-        v[0][j] = lds_get<float>(tt + at);
-        v[1][j] = lds_get<float>(tt + at + 64 * S);
-        v[2][j] = lds_get<float>(tp + at);
-        v[3][j] = lds_get<float>(tp + at + 64 * S);
+        const int at = elem(tt, 32 * s + 4 * g + j, 16 * r + i);
+        if (2 * s >= r) v[0][j] = lds_get<float>(at);
+        v[1][j] = lds_get<float>(at + 64 * S);
       }
-      const Planes<3> t = split<3>(v[0], v[1]), f = split<3>(v[2], v[3]);
+      const Planes<3> t = split<3>(v[0], v[1]);
 #pragma unroll
-      for (int k = 0; k < 3; ++k) {
-        A.trit[(own * 3 + k) * (NB * 64) + u] = t.p[k];
-        A.pri[(own * 3 + k) * (NB * 64) + u] = f.p[k];
-      }
+      for (int k = 0; k < 3; ++k) A.trit[(own * 3 + k) * (NB * 64) + u] = t.p[k];
     }
   }
 }

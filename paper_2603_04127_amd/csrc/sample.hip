@@ -4,10 +4,14 @@
 // those, the shortest beginning that holds top_p of their sum; and of those the ones with w_t >= min_p.  The token drawn is the first, in
 // the order of the tokens' numbers, behind which the kept weights add up to more than u times their sum.
 //
-// A workgroup takes a row.  What is kept but for min_p is a beginning of the order, so that two numbers say it: the last kept logit, and the last
-// kept token of that logit.  Small top_k: a bound from the threads' maxima leaves few candidates, which are sorted in LDS.  Else
-// a histogram of weights (in integers, whose sums have no order) over the logits finds the bin where the beginning ends, and the bin's
-// entries are sorted.  The draw sums the kept weights by waves, each of which holds a contiguous part of the row, and looks into one of them.
+// A workgroup takes a row, whose 16-byte pieces its threads hold where they have room for them.  What is kept but for min_p is a beginning of the
+// order, so that its last entry says it.  Small top_k: a bound from the threads' maxima leaves few candidates, which count those before them
+// and, kept, the weights of those with lower numbers: no further pass.  Else a histogram of weights over the logits finds the bin
+// where the beginning ends, and the bin's entries are sorted.  The draw sums the kept weights by waves, each of which holds a
+// contiguous part of the row, and looks into one of them.
+// Weights are in fp64, by a polynomial, to 2^-31 of their value, and so are their sums; a histogram's are integers, whose sums have no order.
+// In fp32 the borders between a large row's tokens would be off by some 2^-30 of the row's sum each, 2^17 of them together by 2^-13: one
+// row in 8000 would draw a token's neighbour.
 #include <cmath>
 
 #include "common.h"
@@ -24,7 +28,7 @@ constexpr int kHeld = 16;      // pieces of 16 bytes that a thread holds; longer
 constexpr int kBins = 2048;
 constexpr int kList = 2048;    // entries that are sorted
 constexpr int kSmall = 512;    // the largest top_k that goes by the threads' maxima
-constexpr float kLog2e = 1.4426950408889634f;
+constexpr int kCounted = 256;  // entries that count each other; more are sorted by merging
 
 // Monotone in the value for everything but NaN; 0 is below every value.
 __device__ __forceinline__ unsigned ordered(float v) {
@@ -45,8 +49,7 @@ template <typename T>
 struct Row {
   static constexpr int P = 16 / (int)sizeof(T);
   __amdgpu_buffer_rsrc_t at;
-  int begin, V, pieces;   // token of the row's first piece's first element (it may lie before the row); tokens; pieces of a wave, in 64s
-  bool held;
+  int begin, V, pieces;   // token of the row's first piece's first element (it may lie before the row); tokens; pieces of a thread
   u32x4 r[kHeld];
   __device__ u32x4 fetch(int piece) const {   // -infinity where there is no token
     u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(at, (unsigned)piece * 16u, 0, 0);
@@ -67,44 +70,60 @@ struct Row {
   }
   __device__ int piece(int wave, int lane, int i) const { return (wave * pieces + i) * 64 + lane; }
   __device__ void load(int wave, int lane) {
-    held = pieces <= kHeld;
-    if (held) {
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i) r[i] = i < pieces ? fetch(piece(wave, lane, i)) : u32x4{0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u};
-    }
+    for (int i = 0; i < kHeld; ++i)
+      if (i < pieces) r[i] = fetch(piece(wave, lane, i));
   }
   __device__ static float value(u32x4 v, int j) {
     if constexpr (sizeof(T) == 2) return __uint_as_float(j & 1 ? v[j / 2] & 0xffff0000u : v[j / 2] << 16);
     else return __uint_as_float(v[j]);
   }
-  // the same without the held ones, for what is rarely needed: less code
+  __device__ static float largest(u32x4 v) {
+    float m = value(v, 0);
+#pragma unroll
+    for (int j = 1; j < P; ++j) m = fmaxf(m, value(v, j));
+    return m;
+  }
+  // f(element, token) for a piece's elements, in a loop: for what is rarely needed, or needs many registers
   template <typename F>
-  __device__ void again(int wave, int lane, const F& f) const {
+  __device__ static __forceinline__ void elements(u32x4 v, int t, const F& f) {
 #pragma unroll 1
-    for (int i = 0; i < pieces; ++i) f(fetch(piece(wave, lane, i)), begin + piece(wave, lane, i) * P);
+    for (int j = 0; j < P; ++j) {
+      f(value(v, 0), t + j);
+      if constexpr (sizeof(T) == 2) v = u32x4{v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+      else v = u32x4{v[1], v[2], v[3], 0};
+    }
   }
   // f(piece, its first token) for the thread's pieces
-  template <typename F>
-  __device__ void each(int wave, int lane, const F& f) const {
-    if (held) {
+  template <bool HELD, typename F>
+  __device__ __forceinline__ void each(int wave, int lane, const F& f) const {
+    if constexpr (HELD) {
 #pragma unroll
       for (int i = 0; i < kHeld; ++i)
         if (i < pieces) f(r[i], begin + piece(wave, lane, i) * P);
     } else {
-#pragma unroll 2
+#pragma unroll 1
       for (int i = 0; i < pieces; ++i) f(fetch(piece(wave, lane, i)), begin + piece(wave, lane, i) * P);
     }
   }
 };
 
-// exp((x - m) / T): the exponent (x - m) c, c = log2 e / T in two floats, keeps what its rounding leaves.
+// exp((x - m) / T) = 2^z: the sum of z^k ln 2^k / k! up to k = 8 for what rounding z leaves, at most 1/2: off by 2^-32.
 struct Weight {
-  float m, c, c2;
+  double m, c;     // c = log2 e / T
+  float top;
   bool infinite;   // the largest logit is infinite: those that are share everything
-  __device__ float operator()(float x) const {
-    if (infinite) return x == INFINITY ? 1.f : 0.f;
-    const float d = x - m, e = d * c, more = fmaf(d, c, -e) + d * c2, w = __builtin_amdgcn_exp2f(e);
-    return e >= -125.f ? fmaf(w, more * 0.69314718f, w) : 0.f;   // also where x is NaN or -infinity
+  __device__ __forceinline__ double operator()(float x) const {
+    const double z = infinite ? (x == INFINITY ? 0.0 : -2000.0) : ((double)x - m) * c, n = rint(z), f = z - n;
+    double y = fma(f, 1.3215486790144309e-6, 1.5252733804059841e-5);
+    y = fma(f, y, 1.5403530393381609e-4);
+    y = fma(f, y, 1.3333558146428443e-3);
+    y = fma(f, y, 9.6181291076284772e-3);
+    y = fma(f, y, 5.5504108664821580e-2);
+    y = fma(f, y, 2.4022650695910071e-1);
+    y = fma(f, y, 6.9314718055994531e-1);
+    y = fma(f, y, 1.0);
+    return z > -1000.0 ? ldexp(y, (int)n) : 0.0;   // also where x is NaN or -infinity
   }
 };
 
@@ -135,22 +154,31 @@ __device__ __forceinline__ float logit_of(u64 e) { return value_of((unsigned)(e 
 __device__ __forceinline__ int token_of(u64 e) { return (int)~(unsigned)e; }
 
 struct Shared {
-  u64 list[kList];
+  u64 list[kList], sorted[kCounted];
   u64 mass[kBins];
   unsigned count[kBins];
-  double sums[kWaves];
-  double scan[kWaves];
+  double sums[kWaves], scan[kWaves], weights[kSmall];
   float tops[kThreads];
   u64 bound;         // the last entry that is kept
   u64 before;        // weight of the bins before the chosen one
-  int ranks_before, bin, size;
-  unsigned lo, hi;
-  double total;
+  int ranks_before, bin, size, kept;
+  unsigned lo;
 };
 
-// The first n entries of the list in descending order; the others are 0.
+// The list's first n entries in descending order.
 __device__ __forceinline__ void sort(Shared& s, int n, int tid) {
-  int size = 64;
+  if (n <= kCounted) {
+    const u64 own = tid < n ? s.list[tid] : 0;
+    int before = 0;
+    if (tid < n)
+#pragma unroll 4
+      for (int i = 0; i < n; ++i) before += s.list[i] > own;
+    __syncthreads();
+    if (tid < n) s.list[before] = own;   // entries are distinct
+    __syncthreads();
+    return;
+  }
+  int size = kCounted;
   while (size < n) size *= 2;
   for (int i = tid; i < size; i += kThreads)
     if (i >= n) s.list[i] = 0;
@@ -169,7 +197,7 @@ __device__ __forceinline__ void sort(Shared& s, int n, int tid) {
     }
 }
 
-template <typename T>
+template <typename T, bool HELD>
 __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logits, const float* __restrict__ uniform, Setting set,
                                                      int32_t* __restrict__ out_token, float* __restrict__ out_logprob, int V) {
   __shared__ Shared s;
@@ -184,16 +212,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     row.at = __builtin_amdgcn_make_buffer_rsrc(const_cast<T*>(logits + base), 0, (int)((bytes + 3) & ~3LL), 0x00027000);
     row.begin = (int)(base - first);
     row.V = V;
-    const long long all = (first + V - base + P - 1) / P;
-    row.pieces = (int)((all + kThreads - 1) / kThreads);
+    const int all = (int)((first + V - base + P - 1) / P);
+    row.pieces = (all + kThreads - 1) / kThreads;
   }
-  row.load(wave, lane);
+  if (HELD) row.load(wave, lane);
   // the largest logit, of every thread and of all
   float mine = -INFINITY;
-  row.each(wave, lane, [&](u32x4 v, int) {
-#pragma unroll
-    for (int j = 0; j < P; ++j) mine = fmaxf(mine, Row<T>::value(v, j));   // of a NaN and a number: the number
-  });
+  row.template each<HELD>(wave, lane, [&](u32x4 v, int) { mine = fmaxf(mine, Row<T>::largest(v)); });   // of a NaN and a number: the number
   s.tops[tid] = mine;
   __syncthreads();
   float top = -INFINITY;
@@ -208,32 +233,28 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     return;
   }
   const float temp = set.temperature != nullptr ? set.temperature[b] : set.T;
-  const bool greedy = !(temp > 0.f);
   int k = set.top_k != nullptr ? set.top_k[b] : set.k;
   float p = set.top_p != nullptr ? set.top_p[b] : set.p, q = set.min_p != nullptr ? set.min_p[b] : set.q, u = uniform != nullptr ? uniform[b] : 0.f;
   Weight weight;
   weight.m = top;
   weight.infinite = top == INFINITY;
-  {
-    const double c = greedy ? 1.0 : 1.4426950408889634 / (double)temp;
-    weight.c = (float)fmin(c, 3e38);
-    weight.c2 = c < 3e38 ? (float)(c - (double)weight.c) : 0.f;
+  weight.c = fmin(1.4426950408889634 / (double)temp, 1e300);
+  if (!(temp > 0.f)) {   // the largest logit
+    weight.c = 1.0;
+    k = 1;
+    p = 1.f;
   }
-  if (greedy) k = 1, p = 1.f, q = 0.f;
   q = q > 0.f ? fminf(q, 1.f) : 0.f;
+  u = u > 0.f ? u : 0.f;
   if (k <= 0 || k >= V) k = 0;
   const bool by_p = p < 1.f;
   if (!(p > 0.f)) p = by_p ? 0.f : 1.f;
   u64 bound = 0;   // entries from this one on are kept
-  const float high = (float)(1u << (__builtin_clz((unsigned)V) - 2));   // 2^-32 of a weight's unit: V of them stay below 2^62
-  const auto integer = [&](float w) -> u64 {   // w unit, in two halves
-    const float a = w * high;
-    const unsigned h = (unsigned)a;
-    return (u64)h << 32 | (unsigned)((a - (float)h) * 4294967296.f);
-  };
+  const double unit = (double)(1ull << (__builtin_clz((unsigned)V) + 19));   // of an integer weight: V of them stay below 2^51
+  const auto integer = [&](double w) -> u64 { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; };
 
   // The list holds all entries of a part of the order, sorted, behind `rank` entries of weight `held`: the last that is kept of them, by rank
-  // (k > 0) or by weight (target), and the weight up to it.  By one wave.
+  // or by weight (target), and the weight up to it.  By one wave.
   const auto last_of = [&](int n, int rank, u64 held, bool by_rank, int most, u64 target, u64* upto) -> u64 {
     u64 found = 0, sum = held;
     for (int i0 = 0; i0 < n; i0 += 64) {
@@ -246,6 +267,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         const int last = 63 - __builtin_clzll(kept);
         found = __shfl(e, last, 64);
         *upto = __shfl(up, last, 64);
+        if (lane == 0) s.kept = i0 + last + 1;
       }
       sum = __shfl(up, 63, 64);
     }
@@ -255,15 +277,19 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     const int at = atomicAdd(&s.size, 1);
     if (at < kList) s.list[at] = entry(x, t);
   };
+  const auto finish = [&](int token, double w, double all) {
+    out_token[b] = token;
+    if (out_logprob != nullptr) out_logprob[b] = (float)log(w / all);
+  };
 
   bool done = k == 0 && !by_p;
   if (!done && k > 0 && k <= kSmall) {
-    // The k-th largest of the threads' maxima is at most the k-th largest logit: bisection over the 32 bits of its order, by one wave.
+    // The k-th largest of the threads' maxima is at most the k-th largest logit: its first bits, by one wave.
     if (wave == 0) {
       unsigned key[kThreads / 64], cut = 0;
 #pragma unroll
       for (int i = 0; i < kThreads / 64; ++i) key[i] = ordered(s.tops[i * 64 + lane]);
-      for (int bit = 31; bit >= (sizeof(T) == 2 ? 16 : 8); --bit) {
+      for (int bit = 31; bit >= 16; --bit) {
         const unsigned next = cut | 1u << bit;
         int n = 0;
 #pragma unroll
@@ -275,10 +301,11 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     }
     __syncthreads();
     const float least = value_of(s.lo);
-    row.each(wave, lane, [&](u32x4 v, int t) {
-#pragma unroll
-      for (int j = 0; j < P; ++j)
-        if (Row<T>::value(v, j) >= least) append(Row<T>::value(v, j), t + j);
+    row.template each<HELD>(wave, lane, [&](u32x4 v, int t) {
+      if (Row<T>::largest(v) >= least)
+        Row<T>::elements(v, t, [&](float x, int tk) {
+          if (x >= least) append(x, tk);
+        });
     });
     __syncthreads();
     const int n = s.size;
@@ -290,6 +317,52 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         if (lane == 0) s.bound = e;
       }
       __syncthreads();
+      const int m = s.kept;
+      if (m <= kSmall) {
+        // every kept entry adds up those with lower numbers
+        double w = 0.0;
+        if (tid < m) {
+          w = weight(logit_of(s.list[tid]));
+          w = w >= (double)q ? w : 0.0;
+          s.weights[tid] = w;
+        }
+        __syncthreads();
+        double before = 0.0;
+        if (tid < m) {
+          const int own = token_of(s.list[tid]);
+          for (int i = 0; i < m; ++i) before += token_of(s.list[i]) < own ? s.weights[i] : 0.0;
+        }
+        __syncthreads();
+        if (tid < m) s.weights[tid] = before;
+        __syncthreads();
+        if (wave == 0) {
+          double all = 0.0;
+          for (int i0 = 0; i0 < m; i0 += 64) {
+            const double x = i0 + lane < m ? weight(logit_of(s.list[i0 + lane])) : 0.0;
+            all += x >= (double)q ? x : 0.0;
+          }
+          all = wave_sum(all);
+          // the kept entry with the highest number whose sum before it does not exceed u of them all
+          const double target = (double)u * all;
+          int best = -1;
+          float logit = 0.f;
+          for (int i0 = 0; i0 < m; i0 += 64) {
+            if (i0 + lane < m) {
+              const u64 e = s.list[i0 + lane];
+              const double x = weight(logit_of(e));
+              if (x >= (double)q && x > 0.0 && s.weights[i0 + lane] <= target && token_of(e) > best) best = token_of(e), logit = logit_of(e);
+            }
+          }
+#pragma unroll
+          for (int o = 32; o > 0; o >>= 1) {
+            const int t = __shfl_xor(best, o, 64);
+            const float x = __shfl_xor(logit, o, 64);
+            if (t > best) best = t, logit = x;
+          }
+          if (lane == 0) finish(best, weight(logit), all);
+        }
+        return;
+      }
       bound = s.bound;
       done = true;
     }
@@ -297,12 +370,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   }
   if (!done) {
     // Bins over the logits from the largest down, as far as weights matter beside 1 - top_p of the sum (and further for top_k).
-    const float reach = (logf((float)V) + (by_p ? fmaxf(-logf(1.f - p), 0.f) : 0.f) + 3.f) * 1.4426950408889634f / fmaxf(weight.c, 1e-30f);
+    const float reach = (logf((float)V) + (by_p ? fmaxf(-logf(1.f - p), 0.f) : 0.f) + 3.f) * 1.4426950408889634f / (float)fmin(fmax(weight.c, 1e-30), 1e30);
     const float step = fminf((float)(kBins - 1) / reach, 1e30f);
-    const auto bin_of = [&](float x) -> int { return weight.infinite ? (x == INFINITY ? 0 : kBins - 1) : (int)fminf((weight.m - x) * step, (float)(kBins - 1)); };
+    const auto bin_of = [&](float x) -> int { return weight.infinite ? (x == INFINITY ? 0 : kBins - 1) : (int)fminf((top - x) * step, (float)(kBins - 1)); };
     for (int i = tid; i < kBins; i += kThreads) s.mass[i] = 0, s.count[i] = 0;
     __syncthreads();
-    row.each(wave, lane, [&](u32x4 v, int) {
+    row.template each<HELD>(wave, lane, [&](u32x4 v, int) {
 #pragma unroll
       for (int j = 0; j < P; ++j) {
         const float x = Row<T>::value(v, j);
@@ -311,6 +384,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
           atomicAdd(&s.mass[at], integer(weight(x)));
           atomicAdd(&s.count[at], 1u);
         }
+        __builtin_amdgcn_sched_barrier(0);
       }
     });
     __syncthreads();
@@ -360,18 +434,16 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         if (tid == 0) s.list[0] = ~0ull, s.list[1] = 0;
         __syncthreads();
         u64 least = ~0ull, most_e = 0;
-        row.again(wave, lane, [&](u32x4 v, int t) {
-#pragma unroll
-          for (int j = 0; j < P; ++j) {
-            const float x = Row<T>::value(v, j);
+        row.template each<false>(wave, lane, [&](u32x4 v, int t) {
+          Row<T>::elements(v, t, [&](float x, int tk) {
             if (x > -INFINITY && bin_of(x) == bin) {
-              const u64 e = entry(x, t + j);
+              const u64 e = entry(x, tk);
               if (e >= lo && e <= hi) {
                 least = e < least ? e : least;
                 most_e = e > most_e ? e : most_e;
               }
             }
-          }
+          });
         });
         atomicMin(&s.list[0], least);
         atomicMax(&s.list[1], most_e);
@@ -384,19 +456,17 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         const u64 before = s.before;
         const int ranks = s.ranks_before;
         __syncthreads();
-        row.again(wave, lane, [&](u32x4 v, int t) {
-#pragma unroll
-          for (int j = 0; j < P; ++j) {
-            const float x = Row<T>::value(v, j);
+        row.template each<false>(wave, lane, [&](u32x4 v, int t) {
+          Row<T>::elements(v, t, [&](float x, int tk) {
             if (x > -INFINITY && bin_of(x) == bin) {
-              const u64 e = entry(x, t + j);
+              const u64 e = entry(x, tk);
               if (e >= lo && e <= hi) {
                 const int at = (int)((hi - e) >> shift);
                 atomicAdd(&s.mass[at], integer(weight(x)));
                 atomicAdd(&s.count[at], 1u);
               }
             }
-          }
+          });
         });
         __syncthreads();
         choose(by_rank, most - ranks, target > before ? target - before : 0);
@@ -409,15 +479,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         if (tid == 0) s.before += before, s.ranks_before += ranks;
         __syncthreads();
       }
-      row.each(wave, lane, [&](u32x4 v, int t) {
-#pragma unroll
-        for (int j = 0; j < P; ++j) {
-          const float x = Row<T>::value(v, j);
+      row.template each<HELD>(wave, lane, [&](u32x4 v, int t) {
+          Row<T>::elements(v, t, [&](float x, int tk) {
           if (x > -INFINITY && bin_of(x) == bin) {
-            const u64 e = entry(x, t + j);
-            if (e >= lo && e <= hi) append(x, t + j);
+            const u64 e = entry(x, tk);
+            if (e >= lo && e <= hi) append(x, tk);
           }
-        }
+        });
       });
       __syncthreads();
       sort(s, n, tid);
@@ -441,15 +509,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       if (by_p) {   // the histogram anew: gathering may have used it, and what top_k leaves out counts no more
         for (int i = tid; i < kBins; i += kThreads) s.mass[i] = 0, s.count[i] = 0;
         __syncthreads();
-        row.again(wave, lane, [&](u32x4 v, int t) {
-#pragma unroll
-          for (int j = 0; j < P; ++j) {
-            const float x = Row<T>::value(v, j);
-            if (x > -INFINITY && entry(x, t + j) >= bound) {
+        row.template each<false>(wave, lane, [&](u32x4 v, int t) {
+          Row<T>::elements(v, t, [&](float x, int tk) {
+            if (x > -INFINITY && entry(x, tk) >= bound) {
               atomicAdd(&s.mass[bin_of(x)], integer(weight(x)));
               atomicAdd(&s.count[bin_of(x)], 1u);
             }
-          }
+          });
         });
         __syncthreads();
       }
@@ -469,26 +535,32 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   // ---------------------------------------------------------------------------
   // The draw: sums of the kept weights, of each wave's part of the row, then of a sixteenth of one part by each wave.
   // ---------------------------------------------------------------------------
-  const auto kept = [&](float x, int t) -> float {
-    const float w = weight(x);
-    return x > -INFINITY && w >= q && (bound == 0 || entry(x, t) >= bound) ? w : 0.f;
+  const float last_logit = bound != 0 ? logit_of(bound) : -3.402823466e38f;
+  const int last_token = bound != 0 ? token_of(bound) : 0x7fffffff;
+  const auto kept = [&](float x, int t) -> double {
+    const double w = weight(x);
+    return (x > last_logit || (x == last_logit && t <= last_token)) && w >= (double)q ? w : 0.0;
   };
-  const auto sum_of = [&](u32x4 v, int t) -> float {
-    float w = 0.f;
+  const auto sum_of = [&](u32x4 v, int t) -> double {
+    double w = 0.0;
+    if (Row<T>::largest(v) >= last_logit) {
 #pragma unroll
-    for (int j = 0; j < P; ++j) w += kept(Row<T>::value(v, j), t + j);
+      for (int j = 0; j < P; ++j) {
+        w += kept(Row<T>::value(v, j), t + j);
+        __builtin_amdgcn_sched_barrier(0);   // one after the other: eight polynomials at once do not fit the registers, and four waves a SIMD wait for none
+      }
+    }
     return w;
   };
   double sum = 0.0;
-  row.each(wave, lane, [&](u32x4 v, int t) { sum += (double)sum_of(v, t); });
+  row.template each<HELD>(wave, lane, [&](u32x4 v, int t) { sum += sum_of(v, t); });
   sum = wave_sum(sum);
   if (lane == 0) s.sums[wave] = sum;
   __syncthreads();
   double all = 0.0;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) all += s.sums[i];
-  const float uu = u > 0.f ? u : 0.f;
-  double rest = (greedy ? 0.0 : (double)uu) * all;
+  double rest = (double)u * all;
   // the part: the first behind which the sums exceed `rest`; with a random number of 1 or more the last that holds anything
   const auto locate = [&](const double* sums, double& rest) -> int {
     int part = -1;
@@ -505,7 +577,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   sum = 0.0;
   for (int i = begin; i < end; ++i) {
     const int piece = row.piece(part, lane, i);
-    sum += (double)sum_of(row.fetch(piece), row.begin + piece * P);
+    sum += sum_of(row.fetch(piece), row.begin + piece * P);
   }
   sum = wave_sum(sum);
   if (lane == 0) s.scan[wave] = sum;
@@ -514,34 +586,30 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   if (wave != sub) return;
   // 64 pieces at a time: the last with a weight whose sums before it do not exceed `rest`
   int token = -1;
-  float chosen = 0.f;
+  double chosen = 0.0;
   for (int i = begin; i < end; ++i) {
     const int piece = row.piece(part, lane, i);
     const u32x4 v = row.fetch(piece);
     const int t = row.begin + piece * P;
-    const double w = (double)sum_of(v, t);
+    const double w = sum_of(v, t);
     const double upto = wave_prefix(w, lane), before = upto - w;
     const u64 some = __ballot(w > 0.0), reach = __ballot(w > 0.0 && rest < upto);
     if (some == 0) continue;
     const int who = reach != 0 ? __builtin_ctzll(reach) : 63 - __builtin_clzll(some);
     int tk = -1;
-    float wt = 0.f;
-    double left = rest - before;
+    double wt = 0.0, left = rest - before;
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-      const float x = kept(Row<T>::value(v, j), t + j);
-      if (x > 0.f && (tk < 0 || left >= 0.0)) tk = t + j, wt = x;
-      left -= (double)x;
+      const double x = kept(Row<T>::value(v, j), t + j);
+      if (x > 0.0 && (tk < 0 || left >= 0.0)) tk = t + j, wt = x;
+      left -= x;
     }
     token = __shfl(tk, who, 64);
     chosen = __shfl(wt, who, 64);
     if (reach != 0) break;
     rest -= __shfl(upto, 63, 64);
   }
-  if (lane == 0) {
-    out_token[b] = token;
-    if (out_logprob != nullptr) out_logprob[b] = greedy ? 0.f : (float)log((double)chosen / all);
-  }
+  if (lane == 0) finish(token, chosen, all);
 }
 
 dark_status check(const dark_sample_params* p) {
@@ -576,13 +644,17 @@ dark_status dark_sample(const dark_sample_params* p, const void* logits, const f
     return DARK_EINVAL;
   const sample::Setting set{temperature, top_p, min_p, top_k, p->temperature, p->top_p, p->min_p, p->top_k};
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  // whether a thread holds its pieces (a row may begin up to a piece before its first element)
+  const bool held = false && ((long long)p->V * (p->io_dtype == DARK_BF16 ? 2 : 4) + 32) / 16 <= (long long)sample::kThreads * sample::kHeld;
+#define DARK_SAMPLE(T)                                                                                                              \
+  if (held) DARK_LAUNCH(KID_SAMPLE, st, (sample::k_sample<T, true>), dim3(p->B), dim3(sample::kThreads), 0, static_cast<const T*>(logits), uniform, set, out_token, out_logprob, p->V); \
+  else DARK_LAUNCH(KID_SAMPLE, st, (sample::k_sample<T, false>), dim3(p->B), dim3(sample::kThreads), 0, static_cast<const T*>(logits), uniform, set, out_token, out_logprob, p->V)
   if (p->io_dtype == DARK_BF16) {
-    DARK_LAUNCH(KID_SAMPLE, st, sample::k_sample<unsigned short>, dim3(p->B), dim3(sample::kThreads), 0, static_cast<const unsigned short*>(logits),
-                uniform, set, out_token, out_logprob, p->V);
+    DARK_SAMPLE(unsigned short);
   } else {
-    DARK_LAUNCH(KID_SAMPLE, st, sample::k_sample<float>, dim3(p->B), dim3(sample::kThreads), 0, static_cast<const float*>(logits), uniform,
-                set, out_token, out_logprob, p->V);
+    DARK_SAMPLE(float);
   }
+#undef DARK_SAMPLE
   return DARK_OK;
 }
 
