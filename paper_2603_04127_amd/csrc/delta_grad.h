@@ -12,6 +12,7 @@ constexpr int kBlock = 64;
 template <typename T, int D1>
 struct GradLds {
   static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NP = Kind<T>::kOut;
+  static constexpr int NW = D1 == 64 ? 4 : 8;   // waves
   typedef Mat<C, D1, NI> MK;
   typedef Mat<C, kBlock, NI> MO;
   typedef Mat<C, kBlock, 3> MU;
@@ -22,9 +23,9 @@ struct GradLds {
   static constexpr int cross = w + kVecs * C * 4;           // [C / 16][C]
   static constexpr int third = cross + (C / 16) * C * 4;    // [C]
   static constexpr int vdot = third + C * 4;                // [C]
-  static constexpr int dots = vdot + C * 4;                 // [4][4][C]
-  static constexpr int total = dots + 16 * C * 4;           // [4]
-  static constexpr int all = total + 16;
+  static constexpr int dots = vdot + C * 4;                 // [NW][3][C]
+  static constexpr int total = dots + 3 * NW * C * 4;       // [NW]
+  static constexpr int all = total + 4 * NW;
 };
 
 // Sums over the lanes of a row of 16 up to each of them.
@@ -36,13 +37,13 @@ __device__ static inline float row16_prefix(float v) {
   return v;
 }
 
-// A chunk by four waves: each computes its share of the dk columns of dQ and dK, transposed, so that a lane has four neighbouring columns of
+// A chunk by four or eight waves, two a SIMD: each computes its share of the dk columns of dQ and dK, transposed, so that a lane has four neighbouring columns of
 // a row.  The products with the states go over their dv columns in blocks; the states' operands come straight from memory, since
 // no two waves need the same rows of them.
 template <typename T, int D1, bool VEC>
-__global__ __launch_bounds__(256) void k_delta_grad(Args A) {
+__global__ __launch_bounds__((64 * GradLds<T, D1>::NW), 2) void k_delta_grad(Args A) {
   typedef GradLds<T, D1> L;
-  constexpr int C = L::C, NT = C / 16, NI = L::NI, NTH = 256, DT = D1 / 64, NP = L::NP;
+  constexpr int C = L::C, NT = C / 16, NI = L::NI, NW = L::NW, NTH = 64 * NW, DT = D1 / 16 / NW, NP = L::NP;
   typedef typename L::MK MK;
   typedef typename L::MO MO;
   typedef typename L::MU MU;
@@ -86,7 +87,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
 #pragma unroll
   for (int r = 0; r < NT; ++r) N[r] = F[r] = zero4();
   float sg = 0.f;                                   // <S, dS'>
-  constexpr int kUnits = C * kBlock / 8, kEach = kUnits / NTH;
+  constexpr int kUnits = C * kBlock / 8, kEach = (kUnits + NTH - 1) / NTH;   // C = 32: units for half of eight waves
   float vdot[kEach];
 #pragma unroll
   for (int e = 0; e < kEach; ++e) vdot[e] = 0.f;
@@ -101,6 +102,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int x = tid + e * NTH, at = (x / 8) * A.dvp + b0 + (x % 8) * 8;
+      if (kUnits % NTH != 0 && x >= kUnits) break;
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         u[e][k] = *reinterpret_cast<const f32x4*>(us + at + 4 * k);
@@ -112,6 +114,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
 #pragma unroll
     for (int e = 0; e < kEach; ++e) {
       const int x = tid + e * NTH, row = x / 8;
+      if (kUnits % NTH != 0 && x >= kUnits) break;
       MU::put8(L::u, row, x % 8, split<3>(u[e][0], u[e][1]));
       MU::put8(L::d, row, x % 8, split<3>(d[e][0], d[e][1]));
       // dR . v, and dV = beta dR
@@ -180,7 +183,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
     v += __shfl_xor(v, 1, 64);
     v += __shfl_xor(v, 2, 64);
     v += __shfl_xor(v, 4, 64);
-    if ((tid & 7) == 0) lds_put(L::vdot + 4 * ((tid + e * NTH) / 8), v);
+    if ((tid & 7) == 0 && (kUnits % NTH == 0 || tid + e * NTH < kUnits)) lds_put(L::vdot + 4 * ((tid + e * NTH) / 8), v);
   }
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) sg += __shfl_xor(sg, o, 64);
@@ -268,9 +271,9 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
     d1 += xor32(d1);
     d2 += xor32(d2);
     if (l.g == 0) {
-      lds_put(L::dots + 4 * ((wave * 4 + 0) * C + 16 * r + l.i), dq);
-      lds_put(L::dots + 4 * ((wave * 4 + 1) * C + 16 * r + l.i), d1);
-      lds_put(L::dots + 4 * ((wave * 4 + 2) * C + 16 * r + l.i), d2);
+      lds_put(L::dots + 4 * ((wave * 3 + 0) * C + 16 * r + l.i), dq);
+      lds_put(L::dots + 4 * ((wave * 3 + 1) * C + 16 * r + l.i), d1);
+      lds_put(L::dots + 4 * ((wave * 3 + 2) * C + 16 * r + l.i), d2);
     }
   }
   __syncthreads();
@@ -312,10 +315,10 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
   if (wave == 0 && (A.dgate != nullptr || A.dbeta != nullptr)) {
     const int t = lane < C ? lane : 0;
     double dq = 0.0, d1 = 0.0, d2 = 0.0, cross = 0.0;
-    for (int w = 0; w < 4; ++w) {
-      dq += lds_get<float>(L::dots + 4 * ((w * 4 + 0) * C + t));
-      d1 += lds_get<float>(L::dots + 4 * ((w * 4 + 1) * C + t));
-      d2 += lds_get<float>(L::dots + 4 * ((w * 4 + 2) * C + t));
+    for (int w = 0; w < NW; ++w) {
+      dq += lds_get<float>(L::dots + 4 * ((w * 3 + 0) * C + t));
+      d1 += lds_get<float>(L::dots + 4 * ((w * 3 + 1) * C + t));
+      d2 += lds_get<float>(L::dots + 4 * ((w * 3 + 2) * C + t));
       if (w < NT && t > 0) cross += lds_get<float>(L::cross + 4 * (w * C + t - 1));
     }
     // reads of the state by the rows from t on, what the keys before t leave in the next one, and the state that passes through
@@ -329,7 +332,7 @@ __global__ __launch_bounds__(256) void k_delta_grad(Args A) {
     left = __shfl_up(left, 1, 64);
     if (lane == 0) left = 0.0;
     double total = 0.0;
-    for (int w = 0; w < 4; ++w) total += lds_get<float>(L::total + 4 * w);
+    for (int w = 0; w < NW; ++w) total += lds_get<float>(L::total + 4 * w);
     const double gate = reads + left + cross + total * (double)lds_get<float>(L::w + 4 * (3 * C));
     if (lane < nr) {
       if (A.dgate != nullptr) A.dgate[gate_at(A, bh, r0 + lane)] = (float)gate;
@@ -342,7 +345,7 @@ template <typename T, int D1, bool VEC>
 static dark_status go_grad(const Args& a, hipStream_t st) {
   constexpr int lds = GradLds<T, D1>::all;
   DARK_TRY(allow_lds(k_delta_grad<T, D1, VEC>, lds));
-  DARK_LAUNCH(KID_DELTA_GRAD, st, (k_delta_grad<T, D1, VEC>), dim3((unsigned)(a.B * a.H * a.chunks)), dim3(256), lds, a);
+  DARK_LAUNCH(KID_DELTA_GRAD, st, (k_delta_grad<T, D1, VEC>), dim3((unsigned)(a.B * a.H * a.chunks)), dim3(64 * GradLds<T, D1>::NW), lds, a);
   return DARK_OK;
 }
 template <typename T>
