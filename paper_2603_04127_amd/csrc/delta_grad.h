@@ -140,8 +140,8 @@ __global__ __launch_bounds__((64 * GradLds<T, D1>::NW), 2) void k_delta_grad(Arg
       }
     }
     __syncthreads();
-#pragma unroll
-    for (int s = 0; s < kBlock / 32; ++s) {
+#pragma unroll 1
+    for (int s = 0; s < kBlock / 32; ++s) {   // one after the other: the registers of two steps are not there
       Planes<3> S[DT], G[DT];
 #pragma unroll
       for (int i = 0; i < DT; ++i) {
@@ -277,7 +277,7 @@ __global__ __launch_bounds__((64 * GradLds<T, D1>::NW), 2) void k_delta_grad(Arg
     }
   }
   __syncthreads();
-#pragma unroll
+#pragma unroll 1
   for (int s = 0; s < C / 32; ++s) {
 #pragma unroll
     for (int i = 0; i < DT; ++i) {
