@@ -193,8 +193,8 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
 // ---------------------------------------------------------------------------
 // A chunk's operands in LDS (NP: planes of P, 0: neither Q nor P), in one buffer or two.  An instruction's own offset reaches 64 KB: a lane has a
 // base for each operand, and the buffers lie beside each other.
-// DIRECT: bf16 rows that fill the tiles, by loads that end in LDS, issued by one wave; else four waves take them through registers.
-template <typename T, int D1, int NW, int NP, bool DIRECT>
+// Four waves take them there through registers (two beside 256 rows of a state).
+template <typename T, int D1, int NW, int NP>
 struct Chunks {
   static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C), VC = 16 * NW;
   typedef Mat<C, D1, NI> MK;
@@ -202,8 +202,7 @@ struct Chunks {
   static constexpr int kV = MV::kAll, kW = kScanVecs * C * 4, kT = 3 * NB * 1024, kP = NP * NB * 1024, kQ = NP > 0 ? MK::kAll : 0;   // bytes of each
   static constexpr int kBufs = 2 * (MK::kAll + kQ + kV + kW + kT + kP) <= 160 * 1024 ? 2 : 1;
   static constexpr int k = 0, q = k + kBufs * MK::kAll, v = q + kBufs * kQ, w = v + kBufs * kV, t = w + kBufs * kW, p = t + kBufs * kT, all = p + kBufs * kP;
-  static constexpr int kLoaders = DIRECT ? 1 : D1 > 128 ? 2 : 4, kThreads = 64 * (NW + kLoaders), NTH = 64 * kLoaders;
-  static_assert(!DIRECT || kBufs == 2, "loads that end in LDS go to the other buffer");
+  static constexpr int kLoaders = D1 > 128 ? 2 : 4, kThreads = 64 * (NW + kLoaders), NTH = 64 * kLoaders;
 };
 
 // A lane's bases.  The compiler is not to take them apart: it would hold one for every read behind the first 64 KB.
@@ -227,67 +226,46 @@ struct Bases {
 };
 
 // The loading waves: chunk after chunk (REV: from the last to the first), one ahead.
-template <typename L, typename T, int D1, int NP, bool VEC, bool DIRECT, bool REV>
+template <typename L, typename T, int D1, int NP, bool VEC, bool REV>
 __device__ static inline void load_chunks(const Args& A, int bh, const Rows& xk, const Rows& xq, const Rows& xv, int n, int tid) {
   constexpr int C = L::C, NB = L::NB, NTH = L::NTH;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, chunks = (n + C - 1) / C;
+  const int chunks = (n + C - 1) / C;
   const auto chunk = [&](int i) { return REV ? chunks - 1 - i : i; };
   const u32x4* const tri = REV ? A.trit : A.tri;
-  if constexpr (DIRECT) {
-    const auto load = [&](int i, int buf) {
-      const int c = chunk(i), r0 = c * C, nr = min(C, n - r0);
-      const long long own = chunk_at(A, bh, c);
-      Direct<C, D1, NTH>::load(L::k + buf * L::MK::kAll, xk, r0, nr, wave, lane);
-      if (NP > 0) Direct<C, D1, NTH>::load(L::q + buf * L::kQ, xq, r0, nr, wave, lane);
-      Direct<C, L::VC, NTH>::load(L::v + buf * L::kV, xv, r0, nr, wave, lane);
-      direct_copy<3 * NB, NTH>(L::t + buf * L::kT, tri + own * (3 * NB * 64), wave, lane);
-      if (NP > 0) direct_copy<NP * NB, NTH>(L::p + buf * L::kP, A.pri + own * (NP * NB * 64), wave, lane);
-      direct_copy<kScanVecs * C / 256, NTH>(L::w + buf * L::kW, A.vec + own * (kVecs * C), wave, lane);
-    };
-    load(0, 0);
-    wait_vmcnt0();
-    lds_barrier();
-    for (int i = 0; i < chunks; ++i) {
-      if (i + 1 < chunks) load(i + 1, (i + 1) % 2);
-      wait_vmcnt0();
-      lds_barrier();
+  Load<T, C, D1, NTH, VEC> lk, lq;
+  Load<T, C, L::VC, NTH, VEC> lv;
+  LoadTri<NB, 3, NTH> lt;
+  LoadTri<NB, (NP > 0 ? NP : 1), NTH> lp;
+  f32x4 lw;
+  const auto load = [&](int i) {
+    const int c = chunk(i), r0 = c * C, nr = min(C, n - r0);
+    const long long own = chunk_at(A, bh, c);
+    lk.load(xk, r0, nr, tid);
+    if (NP > 0) lq.load(xq, r0, nr, tid);
+    lv.load(xv, r0, nr, tid);
+    lt.load(tri + own * (3 * NB * 64), tid);
+    if (NP > 0) lp.load(A.pri + own * (NP * NB * 64), tid);
+    if (tid < C) lw = reinterpret_cast<const f32x4*>(A.vec + own * (kVecs * C))[tid];
+  };
+  const auto store = [&](int buf) {
+    lk.template store<typename L::MK>(L::k + buf * L::MK::kAll, tid);
+    if (NP > 0) lq.template store<typename L::MK>(L::q + buf * L::kQ, tid);
+    lv.template store<typename L::MV>(L::v + buf * L::kV, tid);
+    lt.store(L::t + buf * L::kT, tid);
+    if (NP > 0) lp.store(L::p + buf * L::kP, tid);
+    if (tid < C) lds_put(L::w + buf * L::kW + 16 * tid, lw);
+  };
+  load(0);
+  store(0);
+  if (chunks > 1) load(1);
+  lds_barrier();
+  for (int i = 0; i < chunks; ++i) {
+    if (L::kBufs == 1) lds_barrier();   // the chunk's readers are done
+    if (i + 1 < chunks) {
+      store((i + 1) % L::kBufs);
+      if (i + 2 < chunks) load(i + 2);
     }
-  } else {
-    Load<T, C, D1, NTH, VEC> lk, lq;
-    Load<T, C, L::VC, NTH, VEC> lv;
-    LoadTri<NB, 3, NTH> lt;
-    LoadTri<NB, (NP > 0 ? NP : 1), NTH> lp;
-    f32x4 lw;
-    const auto load = [&](int i) {
-      const int c = chunk(i), r0 = c * C, nr = min(C, n - r0);
-      const long long own = chunk_at(A, bh, c);
-      lk.load(xk, r0, nr, tid);
-      if (NP > 0) lq.load(xq, r0, nr, tid);
-      lv.load(xv, r0, nr, tid);
-      lt.load(tri + own * (3 * NB * 64), tid);
-      if (NP > 0) lp.load(A.pri + own * (NP * NB * 64), tid);
-      if (tid < C) lw = reinterpret_cast<const f32x4*>(A.vec + own * (kVecs * C))[tid];
-    };
-    const auto store = [&](int buf) {
-      lk.template store<typename L::MK>(L::k + buf * L::MK::kAll, tid);
-      if (NP > 0) lq.template store<typename L::MK>(L::q + buf * L::kQ, tid);
-      lv.template store<typename L::MV>(L::v + buf * L::kV, tid);
-      lt.store(L::t + buf * L::kT, tid);
-      if (NP > 0) lp.store(L::p + buf * L::kP, tid);
-      if (tid < C) lds_put(L::w + buf * L::kW + 16 * tid, lw);
-    };
-    load(0);
-    store(0);
-    if (chunks > 1) load(1);
     lds_barrier();
-    for (int i = 0; i < chunks; ++i) {
-      if (L::kBufs == 1) lds_barrier();   // the chunk's readers are done
-      if (i + 1 < chunks) {
-        store((i + 1) % L::kBufs);
-        if (i + 2 < chunks) load(i + 2);
-      }
-      lds_barrier();
-    }
   }
 }
 // The computing waves: f(chunk, the buffer of its operands, a constant) for every chunk.
@@ -317,10 +295,10 @@ __device__ static inline void put_columns(const f32x4 (&x)[N], float* to, int ro
     for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x[r][j]), b, own, (unsigned)((16 * r + j) * stride) * 4u, 0);
 }
 
-template <typename T, int D1, int NW, bool VEC, bool FWD, bool DIRECT>
-__global__ __launch_bounds__((Chunks<T, D1, NW, 1, DIRECT>::kThreads)) void k_delta_scan(Args A) {
+template <typename T, int D1, int NW, bool VEC, bool FWD>
+__global__ __launch_bounds__((Chunks<T, D1, NW, 1>::kThreads)) void k_delta_scan(Args A) {
   constexpr int NO = Kind<T>::kOut;
-  typedef Chunks<T, D1, NW, (FWD ? NO : 0), DIRECT> L;
+  typedef Chunks<T, D1, NW, (FWD ? NO : 0)> L;
   constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, VC = 16 * NW;
   typedef typename L::MK MK;
   typedef typename L::MV MV;
@@ -331,7 +309,7 @@ __global__ __launch_bounds__((Chunks<T, D1, NW, 1, DIRECT>::kThreads)) void k_de
              xv = rows_at<T>(A.V, A, bh, A.dv, n, col0, min(A.dv - col0, VC)), xo = rows_at<T>(A.out, A, bh, A.dv, n, col0, min(A.dv - col0, VC));
   if (FWD && n < A.L) zero_rows<T>(xo, n, A.L, tid, L::kThreads);
   if (wave >= NW) {
-    if (chunks > 0) load_chunks<L, T, D1, (FWD ? NO : 0), VEC, DIRECT, false>(A, bh, xk, xq, xv, n, tid - 64 * NW);
+    if (chunks > 0) load_chunks<L, T, D1, (FWD ? NO : 0), VEC, false>(A, bh, xk, xq, xv, n, tid - 64 * NW);
     return;
   }
   f32x4 S[KT];
@@ -469,9 +447,9 @@ __global__ __launch_bounds__((Chunks<T, D1, NW, 1, DIRECT>::kThreads)) void k_de
 // ---------------------------------------------------------------------------
 // From the last chunk to the first: the gradient G of the state behind each chunk, and dR.
 // ---------------------------------------------------------------------------
-template <typename T, int D1, int NW, bool VEC, bool DIRECT>
-__global__ __launch_bounds__((Chunks<T, D1, NW, 3, DIRECT>::kThreads)) void k_delta_rev(Args A) {
-  typedef Chunks<T, D1, NW, 3, DIRECT> L;
+template <typename T, int D1, int NW, bool VEC>
+__global__ __launch_bounds__((Chunks<T, D1, NW, 3>::kThreads)) void k_delta_rev(Args A) {
+  typedef Chunks<T, D1, NW, 3> L;
   constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, VC = 16 * NW;
   typedef typename L::MK MK;
   typedef typename L::MV MV;
@@ -481,7 +459,7 @@ __global__ __launch_bounds__((Chunks<T, D1, NW, 3, DIRECT>::kThreads)) void k_de
   if (wave >= NW) {
     const Rows xk = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), xq = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk),
                xo = rows_at<T>(A.dOut, A, bh, A.dv, n, col0, min(A.dv - col0, VC));
-    if (chunks > 0) load_chunks<L, T, D1, 3, VEC, DIRECT, true>(A, bh, xk, xq, xo, n, tid - 64 * NW);
+    if (chunks > 0) load_chunks<L, T, D1, 3, VEC, true>(A, bh, xk, xq, xo, n, tid - 64 * NW);
     return;
   }
   f32x4 G[KT];
@@ -573,24 +551,18 @@ static dark_status launch_prep(const Args& a, bool backward, hipStream_t st) {
   }
 }
 
-// Whether a call's rows fill the tiles of instances that take them straight to LDS.
-template <typename T, int D1>
-static bool direct_of(const Args& a) { return sizeof(T) == 2 && D1 <= 128 && a.dk == D1 && a.dv % 64 == 0; }
-
-template <typename T, int D1, int NW, bool VEC, bool FWD, bool DIRECT>
+template <typename T, int D1, int NW, bool VEC, bool FWD>
 static dark_status go_scan(const Args& a, hipStream_t st) {
-  typedef Chunks<T, D1, NW, (FWD ? Kind<T>::kOut : 0), DIRECT> L;
-  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>, L::all));
+  typedef Chunks<T, D1, NW, (FWD ? Kind<T>::kOut : 0)> L;
+  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD>, L::all));
   const int cols = FWD ? a.dv : a.dvp;
-  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD, DIRECT>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(L::kThreads), L::all, a);
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(L::kThreads), L::all, a);
   return DARK_OK;
 }
 template <typename T, int D1, bool FWD>
 static dark_status go_scan(const Args& a, hipStream_t st) {
-  if constexpr (sizeof(T) == 2 && D1 <= 128)
-    if (direct_of<T, D1>(a)) return go_scan<T, D1, 4, true, FWD, true>(a, st);
   constexpr int NW = D1 > 128 ? 2 : 4;   // 256 rows of a state leave room for one wave a SIMD
-  return vec_of<T>(a) ? go_scan<T, D1, NW, true, FWD, false>(a, st) : go_scan<T, D1, NW, false, FWD, false>(a, st);
+  return vec_of<T>(a) ? go_scan<T, D1, NW, true, FWD>(a, st) : go_scan<T, D1, NW, false, FWD>(a, st);
 }
 template <typename T>
 static dark_status launch_scan(const Args& a, Pass pass, hipStream_t st) {
@@ -601,19 +573,17 @@ static dark_status launch_scan(const Args& a, Pass pass, hipStream_t st) {
   }
 }
 
-template <typename T, int D1, int NW, bool VEC, bool DIRECT>
+template <typename T, int D1, int NW, bool VEC>
 static dark_status go_rev(const Args& a, hipStream_t st) {
-  typedef Chunks<T, D1, NW, 3, DIRECT> L;
-  DARK_TRY(allow_lds(k_delta_rev<T, D1, NW, VEC, DIRECT>, L::all));
-  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_rev<T, D1, NW, VEC, DIRECT>), dim3(a.B * a.H, a.dvp / (16 * NW)), dim3(L::kThreads), L::all, a);
+  typedef Chunks<T, D1, NW, 3> L;
+  DARK_TRY(allow_lds(k_delta_rev<T, D1, NW, VEC>, L::all));
+  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_rev<T, D1, NW, VEC>), dim3(a.B * a.H, a.dvp / (16 * NW)), dim3(L::kThreads), L::all, a);
   return DARK_OK;
 }
 template <typename T, int D1>
 static dark_status go_rev(const Args& a, hipStream_t st) {
-  if constexpr (sizeof(T) == 2 && D1 <= 128)
-    if (direct_of<T, D1>(a)) return go_rev<T, D1, 4, true, true>(a, st);
   constexpr int NW = D1 > 128 ? 2 : 4;
-  return vec_of<T>(a) ? go_rev<T, D1, NW, true, false>(a, st) : go_rev<T, D1, NW, false, false>(a, st);
+  return vec_of<T>(a) ? go_rev<T, D1, NW, true>(a, st) : go_rev<T, D1, NW, false>(a, st);
 }
 template <typename T>
 static dark_status launch_rev(const Args& a, hipStream_t st) {

@@ -116,7 +116,8 @@ __device__ static inline Planes<N> split(f32x4 a, f32x4 b) {
 // transposing reads two neighbouring chunks of eight rows 0 ... 7 (8 ... 15): both on distinct banks for 32 lanes.
 template <int RB>
 __device__ constexpr int swz(int row) {
-  static_assert(RB == 64 || RB == 128 || RB % 256 == 0, "rows of 64, 128 or whole 256 bytes");
+  if (RB == 32) return 0;   // eight rows are 256 bytes by themselves
+  static_assert(RB == 32 || RB == 64 || RB == 128 || RB % 256 == 0, "rows of 64, 128 or whole 256 bytes");
   if (RB == 64) return ((row >> 2) & 1) << 1;
   if (RB == 128) return ((row >> 1) & 3) << 1 | ((row >> 3) & 1);
   return (row & 7) << 1 | ((row >> 3) & 1);
@@ -256,33 +257,6 @@ struct LoadTri {
     }
   }
 };
-// The same ways from memory to LDS without registers, 1 KB an instruction of a wave: for bf16 tiles whose rows fill them.  Rows behind the last
-// are copies of it (their weights are 0: k_delta_prep).  A wave's lanes write where they lie, so that a lane asks for the 16 bytes that
-// the swizzle puts there.  The caller waits for them (wait_loads) before the barrier that hands them out.
-template <int C, int D, int NTH>
-struct Direct {
-  typedef Mat<C, D, 1> M;
-  static constexpr int kLanes = M::RB / 16, kRows = 64 / kLanes, kAll = C / kRows, kEach = kAll / (NTH / 64);   // rows an instruction, instructions
-  static_assert(kAll % (NTH / 64) == 0, "whole instructions a wave");
-  __device__ static void load(int tile, const Rows& x, int r0, int nr, int wave, int lane) {
-    const char* const first = x.head + (long long)r0 * x.row;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = e * (NTH / 64) + wave, row = i * kRows + lane / kLanes;
-      const unsigned off = (unsigned)min(row, nr - 1) * x.row + (unsigned)(((lane % kLanes) ^ swz<M::RB>(row & 15)) << 4);
-      dma16_to_lds(first, off, reinterpret_cast<void*>((uintptr_t)(tile + i * 1024)));
-    }
-  }
-};
-// `bytes` (whole KB) as they are.
-template <int KB, int NTH>
-__device__ static inline void direct_copy(int tile, const void* from, int wave, int lane) {
-#pragma unroll
-  for (int e = 0; e < (KB + NTH / 64 - 1) / (NTH / 64); ++e) {
-    const int i = e * (NTH / 64) + wave;
-    if (KB % (NTH / 64) == 0 || i < KB) dma16_to_lds(static_cast<const char*>(from) + i * 1024, (unsigned)lane * 16u, reinterpret_cast<void*>((uintptr_t)(tile + i * 1024)));
-  }
-}
 // Waits for all memory operations of the wave but the last `N`.
 template <int N>
 __device__ static inline void wait_loads() {
