@@ -4,15 +4,21 @@
 // those, the shortest beginning that holds top_p of their sum; and of those the ones with w_t >= min_p.  The token drawn is the first, in
 // the order of the tokens' numbers, behind which the kept weights add up to more than u times their sum.
 //
-// A workgroup takes a row, whose 16-byte pieces its threads hold where they have room for them.  What is kept but for min_p is a beginning of the
-// order, so that its last entry says it.  Small top_k: a bound from the threads' maxima leaves few candidates, which count those before them
-// and, kept, the weights of those with lower numbers: no further pass.  Else a histogram of weights over the logits finds the bin
-// where the beginning ends, and the bin's entries are sorted.  The draw sums the kept weights by waves, each of which holds a
-// contiguous part of the row, and looks into one of them.
-// Weights are in fp64, by a polynomial, to 2^-31 of their value, and so are their sums; a histogram's are integers, whose sums have no order.
+// A workgroup takes a row, and reads it once for each question: the largest logit; those that top_k can keep, or the weights by bins of their logits; the
+// last that top_p keeps; the sum of what is kept.  What is kept is a beginning of the order, so that its last entry says it.
+//  * Small top_k: a bound from the threads' maxima leaves few candidates, which count those before them and, kept, the weights of those with
+//    lower numbers: two reads of the row.
+//  * Else a histogram of weights over the logits finds the bin where the beginning ends, and the bin's entries are sorted.
+//  * The draw sums the kept weights by waves, each of which holds a contiguous part of the row, and looks into one of them.
+// Weights are in fp64, by a polynomial, to 2^-33 of their value, and so are their sums; a histogram's are integers, whose sums have no order.
 // In fp32 the borders between a large row's tokens would be off by some 2^-30 of the row's sum each, 2^17 of them together by 2^-13: one
 // row in 8000 would draw a token's neighbour.
+// What bounds it: of 256 rows of 131071 bf16 logits the first read takes 10 us (6.7 TB/s), a read that asks a comparison of each logit 9, one that weighs
+// each 24 (19 instructions a logit, four waves a SIMD; the matrix of 67 MB lies in the last cache by then), the histogram's 40 (two more for the
+// addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 32, no filter 47, top_p 0.9 107;
+// one row of 32000 fp32 logits 8, 14, 13 and 31, where the way through the steps counts and not the row.
 #include <cmath>
+#include <type_traits>
 
 #include "common.h"
 
@@ -24,8 +30,8 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
-constexpr int kHeld = 16;      // pieces of 16 bytes that a thread holds; longer rows are read anew in every pass
-constexpr int kBins = 2048;
+constexpr int kAhead = 4;      // pieces of 16 bytes that a thread asks for at once
+constexpr int kBins = 2048;    // 32 for each lane of a wave
 constexpr int kList = 2048;    // entries that are sorted
 constexpr int kSmall = 512;    // the largest top_k that goes by the threads' maxima
 constexpr int kCounted = 256;  // entries that count each other; more are sorted by merging
@@ -50,10 +56,10 @@ struct Row {
   static constexpr int P = 16 / (int)sizeof(T);
   __amdgpu_buffer_rsrc_t at;
   int begin, V, pieces;   // token of the row's first piece's first element (it may lie before the row); tokens; pieces of a thread
-  u32x4 r[kHeld];
-  __device__ u32x4 fetch(int piece) const {   // -infinity where there is no token
-    u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(at, (unsigned)piece * 16u, 0, 0);
-    const int t = begin + piece * P;
+  bool infinite;          // the largest logit is infinite: those that are share everything
+  __device__ u32x4 ask(int piece) const { return __builtin_amdgcn_raw_buffer_load_b128(at, (unsigned)piece * 16u, 0, 0); }
+  // a piece's logits: -infinity where there is no token; in a row with infinite ones these are 0 and all others -infinity
+  __device__ u32x4 logits(u32x4 v, int t) const {
     if (t < 0 || t + P > V) {
 #pragma unroll
       for (int j = 0; j < P; ++j) {
@@ -66,17 +72,24 @@ struct Row {
         }
       }
     }
+    if (infinite) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (sizeof(T) == 2) v[j] = ((v[j] & 0xffffu) == 0x7f80u ? 0u : 0xff80u) | (v[j] >> 16 == 0x7f80u ? 0u : 0xff800000u);
+        else v[j] = v[j] == 0x7f800000u ? 0u : 0xff800000u;
+      }
+    }
     return v;
   }
+  __device__ u32x4 fetch(int piece) const { return logits(ask(piece), begin + piece * P); }
   __device__ int piece(int wave, int lane, int i) const { return (wave * pieces + i) * 64 + lane; }
-  __device__ void load(int wave, int lane) {
-#pragma unroll
-    for (int i = 0; i < kHeld; ++i)
-      if (i < pieces) r[i] = fetch(piece(wave, lane, i));
-  }
   __device__ static float value(u32x4 v, int j) {
     if constexpr (sizeof(T) == 2) return __uint_as_float(j & 1 ? v[j / 2] & 0xffff0000u : v[j / 2] << 16);
     else return __uint_as_float(v[j]);
+  }
+  __device__ static void drop(u32x4& v, int j) {
+    if constexpr (sizeof(T) == 2) v[j / 2] = j & 1 ? (v[j / 2] & 0xffffu) | 0xff800000u : (v[j / 2] & 0xffff0000u) | 0xff80u;
+    else v[j] = 0xff800000u;
   }
   __device__ static float largest(u32x4 v) {
     float m = value(v, 0);
@@ -94,37 +107,58 @@ struct Row {
       else v = u32x4{v[1], v[2], v[3], 0};
     }
   }
-  // f(piece, its first token) for the thread's pieces
-  template <bool HELD, typename F>
-  __device__ __forceinline__ void each(int wave, int lane, const F& f) const {
-    if constexpr (HELD) {
+  // f(element, token) for those of a piece's elements that lie between two values
+  template <typename F>
+  __device__ static __forceinline__ void between(u32x4 v, int t, float from, float to, const F& f) {
+    unsigned hits = 0;
 #pragma unroll
-      for (int i = 0; i < kHeld; ++i)
-        if (i < pieces) f(r[i], begin + piece(wave, lane, i) * P);
-    } else {
+    for (int j = 0; j < P; ++j) hits |= value(v, j) >= from && value(v, j) <= to ? 1u << j : 0u;
+    while (hits != 0) {
+      const int j = __builtin_ctz(hits), w = sizeof(T) == 2 ? j >> 1 : j;
+      const unsigned word = w & 2 ? (w & 1 ? v[3] : v[2]) : (w & 1 ? v[1] : v[0]);
+      f(__uint_as_float(sizeof(T) == 2 ? j & 1 ? word & 0xffff0000u : word << 16 : word), t + j);
+      hits &= hits - 1;
+    }
+  }
+  // f(piece, its first token) for the thread's pieces
+  template <typename F>
+  __device__ __forceinline__ void each(int wave, int lane, const F& f) const {
 #pragma unroll 1
-      for (int i = 0; i < pieces; ++i) f(fetch(piece(wave, lane, i)), begin + piece(wave, lane, i) * P);
+    for (int i = 0; i < pieces; i += kAhead) {
+      u32x4 v[kAhead];
+#pragma unroll
+      for (int k = 0; k < kAhead; ++k) v[k] = ask(piece(wave, lane, i + k));   // behind the row: nothing is read
+      const int n = min(pieces - i, kAhead);
+#pragma unroll 1
+      for (int k = 0; k < n; ++k) {   // one copy of f: the instruction cache is to hold the kernel
+        const int t = begin + piece(wave, lane, i + k) * P;
+        f(logits(v[0], t), t);
+#pragma unroll
+        for (int j = 0; j + 1 < kAhead; ++j) v[j] = v[j + 1];
+      }
     }
   }
 };
 
-// exp((x - m) / T) = 2^z: the sum of z^k ln 2^k / k! up to k = 8 for what rounding z leaves, at most 1/2: off by 2^-32.
+// exp((x - m) / T) = 2^z = 2^n 2^f, f at most 1/2: 2^f = 1 + f g(f), g the polynomial that equals it at the seven zeros of Chebyshev's T_7; off by
+// 2^-33.  Rounding to n by the constant whose last bit is a unit, and the exponent by an integer addition: conversions and ldexp of fp64 cost more.
+// Only for what is not below `floor`, where z is some -1000: weights there are 0.
 struct Weight {
   double m, c;     // c = log2 e / T
-  float top;
-  bool infinite;   // the largest logit is infinite: those that are share everything
+  float floor;
   __device__ __forceinline__ double operator()(float x) const {
-    const double z = infinite ? (x == INFINITY ? 0.0 : -2000.0) : ((double)x - m) * c, n = rint(z), f = z - n;
-    double y = fma(f, 1.3215486790144309e-6, 1.5252733804059841e-5);
-    y = fma(f, y, 1.5403530393381609e-4);
-    y = fma(f, y, 1.3333558146428443e-3);
-    y = fma(f, y, 9.6181291076284772e-3);
-    y = fma(f, y, 5.5504108664821580e-2);
-    y = fma(f, y, 2.4022650695910071e-1);
-    y = fma(f, y, 6.9314718055994531e-1);
+    const double z = ((double)x - m) * c, t = z + 6755399441055744.0, f = z - (t - 6755399441055744.0);
+    double y = fma(f, 1.529732376073432e-05, 1.5461444698569848e-4);
+    y = fma(f, y, 1.3333502386162631e-3);
+    y = fma(f, y, 9.6180566785246356e-3);
+    y = fma(f, y, 5.5504108839096185e-2);
+    y = fma(f, y, 2.4022650922288757e-1);
+    y = fma(f, y, 6.9314718055994529e-1);
     y = fma(f, y, 1.0);
-    return z > -1000.0 ? ldexp(y, (int)n) : 0.0;   // also where x is NaN or -infinity
+    return __hiloint2double(__double2hiint(y) + (int)((unsigned)__double2loint(t) << 20), __double2loint(y));
   }
+  // the same for any logit; -infinity and NaN weigh nothing
+  __device__ __forceinline__ double any(float x) const { return x >= floor ? (*this)(x) : 0.0; }
 };
 
 template <typename T>
@@ -162,7 +196,6 @@ struct Shared {
   u64 bound;         // the last entry that is kept
   u64 before;        // weight of the bins before the chosen one
   int ranks_before, bin, size, kept;
-  unsigned lo;
 };
 
 // The list's first n entries in descending order.
@@ -197,7 +230,7 @@ __device__ __forceinline__ void sort(Shared& s, int n, int tid) {
     }
 }
 
-template <typename T, bool HELD>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logits, const float* __restrict__ uniform, Setting set,
                                                      int32_t* __restrict__ out_token, float* __restrict__ out_logprob, int V) {
   __shared__ Shared s;
@@ -215,10 +248,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     const int all = (int)((first + V - base + P - 1) / P);
     row.pieces = (all + kThreads - 1) / kThreads;
   }
-  if (HELD) row.load(wave, lane);
+  row.infinite = false;
+  const float temp = set.temperature != nullptr ? set.temperature[b] : set.T;
+  int k = set.top_k != nullptr ? set.top_k[b] : set.k;
+  float p = set.top_p != nullptr ? set.top_p[b] : set.p, q = set.min_p != nullptr ? set.min_p[b] : set.q, u = uniform != nullptr ? uniform[b] : 0.f;   // asked for before the row
   // the largest logit, of every thread and of all
   float mine = -INFINITY;
-  row.template each<HELD>(wave, lane, [&](u32x4 v, int) { mine = fmaxf(mine, Row<T>::largest(v)); });   // of a NaN and a number: the number
+  row.each(wave, lane, [&](u32x4 v, int) { mine = fmaxf(mine, Row<T>::largest(v)); });   // of a NaN and a number: the number
   s.tops[tid] = mine;
   __syncthreads();
   float top = -INFINITY;
@@ -232,18 +268,25 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     }
     return;
   }
-  const float temp = set.temperature != nullptr ? set.temperature[b] : set.T;
-  int k = set.top_k != nullptr ? set.top_k[b] : set.k;
-  float p = set.top_p != nullptr ? set.top_p[b] : set.p, q = set.min_p != nullptr ? set.min_p[b] : set.q, u = uniform != nullptr ? uniform[b] : 0.f;
+  if (top == INFINITY) {
+    row.infinite = true;
+    mine = mine == INFINITY ? 0.f : -INFINITY;
+    top = 0.f;
+    __syncthreads();
+    s.tops[tid] = mine;
+    __syncthreads();
+  }
   Weight weight;
   weight.m = top;
-  weight.infinite = top == INFINITY;
   weight.c = fmin(1.4426950408889634 / (double)temp, 1e300);
   if (!(temp > 0.f)) {   // the largest logit
     weight.c = 1.0;
     k = 1;
     p = 1.f;
   }
+  // rounded up: z stays where the exponent holds it; the largest logit weighs 1
+  const double lowest_z = (double)top - 1000.0 / weight.c;
+  weight.floor = lowest_z > -3.402823466e38 ? fminf(value_of(ordered((float)lowest_z) + 1u), top) : -3.402823466e38f;
   q = q > 0.f ? fminf(q, 1.f) : 0.f;
   u = u > 0.f ? u : 0.f;
   if (k <= 0 || k >= V) k = 0;
@@ -251,17 +294,17 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   if (!(p > 0.f)) p = by_p ? 0.f : 1.f;
   u64 bound = 0;   // entries from this one on are kept
   const double unit = (double)(1ull << (__builtin_clz((unsigned)V) + 19));   // of an integer weight: V of them stay below 2^51
-  const auto integer = [&](double w) -> u64 { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; };
+  const auto integer = [&](double w) __attribute__((always_inline)) -> u64 { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; };
 
   // The list holds all entries of a part of the order, sorted, behind `rank` entries of weight `held`: the last that is kept of them, by rank
   // or by weight (target), and the weight up to it.  By one wave.
-  const auto last_of = [&](int n, int rank, u64 held, bool by_rank, int most, u64 target, u64* upto) -> u64 {
+  const auto last_of = [&](int n, int rank, u64 held, bool by_rank, int most, u64 target, u64* upto) __attribute__((always_inline)) -> u64 {
     u64 found = 0, sum = held;
     for (int i0 = 0; i0 < n; i0 += 64) {
       const u64 e = i0 + lane < n ? s.list[i0 + lane] : 0;
-      const u64 w = e != 0 ? integer(weight(logit_of(e))) : 0;
+      const u64 w = e != 0 ? integer(weight.any(logit_of(e))) : 0;
       const u64 up = sum + wave_prefix(w, lane);
-      const bool in = e != 0 && (by_rank ? rank + i0 + lane < most : up - w < target || rank + i0 + lane == 0);
+      const bool in = e != 0 && (by_rank ? rank + i0 + lane < most : up - w < target || (held == 0 && i0 + lane == 0));
       const u64 kept = __ballot(in);
       if (kept != 0) {
         const int last = 63 - __builtin_clzll(kept);
@@ -273,39 +316,39 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     }
     return found;
   };
-  const auto append = [&](float x, int t) {
+  const auto append = [&](float x, int t) __attribute__((always_inline)) {
     const int at = atomicAdd(&s.size, 1);
     if (at < kList) s.list[at] = entry(x, t);
   };
-  const auto finish = [&](int token, double w, double all) {
+  const auto finish = [&](int token, double w, double all) __attribute__((always_inline)) {
     out_token[b] = token;
     if (out_logprob != nullptr) out_logprob[b] = (float)log(w / all);
   };
 
   bool done = k == 0 && !by_p;
   if (!done && k > 0 && k <= kSmall) {
-    // The k-th largest of the threads' maxima is at most the k-th largest logit: its first bits, by one wave.
-    if (wave == 0) {
-      unsigned key[kThreads / 64], cut = 0;
+    // The k-th largest of the threads' maxima is at most the k-th largest logit: its first 16 bits, four at a time, a wave for each value of them.
+    unsigned key[kThreads / 64], cut = k > 1 ? 0 : ordered(top);
 #pragma unroll
-      for (int i = 0; i < kThreads / 64; ++i) key[i] = ordered(s.tops[i * 64 + lane]);
-      for (int bit = 31; bit >= 16; --bit) {
-        const unsigned next = cut | 1u << bit;
-        int n = 0;
+    for (int i = 0; i < kThreads / 64; ++i) key[i] = ordered(s.tops[i * 64 + lane]);
+    if (tid == 0) s.size = 0;
+    if (k == 1) __syncthreads();
+#pragma unroll 1
+    for (int shift = k > 1 ? 28 : 12; shift >= 16; shift -= 4) {   // the largest is known
+      const unsigned next = cut | (unsigned)wave << shift;
+      int n = 0;
 #pragma unroll
-        for (int i = 0; i < kThreads / 64; ++i) n += __builtin_popcountll(__ballot(key[i] >= next));
-        if (n >= k) cut = next;
-      }
-      const unsigned least = ordered(-3.402823466e38f);
-      if (lane == 0) s.lo = cut > least ? cut : least, s.size = 0;
+      for (int i = 0; i < kThreads / 64; ++i) n += __builtin_popcountll(__ballot(key[i] >= next));
+      unsigned* const of = s.count + 4 * shift;   // each round its own
+      if (lane == 0) of[wave] = (unsigned)n;
+      __syncthreads();
+      const u64 reach = __ballot(lane < 16 && (int)of[lane & 15] >= k);   // of 0 always
+      cut |= (unsigned)(63 - __builtin_clzll(reach)) << shift;
     }
-    __syncthreads();
-    const float least = value_of(s.lo);
-    row.template each<HELD>(wave, lane, [&](u32x4 v, int t) {
-      if (Row<T>::largest(v) >= least)
-        Row<T>::elements(v, t, [&](float x, int tk) {
-          if (x >= least) append(x, tk);
-        });
+    const unsigned lowest = ordered(-3.402823466e38f);
+    const float least = value_of(cut > lowest ? cut : lowest);
+    row.each(wave, lane, [&](u32x4 v, int t) {
+      Row<T>::between(v, t, least, INFINITY, append);
     });
     __syncthreads();
     const int n = s.size;
@@ -322,7 +365,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         // every kept entry adds up those with lower numbers
         double w = 0.0;
         if (tid < m) {
-          w = weight(logit_of(s.list[tid]));
+          w = weight.any(logit_of(s.list[tid]));
           w = w >= (double)q ? w : 0.0;
           s.weights[tid] = w;
         }
@@ -338,7 +381,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         if (wave == 0) {
           double all = 0.0;
           for (int i0 = 0; i0 < m; i0 += 64) {
-            const double x = i0 + lane < m ? weight(logit_of(s.list[i0 + lane])) : 0.0;
+            const double x = i0 + lane < m ? weight.any(logit_of(s.list[i0 + lane])) : 0.0;
             all += x >= (double)q ? x : 0.0;
           }
           all = wave_sum(all);
@@ -349,7 +392,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
           for (int i0 = 0; i0 < m; i0 += 64) {
             if (i0 + lane < m) {
               const u64 e = s.list[i0 + lane];
-              const double x = weight(logit_of(e));
+              const double x = weight.any(logit_of(e));
               if (x >= (double)q && x > 0.0 && s.weights[i0 + lane] <= target && token_of(e) > best) best = token_of(e), logit = logit_of(e);
             }
           }
@@ -359,7 +402,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
             const float x = __shfl_xor(logit, o, 64);
             if (t > best) best = t, logit = x;
           }
-          if (lane == 0) finish(best, weight(logit), all);
+          if (lane == 0) finish(best, weight.any(logit), all);
         }
         return;
       }
@@ -372,24 +415,42 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     // Bins over the logits from the largest down, as far as weights matter beside 1 - top_p of the sum (and further for top_k).
     const float reach = (logf((float)V) + (by_p ? fmaxf(-logf(1.f - p), 0.f) : 0.f) + 3.f) * 1.4426950408889634f / (float)fmin(fmax(weight.c, 1e-30), 1e30);
     const float step = fminf((float)(kBins - 1) / reach, 1e30f);
-    const auto bin_of = [&](float x) -> int { return weight.infinite ? (x == INFINITY ? 0 : kBins - 1) : (int)fminf((top - x) * step, (float)(kBins - 1)); };
+    const auto bin_of = [&](float x) __attribute__((always_inline)) -> int { return (int)fminf((top - x) * step, (float)(kBins - 1)); };
     for (int i = tid; i < kBins; i += kThreads) s.mass[i] = 0, s.count[i] = 0;
     __syncthreads();
-    row.template each<HELD>(wave, lane, [&](u32x4 v, int) {
+    // the last bin's, which may be most, add up on their way
+    const auto histogram = [&](auto counted) __attribute__((always_inline)) {
+      u64 far = 0;
+      int far_count = 0;
+      row.each(wave, lane, [&](u32x4 v, int) {
 #pragma unroll
-      for (int j = 0; j < P; ++j) {
-        const float x = Row<T>::value(v, j);
-        if (x > -INFINITY) {
-          const int at = bin_of(x);
-          atomicAdd(&s.mass[at], integer(weight(x)));
-          atomicAdd(&s.count[at], 1u);
+        for (int j = 0; j < P; ++j) {
+          const float x = Row<T>::value(v, j);
+          if (x > -INFINITY) {
+            const int at = bin_of(x);
+            const u64 w = integer(weight.any(x));
+            if (at < kBins - 1) {
+              atomicAdd(&s.mass[at], w);
+              if (counted) atomicAdd(&s.count[at], 1u);
+            } else {
+              far += w;
+              far_count += 1;
+            }
+          }
         }
-        __builtin_amdgcn_sched_barrier(0);
+      });
+      far = wave_sum(far);
+      far_count = wave_sum(far_count);
+      if (lane == 0) {
+        atomicAdd(&s.mass[kBins - 1], far);
+        atomicAdd(&s.count[kBins - 1], (unsigned)far_count);
       }
-    });
+    };
+    if (k > 0) histogram(std::integral_constant<bool, true>());
+    else histogram(std::integral_constant<bool, false>());   // top_p asks for no ranks
     __syncthreads();
     // The bin where the order reaches `most` entries, or a weight of `target`; what lies before it.
-    const auto choose = [&](bool by_rank, int most, u64 target) {
+    const auto choose = [&](bool by_rank, int most, u64 target) __attribute__((always_inline)) {
       if (wave == 0) {
         u64 m = 0;
         int n = 0;
@@ -397,44 +458,58 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         u64 mb = wave_prefix(m, lane) - m;
         int nb = wave_prefix(n, lane) - n;
         // the lane whose bins reach it; the last one with entries if none does
-        const bool reaches = n > 0 && (by_rank ? nb + n >= most : mb + m >= target);
-        const u64 r = __ballot(reaches), some = __ballot(n > 0);
+        const bool any = by_rank ? n > 0 : m > 0, reaches = any && (by_rank ? nb + n >= most : mb + m >= target);
+        const u64 r = __ballot(reaches), some = __ballot(any);
         const int who = r != 0 ? __builtin_ctzll(r) : 63 - __builtin_clzll(some);
-        if (lane == who) {
-          int bin = -1;
-          for (int i = 0; i < kBins / 64; ++i) {
-            const int c = (int)s.count[lane * (kBins / 64) + i];
-            const u64 w = s.mass[lane * (kBins / 64) + i];
-            if (c == 0) continue;
-            if (bin >= 0) {
-              if (by_rank ? nb >= most : mb >= target) break;   // reached before this one
-            }
-            bin = lane * (kBins / 64) + i;
-            s.before = mb;
-            s.ranks_before = nb;
-            mb += w;
-            nb += c;
-          }
-          s.bin = bin;
+        // its bins, one a lane
+        const int at = __shfl(lane, who, 64) * (kBins / 64) + (lane & 31);
+        const u64 base_m = __shfl(mb, who, 64);
+        const int base_n = __shfl(nb, who, 64);
+        const u64 w = lane < 32 ? s.mass[at] : 0;
+        const int c = lane < 32 ? (int)s.count[at] : 0;
+        const u64 upto_m = base_m + wave_prefix(w, lane);
+        const int upto_n = base_n + wave_prefix(c, lane);
+        const bool own = by_rank ? c > 0 : w > 0;
+        const u64 hit = __ballot(own && (by_rank ? upto_n >= most : upto_m >= target)), full = __ballot(own);
+        const int bin = hit != 0 ? __builtin_ctzll(hit) : 63 - __builtin_clzll(full);
+        if (lane == bin) {
+          s.before = upto_m - w;
+          s.ranks_before = upto_n - c;
+          s.bin = at;
           s.size = 0;
         }
       }
       __syncthreads();
     };
     // All entries of a bin, sorted: from a bin of more than the list holds, the part of it where the order reaches its end.
-    const auto gather = [&](bool by_rank, int most, u64 target) {
+    const auto gather = [&](bool by_rank, int most, u64 target) __attribute__((always_inline)) {
       choose(by_rank, most, target);
       const int bin = s.bin;
+      const float width = 1.f / step, slack = 1e-4f * (width * (float)bin + 1e-6f * fabsf(top)) + 1e-6f * fabsf(top);
+      const float to = top - (width * (float)bin - slack), from = bin == kBins - 1 ? -3.402823466e38f : top - (width * (float)(bin + 1) + slack);
       // entries lo ... hi of the order are left; each pass leaves a part of 2048 of them
       u64 lo = bound, hi = ~0ull;   // nothing that top_k left out
-      int n = (int)s.count[bin];
+      const auto list = [&]() __attribute__((always_inline)) {
+        row.each(wave, lane, [&](u32x4 v, int t) {
+          // the logits that the bin can hold, and a little more: what they are exactly is asked of few
+          Row<T>::between(v, t, from, to, [&](float x, int tk) {
+            if (x > -INFINITY && bin_of(x) == bin) {
+              const u64 e = entry(x, tk);
+              if (e >= lo && e <= hi) append(x, tk);
+            }
+          });
+        });
+        __syncthreads();
+        return s.size;
+      };
+      int n = list();
       __syncthreads();
       while (n > kList) {
         // the range of what is left
         if (tid == 0) s.list[0] = ~0ull, s.list[1] = 0;
         __syncthreads();
         u64 least = ~0ull, most_e = 0;
-        row.template each<false>(wave, lane, [&](u32x4 v, int t) {
+        row.each(wave, lane, [&](u32x4 v, int t) {
           Row<T>::elements(v, t, [&](float x, int tk) {
             if (x > -INFINITY && bin_of(x) == bin) {
               const u64 e = entry(x, tk);
@@ -456,13 +531,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         const u64 before = s.before;
         const int ranks = s.ranks_before;
         __syncthreads();
-        row.template each<false>(wave, lane, [&](u32x4 v, int t) {
+        row.each(wave, lane, [&](u32x4 v, int t) {
           Row<T>::elements(v, t, [&](float x, int tk) {
             if (x > -INFINITY && bin_of(x) == bin) {
               const u64 e = entry(x, tk);
               if (e >= lo && e <= hi) {
                 const int at = (int)((hi - e) >> shift);
-                atomicAdd(&s.mass[at], integer(weight(x)));
+                atomicAdd(&s.mass[at], integer(weight.any(x)));
                 atomicAdd(&s.count[at], 1u);
               }
             }
@@ -471,23 +546,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         __syncthreads();
         choose(by_rank, most - ranks, target > before ? target - before : 0);
         const int sub = s.bin;
-        n = (int)s.count[sub];
         const u64 top_e = hi - ((u64)sub << shift);
         const u64 width = (1ull << shift) - 1;
         lo = top_e - lo > width ? top_e - width : lo;
         hi = top_e;
         if (tid == 0) s.before += before, s.ranks_before += ranks;
         __syncthreads();
+        n = list();
+        __syncthreads();
       }
-      row.template each<HELD>(wave, lane, [&](u32x4 v, int t) {
-          Row<T>::elements(v, t, [&](float x, int tk) {
-          if (x > -INFINITY && bin_of(x) == bin) {
-            const u64 e = entry(x, tk);
-            if (e >= lo && e <= hi) append(x, tk);
-          }
-        });
-      });
-      __syncthreads();
       sort(s, n, tid);
       return n;
     };
@@ -509,10 +576,10 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       if (by_p) {   // the histogram anew: gathering may have used it, and what top_k leaves out counts no more
         for (int i = tid; i < kBins; i += kThreads) s.mass[i] = 0, s.count[i] = 0;
         __syncthreads();
-        row.template each<false>(wave, lane, [&](u32x4 v, int t) {
+        row.each(wave, lane, [&](u32x4 v, int t) {
           Row<T>::elements(v, t, [&](float x, int tk) {
             if (x > -INFINITY && entry(x, tk) >= bound) {
-              atomicAdd(&s.mass[bin_of(x)], integer(weight(x)));
+              atomicAdd(&s.mass[bin_of(x)], integer(weight.any(x)));
               atomicAdd(&s.count[bin_of(x)], 1u);
             }
           });
@@ -532,28 +599,48 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       bound = s.bound;
     }
   }
+  if (q > 0.f) {
+    // min_p as a bound: behind the largest logit whose weight is below it.  Six bits at a time, and two; a NaN weighs nothing.
+    unsigned key = 0;
+    const unsigned most = ordered(top);
+#pragma unroll 1
+    for (int shift = 26; shift >= -4; shift -= 6) {
+      const unsigned own = key | (shift >= 0 ? (unsigned)lane << shift : (unsigned)lane & 3u);
+      const u64 below = __ballot(own < most && !(weight.any(value_of(own)) >= (double)q) && (shift >= 0 || lane < 4));
+      const unsigned digit = (unsigned)__builtin_popcountll(below) - 1u;
+      key |= shift >= 0 ? digit << shift : digit;
+    }
+    const u64 least = (u64)(key + 1) << 32 | 0x80000000u;   // with the highest number
+    bound = bound > least ? bound : least;
+  }
   // ---------------------------------------------------------------------------
   // The draw: sums of the kept weights, of each wave's part of the row, then of a sixteenth of one part by each wave.
   // ---------------------------------------------------------------------------
-  const float last_logit = bound != 0 ? logit_of(bound) : -3.402823466e38f;
-  const int last_token = bound != 0 ? token_of(bound) : 0x7fffffff;
-  const auto kept = [&](float x, int t) -> double {
-    const double w = weight(x);
-    return (x > last_logit || (x == last_logit && t <= last_token)) && w >= (double)q ? w : 0.0;
-  };
-  const auto sum_of = [&](u32x4 v, int t) -> double {
-    double w = 0.0;
-    if (Row<T>::largest(v) >= last_logit) {
+  // Kept are logits from `last_logit` on, with numbers behind last_token those above it.  All of them are numbers that the weight takes.
+  float last_logit = bound != 0 ? logit_of(bound) : weight.floor;
+  const int last_token = bound == 0 || last_logit < weight.floor ? 0x7fffffff : token_of(bound);
+  last_logit = fmaxf(last_logit, weight.floor);
+  const float above = value_of(ordered(last_logit) + 1u);
+  const auto sum_of = [&](u32x4 v, int t, auto each_of) __attribute__((always_inline)) {
+    const float from = t > last_token ? above : last_logit;
+    if (t <= last_token && t + P - 1 > last_token) {   // the one piece with numbers on both sides
 #pragma unroll
-      for (int j = 0; j < P; ++j) {
-        w += kept(Row<T>::value(v, j), t + j);
-        __builtin_amdgcn_sched_barrier(0);   // one after the other: eight polynomials at once do not fit the registers, and four waves a SIMD wait for none
-      }
+      for (int j = 0; j < P; ++j)
+        if (t + j > last_token && Row<T>::value(v, j) < above) Row<T>::drop(v, j);
     }
-    return w;
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+      const float x = Row<T>::value(v, j);
+      const double w = weight(x);
+      each_of(x >= from ? w : 0.0, t + j);
+      if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // eight polynomials at once do not fit the registers
+    }
   };
   double sum = 0.0;
-  row.template each<HELD>(wave, lane, [&](u32x4 v, int t) { sum += sum_of(v, t); });
+  const auto add = [&](double w, int) __attribute__((always_inline)) { sum += w; };
+  row.each(wave, lane, [&](u32x4 v, int t) __attribute__((always_inline)) {
+    if (Row<T>::largest(v) >= last_logit) sum_of(v, t, add);
+  });
   sum = wave_sum(sum);
   if (lane == 0) s.sums[wave] = sum;
   __syncthreads();
@@ -562,7 +649,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   for (int i = 0; i < kWaves; ++i) all += s.sums[i];
   double rest = (double)u * all;
   // the part: the first behind which the sums exceed `rest`; with a random number of 1 or more the last that holds anything
-  const auto locate = [&](const double* sums, double& rest) -> int {
+  const auto locate = [&](const double* sums, double& rest) __attribute__((always_inline)) -> int {
     int part = -1;
     for (int i = 0; i < kWaves; ++i) {
       if (!(sums[i] > 0.0)) continue;
@@ -577,7 +664,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   sum = 0.0;
   for (int i = begin; i < end; ++i) {
     const int piece = row.piece(part, lane, i);
-    sum += sum_of(row.fetch(piece), row.begin + piece * P);
+    sum_of(row.fetch(piece), row.begin + piece * P, add);
   }
   sum = wave_sum(sum);
   if (lane == 0) s.scan[wave] = sum;
@@ -591,19 +678,19 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     const int piece = row.piece(part, lane, i);
     const u32x4 v = row.fetch(piece);
     const int t = row.begin + piece * P;
-    const double w = sum_of(v, t);
+    sum = 0.0;
+    sum_of(v, t, add);
+    const double w = sum;
     const double upto = wave_prefix(w, lane), before = upto - w;
     const u64 some = __ballot(w > 0.0), reach = __ballot(w > 0.0 && rest < upto);
     if (some == 0) continue;
     const int who = reach != 0 ? __builtin_ctzll(reach) : 63 - __builtin_clzll(some);
     int tk = -1;
     double wt = 0.0, left = rest - before;
-#pragma unroll
-    for (int j = 0; j < P; ++j) {
-      const double x = kept(Row<T>::value(v, j), t + j);
-      if (x > 0.0 && (tk < 0 || left >= 0.0)) tk = t + j, wt = x;
+    sum_of(v, t, [&](double x, int token_at) __attribute__((always_inline)) {
+      if (x > 0.0 && (tk < 0 || left >= 0.0)) tk = token_at, wt = x;
       left -= x;
-    }
+    });
     token = __shfl(tk, who, 64);
     chosen = __shfl(wt, who, 64);
     if (reach != 0) break;
@@ -644,11 +731,8 @@ dark_status dark_sample(const dark_sample_params* p, const void* logits, const f
     return DARK_EINVAL;
   const sample::Setting set{temperature, top_p, min_p, top_k, p->temperature, p->top_p, p->min_p, p->top_k};
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  // whether a thread holds its pieces (a row may begin up to a piece before its first element)
-  const bool held = false && ((long long)p->V * (p->io_dtype == DARK_BF16 ? 2 : 4) + 32) / 16 <= (long long)sample::kThreads * sample::kHeld;
 #define DARK_SAMPLE(T)                                                                                                              \
-  if (held) DARK_LAUNCH(KID_SAMPLE, st, (sample::k_sample<T, true>), dim3(p->B), dim3(sample::kThreads), 0, static_cast<const T*>(logits), uniform, set, out_token, out_logprob, p->V); \
-  else DARK_LAUNCH(KID_SAMPLE, st, (sample::k_sample<T, false>), dim3(p->B), dim3(sample::kThreads), 0, static_cast<const T*>(logits), uniform, set, out_token, out_logprob, p->V)
+  DARK_LAUNCH(KID_SAMPLE, st, (sample::k_sample<T>), dim3(p->B), dim3(sample::kThreads), 0, static_cast<const T*>(logits), uniform, set, out_token, out_logprob, p->V)
   if (p->io_dtype == DARK_BF16) {
     DARK_SAMPLE(unsigned short);
   } else {
