@@ -71,10 +71,10 @@ dark_status launch_rev_f32(const Args& a, hipStream_t st);
 dark_status launch_grad_bf16(const Args& a, hipStream_t st);
 dark_status launch_grad_f32(const Args& a, hipStream_t st);
 
-// Four waves for 16 columns (delta_team.h): bf16 whose rows fill the tiles.
-bool team_supported(const Args& a);
-dark_status launch_team(const Args& a, Pass pass, hipStream_t st);
-dark_status launch_team_rev(const Args& a, hipStream_t st);
+// A team of waves for 16 columns (delta_team.h), for rows that fill the tiles.
+bool team_supported(const Args& a, bool bf16);
+dark_status launch_team(const Args& a, bool bf16, Pass pass, hipStream_t st);
+dark_status launch_team_rev(const Args& a, bool bf16, hipStream_t st);
 
 // Rows of the state that the kernels hold.
 inline int inner_of(int dk) { return dk > 128 ? 256 : dk > 64 ? 128 : 64; }

@@ -157,8 +157,9 @@ static dark_status prep(const Problem& pb, const Args& a, bool backward) {
   return pb.p.io_dtype == DARK_BF16 ? launch_prep_bf16(a, backward, pb.st) : launch_prep_f32(a, backward, pb.st);
 }
 static dark_status scan(const Problem& pb, const Args& a, Pass pass) {
-  if (pb.p.io_dtype == DARK_BF16 && team_supported(a)) return launch_team(a, pass, pb.st);
-  return pb.p.io_dtype == DARK_BF16 ? launch_scan_bf16(a, pass, pb.st) : launch_scan_f32(a, pass, pb.st);
+  const bool bf16 = pb.p.io_dtype == DARK_BF16;
+  if (team_supported(a, bf16)) return launch_team(a, bf16, pass, pb.st);
+  return bf16 ? launch_scan_bf16(a, pass, pb.st) : launch_scan_f32(a, pass, pb.st);
 }
 
 static dark_status step(const Problem& pb, const void* q, const void* k, const void* v, const float* log_gate, const float* beta,
@@ -311,7 +312,8 @@ dark_status dark_delta_bwd(const dark_delta_params* p, const void* Q, const void
   const bool bf16 = pb.p.io_dtype == DARK_BF16;
   a.s_in = dS_out;
   a.s_out = dS_in;
-  DARK_TRY(!bf16 ? delta::launch_rev_f32(a, pb.st) : delta::team_supported(a) ? delta::launch_team_rev(a, pb.st) : delta::launch_rev_bf16(a, pb.st));
+  if (delta::team_supported(a, bf16)) DARK_TRY(delta::launch_team_rev(a, bf16, pb.st));
+  else DARK_TRY(bf16 ? delta::launch_rev_bf16(a, pb.st) : delta::launch_rev_f32(a, pb.st));
   if (!grads || pb.p.L == 0) return DARK_OK;
   return bf16 ? delta::launch_grad_bf16(a, pb.st) : delta::launch_grad_f32(a, pb.st);
 }

@@ -225,8 +225,8 @@ struct Bases {
   }
 };
 
-// The loading waves: chunk after chunk (REV: from the last to the first), one ahead.
-template <typename L, typename T, int D1, int NP, bool VEC, bool REV>
+// The loading waves: chunk after chunk (REV: from the last to the first), one ahead.  MORE: barriers of a chunk behind its second.
+template <typename L, typename T, int D1, int NP, bool VEC, bool REV, int MORE = 0>
 __device__ static inline void load_chunks(const Args& A, int bh, const Rows& xk, const Rows& xq, const Rows& xv, int n, int tid) {
   constexpr int C = L::C, NB = L::NB, NTH = L::NTH;
   const int chunks = (n + C - 1) / C;
@@ -260,12 +260,14 @@ __device__ static inline void load_chunks(const Args& A, int bh, const Rows& xk,
   if (chunks > 1) load(1);
   lds_barrier();
   for (int i = 0; i < chunks; ++i) {
-    if (L::kBufs == 1) lds_barrier();   // the chunk's readers are done
+    if (L::kBufs == 1 || MORE > 0) lds_barrier();   // with one buffer: the chunk's readers are done
     if (i + 1 < chunks) {
       store((i + 1) % L::kBufs);
       if (i + 2 < chunks) load(i + 2);
     }
     lds_barrier();
+#pragma unroll
+    for (int k = 0; k < MORE; ++k) lds_barrier();
   }
 }
 // The computing waves: f(chunk, the buffer of its operands, a constant) for every chunk.
@@ -471,9 +473,9 @@ __global__ __launch_bounds__((Chunks<T, D1, NW, 3>::kThreads)) void k_delta_rev(
     constexpr int buf = decltype(buffer_of)::value, tk = buf * MK::kAll, tq = base.kFar ? buf * MK::kAll : L::q + buf * MK::kAll, tv = buf * L::kV, tt = buf * L::kT, tp = buf * L::kP, tw = buf * L::kW;
     const int rb = base.rows, cb = base.cols, qb = base.query_cols, vb = base.value, tb = base.tri, pb = base.weights, wb = base.vec;
     put_columns<KT>(G, A.dstates + chunk_at(A, bh, c) * ((long long)D1 * A.dvp), D1, A.dvp, c0, l);
-    f32x4 U[NT], R[NT];
+    f32x4 U[NT], R[NT], W[NT];
 #pragma unroll
-    for (int r = 0; r < NT; ++r) U[r] = R[r] = zero4();
+    for (int r = 0; r < NT; ++r) U[r] = R[r] = W[r] = zero4();
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
       Planes<NI> k[NT];
@@ -481,14 +483,14 @@ __global__ __launch_bounds__((Chunks<T, D1, NW, 3>::kThreads)) void k_delta_rev(
       for (int r = 0; r < NT; ++r) k[r] = MK::row(tk, rb, r, s);
       mma_rows<NI, 3>(k, split<3>(G[2 * s], G[2 * s + 1]), U);
     }
-#pragma unroll
-    for (int r = 0; r < NT; ++r) U[r] *= lds_get<f32x4>(wb + tw + 4 * (C + 16 * r));
     {
       Planes<NI> b[NS];
 #pragma unroll
       for (int s = 0; s < NS; ++s) b[s] = MV::col(tv, vb, 0, s);
-      mma_tri<C, false, false, 3, NI, 3>(tp, pb, b, U);
+      mma_tri<C, false, false, 3, NI, 3>(tp, pb, b, W);
     }
+#pragma unroll
+    for (int r = 0; r < NT; ++r) U[r] = lds_get<f32x4>(wb + tw + 4 * (C + 16 * r)) * U[r] + W[r];
     {
       Planes<3> b[NS];
 #pragma unroll

@@ -1,20 +1,19 @@
-// The gated delta rule's scans with four waves for 16 columns of the state: bf16 rows that fill the tiles (see delta_scan.h for those of one wave).
+// The gated delta rule's scans with a wave for each row tile of 16 columns: rows that fill the tiles (see delta_scan.h for one wave that does all).
 //
 // A wave takes an instruction in seven to twelve cycles, whatever it is, where the chunks' states hang on each other; what a SIMD does in that
-// time grows with its waves.  So the 16 columns' work is dealt to four waves: each has one of the chunk's row tiles and a quarter of the
-// state's rows.  What a wave has as sums and all four need as an operand goes through
-// LDS: the state's planes, R, and U, with a barrier behind each.  Two waves bring the operands, a part between two barriers: the loads of a whole
-// chunk at once keep their wave from the first barrier for as long as a third of the chunk takes.
-// (One wave and four: prompt of 16 x 777 x 128 42 -> 27 us, prefill of 64 x 8192 x 128 415 -> 322, 24 x 4096 x 64 as training runs it 122 -> 78 and
-// backward 160 -> 100; two waves with all loads at once were no faster than one.)
+// time grows with its waves, and a CU with its SIMDs.  So the 16 columns' work is dealt to a team, four waves for bf16's chunks of 64 rows and two for
+// fp32's of 32: each has one of the chunk's row tiles and a part of the state's rows.  What a wave has as sums and all need as an operand goes
+// through LDS: the state's planes, R, and U, with a barrier behind each.  Of bf16 two waves bring the operands by loads that end in LDS, a part between two
+// barriers (a whole chunk's at once keep their wave from the first barrier for a third of the chunk); of fp32 four take them through registers.
+// (One wave and a team: prompt of 16 x 777 x 128 42 -> 27 us, prefill of 64 x 8192 x 128 415 -> 322, 24 x 4096 x 64 as training runs it 122 -> 78 and
+// backward 160 -> 101; of fp32 1000 rows of 8 heads of 64 58 -> 50, backward 70 -> 62.  Two waves of bf16 with all loads at once were no faster than one.)
+// Sums of fp32 operands add up in the same order in both, so that a sequence's results do not depend on how many others there are.
 #pragma once
 
 #include "delta_scan.h"
 
 namespace dark {
 namespace delta {
-
-constexpr int kTeam = 4, kTeamLoaders = 2;   // waves of a team, and waves that load
 
 // Half of an operand: what a tile's four values of a lane are in it.
 template <int N>
@@ -30,18 +29,22 @@ __device__ static inline Half<N> split_half(f32x4 a) {
   return h;
 }
 
-// Operands in LDS: K, V (dO), vectors and one triangle for two chunks; what is needed late in a chunk for one: P forward, Q and T backward.
-template <int D1, int TEAMS, int NP, bool REV>
+// Operands in LDS for two chunks, or, of bf16, for one what is needed late in a chunk: P forward, Q and T backward.
+template <typename T_, int D1, int TEAMS, int NP, bool REV>
 struct TeamChunks {
-  static constexpr int C = 64, NB = 6, VC = 16 * TEAMS, KS = D1 / 32, kThreads = 64 * (kTeam * TEAMS + kTeamLoaders);
-  typedef Mat<C, D1, 1> MK;
-  typedef Mat<C, VC, 1> MV;
+  typedef T_ T;
+  static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C), VC = 16 * TEAMS, KS = D1 / 32;
+  static constexpr bool kDirect = sizeof(T) == 2;
+  static constexpr int kTeam = C / 16, kOwn = D1 / 16 / kTeam;   // waves of a team, tiles of the state of each
+  static constexpr int kLoaders = kDirect ? 2 : 4, kThreads = 64 * (kTeam * TEAMS + kLoaders), NTH = 64 * kLoaders, kBufs = 2;
+  typedef Mat<C, D1, NI> MK;
+  typedef Mat<C, VC, NI> MV;
   static constexpr int kQ = NP > 0 ? MK::kAll : 0, kV = MV::kAll, kW = kScanVecs * C * 4, kT = 3 * NB * 1024, kP = NP * NB * 1024;
-  static constexpr int qs = REV ? 1 : 2, ts = REV ? 1 : 2, ps = REV ? 2 : 1;   // buffers
+  static constexpr int qs = kDirect && REV ? 1 : 2, ts = kDirect && REV ? 1 : 2, ps = kDirect && !REV ? 1 : 2;   // buffers
   static constexpr int k = 0, q = 2 * MK::kAll, v = q + qs * kQ, w = v + 2 * kV, t = w + 2 * kW, p = t + ts * kT, x = p + ps * kP;
   // exchange, of a team: the state's planes, in their place later U's (those of the update, and those of P U or of dO); R's
-  static constexpr int kMore = REV ? 6 * 1024 : 2 * NP * 1024;
-  static constexpr int kFirst = KS * 3 * 1024, kLast = 6 * 1024 + kMore, x1 = 0, x2 = kFirst > kLast ? kFirst : kLast, kX = x2 + 6 * 1024;
+  static constexpr int NS = C / 32, kRows = 3 * 1024 * NS, kMore = REV ? kRows : NP * 1024 * NS;
+  static constexpr int kFirst = KS * 3 * 1024, kLast = kRows + kMore, x1 = 0, x2 = kFirst > kLast ? kFirst : kLast, kX = x2 + kRows;
   static constexpr int all = x + TEAMS * kX;
   static_assert(all <= 160 * 1024, "fits the LDS");
 };
@@ -182,35 +185,43 @@ __device__ static inline void load_rest(const Args& A, int bh, const Rows& xv, i
   }
 }
 
-// A lane's bases: those of row tile h, and of the wave's quarter of the state's rows.
+template <typename L, int D1, int NP, bool REV>
+__device__ static inline void load_team(const Args& A, int bh, const void* values, int col0, int n, int tid) {
+  typedef typename L::T T;
+  const Rows xv = rows_at<T>(values, A, bh, A.dv, n, col0, L::VC);
+  if constexpr (L::kDirect) {
+    if (tid < 64) load_keys<L, D1, NP, REV>(A, bh, n, tid);
+    else load_rest<L, D1, NP, REV>(A, bh, xv, n, tid - 64);
+  } else {
+    load_chunks<L, T, D1, NP, true, REV, 2>(A, bh, rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk), xv, n, tid);
+  }
+}
+
+// A lane's bases: those of row tile h, and of the wave's part of the state's rows.
 template <typename L, bool REV>
 struct TeamBases {
-  static constexpr int RB = L::MK::RB, RV = L::MV::RB, kOwn = RB / 128;   // column tiles of K that are the wave's rows of the state
-  int rows, cols, value, vec, row, tri, weights, planes, own, half;
+  static constexpr int RB = L::MK::RB, RV = L::MV::RB;
+  int rows, query, cols, query_cols, value, vec, row, tri, weights, planes, own, half;
   __device__ TeamBases(Lane l, int lane, int team, int h) {
     rows = L::MK::row_base(l) + h * 16 * RB;
-    cols = L::MK::col_base(l) ^ (h * kOwn << 5);
+    cols = L::MK::col_base(l) ^ (h * L::kOwn << 5);
+    query = rows + L::q;
+    query_cols = cols + L::q;
     value = (L::MV::col_base(l) ^ (team << 5)) + h * 16 * RV + L::v;
     vec = 16 * l.g + L::w + 64 * h;
     row = 4 * l.i + L::w + 64 * h;
-    // a lower triangle's row tile has block (h, 0), and (h, 1) behind it; of an upper one (h, 1), and (h, 0) before it
-    const int first = REV ? (h < 2 ? 2 * h + 1 : h + 2) : h < 2 ? h : 2 * h - 2;
+    // of two steps a lower triangle's row tile has block (h, 0), and (h, 1) behind it; of an upper one (h, 1), and (h, 0) before it
+    const int first = L::NS == 1 ? h : REV ? (h < 2 ? 2 * h + 1 : h + 2) : h < 2 ? h : 2 * h - 2;
     tri = 16 * lane + L::t + 1024 * first;
     weights = 16 * lane + L::p + 1024 * first;
     planes = 16 * lane + L::x + team * L::kX;
-    own = planes + (kOwn == 2 ? h * 3 * 1024 : (h >> 1) * 3 * 1024 + 8 * (h & 1));
+    own = planes + (L::kOwn > 1 ? h * (L::kOwn / 2) * 3 * 1024 : (h >> 1) * 3 * 1024 + 8 * (h & 1));
     half = planes + 8 * (h & 1);
 #pragma unroll
-    for (int* p : {&rows, &cols, &value, &vec, &row, &tri, &weights, &planes, &own, &half}) asm("" : "+v"(*p));
+    for (int* p : {&rows, &query, &cols, &query_cols, &value, &vec, &row, &tri, &weights, &planes, &own, &half}) asm("" : "+v"(*p));
   }
 };
 
-// Inner values 32 s ... of a row at a base of its own.
-__device__ static inline u32x4 row_at(int base, int s) {
-  const int at = base ^ (s << 6);
-  const u32x2 a = lds_get<u32x2>(at), b = lds_get<u32x2>(at ^ 32);
-  return u32x4{a[0], a[1], b[0], b[1]};
-}
 template <int N>
 __device__ static inline void put_half(int at, const Half<N>& f) {
 #pragma unroll
@@ -223,14 +234,25 @@ __device__ static inline Planes<N> get_planes(int at) {
   for (int p = 0; p < N; ++p) f.p[p] = lds_get<u32x4>(at + 1024 * p);
   return f;
 }
-template <int M>
-__device__ static inline void get_block(u32x4 (&t)[M], int at) {
+template <int NB, int M>
+__device__ static inline Planes<M> get_block(int at) {
+  Planes<M> t;
 #pragma unroll
-  for (int i = 0; i < M; ++i) t[i] = lds_get<u32x4>(at + i * 6 * 1024);
+  for (int i = 0; i < M; ++i) t.p[i] = lds_get<u32x4>(at + i * NB * 1024);
+  return t;
 }
-// The four values of a tile's column from two words of bf16.
-__device__ static inline f32x4 widen(u32x2 v) {
-  return f32x4{__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xffff0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xffff0000u)};
+// The four values of a tile's column.
+template <typename M, int N>
+__device__ static inline f32x4 column(int at) {
+  f32x4 x;
+#pragma unroll
+  for (int p = N - 1; p >= 0; --p) {
+    const u32x2 v = lds_get_tr16(at + p * M::kBytes);
+    const f32x4 y = {__uint_as_float(v[0] << 16), __uint_as_float(v[0] & 0xffff0000u), __uint_as_float(v[1] << 16), __uint_as_float(v[1] & 0xffff0000u)};
+    if (p == N - 1) x = y;
+    else x += y;
+  }
+  return x;
 }
 // A tile's column to scratch.
 __device__ static inline void put_tile(f32x4 v, Buffer b, int row, int stride, int c0, Lane l) {
@@ -238,129 +260,150 @@ __device__ static inline void put_tile(f32x4 v, Buffer b, int row, int stride, i
 #pragma unroll
   for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), b, at, (unsigned)(j * stride) * 4u, 0);
 }
-// x + t b for one block of a triangle in M planes (TRANS: b t).
-template <int M, int N, bool TRANS>
-__device__ static inline f32x4 mma_block(const u32x4 (&t)[M], const Planes<N>& b, f32x4 x) {
-  constexpr int W = M > N ? M : N;
+// x + sum_s a_s b_s: one chain (two, and their sum behind them, take longer: instructions count, not what a product waits for).  With one plane on a
+// side all operands are there before the first product: one wait.
+template <int MA, int MB, int S, int NA, int NB>
+__device__ static inline f32x4 mma_steps(const Planes<NA> (&a)[S], const Planes<NB> (&b)[S], f32x4 x) {
+  if constexpr (MA == 1 || MB == 1) {
 #pragma unroll
-  for (int w = W - 1; w >= 0; --w)
+    for (int i = (MA > MB ? MA : MB) - 1; i >= 0; --i)
 #pragma unroll
-    for (int i = 0; i < M; ++i)
-      if (w - i >= 0 && w - i < N) x = TRANS ? mma1(b.p[w - i], t[i], x) : mma1(t[i], b.p[w - i], x);
+      for (int s = 0; s < S; ++s) x = mma1(a[s].p[MA > 1 ? i : 0], b[s].p[MB > 1 ? i : 0], x);
+  } else {
+#pragma unroll
+    for (int s = 0; s < S; ++s) x = mma_of<MA, MB>(a[s], b[s], x);
+  }
   return x;
+}
+// x + t b for a triangle's block, the smallest terms first; of fp32 (STEP) in the order of mma_step (TRANS: b t).
+template <bool STEP, bool TRANS, int M, int N>
+__device__ static inline f32x4 mma_block(const Planes<M>& t, const Planes<N>& b, f32x4 x) {
+  constexpr int W = M > N ? M : N;
+  if constexpr (!STEP) return TRANS ? mma(b, t, x) : mma(t, b, x);
+#pragma unroll
+  for (int i = M - 1; i >= 0; --i)
+#pragma unroll
+    for (int j = W - 1 - i; j >= 0; --j)
+      if (j < N) x = TRANS ? mma1(b.p[j], t.p[i], x) : mma1(t.p[i], b.p[j], x);
+  return x;
+}
+// The computing waves: f(chunk, the buffer of its operands, a constant) for every chunk.
+template <bool REV, typename F>
+__device__ static inline void each_chunk_of_team(int chunks, const F& f) {
+  lds_barrier();
+  for (int i = 0; i < chunks;) {
+    f(REV ? chunks - 1 - i : i, std::integral_constant<int, 0>());
+    if (++i == chunks) break;
+    f(REV ? chunks - 1 - i : i, std::integral_constant<int, 1>());
+    ++i;
+  }
 }
 // The wave's rows of the state as planes, where the team reads them.
 template <int OWN>
 __device__ static inline void put_state(const f32x4 (&S)[OWN], int own) {
-  if constexpr (OWN == 2) {
-    const Planes<3> f = split<3>(S[0], S[1]);
+  if constexpr (OWN > 1) {
 #pragma unroll
-    for (int p = 0; p < 3; ++p) lds_put(own + 1024 * p, f.p[p]);
+    for (int s = 0; s < OWN / 2; ++s) {
+      const Planes<3> f = split<3>(S[2 * s], S[2 * s + 1]);
+#pragma unroll
+      for (int p = 0; p < 3; ++p) lds_put(own + 1024 * (3 * s + p), f.p[p]);
+    }
   } else {
     put_half<3>(own, split_half<3>(S[0]));
   }
 }
+// The state's rows, as planes, times the same rows of K (Q): x_kt + cols_kt u, for the wave's tiles.
+template <typename L, int N>
+__device__ static inline void mma_update(const Planes<L::NI> (&k)[N][L::NS], const Planes<3> (&u)[L::NS], f32x4 (&S)[N]) {
+  constexpr int NI = L::NI;
+#pragma unroll
+  for (int w = 2; w >= 0; --w)
+#pragma unroll
+    for (int i = 0; i < NI; ++i)
+      if (w - i >= 0)
+#pragma unroll
+        for (int s = 0; s < L::NS; ++s)
+#pragma unroll
+          for (int kt = 0; kt < N; ++kt) S[kt] = mma1(k[kt][s].p[i], u[s].p[w - i], S[kt]);
+}
 
-template <int D1, int TEAMS, bool FWD>
-__global__ __launch_bounds__((TeamChunks<D1, TEAMS, (FWD ? 2 : 0), false>::kThreads)) void k_delta_team(Args A) {
-  constexpr int NO = 2, NP = FWD ? NO : 0;
-  typedef TeamChunks<D1, TEAMS, NP, false> L;
-  constexpr int C = L::C, KS = D1 / 32, OWN = D1 / 64;
+template <typename T, int D1, int TEAMS, bool FWD>
+__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, (FWD ? Kind<T>::kOut : 0), false>::kThreads)) void k_delta_team(Args A) {
+  constexpr int NO = Kind<T>::kOut, NP = FWD ? NO : 0;
+  typedef TeamChunks<T, D1, TEAMS, NP, false> L;
+  constexpr int C = L::C, KS = L::KS, NS = L::NS, NB = L::NB, NI = L::NI, OWN = L::kOwn, TEAM = L::kTeam;
   typedef typename L::MK MK;
-  typedef unsigned short T;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, team = wave / kTeam, h = wave % kTeam;
+  typedef typename L::MV MV;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, team = wave / TEAM, h = wave % TEAM;
   const int bh = blockIdx.x, col0 = blockIdx.y * L::VC, n = length_of(A, bh), c0 = col0 + 16 * team, chunks = (n + C - 1) / C;
   const Lane l{lane & 15, lane >> 4};
   const Rows xo = rows_at<T>(A.out, A, bh, A.dv, n, col0, L::VC);
   if (FWD && n < A.L) zero_rows<T>(xo, n, A.L, tid, L::kThreads);
-  if (wave >= kTeam * TEAMS) {
-    if (chunks == 0) return;
-    if (wave == kTeam * TEAMS) load_keys<L, D1, NP, false>(A, bh, n, lane);
-    else load_rest<L, D1, NP, false>(A, bh, rows_at<T>(A.V, A, bh, A.dv, n, col0, L::VC), n, lane);
+  if (wave >= TEAM * TEAMS) {
+    if (chunks > 0) load_team<L, D1, NP, false>(A, bh, A.V, col0, n, tid - 64 * TEAM * TEAMS);
     return;
   }
   f32x4 S[OWN];
 #pragma unroll
   for (int kt = 0; kt < OWN; ++kt) S[kt] = zero4();
-  if (A.s_in != nullptr) load_state<OWN, true>(S, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g, h * (D1 / 4));
+  if (A.s_in != nullptr) load_state<OWN, true>(S, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g, h * 16 * OWN);
   const TeamBases<L, false> base(l, lane, team, h);
-  const bool two = h >= 2;   // blocks of the wave's row tile
+  const bool two = NS == 2 && h >= 2;   // blocks of the wave's row tile
   const auto step = [&](int c, auto buffer_of) {
-    constexpr int buf = decltype(buffer_of)::value, tk = buf * MK::kAll, tq = L::q + buf * L::kQ, tv = buf * L::kV, tt = buf * L::kT, tw = buf * L::kW;
+    constexpr int buf = decltype(buffer_of)::value, tk = buf * MK::kAll, tq = buf * L::kQ, tv = buf * L::kV, tt = buf * L::kT, tp = L::ps == 2 ? buf * L::kP : 0, tw = buf * L::kW;
     const int r0 = c * C, nr = min(C, n - r0);
     put_state(S, base.own);
     if (!FWD) {
       const Buffer to = buffer(A.states + chunk_at(A, bh, c) * ((long long)D1 * A.dvp), (unsigned)(D1 * A.dvp) * 4u);
 #pragma unroll
-      for (int kt = 0; kt < OWN; ++kt) put_tile(S[kt], to, h * (D1 / 4) + 16 * kt, A.dvp, c0, l);
+      for (int kt = 0; kt < OWN; ++kt) put_tile(S[kt], to, h * 16 * OWN + 16 * kt, A.dvp, c0, l);
     }
-    u32x4 k[KS], q[KS];
+    Planes<NI> k[KS], q[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      k[s] = row_at(base.rows + tk, s);
-      if (FWD) q[s] = row_at(base.rows + tq, s);
+      k[s] = MK::row(tk, base.rows, 0, s);
+      if (FWD) q[s] = MK::row(tq, base.query, 0, s);
     }
     const f32x4 gamma = lds_get<f32x4>(base.vec + tw), left = lds_get<f32x4>(base.vec + tw + 4 * C), beta = lds_get<f32x4>(base.vec + tw + 4 * 2 * C);
-    const f32x4 V = widen(lds_get_tr16(base.value + tv));
+    const f32x4 V = column<MV, NI>(base.value + tv);
     lds_barrier();
     Planes<3> b[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) b[s] = get_planes<3>(base.planes + 3 * 1024 * s);
-    f32x4 R = zero4(), O = zero4(), U = zero4();
-#pragma unroll
-    for (int i = 2; i >= 0; --i)
-#pragma unroll
-      for (int s = 0; s < KS; ++s) R = mma1(k[s], b[s].p[i], R);
+    const f32x4 R = mma_steps<NI, 3>(k, b, zero4());
     put_half<3>(base.half + L::x2 + (h >> 1) * 3 * 1024, split_half<3>(beta * (V - gamma * R)));
-    u32x4 t0[3], t1[3];
-    get_block<3>(t0, base.tri + tt);
-    get_block<3>(t1, base.tri + tt + (two ? 1024 : 0));
-    if (FWD) {
-#pragma unroll
-      for (int i = NO - 1; i >= 0; --i)
-#pragma unroll
-        for (int s = 0; s < KS; ++s) O = mma1(b[s].p[i], q[s], O);
-    }
+    Planes<3> t[2] = {get_block<NB, 3>(base.tri + tt)};
+    if (NS == 2) t[1] = get_block<NB, 3>(base.tri + tt + (two ? 1024 : 0));
+    f32x4 O = zero4(), U = zero4();
+    if (FWD) O = mma_steps<NO, NI>(b, q, O);
     lds_barrier();
     {
-      const Planes<3> r0 = get_planes<3>(base.planes + L::x2);
-      if (two) {
-        const Planes<3> r1 = get_planes<3>(base.planes + L::x2 + 3 * 1024);
-        U = mma_block<3, 3, false>(t1, r1, U);
-      }
-      U = mma_block<3, 3, false>(t0, r0, U);
+      const Planes<3> r = get_planes<3>(base.planes + L::x2);
+      if (two) U = mma_block<NI == 3, false>(t[1], get_planes<3>(base.planes + L::x2 + 3 * 1024), U);
+      U = mma_block<NI == 3, false>(t[0], r, U);
     }
     put_half<3>(base.half + (h >> 1) * 3 * 1024, split_half<3>(left * U));
-    if (FWD) put_half<NO>(base.half + 6 * 1024 + (h >> 1) * NO * 1024, split_half<NO>(U));
+    if (FWD) put_half<NO>(base.half + L::kRows + (h >> 1) * NO * 1024, split_half<NO>(U));
     const float Gamma = lds_get<float>(base.vec + tw + 4 * 3 * C);
-    u32x4 kt0[OWN], kt1[OWN];
+    Planes<NI> kc[OWN][NS];
 #pragma unroll
     for (int kt = 0; kt < OWN; ++kt) {
       S[kt] *= Gamma;
-      kt0[kt] = MK::col(tk, base.cols, kt, 0).p[0];
-      kt1[kt] = MK::col(tk, base.cols, kt, 1).p[0];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) kc[kt][s] = MK::col(tk, base.cols, kt, s);
     }
     lds_barrier();
     {
-      const Planes<3> u0 = get_planes<3>(base.planes), u1 = get_planes<3>(base.planes + 3 * 1024);
+      Planes<3> u[NS];
 #pragma unroll
-      for (int i = 2; i >= 0; --i) {
-#pragma unroll
-        for (int kt = 0; kt < OWN; ++kt) S[kt] = mma1(kt0[kt], u0.p[i], S[kt]);
-#pragma unroll
-        for (int kt = 0; kt < OWN; ++kt) S[kt] = mma1(kt1[kt], u1.p[i], S[kt]);
-      }
+      for (int s = 0; s < NS; ++s) u[s] = get_planes<3>(base.planes + 3 * 1024 * s);
+      mma_update<L>(kc, u, S);
     }
     if (FWD) {
-      u32x4 p0[NO];
-      get_block<NO>(p0, base.weights);
+      const Planes<NO> p0 = get_block<NB, NO>(base.weights + tp), u0 = get_planes<NO>(base.planes + L::kRows);
       O *= lds_get<float>(base.row + tw);
-      if (two) {
-        u32x4 p1[NO];
-        get_block<NO>(p1, base.weights + 1024);
-        O = mma_block<NO, NO, true>(p1, get_planes<NO>(base.planes + 6 * 1024 + NO * 1024), O);
-      }
-      O = mma_block<NO, NO, true>(p0, get_planes<NO>(base.planes + 6 * 1024), O);
+      if (two) O = mma_block<NI == 3, true>(get_block<NB, NO>(base.weights + tp + 1024), get_planes<NO>(base.planes + L::kRows + NO * 1024), O);
+      O = mma_block<NI == 3, true>(p0, u0, O);
       const int row = 16 * h + l.i;
       buffer_quad<T>(xo.rows(r0, nr), row < nr ? (unsigned)row * xo.row + (unsigned)((16 * team + 4 * l.g) * (int)sizeof(T)) : kNowhere, A.scale * O);
     } else {
@@ -368,163 +411,136 @@ __global__ __launch_bounds__((TeamChunks<D1, TEAMS, (FWD ? 2 : 0), false>::kThre
     }
     lds_barrier();
   };
-  if (chunks > 0) {
-    lds_barrier();
-    for (int i = 0; i < chunks;) {
-      step(i, std::integral_constant<int, 0>());
-      if (++i == chunks) break;
-      step(i, std::integral_constant<int, 1>());
-      ++i;
-    }
-  }
-  if (A.s_out != nullptr) store_state<OWN>(S, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g, h * (D1 / 4));
+  if (chunks > 0) each_chunk_of_team<false>(chunks, step);
+  if (A.s_out != nullptr) store_state<OWN>(S, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g, h * 16 * OWN);
 }
 
-template <int D1, int TEAMS>
-__global__ __launch_bounds__((TeamChunks<D1, TEAMS, 3, true>::kThreads)) void k_delta_team_rev(Args A) {
-  typedef TeamChunks<D1, TEAMS, 3, true> L;
-  constexpr int C = L::C, KS = D1 / 32, OWN = D1 / 64;
+template <typename T, int D1, int TEAMS>
+__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true>::kThreads)) void k_delta_team_rev(Args A) {
+  typedef TeamChunks<T, D1, TEAMS, 3, true> L;
+  constexpr int C = L::C, KS = L::KS, NS = L::NS, NB = L::NB, NI = L::NI, OWN = L::kOwn, TEAM = L::kTeam;
   typedef typename L::MK MK;
   typedef typename L::MV MV;
-  typedef unsigned short T;
-  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, team = wave / kTeam, h = wave % kTeam;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, team = wave / TEAM, h = wave % TEAM;
   const int bh = blockIdx.x, col0 = blockIdx.y * L::VC, n = length_of(A, bh), c0 = col0 + 16 * team, chunks = (n + C - 1) / C;
   const Lane l{lane & 15, lane >> 4};
-  if (wave >= kTeam * TEAMS) {
-    if (chunks == 0) return;
-    if (wave == kTeam * TEAMS) load_keys<L, D1, 3, true>(A, bh, n, lane);
-    else load_rest<L, D1, 3, true>(A, bh, rows_at<T>(A.dOut, A, bh, A.dv, n, col0, L::VC), n, lane);
+  if (wave >= TEAM * TEAMS) {
+    if (chunks > 0) load_team<L, D1, 3, true>(A, bh, A.dOut, col0, n, tid - 64 * TEAM * TEAMS);
     return;
   }
   f32x4 G[OWN];
 #pragma unroll
   for (int kt = 0; kt < OWN; ++kt) G[kt] = zero4();
-  if (A.s_in != nullptr) load_state<OWN, true>(G, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g, h * (D1 / 4));
+  if (A.s_in != nullptr) load_state<OWN, true>(G, A.s_in + (long long)bh * A.dk * A.dv, A.dk, A.dv, 0, c0 + l.i, l.g, h * 16 * OWN);
   const TeamBases<L, true> base(l, lane, team, h);
-  const bool two = h < 2;
+  const bool two = NS == 2 && h < 2;
   int vc = (MV::col_base(l) ^ (team << 5)) + L::v;
   asm("" : "+v"(vc));
   const auto step = [&](int c, auto buffer_of) {
-    constexpr int buf = decltype(buffer_of)::value, tk = buf * MK::kAll, tv = buf * L::kV, tp = buf * L::kP, tw = buf * L::kW;
+    constexpr int buf = decltype(buffer_of)::value, tk = buf * MK::kAll, tq = L::qs == 2 ? buf * L::kQ : 0, tv = buf * L::kV, tt = L::ts == 2 ? buf * L::kT : 0, tp = buf * L::kP, tw = buf * L::kW;
     put_state(G, base.own);
     {
       const Buffer to = buffer(A.dstates + chunk_at(A, bh, c) * ((long long)D1 * A.dvp), (unsigned)(D1 * A.dvp) * 4u);
 #pragma unroll
-      for (int kt = 0; kt < OWN; ++kt) put_tile(G[kt], to, h * (D1 / 4) + 16 * kt, A.dvp, c0, l);
+      for (int kt = 0; kt < OWN; ++kt) put_tile(G[kt], to, h * 16 * OWN + 16 * kt, A.dvp, c0, l);
     }
-    u32x4 k[KS];
+    Planes<NI> k[KS];
 #pragma unroll
-    for (int s = 0; s < KS; ++s) k[s] = row_at(base.rows + tk, s);
+    for (int s = 0; s < KS; ++s) k[s] = MK::row(tk, base.rows, 0, s);
     const f32x4 gamma = lds_get<f32x4>(base.vec + tw), left = lds_get<f32x4>(base.vec + tw + 4 * C), beta = lds_get<f32x4>(base.vec + tw + 4 * 2 * C);
-    f32x4 U = zero4(), R = zero4(), D = zero4();
+    f32x4 D = zero4();
     {
-      u32x4 p1[3];
-      get_block<3>(p1, base.weights + tp);
-      const u32x4 o1 = MV::col(tv, vc, 0, 1).p[0];
-#pragma unroll
-      for (int i = 2; i >= 0; --i) D = mma1(p1[i], o1, D);
-      if (two) {
-        u32x4 p0[3];
-        get_block<3>(p0, base.weights + tp - 1024);
-        const u32x4 o0 = MV::col(tv, vc, 0, 0).p[0];
-#pragma unroll
-        for (int i = 2; i >= 0; --i) D = mma1(p0[i], o0, D);
-      }
+      const Planes<3> p1 = get_block<NB, 3>(base.weights + tp);
+      const Planes<NI> o1 = MV::col(tv, vc, 0, NS - 1);
+      if (two) D = mma_block<NI == 3, false>(get_block<NB, 3>(base.weights + tp - 1024), MV::col(tv, vc, 0, 0), D);
+      D = mma_block<NI == 3, false>(p1, o1, D);
     }
     lds_barrier();
     Planes<3> b[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) b[s] = get_planes<3>(base.planes + 3 * 1024 * s);
-#pragma unroll
-    for (int i = 2; i >= 0; --i)
-#pragma unroll
-      for (int s = 0; s < KS; ++s) U = mma1(k[s], b[s].p[i], U);
+    const f32x4 U = mma_steps<NI, 3>(k, b, zero4());
     put_half<3>(base.half + L::x2 + (h >> 1) * 3 * 1024, split_half<3>(left * U + D));
-    const Half<3> o = split_half<3>(A.scale * gamma * widen(lds_get_tr16(base.value + tv)));
+    const Half<3> o = split_half<3>(A.scale * gamma * column<MV, NI>(base.value + tv));
     lds_barrier();
+    f32x4 R = zero4();
     {
-      u32x4 t1[3];
-      get_block<3>(t1, base.tri);
-      const Planes<3> r1 = get_planes<3>(base.planes + L::x2 + 3 * 1024);
-      if (two) {
-        u32x4 t0[3];
-        get_block<3>(t0, base.tri - 1024);
-        R = mma_block<3, 3, false>(t0, get_planes<3>(base.planes + L::x2), R);
-      }
-      R = mma_block<3, 3, false>(t1, r1, R);
+      const Planes<3> t1 = get_block<NB, 3>(base.tri + tt), r1 = get_planes<3>(base.planes + L::x2 + (NS - 1) * 3 * 1024);
+      if (two) R = mma_block<NI == 3, false>(get_block<NB, 3>(base.tri + tt - 1024), get_planes<3>(base.planes + L::x2), R);
+      R = mma_block<NI == 3, false>(t1, r1, R);
     }
     put_half<3>(base.half + (h >> 1) * 3 * 1024, split_half<3>(-(gamma * beta) * R));
-    put_half<3>(base.half + 6 * 1024 + (h >> 1) * 3 * 1024, o);
+    put_half<3>(base.half + L::kRows + (h >> 1) * 3 * 1024, o);
     const float Gamma = lds_get<float>(base.vec + tw + 4 * 3 * C);
-    u32x4 kt0[OWN], kt1[OWN];
+    Planes<NI> kc[OWN][NS];
 #pragma unroll
     for (int kt = 0; kt < OWN; ++kt) {
       G[kt] *= Gamma;
-      kt0[kt] = MK::col(tk, base.cols, kt, 0).p[0];
-      kt1[kt] = MK::col(tk, base.cols, kt, 1).p[0];
+#pragma unroll
+      for (int s = 0; s < NS; ++s) kc[kt][s] = MK::col(tk, base.cols, kt, s);
     }
     lds_barrier();
     {
-      const Planes<3> u0 = get_planes<3>(base.planes), u1 = get_planes<3>(base.planes + 3 * 1024);
-      const Planes<3> o0 = get_planes<3>(base.planes + 6 * 1024), o1 = get_planes<3>(base.planes + 9 * 1024);
-      u32x4 q0[OWN], q1[OWN];
+      Planes<3> u[NS], w[NS];
+      Planes<NI> qc[OWN][NS];
 #pragma unroll
-      for (int kt = 0; kt < OWN; ++kt) {
-        q0[kt] = MK::col(L::q, base.cols, kt, 0).p[0];
-        q1[kt] = MK::col(L::q, base.cols, kt, 1).p[0];
+      for (int s = 0; s < NS; ++s) {
+        u[s] = get_planes<3>(base.planes + 3 * 1024 * s);
+        w[s] = get_planes<3>(base.planes + L::kRows + 3 * 1024 * s);
+#pragma unroll
+        for (int kt = 0; kt < OWN; ++kt) qc[kt][s] = MK::col(tq, base.query_cols, kt, s);
       }
-#pragma unroll
-      for (int i = 2; i >= 0; --i) {
-#pragma unroll
-        for (int kt = 0; kt < OWN; ++kt) G[kt] = mma1(kt0[kt], u0.p[i], G[kt]);
-#pragma unroll
-        for (int kt = 0; kt < OWN; ++kt) G[kt] = mma1(kt1[kt], u1.p[i], G[kt]);
-#pragma unroll
-        for (int kt = 0; kt < OWN; ++kt) G[kt] = mma1(q0[kt], o0.p[i], G[kt]);
-#pragma unroll
-        for (int kt = 0; kt < OWN; ++kt) G[kt] = mma1(q1[kt], o1.p[i], G[kt]);
-      }
+      mma_update<L>(qc, w, G);
+      mma_update<L>(kc, u, G);
     }
     put_tile(R, buffer(A.dr + chunk_at(A, bh, c) * ((long long)C * A.dvp), (unsigned)(C * A.dvp) * 4u), 16 * h, A.dvp, c0, l);
     lds_barrier();
   };
-  if (chunks > 0) {
-    lds_barrier();
-    for (int i = 0; i < chunks;) {
-      step(chunks - 1 - i, std::integral_constant<int, 0>());
-      if (++i == chunks) break;
-      step(chunks - 1 - i, std::integral_constant<int, 1>());
-      ++i;
-    }
-  }
-  if (A.s_out != nullptr) store_state<OWN>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g, h * (D1 / 4));
+  if (chunks > 0) each_chunk_of_team<true>(chunks, step);
+  if (A.s_out != nullptr) store_state<OWN>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g, h * 16 * OWN);
 }
 
-// Whether a call takes these kernels.
-static bool teamed(const Args& a) { return (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0; }
+// Whether a call takes these kernels: rows that fill the tiles; of fp32, whose operands go through registers, while each team has a CU to itself.
+constexpr int kCUs = 256;
+static bool one_team(const Args& a) { return (long long)a.B * a.H * (a.dv / 16) <= kCUs; }
+template <typename T>
+static bool teamed(const Args& a) { return (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0 && (sizeof(T) == 2 || one_team(a)); }
 
 // One team a workgroup as long as each of those has a CU to itself: the reads of LDS, 128 bytes a cycle, are what two share (24 x 4096 x 64 with
 // one and two: 78 and 98 us, backward 100 and 124).
-constexpr int kCUs = 256;
-template <int D1, int TEAMS, bool FWD>
+template <typename T, int D1, int TEAMS, bool FWD>
 static dark_status go_team(const Args& a, hipStream_t st) {
-  typedef TeamChunks<D1, TEAMS, (FWD ? 2 : 0), false> L;
-  DARK_TRY(allow_lds(k_delta_team<D1, TEAMS, FWD>, L::all));
-  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_team<D1, TEAMS, FWD>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
+  typedef TeamChunks<T, D1, TEAMS, (FWD ? Kind<T>::kOut : 0), false> L;
+  DARK_TRY(allow_lds(k_delta_team<T, D1, TEAMS, FWD>, L::all));
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_team<T, D1, TEAMS, FWD>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
   return DARK_OK;
 }
-template <int D1, int TEAMS>
+template <typename T, int D1, int TEAMS>
 static dark_status go_team_rev(const Args& a, hipStream_t st) {
-  typedef TeamChunks<D1, TEAMS, 3, true> L;
-  DARK_TRY(allow_lds(k_delta_team_rev<D1, TEAMS>, L::all));
-  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_team_rev<D1, TEAMS>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
+  typedef TeamChunks<T, D1, TEAMS, 3, true> L;
+  DARK_TRY(allow_lds(k_delta_team_rev<T, D1, TEAMS>, L::all));
+  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_team_rev<T, D1, TEAMS>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
   return DARK_OK;
 }
-static bool one_team(const Args& a) { return (long long)a.B * a.H * (a.dv / 16) <= kCUs; }
-template <int D1, bool FWD>
-static dark_status go_team(const Args& a, hipStream_t st) { return one_team(a) ? go_team<D1, 1, FWD>(a, st) : go_team<D1, 2, FWD>(a, st); }
-template <int D1>
-static dark_status go_team_rev(const Args& a, hipStream_t st) { return one_team(a) ? go_team_rev<D1, 1>(a, st) : go_team_rev<D1, 2>(a, st); }
+template <typename T, int D1, bool FWD>
+static dark_status go_team(const Args& a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (!one_team(a)) return go_team<T, D1, 2, FWD>(a, st);
+  return go_team<T, D1, 1, FWD>(a, st);
+}
+template <typename T, int D1>
+static dark_status go_team_rev(const Args& a, hipStream_t st) {
+  if constexpr (sizeof(T) == 2)
+    if (!one_team(a)) return go_team_rev<T, D1, 2>(a, st);
+  return go_team_rev<T, D1, 1>(a, st);
+}
+template <typename T>
+static dark_status launch_team(const Args& a, Pass pass, hipStream_t st) {
+  if (a.dk == 64) return pass == kForward ? go_team<T, 64, true>(a, st) : go_team<T, 64, false>(a, st);
+  return pass == kForward ? go_team<T, 128, true>(a, st) : go_team<T, 128, false>(a, st);
+}
+template <typename T>
+static dark_status launch_team_rev(const Args& a, hipStream_t st) { return a.dk == 64 ? go_team_rev<T, 64>(a, st) : go_team_rev<T, 128>(a, st); }
 
 }  // namespace delta
 }  // namespace dark
