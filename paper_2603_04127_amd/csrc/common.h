@@ -47,8 +47,8 @@ enum KernelId : int {
   KID_DECAY_COPY,      // decayed linear attention: copy of a state that is updated in place
   KID_DECAY_STEP,      // decayed linear attention: one token
   KID_DELTA_PREP,      // gated delta rule: triangles of every chunk
-  KID_DELTA_SCAN,      // gated delta rule: chunk after chunk (outputs, or states)
-  KID_DELTA_REV,       // gated delta rule: gradients of the states, from the last chunk to the first
+  KID_DELTA_SCAN,      // gated delta rule: chunk after chunk
+  KID_DELTA_BACK,      // gated delta rule: states, and their gradients from the last chunk to the first
   KID_DELTA_GRAD,      // gated delta rule: gradients of a chunk
   KID_DELTA_STEP,      // gated delta rule: one token
   KID_BEAM_ROWS,       // beam search: sums and largest logits of every slice of a row

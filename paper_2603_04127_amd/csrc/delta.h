@@ -15,8 +15,10 @@
 //   dK = -diag(gamma beta) dR S^T + diag(left) U dS'^T + M K + M^T K + N^T Q,
 //   dbeta_t = dR_t . v_t - gamma_t k_t . (S dR_t) - sum_(i<t) E_ti (dR_t . u_i),
 // and the gradient of log gate t sums, over all weights exp(G_r - G_i) with i < t <= r, the weight times its gradient.
-// Three kernels forward: k_delta_prep (T and P of every chunk, in parallel), k_delta_scan (chunk after chunk); backward k_delta_prep,
-// k_delta_scan (states and U), k_delta_rev (dS' and dR, from the last chunk to the first), k_delta_grad (the rest, in parallel).
+// Two kernels forward: k_delta_prep (T and P of every chunk, in parallel) and k_delta_scan (chunk after chunk); three backward: k_delta_prep,
+// k_delta_back (the states and U, chunk after chunk, and, beside them, dS' and dR, from the last chunk to the first: neither asks for the other) and
+// k_delta_grad (the rest, in parallel).  The scans have two forms: one wave for 16 columns of the state (delta_scan.h: any size), or a team of waves
+// (delta_team.h: k_delta_team, k_delta_team_back).
 #pragma once
 
 #include "rows.h"
@@ -44,8 +46,8 @@ struct Args {
   const int32_t* lengths;
   void *out, *dQ, *dK, *dV;
   float *dgate, *dbeta;
-  const float* s_in;      // state before the first row (scan), gradient of the state behind the last (rev); null: zero
-  float* s_out;           // state behind the last row (scan), gradient of that before the first (rev); null: not asked for
+  const float* s_in;      // state before the first row; null: zero
+  float* s_out;           // state behind the last row; null: not asked for
   int B, H, L, dk, dv, layout, chunks;
   int dvp;                // columns of scratch states and rows: dv, rounded up to 64
   float scale;
@@ -59,22 +61,21 @@ struct Args {
   float *u, *dr;          // [C, dvp]
 };
 
-// What the launches of a call share beside the arguments.
-enum Pass { kForward, kStates };
-
 dark_status launch_prep_bf16(const Args& a, bool backward, hipStream_t st);
 dark_status launch_prep_f32(const Args& a, bool backward, hipStream_t st);
-dark_status launch_scan_bf16(const Args& a, Pass pass, hipStream_t st);
-dark_status launch_scan_f32(const Args& a, Pass pass, hipStream_t st);
-dark_status launch_rev_bf16(const Args& a, hipStream_t st);
-dark_status launch_rev_f32(const Args& a, hipStream_t st);
+dark_status launch_scan_bf16(const Args& a, hipStream_t st);
+dark_status launch_scan_f32(const Args& a, hipStream_t st);
+// Backward, in one launch: from the last chunk to the first from the gradient g_in of the state behind it to g_out, of that before the first; and, if asked
+// for, the states before the chunks, and U.
+dark_status launch_back_bf16(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st);
+dark_status launch_back_f32(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st);
 dark_status launch_grad_bf16(const Args& a, hipStream_t st);
 dark_status launch_grad_f32(const Args& a, hipStream_t st);
 
 // A team of waves for 16 columns (delta_team.h), for rows that fill the tiles.
 bool team_supported(const Args& a, bool bf16);
-dark_status launch_team(const Args& a, bool bf16, Pass pass, hipStream_t st);
-dark_status launch_team_rev(const Args& a, bool bf16, hipStream_t st);
+dark_status launch_team(const Args& a, bool bf16, hipStream_t st);
+dark_status launch_team_back(const Args& a, bool bf16, const float* g_in, float* g_out, bool states, hipStream_t st);
 
 // Rows of the state that the kernels hold.
 inline int inner_of(int dk) { return dk > 128 ? 256 : dk > 64 ? 128 : 64; }

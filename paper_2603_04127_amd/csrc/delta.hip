@@ -156,10 +156,15 @@ static void plan(const Problem& pb, Arena& ar, bool backward, Args* a) {
 static dark_status prep(const Problem& pb, const Args& a, bool backward) {
   return pb.p.io_dtype == DARK_BF16 ? launch_prep_bf16(a, backward, pb.st) : launch_prep_f32(a, backward, pb.st);
 }
-static dark_status scan(const Problem& pb, const Args& a, Pass pass) {
+static dark_status scan(const Problem& pb, const Args& a) {
   const bool bf16 = pb.p.io_dtype == DARK_BF16;
-  if (team_supported(a, bf16)) return launch_team(a, bf16, pass, pb.st);
-  return bf16 ? launch_scan_bf16(a, pass, pb.st) : launch_scan_f32(a, pass, pb.st);
+  if (team_supported(a, bf16)) return launch_team(a, bf16, pb.st);
+  return bf16 ? launch_scan_bf16(a, pb.st) : launch_scan_f32(a, pb.st);
+}
+static dark_status back(const Problem& pb, const Args& a, const float* g_in, float* g_out, bool states) {
+  const bool bf16 = pb.p.io_dtype == DARK_BF16;
+  if (team_supported(a, bf16)) return launch_team_back(a, bf16, g_in, g_out, states, pb.st);
+  return bf16 ? launch_back_bf16(a, g_in, g_out, states, pb.st) : launch_back_f32(a, g_in, g_out, states, pb.st);
 }
 
 static dark_status step(const Problem& pb, const void* q, const void* k, const void* v, const float* log_gate, const float* beta,
@@ -264,7 +269,7 @@ dark_status dark_delta_fwd(const dark_delta_params* p, const void* Q, const void
     if (ar.overflow) return DARK_EWORKSPACE;
     DARK_TRY(delta::prep(pb, a, false));
   }
-  return delta::scan(pb, a, delta::kForward);
+  return delta::scan(pb, a);
 }
 
 dark_status dark_delta_bwd(const dark_delta_params* p, const void* Q, const void* K, const void* V, const float* log_gate,
@@ -305,17 +310,10 @@ dark_status dark_delta_bwd(const dark_delta_params* p, const void* Q, const void
     if (ar.overflow) return DARK_EWORKSPACE;
     DARK_TRY(delta::prep(pb, a, true));
   }
-  if (grads && pb.p.L > 0) {
-    a.s_in = S_in;
-    DARK_TRY(delta::scan(pb, a, delta::kStates));
-  }
-  const bool bf16 = pb.p.io_dtype == DARK_BF16;
-  a.s_in = dS_out;
-  a.s_out = dS_in;
-  if (delta::team_supported(a, bf16)) DARK_TRY(delta::launch_team_rev(a, bf16, pb.st));
-  else DARK_TRY(bf16 ? delta::launch_rev_bf16(a, pb.st) : delta::launch_rev_f32(a, pb.st));
+  a.s_in = S_in;
+  DARK_TRY(delta::back(pb, a, dS_out, dS_in, grads && pb.p.L > 0));
   if (!grads || pb.p.L == 0) return DARK_OK;
-  return bf16 ? delta::launch_grad_bf16(a, pb.st) : delta::launch_grad_f32(a, pb.st);
+  return pb.p.io_dtype == DARK_BF16 ? delta::launch_grad_bf16(a, pb.st) : delta::launch_grad_f32(a, pb.st);
 }
 
 dark_status dark_delta_step(const dark_delta_params* p, const void* q, const void* k, const void* v, const float* log_gate,

@@ -5,8 +5,8 @@ namespace dark {
 namespace delta {
 
 dark_status launch_prep_f32(const Args& a, bool backward, hipStream_t st) { return launch_prep<float>(a, backward, st); }
-dark_status launch_scan_f32(const Args& a, Pass pass, hipStream_t st) { return launch_scan<float>(a, pass, st); }
-dark_status launch_rev_f32(const Args& a, hipStream_t st) { return launch_rev<float>(a, st); }
+dark_status launch_scan_f32(const Args& a, hipStream_t st) { return launch_scan<float>(a, st); }
+dark_status launch_back_f32(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) { return launch_back<float>(a, g_in, g_out, states, st); }
 
 }  // namespace delta
 }  // namespace dark

@@ -298,7 +298,7 @@ __device__ static inline void put_columns(const f32x4 (&x)[N], float* to, int ro
 }
 
 template <typename T, int D1, int NW, bool VEC, bool FWD>
-__global__ __launch_bounds__((Chunks<T, D1, NW, 1>::kThreads)) void k_delta_scan(Args A) {
+__device__ static __forceinline__ void scan(const Args& A) {
   constexpr int NO = Kind<T>::kOut;
   typedef Chunks<T, D1, NW, (FWD ? NO : 0)> L;
   constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, VC = 16 * NW;
@@ -450,7 +450,7 @@ __global__ __launch_bounds__((Chunks<T, D1, NW, 1>::kThreads)) void k_delta_scan
 // From the last chunk to the first: the gradient G of the state behind each chunk, and dR.
 // ---------------------------------------------------------------------------
 template <typename T, int D1, int NW, bool VEC>
-__global__ __launch_bounds__((Chunks<T, D1, NW, 3>::kThreads)) void k_delta_rev(Args A) {
+__device__ static __forceinline__ void scan_back(const Args& A) {
   typedef Chunks<T, D1, NW, 3> L;
   constexpr int C = L::C, NT = C / 16, NS = C / 32, KT = D1 / 16, KS = D1 / 32, NI = L::NI, VC = 16 * NW;
   typedef typename L::MK MK;
@@ -526,6 +526,22 @@ __global__ __launch_bounds__((Chunks<T, D1, NW, 3>::kThreads)) void k_delta_rev(
   if (A.s_out != nullptr) store_state<KT>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g);
 }
 
+template <typename T, int D1, int NW, bool VEC>
+__global__ __launch_bounds__((Chunks<T, D1, NW, 1>::kThreads)) void k_delta_scan(Args A) {
+  scan<T, D1, NW, VEC, true>(A);
+}
+// Backward: the gradients of the states (z = 0) and the states (z = 1) do not wait for each other.
+template <typename T, int D1, int NW, bool VEC>
+__global__ __launch_bounds__((Chunks<T, D1, NW, 3>::kThreads)) void k_delta_back(Args A, const float* g_in, float* g_out) {
+  if (blockIdx.z == 0) {
+    A.s_in = g_in;
+    A.s_out = g_out;
+    scan_back<T, D1, NW, VEC>(A);
+  } else {
+    scan<T, D1, NW, VEC, false>(A);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Launches: the instance that holds dk inner values.
 // ---------------------------------------------------------------------------
@@ -553,46 +569,49 @@ static dark_status launch_prep(const Args& a, bool backward, hipStream_t st) {
   }
 }
 
-template <typename T, int D1, int NW, bool VEC, bool FWD>
-static dark_status go_scan(const Args& a, hipStream_t st) {
-  typedef Chunks<T, D1, NW, (FWD ? Kind<T>::kOut : 0)> L;
-  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC, FWD>, L::all));
-  const int cols = FWD ? a.dv : a.dvp;
-  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC, FWD>), dim3(a.B * a.H, (cols + 16 * NW - 1) / (16 * NW)), dim3(L::kThreads), L::all, a);
-  return DARK_OK;
-}
-template <typename T, int D1, bool FWD>
-static dark_status go_scan(const Args& a, hipStream_t st) {
-  constexpr int NW = D1 > 128 ? 2 : 4;   // 256 rows of a state leave room for one wave a SIMD
-  return vec_of<T>(a) ? go_scan<T, D1, NW, true, FWD>(a, st) : go_scan<T, D1, NW, false, FWD>(a, st);
-}
-template <typename T>
-static dark_status launch_scan(const Args& a, Pass pass, hipStream_t st) {
-  switch (inner_of(a.dk)) {
-    case 64: return pass == kForward ? go_scan<T, 64, true>(a, st) : go_scan<T, 64, false>(a, st);
-    case 128: return pass == kForward ? go_scan<T, 128, true>(a, st) : go_scan<T, 128, false>(a, st);
-    default: return pass == kForward ? go_scan<T, 256, true>(a, st) : go_scan<T, 256, false>(a, st);
-  }
-}
+// 256 rows of a state leave room for one wave a SIMD.
+template <int D1>
+constexpr int waves_of() { return D1 > 128 ? 2 : 4; }
 
 template <typename T, int D1, int NW, bool VEC>
-static dark_status go_rev(const Args& a, hipStream_t st) {
+static dark_status go_scan(const Args& a, hipStream_t st) {
+  typedef Chunks<T, D1, NW, Kind<T>::kOut> L;
+  DARK_TRY(allow_lds(k_delta_scan<T, D1, NW, VEC>, L::all));
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_scan<T, D1, NW, VEC>), dim3(a.B * a.H, (a.dv + 16 * NW - 1) / (16 * NW)), dim3(L::kThreads), L::all, a);
+  return DARK_OK;
+}
+template <typename T, int D1, int NW, bool VEC>
+static dark_status go_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
   typedef Chunks<T, D1, NW, 3> L;
-  DARK_TRY(allow_lds(k_delta_rev<T, D1, NW, VEC>, L::all));
-  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_rev<T, D1, NW, VEC>), dim3(a.B * a.H, a.dvp / (16 * NW)), dim3(L::kThreads), L::all, a);
+  constexpr int lds = L::all > Chunks<T, D1, NW, 0>::all ? L::all : Chunks<T, D1, NW, 0>::all;
+  DARK_TRY(allow_lds(k_delta_back<T, D1, NW, VEC>, lds));
+  DARK_LAUNCH(KID_DELTA_BACK, st, (k_delta_back<T, D1, NW, VEC>), dim3(a.B * a.H, a.dvp / (16 * NW), states ? 2 : 1), dim3(L::kThreads), lds, a, g_in, g_out);
   return DARK_OK;
 }
 template <typename T, int D1>
-static dark_status go_rev(const Args& a, hipStream_t st) {
-  constexpr int NW = D1 > 128 ? 2 : 4;
-  return vec_of<T>(a) ? go_rev<T, D1, NW, true>(a, st) : go_rev<T, D1, NW, false>(a, st);
+static dark_status go_scan(const Args& a, hipStream_t st) {
+  constexpr int NW = waves_of<D1>();
+  return vec_of<T>(a) ? go_scan<T, D1, NW, true>(a, st) : go_scan<T, D1, NW, false>(a, st);
+}
+template <typename T, int D1>
+static dark_status go_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
+  constexpr int NW = waves_of<D1>();
+  return vec_of<T>(a) ? go_back<T, D1, NW, true>(a, g_in, g_out, states, st) : go_back<T, D1, NW, false>(a, g_in, g_out, states, st);
 }
 template <typename T>
-static dark_status launch_rev(const Args& a, hipStream_t st) {
+static dark_status launch_scan(const Args& a, hipStream_t st) {
   switch (inner_of(a.dk)) {
-    case 64: return go_rev<T, 64>(a, st);
-    case 128: return go_rev<T, 128>(a, st);
-    default: return go_rev<T, 256>(a, st);
+    case 64: return go_scan<T, 64>(a, st);
+    case 128: return go_scan<T, 128>(a, st);
+    default: return go_scan<T, 256>(a, st);
+  }
+}
+template <typename T>
+static dark_status launch_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
+  switch (inner_of(a.dk)) {
+    case 64: return go_back<T, 64>(a, g_in, g_out, states, st);
+    case 128: return go_back<T, 128>(a, g_in, g_out, states, st);
+    default: return go_back<T, 256>(a, g_in, g_out, states, st);
   }
 }
 

@@ -328,7 +328,7 @@ __device__ static inline void mma_update(const Planes<L::NI> (&k)[N][L::NS], con
 }
 
 template <typename T, int D1, int TEAMS, bool FWD>
-__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, (FWD ? Kind<T>::kOut : 0), false>::kThreads)) void k_delta_team(Args A) {
+__device__ static __forceinline__ void team_scan(const Args& A) {
   constexpr int NO = Kind<T>::kOut, NP = FWD ? NO : 0;
   typedef TeamChunks<T, D1, TEAMS, NP, false> L;
   constexpr int C = L::C, KS = L::KS, NS = L::NS, NB = L::NB, NI = L::NI, OWN = L::kOwn, TEAM = L::kTeam;
@@ -416,7 +416,7 @@ __global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, (FWD ? Kind<T>::kOut : 0)
 }
 
 template <typename T, int D1, int TEAMS>
-__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true>::kThreads)) void k_delta_team_rev(Args A) {
+__device__ static __forceinline__ void team_rev(const Args& A) {
   typedef TeamChunks<T, D1, TEAMS, 3, true> L;
   constexpr int C = L::C, KS = L::KS, NS = L::NS, NB = L::NB, NI = L::NI, OWN = L::kOwn, TEAM = L::kTeam;
   typedef typename L::MK MK;
@@ -500,47 +500,63 @@ __global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true>::kThreads)) void
   if (A.s_out != nullptr) store_state<OWN>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g, h * 16 * OWN);
 }
 
+template <typename T, int D1, int TEAMS>
+__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true>::kThreads)) void k_delta_team(Args A) {
+  team_scan<T, D1, TEAMS, true>(A);
+}
+// Backward: the gradients of the states (z = 0) and the states (z = 1) do not wait for each other.
+template <typename T, int D1, int TEAMS>
+__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true>::kThreads)) void k_delta_team_back(Args A, const float* g_in, float* g_out) {
+  if (blockIdx.z == 0) {
+    A.s_in = g_in;
+    A.s_out = g_out;
+    team_rev<T, D1, TEAMS>(A);
+  } else {
+    team_scan<T, D1, TEAMS, false>(A);
+  }
+}
+
 // Whether a call takes these kernels: rows that fill the tiles; of fp32, whose operands go through registers, while each team has a CU to itself.
 constexpr int kCUs = 256;
-static bool one_team(const Args& a) { return (long long)a.B * a.H * (a.dv / 16) <= kCUs; }
+static long long teams_of(const Args& a) { return (long long)a.B * a.H * (a.dv / 16); }
 template <typename T>
-static bool teamed(const Args& a) { return (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0 && (sizeof(T) == 2 || one_team(a)); }
+static bool teamed(const Args& a) { return (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0 && (sizeof(T) == 2 || teams_of(a) <= kCUs); }
 
 // One team a workgroup as long as each of those has a CU to itself: the reads of LDS, 128 bytes a cycle, are what two share (24 x 4096 x 64 with
 // one and two: 78 and 98 us, backward 100 and 124).
-template <typename T, int D1, int TEAMS, bool FWD>
+template <typename T, int D1, int TEAMS>
 static dark_status go_team(const Args& a, hipStream_t st) {
-  typedef TeamChunks<T, D1, TEAMS, (FWD ? Kind<T>::kOut : 0), false> L;
-  DARK_TRY(allow_lds(k_delta_team<T, D1, TEAMS, FWD>, L::all));
-  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_team<T, D1, TEAMS, FWD>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
+  typedef TeamChunks<T, D1, TEAMS, Kind<T>::kOut, false> L;
+  DARK_TRY(allow_lds(k_delta_team<T, D1, TEAMS>, L::all));
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_team<T, D1, TEAMS>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
   return DARK_OK;
 }
 template <typename T, int D1, int TEAMS>
-static dark_status go_team_rev(const Args& a, hipStream_t st) {
+static dark_status go_team_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
   typedef TeamChunks<T, D1, TEAMS, 3, true> L;
-  DARK_TRY(allow_lds(k_delta_team_rev<T, D1, TEAMS>, L::all));
-  DARK_LAUNCH(KID_DELTA_REV, st, (k_delta_team_rev<T, D1, TEAMS>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
+  constexpr int lds = L::all > TeamChunks<T, D1, TEAMS, 0, false>::all ? L::all : TeamChunks<T, D1, TEAMS, 0, false>::all;
+  DARK_TRY(allow_lds(k_delta_team_back<T, D1, TEAMS>, lds));
+  DARK_LAUNCH(KID_DELTA_BACK, st, (k_delta_team_back<T, D1, TEAMS>), dim3(a.B * a.H, a.dv / L::VC, states ? 2 : 1), dim3(L::kThreads), lds, a, g_in, g_out);
   return DARK_OK;
 }
-template <typename T, int D1, bool FWD>
+template <typename T, int D1>
 static dark_status go_team(const Args& a, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (!one_team(a)) return go_team<T, D1, 2, FWD>(a, st);
-  return go_team<T, D1, 1, FWD>(a, st);
+    if (teams_of(a) > kCUs) return go_team<T, D1, 2>(a, st);
+  return go_team<T, D1, 1>(a, st);
 }
 template <typename T, int D1>
-static dark_status go_team_rev(const Args& a, hipStream_t st) {
+static dark_status go_team_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (!one_team(a)) return go_team_rev<T, D1, 2>(a, st);
-  return go_team_rev<T, D1, 1>(a, st);
+    if (teams_of(a) * (states ? 2 : 1) > kCUs) return go_team_back<T, D1, 2>(a, g_in, g_out, states, st);
+  return go_team_back<T, D1, 1>(a, g_in, g_out, states, st);
 }
 template <typename T>
-static dark_status launch_team(const Args& a, Pass pass, hipStream_t st) {
-  if (a.dk == 64) return pass == kForward ? go_team<T, 64, true>(a, st) : go_team<T, 64, false>(a, st);
-  return pass == kForward ? go_team<T, 128, true>(a, st) : go_team<T, 128, false>(a, st);
-}
+static dark_status launch_team(const Args& a, hipStream_t st) { return a.dk == 64 ? go_team<T, 64>(a, st) : go_team<T, 128>(a, st); }
 template <typename T>
-static dark_status launch_team_rev(const Args& a, hipStream_t st) { return a.dk == 64 ? go_team_rev<T, 64>(a, st) : go_team_rev<T, 128>(a, st); }
+static dark_status launch_team_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
+  return a.dk == 64 ? go_team_back<T, 64>(a, g_in, g_out, states, st) : go_team_back<T, 128>(a, g_in, g_out, states, st);
+}
 
 }  // namespace delta
 }  // namespace dark

@@ -5,8 +5,10 @@ namespace dark {
 namespace delta {
 
 bool team_supported(const Args& a, bool bf16) { return bf16 ? teamed<unsigned short>(a) : teamed<float>(a); }
-dark_status launch_team(const Args& a, bool bf16, Pass pass, hipStream_t st) { return bf16 ? launch_team<unsigned short>(a, pass, st) : launch_team<float>(a, pass, st); }
-dark_status launch_team_rev(const Args& a, bool bf16, hipStream_t st) { return bf16 ? launch_team_rev<unsigned short>(a, st) : launch_team_rev<float>(a, st); }
+dark_status launch_team(const Args& a, bool bf16, hipStream_t st) { return bf16 ? launch_team<unsigned short>(a, st) : launch_team<float>(a, st); }
+dark_status launch_team_back(const Args& a, bool bf16, const float* g_in, float* g_out, bool states, hipStream_t st) {
+  return bf16 ? launch_team_back<unsigned short>(a, g_in, g_out, states, st) : launch_team_back<float>(a, g_in, g_out, states, st);
+}
 
 }  // namespace delta
 }  // namespace dark
