@@ -9,14 +9,15 @@
 //  * Small top_k: a bound from the threads' maxima leaves few candidates, which count those before them and, kept, the weights of those with
 //    lower numbers: two reads of the row.
 //  * Else a histogram of weights over the logits finds the bin where the beginning ends, and the bin's entries are sorted.
-//  * The draw sums the kept weights by waves, each of which holds a contiguous part of the row, and looks into one of them.
+//  * The draw sums the kept weights by waves, each of which holds a contiguous part of the row, and looks into one of them.  A row that keeps
+//    everything has these sums from the first read.
 // Weights are in fp64, by a polynomial, to 2^-33 of their value, and so are their sums; a histogram's are integers, whose sums have no order.
 // In fp32 the borders between a large row's tokens would be off by some 2^-30 of the row's sum each, 2^17 of them together by 2^-13: one
 // row in 8000 would draw a token's neighbour.
 // What bounds it: of 256 rows of 131071 bf16 logits the first read takes 10 us (6.7 TB/s), a read that asks a comparison of each logit 9, one that weighs
 // each 24 (19 instructions a logit, four waves a SIMD; the matrix of 67 MB lies in the last cache by then), the histogram's 40 (two more for the
-// addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 32, no filter 47, top_p 0.9 107;
-// one row of 32000 fp32 logits 8, 14, 13 and 31, where the way through the steps counts and not the row.
+// addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 32, no filter 37 (weighed in a read of its
+// own behind that for the largest: 47), top_p 0.9 107; one row of 32000 fp32 logits 8, 14, 12 and 31, where the way through the steps counts and not the row.
 #include <cmath>
 #include <type_traits>
 
@@ -195,7 +196,7 @@ struct Shared {
   float tops[kThreads];
   u64 bound;         // the last entry that is kept
   u64 before;        // weight of the bins before the chosen one
-  int ranks_before, bin, size, kept;
+  int ranks_before, bin, size, kept, again;
 };
 
 // The list's first n entries in descending order.
@@ -252,10 +253,43 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   const float temp = set.temperature != nullptr ? set.temperature[b] : set.T;
   int k = set.top_k != nullptr ? set.top_k[b] : set.k;
   float p = set.top_p != nullptr ? set.top_p[b] : set.p, q = set.min_p != nullptr ? set.min_p[b] : set.q, u = uniform != nullptr ? uniform[b] : 0.f;   // asked for before the row
-  // the largest logit, of every thread and of all
-  float mine = -INFINITY;
-  row.each(wave, lane, [&](u32x4 v, int) { mine = fmaxf(mine, Row<T>::largest(v)); });   // of a NaN and a number: the number
+  Weight weight;
+  weight.c = temp > 0.f ? fmin(1.4426950408889634 / (double)temp, 1e300) : 1.0;
+  const auto set_floor = [&]() __attribute__((always_inline)) {
+    // rounded up: z stays where the exponent holds it; the largest logit weighs 1
+    const double least = weight.m - 1000.0 / weight.c;
+    weight.floor = least > -3.402823466e38 ? fminf(value_of(ordered((float)least) + 1u), (float)weight.m) : -3.402823466e38f;
+  };
+  // The largest logit, of every thread and of all.  A row that keeps everything is weighed on the way, beside the largest of the wave's first logits: the
+  // exponent holds what is larger, up to 2^900 (else, and where those are all masked, it is weighed again).
+  const bool everything = temp > 0.f && (k <= 0 || k >= V) && !(p < 1.f) && !(q > 0.f);
+  float mine = -INFINITY, beside = -INFINITY;
+  double sum = 0.0;
+  if (everything) {
+    bool first = true;
+    row.each(wave, lane, [&](u32x4 v, int) __attribute__((always_inline)) {
+      const float most = Row<T>::largest(v);   // of a NaN and a number: the number
+      mine = fmaxf(mine, most);
+      if (first) {
+        first = false;
+        beside = wave_max(most);
+        weight.m = fabsf(beside) < INFINITY ? beside : 0.0;
+        set_floor();
+      }
+#pragma unroll
+      for (int j = 0; j < P; ++j) {
+        const float x = Row<T>::value(v, j);
+        const double w = weight(x);
+        sum += x >= weight.floor ? w : 0.0;
+        if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+      }
+    });
+    sum = wave_sum(sum);
+  } else {
+    row.each(wave, lane, [&](u32x4 v, int) __attribute__((always_inline)) { mine = fmaxf(mine, Row<T>::largest(v)); });
+  }
   s.tops[tid] = mine;
+  if (tid == 0) s.again = 0;
   __syncthreads();
   float top = -INFINITY;
 #pragma unroll
@@ -276,17 +310,12 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     s.tops[tid] = mine;
     __syncthreads();
   }
-  Weight weight;
   weight.m = top;
-  weight.c = fmin(1.4426950408889634 / (double)temp, 1e300);
   if (!(temp > 0.f)) {   // the largest logit
-    weight.c = 1.0;
     k = 1;
     p = 1.f;
   }
-  // rounded up: z stays where the exponent holds it; the largest logit weighs 1
-  const double lowest_z = (double)top - 1000.0 / weight.c;
-  weight.floor = lowest_z > -3.402823466e38 ? fminf(value_of(ordered((float)lowest_z) + 1u), top) : -3.402823466e38f;
+  set_floor();
   q = q > 0.f ? fminf(q, 1.f) : 0.f;
   u = u > 0.f ? u : 0.f;
   if (k <= 0 || k >= V) k = 0;
@@ -636,14 +665,28 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);   // eight polynomials at once do not fit the registers
     }
   };
-  double sum = 0.0;
   const auto add = [&](double w, int) __attribute__((always_inline)) { sum += w; };
-  row.each(wave, lane, [&](u32x4 v, int t) __attribute__((always_inline)) {
-    if (Row<T>::largest(v) >= last_logit) sum_of(v, t, add);
-  });
-  sum = wave_sum(sum);
-  if (lane == 0) s.sums[wave] = sum;
-  __syncthreads();
+  bool weighed = everything && !row.infinite;
+  if (weighed) {
+    // a wave without logits beside its first ones has none, or is weighed again, and so are all
+    const bool none = !(wave_max(mine) > -INFINITY);
+    const bool held = fabsf(beside) < INFINITY && ((double)top - (double)beside) * weight.c <= 900.0;
+    sum = held && !none ? sum * weight.any(beside) : 0.0;
+    if (!held && !none && lane == 0) s.again = 1;
+    if (lane == 0) s.sums[wave] = sum;
+    __syncthreads();
+    weighed = s.again == 0;
+    __syncthreads();
+  }
+  if (!weighed) {
+    sum = 0.0;
+    row.each(wave, lane, [&](u32x4 v, int t) __attribute__((always_inline)) {
+      if (Row<T>::largest(v) >= last_logit) sum_of(v, t, add);
+    });
+    sum = wave_sum(sum);
+    if (lane == 0) s.sums[wave] = sum;
+    __syncthreads();
+  }
   double all = 0.0;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) all += s.sums[i];

@@ -108,6 +108,26 @@ def test_masked_logits(dtype):
         assert token[0] == token[1] == -1 and token[2] == 0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_without_filters_weighed_on_the_way(dtype):
+    # a row's first logits say little about the others: masked, far below or far above them, all alike
+    rng = np.random.default_rng(14)
+    V = 70001
+    x = _logits(rng, 9, V, dtype)
+    x[0, :40000] = float("-inf")
+    x[1, :60000] -= 5e3
+    x[2, 5000:] -= 5e3
+    x[3, 1:] = float("-inf")
+    x[4, :-1] = float("-inf")
+    x[5] = torch.linspace(-2e4, 2e4, V)
+    x[6] = torch.linspace(2e4, -2e4, V)
+    x[7, 30000] = float("inf")
+    x[8] = 0.0
+    u = np.array([0.3, 0.999, 0.5, 0.5, 0.5, 0.7, 0.1, 0.9, 0.4], dtype=np.float32)
+    for kw in (dict(), dict(temperature=0.01), dict(temperature=30.0), dict(temperature=1e-6), dict(temperature=np.linspace(0.0, 2.0, 9))):
+        _run(x, u, **kw)
+
+
 def test_settings_at_their_ends():
     rng = np.random.default_rng(5)
     x = _logits(rng, 4, 2000, "f32")
