@@ -12,6 +12,8 @@ namespace delta {
 // T = (I + diag(beta) E)^-1 and P = D o (Q K^T) of every chunk, in operand order; backward their transposes, P times scale.
 // The inverse: blocks of 16 x 16 on the diagonal by substitution, row after row; below it T_rc = -T_rr sum_m A_rm T_mc, by fp32 matrix
 // products, one diagonal of blocks after the other.  Substitution and products are backward stable for any beta and keys.
+// A chunk a workgroup.  Many chunks are bound by memory: 8192 of 64 x 128 in bf16 take 105 us, 62 KB each (K and Q read, T in three planes and P in two
+// written), 4.8 TB/s; 1536 of 64 x 64 22, backward, with T^T and a third plane of P, 26.  Few are bound by the steps one after the other: 208 take 10.
 // ---------------------------------------------------------------------------
 template <typename T, int D1>
 constexpr int prep_lds() {

@@ -1,5 +1,5 @@
 // Device helpers and host-side hooks shared by the fused MFMA translation units (gfx950).
-// Every translation unit that includes this header is compiled with -fno-honor-nans.
+// The fused and decayed kernels' translation units are compiled with -fno-honor-nans; those of delta*.hip, where NaN has to come through, are not.
 #pragma once
 
 #include <atomic>
@@ -61,7 +61,7 @@ __device__ static inline float dot2_bf16(unsigned a, unsigned b, float acc) {
   return __builtin_amdgcn_fdot2_f32_bf16(*reinterpret_cast<bf16x2*>(&a), *reinterpret_cast<bf16x2*>(&b), acc, false);
 }
 constexpr unsigned kOnesBf16x2 = 0x3f803f80u;
-// max(a, b, c).  This file is compiled with -fno-honor-nans, so the compiler needs no NaN
+// max(a, b, c).  With -fno-honor-nans the compiler needs no NaN
 // canonicalisation and forms v_max3_f32.  (Not inline asm: the compiler must see the reads of
 // MFMA results to insert the wait states they need.)
 __device__ static inline float max3(float a, float b, float c) { return __builtin_fmaxf(a, __builtin_fmaxf(b, c)); }

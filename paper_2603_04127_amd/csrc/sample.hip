@@ -8,7 +8,8 @@
 // last that top_p keeps; the sum of what is kept.  What is kept is a beginning of the order, so that its last entry says it.
 //  * Small top_k: a bound from the threads' maxima leaves few candidates, which count those before them and, kept, the weights of those with
 //    lower numbers: two reads of the row.
-//  * Else a histogram of weights over the logits finds the bin where the beginning ends, and the bin's entries are sorted.
+//  * Else a histogram of weights over the logits finds the bin where the beginning ends; the read that lists its entries, for them to be sorted, adds up
+//    the weights before it.
 //  * The draw sums the kept weights by waves, each of which holds a contiguous part of the row, and looks into one of them.  A row that keeps
 //    everything has these sums from the first read.
 // Weights are in fp64, by a polynomial, to 2^-33 of their value, and so are their sums; a histogram's are integers, whose sums have no order.
@@ -17,7 +18,8 @@
 // What bounds it: of 256 rows of 131071 bf16 logits the first read takes 10 us (6.7 TB/s), a read that asks a comparison of each logit 9, one that weighs
 // each 24 (19 instructions a logit, four waves a SIMD; the matrix of 67 MB lies in the last cache by then), the histogram's 40 (two more for the
 // addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 32, no filter 37 (weighed in a read of its
-// own behind that for the largest: 47), top_p 0.9 107; one row of 32000 fp32 logits 8, 14, 12 and 31, where the way through the steps counts and not the row.
+// own behind that for the largest: 47), top_p 0.9 103 (with
+// a read for the list and one for the sum 107); one row of 32000 fp32 logits 8, 14, 12 and 29, where the way through the steps counts and not the row.
 #include <cmath>
 #include <type_traits>
 
@@ -355,6 +357,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   };
 
   bool done = k == 0 && !by_p;
+  bool summed = false;   // whether `sum` is that of a thread's weights before the bin that holds the bound, and the list's first s.kept are what is kept of it
   if (!done && k > 0 && k <= kSmall) {
     // The k-th largest of the threads' maxima is at most the k-th largest logit: its first 16 bits, four at a time, a wave for each value of them.
     unsigned key[kThreads / 64], cut = k > 1 ? 0 : ordered(top);
@@ -518,20 +521,33 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       const float to = top - (width * (float)bin - slack), from = bin == kBins - 1 ? -3.402823466e38f : top - (width * (float)(bin + 1) + slack);
       // entries lo ... hi of the order are left; each pass leaves a part of 2048 of them
       u64 lo = bound, hi = ~0ull;   // nothing that top_k left out
-      const auto list = [&]() __attribute__((always_inline)) {
-        row.each(wave, lane, [&](u32x4 v, int t) {
-          // the logits that the bin can hold, and a little more: what they are exactly is asked of few
-          Row<T>::between(v, t, from, to, [&](float x, int tk) {
-            if (x > -INFINITY && bin_of(x) == bin) {
-              const u64 e = entry(x, tk);
-              if (e >= lo && e <= hi) append(x, tk);
-            }
-          });
+      // the logits that the bin can hold, and a little more: what they are exactly is asked of few
+      const auto in_bin = [&](u32x4 v, int t, auto other) __attribute__((always_inline)) {
+        Row<T>::between(v, t, from, to, [&](float x, int tk) __attribute__((always_inline)) {
+          if (x > -INFINITY) {
+            const int at = bin_of(x);
+            const u64 e = entry(x, tk);
+            if (at < bin) other(x);
+            if (at == bin && e >= lo && e <= hi) append(x, tk);
+          }
         });
-        __syncthreads();
-        return s.size;
       };
-      int n = list();
+      // on the way, the sums of the weights before the bin, which are kept whatever is left of the bin itself
+      sum = 0.0;
+      const float beyond = fmaxf(to, weight.floor);
+      row.each(wave, lane, [&](u32x4 v, int t) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+          const float x = Row<T>::value(v, j);
+          const double w = weight(x);
+          sum += x > beyond ? w : 0.0;
+          if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+        }
+        in_bin(v, t, [&](float x) { sum += weight.any(x); });
+      });
+      __syncthreads();
+      int n = s.size;
+      summed = n <= kList;
       __syncthreads();
       while (n > kList) {
         // the range of what is left
@@ -581,7 +597,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         hi = top_e;
         if (tid == 0) s.before += before, s.ranks_before += ranks;
         __syncthreads();
-        n = list();
+        row.each(wave, lane, [&](u32x4 v, int t) __attribute__((always_inline)) { in_bin(v, t, [](float) {}); });
+        __syncthreads();
+        n = s.size;
         __syncthreads();
       }
       sort(s, n, tid);
@@ -640,7 +658,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       key |= shift >= 0 ? digit << shift : digit;
     }
     const u64 least = (u64)(key + 1) << 32 | 0x80000000u;   // with the highest number
-    bound = bound > least ? bound : least;
+    if (least > bound) bound = least, summed = false;
   }
   // ---------------------------------------------------------------------------
   // The draw: sums of the kept weights, of each wave's part of the row, then of a sixteenth of one part by each wave.
@@ -677,6 +695,16 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     __syncthreads();
     weighed = s.again == 0;
     __syncthreads();
+  }
+  if (!weighed && summed) {
+    for (int i = lane; i < s.kept; i += 64) {
+      const int piece = (token_of(s.list[i]) - row.begin) / P;
+      if (piece / (64 * row.pieces) == wave) sum += weight.any(logit_of(s.list[i]));
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) s.sums[wave] = sum;
+    __syncthreads();
+    weighed = true;
   }
   if (!weighed) {
     sum = 0.0;

@@ -348,6 +348,28 @@ def test_two_graphs_replay_in_turn():
 
 
 # ---------------------------------------------------------------------------
+# a sequence's results, bit by bit, beside few others and beside more than there are compute units
+# ---------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d", [("f32", 64), ("f32", 128), ("bf16", 64), ("bf16", 128)])
+def test_results_do_not_depend_on_the_batch(dtype, d):
+    B, H, L = 24, 4, 150
+    g = torch.Generator(device="cuda").manual_seed(8)
+    q, k, v, o = (torch.randn(B, H, L, d, generator=g, device="cuda") for _ in range(4))
+    q, k, v, o = (x.to(U.TORCH[dtype]) for x in (q / 8, k / k.norm(dim=-1, keepdim=True), v, o))
+    a, beta = -0.1 * torch.rand(B, H, L, generator=g, device="cuda"), torch.rand(B, H, L, generator=g, device="cuda")
+    lengths = torch.randint(0, L + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
+    state, dstate = (torch.randn(B, H, d, d, generator=g, device="cuda") for _ in range(2))
+    out, last = dk.dark_delta_fwd(q, k, v, a, beta, lengths=lengths, state=state, want_state=True)
+    grads = dk.dark_delta_bwd(q, k, v, a, beta, o, lengths=lengths, state=state, dstate=dstate)
+    for b in (0, B - 1):
+        q1, k1, v1, a1, b1, o1, n1, s1, d1 = (x[b:b + 1].clone() for x in (q, k, v, a, beta, o, lengths, state, dstate))
+        out1, last1 = dk.dark_delta_fwd(q1, k1, v1, a1, b1, lengths=n1, state=s1, want_state=True)
+        assert torch.equal(out[b:b + 1], out1) and torch.equal(last[b:b + 1], last1)
+        for name, x in dk.dark_delta_bwd(q1, k1, v1, a1, b1, o1, lengths=n1, state=s1, dstate=d1).items():
+            assert torch.equal(grads[name][b:b + 1], x), name
+
+
+# ---------------------------------------------------------------------------
 # tensors of more than 2^32 bytes: the last sequence against a call of its own
 # ---------------------------------------------------------------------------
 @pytest.mark.parametrize("layout", ["bhld", "blhd"])
