@@ -72,10 +72,15 @@ dark_status launch_back_f32(const Args& a, const float* g_in, float* g_out, bool
 dark_status launch_grad_bf16(const Args& a, hipStream_t st);
 dark_status launch_grad_f32(const Args& a, hipStream_t st);
 
-// A team of waves for 16 columns (delta_team.h), for rows that fill the tiles.
-bool team_supported(const Args& a, bool bf16);
-dark_status launch_team(const Args& a, bool bf16, hipStream_t st);
-dark_status launch_team_back(const Args& a, bool bf16, const float* g_in, float* g_out, bool states, hipStream_t st);
+// A team of waves for 16 columns (delta_team.h), and whether a call takes it.
+bool team_bf16(const Args& a);
+bool team_f32(const Args& a);
+bool team_back_bf16(const Args& a, bool states);
+bool team_back_f32(const Args& a, bool states);
+dark_status launch_team_bf16(const Args& a, hipStream_t st);
+dark_status launch_team_f32(const Args& a, hipStream_t st);
+dark_status launch_team_back_bf16(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st);
+dark_status launch_team_back_f32(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st);
 
 // Rows of the state that the kernels hold.
 inline int inner_of(int dk) { return dk > 128 ? 256 : dk > 64 ? 128 : 64; }

@@ -157,14 +157,13 @@ static dark_status prep(const Problem& pb, const Args& a, bool backward) {
   return pb.p.io_dtype == DARK_BF16 ? launch_prep_bf16(a, backward, pb.st) : launch_prep_f32(a, backward, pb.st);
 }
 static dark_status scan(const Problem& pb, const Args& a) {
-  const bool bf16 = pb.p.io_dtype == DARK_BF16;
-  if (team_supported(a, bf16)) return launch_team(a, bf16, pb.st);
-  return bf16 ? launch_scan_bf16(a, pb.st) : launch_scan_f32(a, pb.st);
+  if (pb.p.io_dtype == DARK_BF16) return team_bf16(a) ? launch_team_bf16(a, pb.st) : launch_scan_bf16(a, pb.st);
+  return team_f32(a) ? launch_team_f32(a, pb.st) : launch_scan_f32(a, pb.st);
 }
 static dark_status back(const Problem& pb, const Args& a, const float* g_in, float* g_out, bool states) {
-  const bool bf16 = pb.p.io_dtype == DARK_BF16;
-  if (team_supported(a, bf16)) return launch_team_back(a, bf16, g_in, g_out, states, pb.st);
-  return bf16 ? launch_back_bf16(a, g_in, g_out, states, pb.st) : launch_back_f32(a, g_in, g_out, states, pb.st);
+  if (pb.p.io_dtype == DARK_BF16)
+    return team_back_bf16(a, states) ? launch_team_back_bf16(a, g_in, g_out, states, pb.st) : launch_back_bf16(a, g_in, g_out, states, pb.st);
+  return team_back_f32(a, states) ? launch_team_back_f32(a, g_in, g_out, states, pb.st) : launch_back_f32(a, g_in, g_out, states, pb.st);
 }
 
 static dark_status step(const Problem& pb, const void* q, const void* k, const void* v, const float* log_gate, const float* beta,

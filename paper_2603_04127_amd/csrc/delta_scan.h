@@ -227,8 +227,8 @@ struct Bases {
   }
 };
 
-// The loading waves: chunk after chunk (REV: from the last to the first), one ahead.  MORE: barriers of a chunk behind its second.
-template <typename L, typename T, int D1, int NP, bool VEC, bool REV, int MORE = 0>
+// The loading waves: chunk after chunk (REV: from the last to the first), one ahead.
+template <typename L, typename T, int D1, int NP, bool VEC, bool REV>
 __device__ static inline void load_chunks(const Args& A, int bh, const Rows& xk, const Rows& xq, const Rows& xv, int n, int tid) {
   constexpr int C = L::C, NB = L::NB, NTH = L::NTH;
   const int chunks = (n + C - 1) / C;
@@ -262,14 +262,12 @@ __device__ static inline void load_chunks(const Args& A, int bh, const Rows& xk,
   if (chunks > 1) load(1);
   lds_barrier();
   for (int i = 0; i < chunks; ++i) {
-    if (L::kBufs == 1 || MORE > 0) lds_barrier();   // with one buffer: the chunk's readers are done
+    if (L::kBufs == 1) lds_barrier();   // the chunk's readers are done
     if (i + 1 < chunks) {
       store((i + 1) % L::kBufs);
       if (i + 2 < chunks) load(i + 2);
     }
     lds_barrier();
-#pragma unroll
-    for (int k = 0; k < MORE; ++k) lds_barrier();
   }
 }
 // The computing waves: f(chunk, the buffer of its operands, a constant) for every chunk.

@@ -1,13 +1,16 @@
-// The gated delta rule's scans with a wave for each row tile of 16 columns: rows that fill the tiles (see delta_scan.h for one wave that does all).
+// The gated delta rule's scans with a wave for each row tile of 16 columns of the state (see delta_scan.h for one wave that does all).
 //
 // A wave takes an instruction in seven to twelve cycles, whatever it is, where the chunks' states hang on each other; what a SIMD does in that
 // time grows with its waves, and a CU with its SIMDs.  So the 16 columns' work is dealt to a team, four waves for bf16's chunks of 64 rows and two for
 // fp32's of 32: each has one of the chunk's row tiles and a part of the state's rows.  What a wave has as sums and all need as an operand goes
-// through LDS: the state's planes, R, and U, with a barrier behind each.  Of bf16 two waves bring the operands by loads that end in LDS, a part between two
-// barriers (a whole chunk's at once keep their wave from the first barrier for a third of the chunk); of fp32 four take them through registers.
-// (One wave and a team: prompt of 16 x 777 x 128 42 -> 27 us, prefill of 64 x 8192 x 128 415 -> 322, 24 x 4096 x 64 as training runs it 122 -> 78 and
-// backward 160 -> 101; of fp32 1000 rows of 8 heads of 64 58 -> 50, backward 70 -> 62.  Two waves of bf16 with all loads at once were no faster than one.)
-// Sums of fp32 operands add up in the same order in both, so that a sequence's results do not depend on how many others there are.
+// through LDS: the state's planes, R, and U, with a barrier behind each.  bf16 rows that fill the tiles are brought by two waves and loads that end in
+// LDS (DIRECT), a part between two barriers: a whole chunk's at once, six instructions each, kept their wave from the first barrier for a third of the
+// chunk.  All others go through the registers of eight waves (of four, with as long between the same barriers: 5 to 13 % more; four where fp32 rows of
+// 128 leave no registers for eight).
+// One wave and a team, DIRECT: prompt of 16 x 777 x 128 42 -> 26 us, prefill of 64 x 8192 x 128 415 -> 320, 24 x 4096 x 64 as training runs it 122 -> 72 and
+// backward 160 -> 100 (two waves a team, with all loads at once: no faster than one).  Heads of 100 and 128 for that prompt 45 -> 38, 8 heads of 1000 x 96 and 80
+// backward 63 -> 39; fp32, 8 heads of 1000 x 64 58 -> 55, backward 70 -> 56.
+// What is not DIRECT adds up in the same order here and there, so that a sequence's results do not depend on how many others there are.
 #pragma once
 
 #include "delta_scan.h"
@@ -29,14 +32,14 @@ __device__ static inline Half<N> split_half(f32x4 a) {
   return h;
 }
 
-// Operands in LDS for two chunks, or, of bf16, for one what is needed late in a chunk: P forward, Q and T backward.
-template <typename T_, int D1, int TEAMS, int NP, bool REV>
+// Operands in LDS for two chunks, or, of those that go straight there, for one what is needed late in a chunk: P forward, Q and T backward.
+template <typename T_, int D1, int TEAMS, int NP, bool REV, bool DIRECT>
 struct TeamChunks {
   typedef T_ T;
   static constexpr int C = Kind<T>::kChunk, NI = Kind<T>::kIn, NB = blocks_of(C), VC = 16 * TEAMS, KS = D1 / 32;
-  static constexpr bool kDirect = sizeof(T) == 2;
+  static constexpr bool kDirect = DIRECT;
   static constexpr int kTeam = C / 16, kOwn = D1 / 16 / kTeam;   // waves of a team, tiles of the state of each
-  static constexpr int kLoaders = kDirect ? 2 : 4, kThreads = 64 * (kTeam * TEAMS + kLoaders), NTH = 64 * kLoaders, kBufs = 2;
+  static constexpr int kLoaders = kDirect ? 2 : NI == 3 && D1 > 64 ? 4 : 8, kThreads = 64 * (kTeam * TEAMS + kLoaders), NTH = 64 * kLoaders;
   typedef Mat<C, D1, NI> MK;
   typedef Mat<C, VC, NI> MV;
   static constexpr int kQ = NP > 0 ? MK::kAll : 0, kV = MV::kAll, kW = kScanVecs * C * 4, kT = 3 * NB * 1024, kP = NP * NB * 1024;
@@ -185,15 +188,85 @@ __device__ static inline void load_rest(const Args& A, int bh, const Rows& xv, i
   }
 }
 
-template <typename L, int D1, int NP, bool REV>
-__device__ static inline void load_team(const Args& A, int bh, const void* values, int col0, int n, int tid) {
+// Through registers: between the first barrier and the second the next chunk's operands go to LDS, and those of the chunk behind it are asked for.
+template <typename L, int D1, int NP, bool VEC, bool REV>
+__device__ static inline void load_through(const Args& A, int bh, const Rows& xv, int n, int tid) {
   typedef typename L::T T;
-  const Rows xv = rows_at<T>(values, A, bh, A.dv, n, col0, L::VC);
+  constexpr int C = L::C, NB = L::NB, NTH = L::NTH;
+  const Rows xk = rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), xq = rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk);
+  const u32x4* const tri = REV ? A.trit : A.tri;
+  const int chunks = (n + C - 1) / C;
+  Load<T, C, D1, NTH, VEC> lk, lq;
+  Load<T, C, L::VC, NTH, VEC> lv;
+  LoadTri<NB, 3, NTH> lt;
+  LoadTri<NB, (NP > 0 ? NP : 1), NTH> lp;
+  f32x4 lw = zero4();
+  const auto chunk = [&](int i) { return REV ? chunks - 1 - i : i; };
+  const auto rows = [&](auto& l, const Rows& x, int i) __attribute__((always_inline)) { l.load(x, chunk(i) * C, min(C, n - chunk(i) * C), tid); };
+  const auto keys = [&](int i) __attribute__((always_inline)) { rows(lk, xk, i); };
+  const auto queries = [&](int i) __attribute__((always_inline)) { if (NP > 0) rows(lq, xq, i); };
+  const auto values = [&](int i) __attribute__((always_inline)) {
+    rows(lv, xv, i);
+    if (tid < C) lw = reinterpret_cast<const f32x4*>(A.vec + chunk_at(A, bh, chunk(i)) * (kVecs * C))[tid];
+  };
+  const auto triangles = [&](int i) __attribute__((always_inline)) {
+    lt.load(tri + chunk_at(A, bh, chunk(i)) * (3 * NB * 64), tid);
+    if (NP > 0) lp.load(A.pri + chunk_at(A, bh, chunk(i)) * (NP * NB * 64), tid);
+  };
+  const auto put_keys = [&](int buf) __attribute__((always_inline)) { lk.template store<typename L::MK>(L::k + buf * L::MK::kAll, tid); };
+  const auto put_queries = [&](int buf) __attribute__((always_inline)) { if (NP > 0) lq.template store<typename L::MK>(L::q + buf * L::kQ, tid); };
+  const auto put_values = [&](int buf) __attribute__((always_inline)) {
+    lv.template store<typename L::MV>(L::v + buf * L::kV, tid);
+    if (tid < C) lds_put(L::w + buf * L::kW + 16 * tid, lw);
+  };
+  const auto put_triangles = [&](int buf) __attribute__((always_inline)) {
+    lt.store(L::t + buf * L::kT, tid);
+    if (NP > 0) lp.store(L::p + buf * L::kP, tid);
+  };
+  keys(0);
+  queries(0);
+  values(0);
+  triangles(0);
+  put_keys(0);
+  put_queries(0);
+  put_values(0);
+  put_triangles(0);
+  if (chunks > 1) {
+    keys(1);
+    queries(1);
+    values(1);
+    triangles(1);
+  }
+  lds_barrier();
+  for (int i = 0; i < chunks; ++i) {
+    const bool next = i + 1 < chunks, more = i + 2 < chunks;
+    const int buf = (i + 1) & 1;
+    lds_barrier();
+    if (next) {
+      put_keys(buf);
+      put_queries(buf);
+      put_values(buf);
+      put_triangles(buf);
+    }
+    if (more) {
+      keys(i + 2);
+      queries(i + 2);
+      values(i + 2);
+      triangles(i + 2);
+    }
+    lds_barrier();
+    lds_barrier();
+    lds_barrier();
+  }
+}
+template <typename L, int D1, int NP, bool VEC, bool REV>
+__device__ static inline void load_team(const Args& A, int bh, const void* values, int col0, int n, int tid) {
+  const Rows xv = rows_at<typename L::T>(values, A, bh, A.dv, n, col0, min(A.dv - col0, L::VC));
   if constexpr (L::kDirect) {
     if (tid < 64) load_keys<L, D1, NP, REV>(A, bh, n, tid);
     else load_rest<L, D1, NP, REV>(A, bh, xv, n, tid - 64);
   } else {
-    load_chunks<L, T, D1, NP, true, REV, 2>(A, bh, rows_at<T>(A.K, A, bh, A.dk, n, 0, A.dk), rows_at<T>(A.Q, A, bh, A.dk, n, 0, A.dk), xv, n, tid);
+    load_through<L, D1, NP, VEC, REV>(A, bh, xv, n, tid);
   }
 }
 
@@ -260,11 +333,11 @@ __device__ static inline void put_tile(f32x4 v, Buffer b, int row, int stride, i
 #pragma unroll
   for (int j = 0; j < 4; ++j) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[j]), b, at, (unsigned)(j * stride) * 4u, 0);
 }
-// x + sum_s a_s b_s: one chain (two, and their sum behind them, take longer: instructions count, not what a product waits for).  With one plane on a
-// side all operands are there before the first product: one wait.
-template <int MA, int MB, int S, int NA, int NB>
+// x + sum_s a_s b_s: one chain (two, and their sum behind them, take longer: instructions count, not what a product waits for).  One step's products behind
+// the other's (STEP), or, with one plane on a side, the smallest terms of all first: all operands are there before the first product, one wait.
+template <bool STEP, int MA, int MB, int S, int NA, int NB>
 __device__ static inline f32x4 mma_steps(const Planes<NA> (&a)[S], const Planes<NB> (&b)[S], f32x4 x) {
-  if constexpr (MA == 1 || MB == 1) {
+  if constexpr (!STEP && (MA == 1 || MB == 1)) {
 #pragma unroll
     for (int i = (MA > MB ? MA : MB) - 1; i >= 0; --i)
 #pragma unroll
@@ -275,7 +348,7 @@ __device__ static inline f32x4 mma_steps(const Planes<NA> (&a)[S], const Planes<
   }
   return x;
 }
-// x + t b for a triangle's block, the smallest terms first; of fp32 (STEP) in the order of mma_step (TRANS: b t).
+// x + t b for a triangle's block, the smallest terms first, or (STEP) in the order of mma_step (TRANS: b t).
 template <bool STEP, bool TRANS, int M, int N>
 __device__ static inline f32x4 mma_block(const Planes<M>& t, const Planes<N>& b, f32x4 x) {
   constexpr int W = M > N ? M : N;
@@ -312,35 +385,44 @@ __device__ static inline void put_state(const f32x4 (&S)[OWN], int own) {
     put_half<3>(own, split_half<3>(S[0]));
   }
 }
-// The state's rows, as planes, times the same rows of K (Q): x_kt + cols_kt u, for the wave's tiles.
+// The wave's tiles of the state + K^T (Q^T) u: all steps' smallest terms first, or one step's products behind the other's (STEP).
 template <typename L, int N>
 __device__ static inline void mma_update(const Planes<L::NI> (&k)[N][L::NS], const Planes<3> (&u)[L::NS], f32x4 (&S)[N]) {
-  constexpr int NI = L::NI;
 #pragma unroll
   for (int w = 2; w >= 0; --w)
 #pragma unroll
-    for (int i = 0; i < NI; ++i)
+    for (int i = 0; i < L::NI; ++i)
       if (w - i >= 0)
 #pragma unroll
         for (int s = 0; s < L::NS; ++s)
 #pragma unroll
           for (int kt = 0; kt < N; ++kt) S[kt] = mma1(k[kt][s].p[i], u[s].p[w - i], S[kt]);
 }
+template <typename L, int N>
+__device__ static inline void mma_update_step(const Planes<L::NI> (&k)[N][L::NS], const Planes<3> (&u)[L::NS], int s, f32x4 (&S)[N]) {
+#pragma unroll
+  for (int w = 2; w >= 0; --w)
+#pragma unroll
+    for (int i = 0; i < L::NI; ++i)
+      if (w - i >= 0)
+#pragma unroll
+        for (int kt = 0; kt < N; ++kt) S[kt] = mma1(k[kt][s].p[i], u[s].p[w - i], S[kt]);
+}
 
-template <typename T, int D1, int TEAMS, bool FWD>
+template <typename T, int D1, int TEAMS, bool DIRECT, bool VEC, bool FWD>
 __device__ static __forceinline__ void team_scan(const Args& A) {
   constexpr int NO = Kind<T>::kOut, NP = FWD ? NO : 0;
-  typedef TeamChunks<T, D1, TEAMS, NP, false> L;
+  typedef TeamChunks<T, D1, TEAMS, NP, false, DIRECT> L;
   constexpr int C = L::C, KS = L::KS, NS = L::NS, NB = L::NB, NI = L::NI, OWN = L::kOwn, TEAM = L::kTeam;
   typedef typename L::MK MK;
   typedef typename L::MV MV;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, team = wave / TEAM, h = wave % TEAM;
   const int bh = blockIdx.x, col0 = blockIdx.y * L::VC, n = length_of(A, bh), c0 = col0 + 16 * team, chunks = (n + C - 1) / C;
   const Lane l{lane & 15, lane >> 4};
-  const Rows xo = rows_at<T>(A.out, A, bh, A.dv, n, col0, L::VC);
+  const Rows xo = rows_at<T>(A.out, A, bh, A.dv, n, col0, min(A.dv - col0, L::VC));
   if (FWD && n < A.L) zero_rows<T>(xo, n, A.L, tid, L::kThreads);
   if (wave >= TEAM * TEAMS) {
-    if (chunks > 0) load_team<L, D1, NP, false>(A, bh, A.V, col0, n, tid - 64 * TEAM * TEAMS);
+    if (chunks > 0) load_team<L, D1, NP, VEC, false>(A, bh, A.V, col0, n, tid - 64 * TEAM * TEAMS);
     return;
   }
   f32x4 S[OWN];
@@ -370,17 +452,18 @@ __device__ static __forceinline__ void team_scan(const Args& A) {
     Planes<3> b[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) b[s] = get_planes<3>(base.planes + 3 * 1024 * s);
-    const f32x4 R = mma_steps<NI, 3>(k, b, zero4());
+    const f32x4 R = mma_steps<!DIRECT, NI, 3>(k, b, zero4());
     put_half<3>(base.half + L::x2 + (h >> 1) * 3 * 1024, split_half<3>(beta * (V - gamma * R)));
     Planes<3> t[2] = {get_block<NB, 3>(base.tri + tt)};
     if (NS == 2) t[1] = get_block<NB, 3>(base.tri + tt + (two ? 1024 : 0));
     f32x4 O = zero4(), U = zero4();
-    if (FWD) O = mma_steps<NO, NI>(b, q, O);
+    if (FWD) O = mma_steps<!DIRECT, NO, NI>(b, q, O);
     lds_barrier();
     {
       const Planes<3> r = get_planes<3>(base.planes + L::x2);
-      if (two) U = mma_block<NI == 3, false>(t[1], get_planes<3>(base.planes + L::x2 + 3 * 1024), U);
-      U = mma_block<NI == 3, false>(t[0], r, U);
+      if (!DIRECT) U = mma_block<true, false>(t[0], r, U);
+      if (two) U = mma_block<!DIRECT, false>(t[1], get_planes<3>(base.planes + L::x2 + 3 * 1024), U);
+      if (DIRECT) U = mma_block<false, false>(t[0], r, U);
     }
     put_half<3>(base.half + (h >> 1) * 3 * 1024, split_half<3>(left * U));
     if (FWD) put_half<NO>(base.half + L::kRows + (h >> 1) * NO * 1024, split_half<NO>(U));
@@ -397,15 +480,23 @@ __device__ static __forceinline__ void team_scan(const Args& A) {
       Planes<3> u[NS];
 #pragma unroll
       for (int s = 0; s < NS; ++s) u[s] = get_planes<3>(base.planes + 3 * 1024 * s);
-      mma_update<L>(kc, u, S);
+      if constexpr (DIRECT) {
+        mma_update<L>(kc, u, S);
+      } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) mma_update_step<L>(kc, u, s, S);
+      }
     }
     if (FWD) {
       const Planes<NO> p0 = get_block<NB, NO>(base.weights + tp), u0 = get_planes<NO>(base.planes + L::kRows);
       O *= lds_get<float>(base.row + tw);
-      if (two) O = mma_block<NI == 3, true>(get_block<NB, NO>(base.weights + tp + 1024), get_planes<NO>(base.planes + L::kRows + NO * 1024), O);
-      O = mma_block<NI == 3, true>(p0, u0, O);
+      if (!DIRECT) O = mma_block<true, true>(p0, u0, O);
+      if (two) O = mma_block<!DIRECT, true>(get_block<NB, NO>(base.weights + tp + 1024), get_planes<NO>(base.planes + L::kRows + NO * 1024), O);
+      if (DIRECT) O = mma_block<false, true>(p0, u0, O);
       const int row = 16 * h + l.i;
-      buffer_quad<T>(xo.rows(r0, nr), row < nr ? (unsigned)row * xo.row + (unsigned)((16 * team + 4 * l.g) * (int)sizeof(T)) : kNowhere, A.scale * O);
+      const unsigned col = (unsigned)((16 * team + 4 * l.g) * (int)sizeof(T));
+      if (VEC) buffer_quad<T>(xo.rows(r0, nr), row < nr && (DIRECT || col < xo.width) ? (unsigned)row * xo.row + col : kNowhere, A.scale * O);
+      else if (row < nr && col < xo.width) store_quad<T>(xo.at(r0 + row) + col, (int)(xo.width - col), A.scale * O);
     } else {
       put_tile(U, buffer(A.u + chunk_at(A, bh, c) * ((long long)C * A.dvp), (unsigned)(C * A.dvp) * 4u), 16 * h, A.dvp, c0, l);
     }
@@ -415,9 +506,9 @@ __device__ static __forceinline__ void team_scan(const Args& A) {
   if (A.s_out != nullptr) store_state<OWN>(S, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g, h * 16 * OWN);
 }
 
-template <typename T, int D1, int TEAMS>
+template <typename T, int D1, int TEAMS, bool DIRECT, bool VEC>
 __device__ static __forceinline__ void team_rev(const Args& A) {
-  typedef TeamChunks<T, D1, TEAMS, 3, true> L;
+  typedef TeamChunks<T, D1, TEAMS, 3, true, DIRECT> L;
   constexpr int C = L::C, KS = L::KS, NS = L::NS, NB = L::NB, NI = L::NI, OWN = L::kOwn, TEAM = L::kTeam;
   typedef typename L::MK MK;
   typedef typename L::MV MV;
@@ -425,7 +516,7 @@ __device__ static __forceinline__ void team_rev(const Args& A) {
   const int bh = blockIdx.x, col0 = blockIdx.y * L::VC, n = length_of(A, bh), c0 = col0 + 16 * team, chunks = (n + C - 1) / C;
   const Lane l{lane & 15, lane >> 4};
   if (wave >= TEAM * TEAMS) {
-    if (chunks > 0) load_team<L, D1, 3, true>(A, bh, A.dOut, col0, n, tid - 64 * TEAM * TEAMS);
+    if (chunks > 0) load_team<L, D1, 3, VEC, true>(A, bh, A.dOut, col0, n, tid - 64 * TEAM * TEAMS);
     return;
   }
   f32x4 G[OWN];
@@ -452,22 +543,24 @@ __device__ static __forceinline__ void team_rev(const Args& A) {
     {
       const Planes<3> p1 = get_block<NB, 3>(base.weights + tp);
       const Planes<NI> o1 = MV::col(tv, vc, 0, NS - 1);
-      if (two) D = mma_block<NI == 3, false>(get_block<NB, 3>(base.weights + tp - 1024), MV::col(tv, vc, 0, 0), D);
-      D = mma_block<NI == 3, false>(p1, o1, D);
+      if (two) D = mma_block<!DIRECT, false>(get_block<NB, 3>(base.weights + tp - 1024), MV::col(tv, vc, 0, 0), D);
+      if (DIRECT) D = mma_block<false, false>(p1, o1, D);
+      else D += mma_block<true, false>(p1, o1, zero4());
     }
     lds_barrier();
     Planes<3> b[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) b[s] = get_planes<3>(base.planes + 3 * 1024 * s);
-    const f32x4 U = mma_steps<NI, 3>(k, b, zero4());
+    const f32x4 U = mma_steps<!DIRECT, NI, 3>(k, b, zero4());
     put_half<3>(base.half + L::x2 + (h >> 1) * 3 * 1024, split_half<3>(left * U + D));
     const Half<3> o = split_half<3>(A.scale * gamma * column<MV, NI>(base.value + tv));
     lds_barrier();
     f32x4 R = zero4();
     {
       const Planes<3> t1 = get_block<NB, 3>(base.tri + tt), r1 = get_planes<3>(base.planes + L::x2 + (NS - 1) * 3 * 1024);
-      if (two) R = mma_block<NI == 3, false>(get_block<NB, 3>(base.tri + tt - 1024), get_planes<3>(base.planes + L::x2), R);
-      R = mma_block<NI == 3, false>(t1, r1, R);
+      if (two) R = mma_block<!DIRECT, false>(get_block<NB, 3>(base.tri + tt - 1024), get_planes<3>(base.planes + L::x2), R);
+      if (DIRECT) R = mma_block<false, false>(t1, r1, R);
+      else R += mma_block<true, false>(t1, r1, zero4());
     }
     put_half<3>(base.half + (h >> 1) * 3 * 1024, split_half<3>(-(gamma * beta) * R));
     put_half<3>(base.half + L::kRows + (h >> 1) * 3 * 1024, o);
@@ -490,8 +583,16 @@ __device__ static __forceinline__ void team_rev(const Args& A) {
 #pragma unroll
         for (int kt = 0; kt < OWN; ++kt) qc[kt][s] = MK::col(tq, base.query_cols, kt, s);
       }
-      mma_update<L>(qc, w, G);
-      mma_update<L>(kc, u, G);
+      if constexpr (DIRECT) {
+        mma_update<L>(qc, w, G);
+        mma_update<L>(kc, u, G);
+      } else {
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          mma_update_step<L>(qc, w, s, G);
+          mma_update_step<L>(kc, u, s, G);
+        }
+      }
     }
     put_tile(R, buffer(A.dr + chunk_at(A, bh, c) * ((long long)C * A.dvp), (unsigned)(C * A.dvp) * 4u), 16 * h, A.dvp, c0, l);
     lds_barrier();
@@ -500,62 +601,68 @@ __device__ static __forceinline__ void team_rev(const Args& A) {
   if (A.s_out != nullptr) store_state<OWN>(G, A.s_out + (long long)bh * A.dk * A.dv, A.dk, A.dv, c0 + l.i, l.g, h * 16 * OWN);
 }
 
-template <typename T, int D1, int TEAMS>
-__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true>::kThreads)) void k_delta_team(Args A) {
-  team_scan<T, D1, TEAMS, true>(A);
+template <typename T, int D1, int TEAMS, bool DIRECT, bool VEC>
+__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true, DIRECT>::kThreads)) void k_delta_team(Args A) {
+  team_scan<T, D1, TEAMS, DIRECT, VEC, true>(A);
 }
 // Backward: the gradients of the states (z = 0) and the states (z = 1) do not wait for each other.
-template <typename T, int D1, int TEAMS>
-__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true>::kThreads)) void k_delta_team_back(Args A, const float* g_in, float* g_out) {
+template <typename T, int D1, int TEAMS, bool DIRECT, bool VEC>
+__global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true, DIRECT>::kThreads)) void k_delta_team_back(Args A, const float* g_in, float* g_out) {
   if (blockIdx.z == 0) {
     A.s_in = g_in;
     A.s_out = g_out;
-    team_rev<T, D1, TEAMS>(A);
+    team_rev<T, D1, TEAMS, DIRECT, VEC>(A);
   } else {
-    team_scan<T, D1, TEAMS, false>(A);
+    team_scan<T, D1, TEAMS, DIRECT, VEC, false>(A);
   }
 }
 
-// Whether a call takes these kernels: rows that fill the tiles; of fp32, whose operands go through registers, while each team has a CU to itself.
+// Whether a call takes these kernels: DIRECT always; what goes through registers while each team of the launch has a CU to itself (48 heads of 1000 x 96 and
+// 80, 240 teams: 42 us, one wave for 16 columns 53; fp32, 48 heads of 1000 x 64 backward, 384 teams: 102, one wave 68).
 constexpr int kCUs = 256;
-static long long teams_of(const Args& a) { return (long long)a.B * a.H * (a.dv / 16); }
+static long long teams_of(const Args& a, int cols) { return (long long)a.B * a.H * ((cols + 15) / 16); }
 template <typename T>
-static bool teamed(const Args& a) { return (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0 && (sizeof(T) == 2 || teams_of(a) <= kCUs); }
+static bool direct(const Args& a) { return sizeof(T) == 2 && (a.dk == 64 || a.dk == 128) && a.dv % 64 == 0; }
+template <typename T>
+static bool teamed(const Args& a) { return direct<T>(a) || (a.dk <= 128 && teams_of(a, a.dv) <= kCUs); }
+template <typename T>
+static bool teamed_back(const Args& a, bool states) { return direct<T>(a) || (a.dk <= 128 && teams_of(a, a.dvp) * (states ? 2 : 1) <= kCUs); }
 
 // One team a workgroup as long as each of those has a CU to itself: the reads of LDS, 128 bytes a cycle, are what two share (24 x 4096 x 64 with
 // one and two: 78 and 98 us, backward 100 and 124).
-template <typename T, int D1, int TEAMS>
+template <typename T, int D1, int TEAMS, bool DIRECT, bool VEC>
 static dark_status go_team(const Args& a, hipStream_t st) {
-  typedef TeamChunks<T, D1, TEAMS, Kind<T>::kOut, false> L;
-  DARK_TRY(allow_lds(k_delta_team<T, D1, TEAMS>, L::all));
-  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_team<T, D1, TEAMS>), dim3(a.B * a.H, a.dv / L::VC), dim3(L::kThreads), L::all, a);
+  typedef TeamChunks<T, D1, TEAMS, Kind<T>::kOut, false, DIRECT> L;
+  DARK_TRY(allow_lds(k_delta_team<T, D1, TEAMS, DIRECT, VEC>, L::all));
+  DARK_LAUNCH(KID_DELTA_SCAN, st, (k_delta_team<T, D1, TEAMS, DIRECT, VEC>), dim3(a.B * a.H, (a.dv + L::VC - 1) / L::VC), dim3(L::kThreads), L::all, a);
   return DARK_OK;
 }
-template <typename T, int D1, int TEAMS>
+template <typename T, int D1, int TEAMS, bool DIRECT, bool VEC>
 static dark_status go_team_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
-  typedef TeamChunks<T, D1, TEAMS, 3, true> L;
-  constexpr int lds = L::all > TeamChunks<T, D1, TEAMS, 0, false>::all ? L::all : TeamChunks<T, D1, TEAMS, 0, false>::all;
-  DARK_TRY(allow_lds(k_delta_team_back<T, D1, TEAMS>, lds));
-  DARK_LAUNCH(KID_DELTA_BACK, st, (k_delta_team_back<T, D1, TEAMS>), dim3(a.B * a.H, a.dv / L::VC, states ? 2 : 1), dim3(L::kThreads), lds, a, g_in, g_out);
+  typedef TeamChunks<T, D1, TEAMS, 3, true, DIRECT> L;
+  constexpr int more = TeamChunks<T, D1, TEAMS, 0, false, DIRECT>::all, lds = L::all > more ? L::all : more;
+  DARK_TRY(allow_lds(k_delta_team_back<T, D1, TEAMS, DIRECT, VEC>, lds));
+  DARK_LAUNCH(KID_DELTA_BACK, st, (k_delta_team_back<T, D1, TEAMS, DIRECT, VEC>), dim3(a.B * a.H, a.dvp / L::VC, states ? 2 : 1), dim3(L::kThreads), lds, a, g_in, g_out);
   return DARK_OK;
 }
 template <typename T, int D1>
 static dark_status go_team(const Args& a, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (teams_of(a) > kCUs) return go_team<T, D1, 2>(a, st);
-  return go_team<T, D1, 1>(a, st);
+    if (direct<T>(a)) return teams_of(a, a.dv) > kCUs ? go_team<T, D1, 2, true, true>(a, st) : go_team<T, D1, 1, true, true>(a, st);
+  return vec_of<T>(a) ? go_team<T, D1, 1, false, true>(a, st) : go_team<T, D1, 1, false, false>(a, st);
 }
 template <typename T, int D1>
 static dark_status go_team_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
   if constexpr (sizeof(T) == 2)
-    if (teams_of(a) * (states ? 2 : 1) > kCUs) return go_team_back<T, D1, 2>(a, g_in, g_out, states, st);
-  return go_team_back<T, D1, 1>(a, g_in, g_out, states, st);
+    if (direct<T>(a))
+      return teams_of(a, a.dv) * (states ? 2 : 1) > kCUs ? go_team_back<T, D1, 2, true, true>(a, g_in, g_out, states, st) : go_team_back<T, D1, 1, true, true>(a, g_in, g_out, states, st);
+  return vec_of<T>(a) ? go_team_back<T, D1, 1, false, true>(a, g_in, g_out, states, st) : go_team_back<T, D1, 1, false, false>(a, g_in, g_out, states, st);
 }
 template <typename T>
-static dark_status launch_team(const Args& a, hipStream_t st) { return a.dk == 64 ? go_team<T, 64>(a, st) : go_team<T, 128>(a, st); }
+static dark_status launch_team(const Args& a, hipStream_t st) { return a.dk <= 64 ? go_team<T, 64>(a, st) : go_team<T, 128>(a, st); }
 template <typename T>
 static dark_status launch_team_back(const Args& a, const float* g_in, float* g_out, bool states, hipStream_t st) {
-  return a.dk == 64 ? go_team_back<T, 64>(a, g_in, g_out, states, st) : go_team_back<T, 128>(a, g_in, g_out, states, st);
+  return a.dk <= 64 ? go_team_back<T, 64>(a, g_in, g_out, states, st) : go_team_back<T, 128>(a, g_in, g_out, states, st);
 }
 
 }  // namespace delta

@@ -350,15 +350,16 @@ def test_two_graphs_replay_in_turn():
 # ---------------------------------------------------------------------------
 # a sequence's results, bit by bit, beside few others and beside more than there are compute units
 # ---------------------------------------------------------------------------
-@pytest.mark.parametrize("dtype,d", [("f32", 64), ("f32", 128), ("bf16", 64), ("bf16", 128)])
-def test_results_do_not_depend_on_the_batch(dtype, d):
+@pytest.mark.parametrize("dtype,dk_,dv", [("f32", 64, 64), ("f32", 128, 128), ("f32", 48, 56), ("f32", 31, 33), ("bf16", 64, 64), ("bf16", 128, 128), ("bf16", 96, 80),
+                                          ("bf16", 33, 65), ("bf16", 64, 72), ("bf16", 256, 64)])
+def test_results_do_not_depend_on_the_batch(dtype, dk_, dv):
     B, H, L = 24, 4, 150
     g = torch.Generator(device="cuda").manual_seed(8)
-    q, k, v, o = (torch.randn(B, H, L, d, generator=g, device="cuda") for _ in range(4))
+    q, k, v, o = (torch.randn(B, H, L, d, generator=g, device="cuda") for d in (dk_, dk_, dv, dv))
     q, k, v, o = (x.to(U.TORCH[dtype]) for x in (q / 8, k / k.norm(dim=-1, keepdim=True), v, o))
     a, beta = -0.1 * torch.rand(B, H, L, generator=g, device="cuda"), torch.rand(B, H, L, generator=g, device="cuda")
     lengths = torch.randint(0, L + 1, (B,), generator=g, device="cuda", dtype=torch.int32)
-    state, dstate = (torch.randn(B, H, d, d, generator=g, device="cuda") for _ in range(2))
+    state, dstate = (torch.randn(B, H, dk_, dv, generator=g, device="cuda") for _ in range(2))
     out, last = dk.dark_delta_fwd(q, k, v, a, beta, lengths=lengths, state=state, want_state=True)
     grads = dk.dark_delta_bwd(q, k, v, a, beta, o, lengths=lengths, state=state, dstate=dstate)
     for b in (0, B - 1):
