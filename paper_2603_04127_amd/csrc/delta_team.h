@@ -47,7 +47,7 @@ struct TeamChunks {
   static constexpr int k = 0, q = 2 * MK::kAll, v = q + qs * kQ, w = v + 2 * kV, t = w + 2 * kW, p = t + ts * kT, x = p + ps * kP;
   // exchange, of a team: the state's planes, in their place later U's (those of the update, and those of P U or of dO); R's
   static constexpr int NS = C / 32, kRows = 3 * 1024 * NS, kMore = REV ? kRows : NP * 1024 * NS;
-  static constexpr int kFirst = KS * 3 * 1024, kLast = kRows + kMore, x1 = 0, x2 = kFirst > kLast ? kFirst : kLast, kX = x2 + kRows;
+  static constexpr int kFirst = KS * 3 * 1024, kLast = kRows + kMore, x2 = kFirst > kLast ? kFirst : kLast, kX = x2 + kRows;
   static constexpr int all = x + TEAMS * kX;
   static_assert(all <= 160 * 1024, "fits the LDS");
 };
@@ -59,8 +59,8 @@ __device__ static inline void dma64_to_lds(const void* base, const unsigned (&of
   const unsigned dst = __builtin_amdgcn_readfirstlane((unsigned)to);
   const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)base), hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)base >> 32));
   asm volatile(
-      "s_mov_b32 m0, %5\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:1024\n\t"
-      "global_load_lds_dwordx4 %2, %4 offset:2048\n\tglobal_load_lds_dwordx4 %3, %4 offset:3072" ::"v"(off[0]),
+      "s_mov_b32 m0, %5\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %0, %4\n\tglobal_load_lds_dwordx4 %1, %4 offset:0x400\n\t"
+      "global_load_lds_dwordx4 %2, %4 offset:0x800\n\tglobal_load_lds_dwordx4 %3, %4 offset:0xc00" ::"v"(off[0]),
       "v"(off[1]), "v"(off[2]), "v"(off[3]), "s"((unsigned long long)hi << 32 | lo), "s"(dst)
       : "memory", "m0");
 }

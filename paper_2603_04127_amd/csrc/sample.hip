@@ -443,6 +443,20 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     }
     __syncthreads();
   }
+  u64 least = 0;
+  if (q > 0.f) {
+    // min_p as a bound: behind the largest logit whose weight is below it.  Six bits at a time, and two; a NaN weighs nothing.
+    unsigned key = 0;
+    const unsigned most = ordered(top);
+#pragma unroll 1
+    for (int shift = 26; shift >= -4; shift -= 6) {
+      const unsigned own = key | (shift >= 0 ? (unsigned)lane << shift : (unsigned)lane & 3u);
+      const u64 below = __ballot(own < most && !(weight.any(value_of(own)) >= (double)q) && (shift >= 0 || lane < 4));
+      const unsigned digit = (unsigned)__builtin_popcountll(below) - 1u;
+      key |= shift >= 0 ? digit << shift : digit;
+    }
+    least = (u64)(key + 1) << 32 | 0x80000000u;   // with the highest number
+  }
   if (!done) {
     // Bins over the logits from the largest down, as far as weights matter beside 1 - top_p of the sum (and further for top_k).
     const float reach = (logf((float)V) + (by_p ? fmaxf(-logf(1.f - p), 0.f) : 0.f) + 3.f) * 1.4426950408889634f / (float)fmin(fmax(weight.c, 1e-30), 1e30);
@@ -532,18 +546,18 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
           }
         });
       };
-      // on the way, the sums of the weights before the bin, which are kept whatever is left of the bin itself
+      // on the way, the sums of the weights before the bin (and from min_p's bound on), which are kept whatever is left of the bin itself
       sum = 0.0;
-      const float beyond = fmaxf(to, weight.floor);
+      const float beyond = fmaxf(value_of(ordered(fmaxf(to, weight.floor)) + 1u), least != 0 ? logit_of(least) : -INFINITY);
       row.each(wave, lane, [&](u32x4 v, int t) __attribute__((always_inline)) {
 #pragma unroll
         for (int j = 0; j < P; ++j) {
           const float x = Row<T>::value(v, j);
           const double w = weight(x);
-          sum += x > beyond ? w : 0.0;
+          sum += x >= beyond ? w : 0.0;
           if (j % 4 == 3) __builtin_amdgcn_sched_barrier(0);
         }
-        in_bin(v, t, [&](float x) { sum += weight.any(x); });
+        in_bin(v, t, [&](float x) { sum += least == 0 || x >= logit_of(least) ? weight.any(x) : 0.0; });
       });
       __syncthreads();
       int n = s.size;
@@ -646,20 +660,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       bound = s.bound;
     }
   }
-  if (q > 0.f) {
-    // min_p as a bound: behind the largest logit whose weight is below it.  Six bits at a time, and two; a NaN weighs nothing.
-    unsigned key = 0;
-    const unsigned most = ordered(top);
-#pragma unroll 1
-    for (int shift = 26; shift >= -4; shift -= 6) {
-      const unsigned own = key | (shift >= 0 ? (unsigned)lane << shift : (unsigned)lane & 3u);
-      const u64 below = __ballot(own < most && !(weight.any(value_of(own)) >= (double)q) && (shift >= 0 || lane < 4));
-      const unsigned digit = (unsigned)__builtin_popcountll(below) - 1u;
-      key |= shift >= 0 ? digit << shift : digit;
-    }
-    const u64 least = (u64)(key + 1) << 32 | 0x80000000u;   // with the highest number
-    if (least > bound) bound = least, summed = false;
-  }
+  bound = bound > least ? bound : least;
   // ---------------------------------------------------------------------------
   // The draw: sums of the kept weights, of each wave's part of the row, then of a sixteenth of one part by each wave.
   // ---------------------------------------------------------------------------
@@ -699,7 +700,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   if (!weighed && summed) {
     for (int i = lane; i < s.kept; i += 64) {
       const int piece = (token_of(s.list[i]) - row.begin) / P;
-      if (piece / (64 * row.pieces) == wave) sum += weight.any(logit_of(s.list[i]));
+      if (piece / (64 * row.pieces) == wave && s.list[i] >= bound) sum += weight.any(logit_of(s.list[i]));
     }
     sum = wave_sum(sum);
     if (lane == 0) s.sums[wave] = sum;

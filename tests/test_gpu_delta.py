@@ -166,6 +166,15 @@ def test_no_gate_is_a_gate_of_zero(dtype):
     assert all(torch.equal(x, y) for x, y in zip((*_forward(d), *g.values()), want[:6] + want[7:]))
 
 
+@pytest.mark.parametrize("dtype,widths,B", [("bf16", (64, 64), 1), ("bf16", (128, 128), 7), ("bf16", (33, 65), 1), ("f32", (64, 64), 1), ("f32", (31, 33), 1)])
+def test_gradients_one_by_one(dtype, widths, B):
+    d = _device(U.problem(21, B, 3, 200, *widths, dtype, state=True, dstate=True))
+    want = _backward(d)
+    for name, t in want.items():
+        alone = _backward(d, need=(name,))
+        assert list(alone) == [name] and torch.equal(alone[name], t), name
+
+
 def test_state_in_place_and_continued_prompts():
     p = U.problem(13, 2, 2, 300, 64, 64, "bf16", state=True)
     d = _device(p)
