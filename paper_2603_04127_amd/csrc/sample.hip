@@ -17,9 +17,9 @@
 // row in 8000 would draw a token's neighbour.
 // What bounds it: of 256 rows of 131071 bf16 logits the first read takes 10 us (6.7 TB/s), a read that asks a comparison of each logit 9, one that weighs
 // each 24 (19 instructions a logit, four waves a SIMD; the matrix of 67 MB lies in the last cache by then), the histogram's 40 (two more for the
-// addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 32, no filter 37 (weighed in a read of its
-// own behind that for the largest: 47), top_p 0.9 103 (with
-// a read for the list and one for the sum 107); one row of 32000 fp32 logits 8, 14, 12 and 29, where the way through the steps counts and not the row.
+// addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 31, no filter 37 (weighed in a read of its own behind that for the largest:
+// 47), top_p 0.9 101 (with a read for the list and one for the sum 107); one row of 32000 fp32 logits 8, 12.5, 12 and 29, where the way through the
+// steps counts and not the row (top_k 50 with the bound's bits four at a time alone: 14.4).
 #include <cmath>
 #include <type_traits>
 
@@ -205,10 +205,13 @@ struct Shared {
 __device__ __forceinline__ void sort(Shared& s, int n, int tid) {
   if (n <= kCounted) {
     const u64 own = tid < n ? s.list[tid] : 0;
+    if (tid >= n && tid < n + 8) s.list[tid] = 0;
+    __syncthreads();
     int before = 0;
     if (tid < n)
-#pragma unroll 4
-      for (int i = 0; i < n; ++i) before += s.list[i] > own;
+      for (int i = 0; i < n; i += 8)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) before += s.list[i + j] > own;
     __syncthreads();
     if (tid < n) s.list[before] = own;   // entries are distinct
     __syncthreads();
@@ -359,24 +362,39 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   bool done = k == 0 && !by_p;
   bool summed = false;   // whether `sum` is that of a thread's weights before the bin that holds the bound, and the list's first s.kept are what is kept of it
   if (!done && k > 0 && k <= kSmall) {
-    // The k-th largest of the threads' maxima is at most the k-th largest logit: its first 16 bits, four at a time, a wave for each value of them.
-    unsigned key[kThreads / 64], cut = k > 1 ? 0 : ordered(top);
-#pragma unroll
-    for (int i = 0; i < kThreads / 64; ++i) key[i] = ordered(s.tops[i * 64 + lane]);
+    // The k-th largest of the threads' maxima is at most the k-th largest logit.  Most often it is within a factor of two of the largest: then 64 counters
+    // of what lies so many 2^17 units of the last place below that say where it is; else its first 16 bits, four at a time, a wave for each value of them.
+    const unsigned most = ordered(top);
+    unsigned cut = most;
     if (tid == 0) s.size = 0;
-    if (k == 1) __syncthreads();
-#pragma unroll 1
-    for (int shift = k > 1 ? 28 : 12; shift >= 16; shift -= 4) {   // the largest is known
-      const unsigned next = cut | (unsigned)wave << shift;
-      int n = 0;
-#pragma unroll
-      for (int i = 0; i < kThreads / 64; ++i) n += __builtin_popcountll(__ballot(key[i] >= next));
-      unsigned* const of = s.count + 4 * shift;   // each round its own
-      if (lane == 0) of[wave] = (unsigned)n;
+    if (k > 1) {
+      if (tid < 64) s.count[tid] = 0;
       __syncthreads();
-      const u64 reach = __ballot(lane < 16 && (int)of[lane & 15] >= k);   // of 0 always
-      cut |= (unsigned)(63 - __builtin_clzll(reach)) << shift;
+      const unsigned below = (most - ordered(mine)) >> 17;
+      if (below < 64) atomicAdd(&s.count[below], 1u);
+      __syncthreads();
+      const int upto = wave_prefix((int)s.count[lane], lane);
+      const u64 there = __ballot(upto >= k);
+      cut = there != 0 ? most - ((unsigned)(__builtin_ctzll(there) + 1) << 17) + 1u : 0;
     }
+    if (cut == 0) {
+      unsigned key[kThreads / 64];
+#pragma unroll
+      for (int i = 0; i < kThreads / 64; ++i) key[i] = ordered(s.tops[i * 64 + lane]);
+#pragma unroll 1
+      for (int shift = 28; shift >= 16; shift -= 4) {
+        const unsigned next = cut | (unsigned)wave << shift;
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kThreads / 64; ++i) n += __builtin_popcountll(__ballot(key[i] >= next));
+        unsigned* const of = s.count + 4 * shift;   // each round its own, and not the counters above
+        if (lane == 0) of[wave] = (unsigned)n;
+        __syncthreads();
+        const u64 reach = __ballot(lane < 16 && (int)of[lane & 15] >= k);   // of 0 always
+        cut |= (unsigned)(63 - __builtin_clzll(reach)) << shift;
+      }
+    }
+    if (k == 1) __syncthreads();
     const unsigned lowest = ordered(-3.402823466e38f);
     const float least = value_of(cut > lowest ? cut : lowest);
     row.each(wave, lane, [&](u32x4 v, int t) {
@@ -405,7 +423,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         double before = 0.0;
         if (tid < m) {
           const int own = token_of(s.list[tid]);
-          for (int i = 0; i < m; ++i) before += token_of(s.list[i]) < own ? s.weights[i] : 0.0;
+          for (int i = 0; i < m; i += 4)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) before += i + j < m && token_of(s.list[i + j]) < own ? s.weights[i + j] : 0.0;
         }
         __syncthreads();
         if (tid < m) s.weights[tid] = before;
