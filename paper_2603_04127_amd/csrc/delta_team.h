@@ -457,10 +457,10 @@ __device__ static __forceinline__ void team_scan(const Args& A) {
     Planes<3> t[2] = {get_block<NB, 3>(base.tri + tt)};
     if (NS == 2) t[1] = get_block<NB, 3>(base.tri + tt + (two ? 1024 : 0));
     f32x4 O = zero4(), U = zero4();
-    if (FWD) O = mma_steps<!DIRECT, NO, NI>(b, q, O);
     lds_barrier();
     {
       const Planes<3> r = get_planes<3>(base.planes + L::x2);
+      if (FWD) O = mma_steps<!DIRECT, NO, NI>(b, q, O);   // while the reads are on their way
       if (!DIRECT) U = mma_block<true, false>(t[0], r, U);
       if (two) U = mma_block<!DIRECT, false>(t[1], get_planes<3>(base.planes + L::x2 + 3 * 1024), U);
       if (DIRECT) U = mma_block<false, false>(t[0], r, U);
@@ -539,7 +539,11 @@ __device__ static __forceinline__ void team_rev(const Args& A) {
 #pragma unroll
     for (int s = 0; s < KS; ++s) k[s] = MK::row(tk, base.rows, 0, s);
     const f32x4 gamma = lds_get<f32x4>(base.vec + tw), left = lds_get<f32x4>(base.vec + tw + 4 * C), beta = lds_get<f32x4>(base.vec + tw + 4 * 2 * C);
-    f32x4 D = zero4();
+    lds_barrier();
+    Planes<3> b[KS];
+#pragma unroll
+    for (int s = 0; s < KS; ++s) b[s] = get_planes<3>(base.planes + 3 * 1024 * s);
+    f32x4 D = zero4();   // scale P^T dO, while the reads are on their way
     {
       const Planes<3> p1 = get_block<NB, 3>(base.weights + tp);
       const Planes<NI> o1 = MV::col(tv, vc, 0, NS - 1);
@@ -547,10 +551,6 @@ __device__ static __forceinline__ void team_rev(const Args& A) {
       if (DIRECT) D = mma_block<false, false>(p1, o1, D);
       else D += mma_block<true, false>(p1, o1, zero4());
     }
-    lds_barrier();
-    Planes<3> b[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) b[s] = get_planes<3>(base.planes + 3 * 1024 * s);
     const f32x4 U = mma_steps<!DIRECT, NI, 3>(k, b, zero4());
     put_half<3>(base.half + L::x2 + (h >> 1) * 3 * 1024, split_half<3>(left * U + D));
     const Half<3> o = split_half<3>(A.scale * gamma * column<MV, NI>(base.value + tv));
