@@ -327,7 +327,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   const bool by_p = p < 1.f;
   if (!(p > 0.f)) p = by_p ? 0.f : 1.f;
   u64 bound = 0;   // entries from this one on are kept
-  const double unit = (double)(1ull << (__builtin_clz((unsigned)V) + 19));   // of an integer weight: V of them stay below 2^51
+  const double unit = (double)(1ull << min(__builtin_clz((unsigned)V) + 30, 51));   // of an integer weight: it stays below 2^52, and V of them below 2^63
   const auto integer = [&](double w) __attribute__((always_inline)) -> u64 { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; };
 
   // The list holds all entries of a part of the order, sorted, behind `rank` entries of weight `held`: the last that is kept of them, by rank

@@ -109,6 +109,27 @@ def test_masked_logits(dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_shares_of_very_long_rows(dtype):
+    # Tokens of 1e-7 of the sum each: the share before and behind the drawn one says more than its number.  Where top_p is looked for a weight is off
+    # by half a unit of 2^-36 of the largest at most, 2^25 of them by 2^-12; their sum is more than 100 times the largest: 2.4e-6 of it, twice that for
+    # the whole and the part.
+    V, tol = (1 << 25) + 1, 5e-6
+    g = torch.Generator(device="cuda").manual_seed(15)
+    x = (3.0 * torch.randn(1, V, generator=g, device="cuda")).to(TORCH[dtype])
+    z, at = torch.sort(x[0].float(), descending=True, stable=True)
+    e = torch.exp(z.double() - z[0].double())
+    assert e.sum() > 100
+    for u, p, q in ((0.3, 0.9, 0.0), (0.85, 0.9, 0.0), (0.5, 0.999, 0.0), (0.6, 0.9, 1e-5), (0.25, 1.0, 0.0)):
+        t = int(dk.dark_sample(x, torch.full((1,), u, device="cuda"), top_p=p, min_p=q))
+        n = V if p >= 1.0 else int((torch.cumsum(e, 0) - e < float(np.float32(p)) * e.sum()).sum())
+        w = torch.zeros(V, dtype=torch.float64, device="cuda")
+        w[at[:n]] = torch.where(e[:n] >= float(np.float32(q)), e[:n], 0.0)
+        c = torch.cumsum(w, 0)
+        share = c[t] / c[-1], (c[t] - w[t]) / c[-1]
+        assert share[0] >= u - tol and share[1] <= u + tol, (u, p, q, float(share[0]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 def test_rows_without_filters_weighed_on_the_way(dtype):
     # a row's first logits say little about the others: masked, far below or far above them, all alike
     rng = np.random.default_rng(14)
