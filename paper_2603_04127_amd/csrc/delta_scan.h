@@ -192,6 +192,7 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
 // all of a chunk's products by itself: its state is an operand of K S and Q S, R of T R, U of P U and of the update, all without a way
 // through LDS or another wave.  Further waves bring the next chunk's operands to LDS meanwhile: a wave that has its SIMD to itself issues an
 // instruction in five or six cycles, whatever it is, so that the chain from state to state is as long as it has instructions.
+// (bf16, 64 heads of 8192 x 120 and 128: 430 us; 64 heads of 2048 x 256 and 128: 196; fp32, 96 heads of 1024 x 64: 65, backward 90.)
 // ---------------------------------------------------------------------------
 // A chunk's operands in LDS (NP: planes of P, 0: neither Q nor P), in one buffer or two.  An instruction's own offset reaches 64 KB: a lane has a
 // base for each operand, and the buffers lie beside each other.
