@@ -465,8 +465,7 @@ dark_status dark_beam_select(const dark_beam_params* p, const void* logits, cons
  *   out_token [B] int32, out_logprob [B] float32 or NULL.
  *   Logits that are -infinity or NaN are never drawn, nor counted; if a row has no others, its token is -1, its logarithm -infinity.  Where
  *   logits are +infinity, those share everything.
- * w and its sums are in fp64, w to 2^-33 of its value; what is below 2^-1000 counts as 0.  Where top_p ends is sought in whole units of w, 2^-34 or less
- * (2^-45 for 2^17 tokens).  No workspace.  V <= 2^27, B <= 2^22 (else DARK_EUNSUPPORTED).
+ * w and its sums are in fp64, w to 2^-32 of its value; what is below 2^-1000 counts as 0.  No workspace.  V <= 2^27, B <= 2^22 (else DARK_EUNSUPPORTED).
  */
 typedef struct {
   int32_t B, V;        /* rows, vocabulary */

@@ -12,7 +12,8 @@
 //    the weights before it.
 //  * The draw sums the kept weights by waves, each of which holds a contiguous part of the row, and looks into one of them.  A row that keeps
 //    everything has these sums from the first read.
-// Weights are in fp64, by a polynomial, to 2^-33 of their value, and so are their sums; a histogram's are integers, whose sums have no order.
+// Weights are in fp64, by a polynomial, to 2^-33 of their value, and so are their sums; a histogram's are integers, whose sums have no order, in units that go
+// with the bins.  (With one unit for all bins, of the largest weight, a long tail counted as nothing: of one token and 2^25 of 2^-37 each, top_p 0.9999 kept the one alone.)
 // In fp32 the borders between a large row's tokens would be off by some 2^-30 of the row's sum each, 2^17 of them together by 2^-13: one
 // row in 8000 would draw a token's neighbour.
 // What bounds it: of 256 rows of 131071 bf16 logits the first read takes 10 us (6.7 TB/s), a read that asks a comparison of each logit 9, one that weighs
@@ -149,7 +150,8 @@ struct Row {
 struct Weight {
   double m, c;     // c = log2 e / T
   float floor;
-  __device__ __forceinline__ double operator()(float x) const {
+  // times 2^up
+  __device__ __forceinline__ double operator()(float x, int up = 0) const {
     const double z = ((double)x - m) * c, t = z + 6755399441055744.0, f = z - (t - 6755399441055744.0);
     double y = fma(f, 1.529732376073432e-05, 1.5461444698569848e-4);
     y = fma(f, y, 1.3333502386162631e-3);
@@ -158,10 +160,10 @@ struct Weight {
     y = fma(f, y, 2.4022650922288757e-1);
     y = fma(f, y, 6.9314718055994529e-1);
     y = fma(f, y, 1.0);
-    return __hiloint2double(__double2hiint(y) + (int)((unsigned)__double2loint(t) << 20), __double2loint(y));
+    return __hiloint2double(__double2hiint(y) + (int)((unsigned)(__double2loint(t) + up) << 20), __double2loint(y));
   }
   // the same for any logit; -infinity and NaN weigh nothing
-  __device__ __forceinline__ double any(float x) const { return x >= floor ? (*this)(x) : 0.0; }
+  __device__ __forceinline__ double any(float x, int up = 0) const { return x >= floor ? (*this)(x, up) : 0.0; }
 };
 
 template <typename T>
@@ -197,7 +199,8 @@ struct Shared {
   double sums[kWaves], scan[kWaves], weights[kSmall];
   float tops[kThreads];
   u64 bound;         // the last entry that is kept
-  u64 before;        // weight of the bins before the chosen one
+  double before;     // weight of the bins before the chosen one
+  double target;     // the weight that top_p asks for
   int ranks_before, bin, size, kept, again;
 };
 
@@ -327,18 +330,22 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   const bool by_p = p < 1.f;
   if (!(p > 0.f)) p = by_p ? 0.f : 1.f;
   u64 bound = 0;   // entries from this one on are kept
-  const double unit = (double)(1ull << min(__builtin_clz((unsigned)V) + 30, 51));   // of an integer weight: it stays below 2^52, and V of them below 2^63
+  // A histogram's weights are whole numbers, of a unit that every octave of the order has for itself: a weight of 2^-(o+1) ... 2^-o counts as 2^(bits-1) ...
+  // 2^bits, so that it keeps 2^-bits of its value, 2^-34 at least, however many there are; it stays below 2^52, and V of them below 2^63.
+  const int bits = min(__builtin_clz((unsigned)V) + 30, 51);
+  const double unit = (double)(1ull << bits);
   const auto integer = [&](double w) __attribute__((always_inline)) -> u64 { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; };
+  const auto value_in = [&](u64 sum, int octave) __attribute__((always_inline)) -> double { return (double)sum * __hiloint2double((1023 - bits - octave) << 20, 0); };
 
   // The list holds all entries of a part of the order, sorted, behind `rank` entries of weight `held`: the last that is kept of them, by rank
-  // or by weight (target), and the weight up to it.  By one wave.
-  const auto last_of = [&](int n, int rank, u64 held, bool by_rank, int most, u64 target, u64* upto) __attribute__((always_inline)) -> u64 {
-    u64 found = 0, sum = held;
+  // or by weight (target; the first at least), and the weight up to it.  By one wave.
+  const auto last_of = [&](int n, int rank, double held, bool by_rank, int most, double target, double* upto) __attribute__((always_inline)) -> u64 {
+    u64 found = 0;
+    double sum = held;
     for (int i0 = 0; i0 < n; i0 += 64) {
       const u64 e = i0 + lane < n ? s.list[i0 + lane] : 0;
-      const u64 w = e != 0 ? integer(weight.any(logit_of(e))) : 0;
-      const u64 up = sum + wave_prefix(w, lane);
-      const bool in = e != 0 && (by_rank ? rank + i0 + lane < most : up - w < target || (held == 0 && i0 + lane == 0));
+      const double up = sum + wave_prefix(e != 0 ? weight.any(logit_of(e)) : 0.0, lane), below = __shfl_up(up, 1, 64);
+      const bool in = e != 0 && (by_rank ? rank + i0 + lane < most : (lane == 0 ? sum : below) < target || i0 + lane == 0);
       const u64 kept = __ballot(in);
       if (kept != 0) {
         const int last = 63 - __builtin_clzll(kept);
@@ -405,8 +412,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     if (n <= kList) {
       sort(s, n, tid);
       if (wave == 0) {
-        u64 upto = 0, e = last_of(n, 0, 0, true, k, 0, &upto);
-        if (by_p) e = last_of(min(n, k), 0, 0, false, 0, (u64)((double)p * (double)upto), &upto);
+        double upto = 0.0;
+        u64 e = last_of(n, 0, 0.0, true, k, 0.0, &upto);
+        if (by_p) e = last_of(min(n, k), 0, 0.0, false, 0, (double)p * upto, &upto);
         if (lane == 0) s.bound = e;
       }
       __syncthreads();
@@ -478,10 +486,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     least = (u64)(key + 1) << 32 | 0x80000000u;   // with the highest number
   }
   if (!done) {
-    // Bins over the logits from the largest down, as far as weights matter beside 1 - top_p of the sum (and further for top_k).
-    const float reach = (logf((float)V) + (by_p ? fmaxf(-logf(1.f - p), 0.f) : 0.f) + 3.f) * 1.4426950408889634f / (float)fmin(fmax(weight.c, 1e-30), 1e30);
-    const float step = fminf((float)(kBins - 1) / reach, 1e30f);
-    const auto bin_of = [&](float x) __attribute__((always_inline)) -> int { return (int)fminf((top - x) * step, (float)(kBins - 1)); };
+    // Bins over the logits from the largest down, as far as weights matter beside 1 - top_p of the sum (and further for top_k): 2^fine of them an octave of the
+    // weights, 32 at least (as far is 56 octaves at most).  Differences are halved: those of the largest numbers stay finite.
+    const float reach = (logf((float)V) + (by_p ? fmaxf(-logf(1.f - p), 0.f) : 0.f) + 3.f) * 1.4426950408889634f;
+    int fine = 5;
+    while (fine < 9 && reach * (float)(2 << fine) <= (float)(kBins - 1)) ++fine;
+    const float step = (float)fmin(fmax(weight.c * (double)(2 << fine), 2e-38), 3e38), half = 0.5f * top;
+    const auto bin_of = [&](float x) __attribute__((always_inline)) -> int { return (int)fminf(fmaf(x, -0.5f, half) * step, (float)(kBins - 1)); };
     for (int i = tid; i < kBins; i += kThreads) s.mass[i] = 0, s.count[i] = 0;
     __syncthreads();
     // the last bin's, which may be most, add up on their way
@@ -494,7 +505,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
           const float x = Row<T>::value(v, j);
           if (x > -INFINITY) {
             const int at = bin_of(x);
-            const u64 w = integer(weight.any(x));
+            const u64 w = integer(weight.any(x, at >> fine));
             if (at < kBins - 1) {
               atomicAdd(&s.mass[at], w);
               if (counted) atomicAdd(&s.count[at], 1u);
@@ -515,31 +526,37 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     if (k > 0) histogram(std::integral_constant<bool, true>());
     else histogram(std::integral_constant<bool, false>());   // top_p asks for no ranks
     __syncthreads();
-    // The bin where the order reaches `most` entries, or a weight of `target`; what lies before it.
-    const auto choose = [&](bool by_rank, int most, u64 target) __attribute__((always_inline)) {
+    // The bin where the order reaches `most` entries, or a weight of `target` (below 0: top_p of them all); what lies before it.  Of the order's bins, or (octave
+    // >= 0) of the parts of one in that octave.
+    const auto choose = [&](bool by_rank, int most, double target, int octave) __attribute__((always_inline)) {
       if (wave == 0) {
-        u64 m = 0;
+        const auto octave_of = [&](int i) __attribute__((always_inline)) -> int { return octave >= 0 ? octave : i >> fine; };
+        u64 m = 0;   // a lane's bins lie in one octave
         int n = 0;
         for (int i = 0; i < kBins / 64; ++i) m += s.mass[lane * (kBins / 64) + i], n += (int)s.count[lane * (kBins / 64) + i];
-        u64 mb = wave_prefix(m, lane) - m;
-        int nb = wave_prefix(n, lane) - n;
+        const double um = wave_prefix(value_in(m, octave_of(lane * (kBins / 64))), lane), mb = __shfl_up(um, 1, 64);
+        const int un = wave_prefix(n, lane);
+        if (!by_rank && target < 0.0) {
+          target = (double)p * __shfl(um, 63, 64);
+          if (lane == 0) s.target = target;
+        }
         // the lane whose bins reach it; the last one with entries if none does
-        const bool any = by_rank ? n > 0 : m > 0, reaches = any && (by_rank ? nb + n >= most : mb + m >= target);
+        const bool any = by_rank ? n > 0 : m > 0, reaches = any && (by_rank ? un >= most : um >= target);
         const u64 r = __ballot(reaches), some = __ballot(any);
         const int who = r != 0 ? __builtin_ctzll(r) : 63 - __builtin_clzll(some);
         // its bins, one a lane
         const int at = __shfl(lane, who, 64) * (kBins / 64) + (lane & 31);
-        const u64 base_m = __shfl(mb, who, 64);
-        const int base_n = __shfl(nb, who, 64);
-        const u64 w = lane < 32 ? s.mass[at] : 0;
+        const double base_m = __shfl(lane > 0 ? mb : 0.0, who, 64);
+        const int base_n = __shfl(un - n, who, 64);
+        const double w = lane < 32 ? value_in(s.mass[at], octave_of(at)) : 0.0;
         const int c = lane < 32 ? (int)s.count[at] : 0;
-        const u64 upto_m = base_m + wave_prefix(w, lane);
+        const double upto_m = base_m + wave_prefix(w, lane), below = __shfl_up(upto_m, 1, 64);
         const int upto_n = base_n + wave_prefix(c, lane);
-        const bool own = by_rank ? c > 0 : w > 0;
+        const bool own = by_rank ? c > 0 : w > 0.0;
         const u64 hit = __ballot(own && (by_rank ? upto_n >= most : upto_m >= target)), full = __ballot(own);
         const int bin = hit != 0 ? __builtin_ctzll(hit) : 63 - __builtin_clzll(full);
         if (lane == bin) {
-          s.before = upto_m - w;
+          s.before = lane > 0 ? below : base_m;
           s.ranks_before = upto_n - c;
           s.bin = at;
           s.size = 0;
@@ -548,11 +565,13 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       __syncthreads();
     };
     // All entries of a bin, sorted: from a bin of more than the list holds, the part of it where the order reaches its end.
-    const auto gather = [&](bool by_rank, int most, u64 target) __attribute__((always_inline)) {
-      choose(by_rank, most, target);
+    const auto gather = [&](bool by_rank, int most) __attribute__((always_inline)) {
+      choose(by_rank, most, -1.0, -1);
       const int bin = s.bin;
-      const float width = 1.f / step, slack = 1e-4f * (width * (float)bin + 1e-6f * fabsf(top)) + 1e-6f * fabsf(top);
-      const float to = top - (width * (float)bin - slack), from = bin == kBins - 1 ? -3.402823466e38f : top - (width * (float)(bin + 1) + slack);
+      const double target = by_rank ? 0.0 : s.target;
+      const float width = 1.f / step, slack = 1e-4f * width * (float)(bin + 1) + 5e-7f * fabsf(top);   // of halves, as in bin_of
+      const float to = 2.f * (half - (width * (float)bin - slack)),
+                  from = bin == kBins - 1 ? -3.402823466e38f : fmaxf(2.f * (half - (width * (float)(bin + 1) + slack)), -3.402823466e38f);
       // entries lo ... hi of the order are left; each pass leaves a part of 2048 of them
       u64 lo = bound, hi = ~0ull;   // nothing that top_k left out
       // the logits that the bin can hold, and a little more: what they are exactly is asked of few
@@ -607,7 +626,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         hi = s.list[1];
         int shift = 0;
         while ((hi - lo) >> shift >= kBins) ++shift;
-        const u64 before = s.before;
+        const double before = s.before;
         const int ranks = s.ranks_before;
         __syncthreads();
         row.each(wave, lane, [&](u32x4 v, int t) {
@@ -616,14 +635,14 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
               const u64 e = entry(x, tk);
               if (e >= lo && e <= hi) {
                 const int at = (int)((hi - e) >> shift);
-                atomicAdd(&s.mass[at], integer(weight.any(x)));
+                atomicAdd(&s.mass[at], integer(weight.any(x, bin >> fine)));
                 atomicAdd(&s.count[at], 1u);
               }
             }
           });
         });
         __syncthreads();
-        choose(by_rank, most - ranks, target > before ? target - before : 0);
+        choose(by_rank, most - ranks, target > before ? target - before : 0.0, bin >> fine);
         const int sub = s.bin;
         const u64 top_e = hi - ((u64)sub << shift);
         const u64 width = (1ull << shift) - 1;
@@ -639,20 +658,15 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       sort(s, n, tid);
       return n;
     };
-    u64 whole = 0;
-    for (int i = 0; i < kBins; i += 64) whole += s.mass[i + lane];
-    whole = wave_sum(whole);
-    __syncthreads();
     if (k > 0) {
-      const int n = gather(true, k, 0);
+      const int n = gather(true, k);
       if (wave == 0) {
-        u64 upto = 0;
-        const u64 e = last_of(n, s.ranks_before, s.before, true, k, 0, &upto);
-        if (lane == 0) s.bound = e, s.before = upto;
+        double upto = 0.0;
+        const u64 e = last_of(n, s.ranks_before, s.before, true, k, 0.0, &upto);
+        if (lane == 0) s.bound = e;
       }
       __syncthreads();
       bound = s.bound;
-      whole = s.before;
       __syncthreads();
       if (by_p) {   // the histogram anew: gathering may have used it, and what top_k leaves out counts no more
         for (int i = tid; i < kBins; i += kThreads) s.mass[i] = 0, s.count[i] = 0;
@@ -660,7 +674,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         row.each(wave, lane, [&](u32x4 v, int t) {
           Row<T>::elements(v, t, [&](float x, int tk) {
             if (x > -INFINITY && entry(x, tk) >= bound) {
-              atomicAdd(&s.mass[bin_of(x)], integer(weight.any(x)));
+              atomicAdd(&s.mass[bin_of(x)], integer(weight.any(x, bin_of(x) >> fine)));
               atomicAdd(&s.count[bin_of(x)], 1u);
             }
           });
@@ -669,11 +683,10 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       }
     }
     if (by_p) {
-      const u64 target = (u64)((double)p * (double)whole);
-      const int n = gather(false, 0, target);
+      const int n = gather(false, 0);
       if (wave == 0) {
-        u64 upto = 0;
-        const u64 e = last_of(n, s.ranks_before, s.before, false, 0, target, &upto);
+        double upto = 0.0;
+        const u64 e = last_of(n, s.ranks_before, s.before, false, 0, s.target, &upto);
         if (lane == 0) s.bound = e > bound ? e : bound;
       }
       __syncthreads();
