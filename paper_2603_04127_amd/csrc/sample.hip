@@ -21,6 +21,7 @@
 // addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 31, no filter 37 (weighed in a read of its own behind that for the largest:
 // 47), top_p 0.9 101 (with a read for the list and one for the sum 107); one row of 32000 fp32 logits 8, 12.5, 12 and 29, where the way through the
 // steps counts and not the row (top_k 50 with the bound's bits four at a time alone: 14.4).
+#include <algorithm>
 #include <cmath>
 #include <type_traits>
 
@@ -34,6 +35,7 @@ typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned long long u64;
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64;
+constexpr int kMostGroups = 1 << 21;   // workgroups in one dimension of a grid: 2^31 threads, of less than 2^32
 constexpr int kAhead = 4;      // pieces of 16 bytes that a thread asks for at once
 constexpr int kBins = 2048;    // 32 for each lane of a wave
 constexpr int kList = 2048;    // entries that are sorted
@@ -241,11 +243,12 @@ __device__ __forceinline__ void sort(Shared& s, int n, int tid) {
 
 template <typename T>
 __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logits, const float* __restrict__ uniform, Setting set,
-                                                     int32_t* __restrict__ out_token, float* __restrict__ out_logprob, int V) {
+                                                     int32_t* __restrict__ out_token, float* __restrict__ out_logprob, int B, int V) {
   __shared__ Shared s;
   // Bit 9 of MODE, IEEE, off: a maximum of a signalling NaN and a number is the number.
   __builtin_amdgcn_s_setreg(1 | 9 << 6, 0);
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.y * kMostGroups + blockIdx.x;
+  if (b >= B) return;
   constexpr int P = Row<T>::P;
   Row<T> row;
   {
@@ -836,8 +839,9 @@ dark_status dark_sample(const dark_sample_params* p, const void* logits, const f
     return DARK_EINVAL;
   const sample::Setting set{temperature, top_p, min_p, top_k, p->temperature, p->top_p, p->min_p, p->top_k};
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const dim3 grid((unsigned)std::min(p->B, sample::kMostGroups), (unsigned)((p->B - 1) / sample::kMostGroups + 1));
 #define DARK_SAMPLE(T)                                                                                                              \
-  DARK_LAUNCH(KID_SAMPLE, st, (sample::k_sample<T>), dim3(p->B), dim3(sample::kThreads), 0, static_cast<const T*>(logits), uniform, set, out_token, out_logprob, p->V)
+  DARK_LAUNCH(KID_SAMPLE, st, (sample::k_sample<T>), grid, dim3(sample::kThreads), 0, static_cast<const T*>(logits), uniform, set, out_token, out_logprob, p->B, p->V)
   if (p->io_dtype == DARK_BF16) {
     DARK_SAMPLE(unsigned short);
   } else {
