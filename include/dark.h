@@ -381,7 +381,8 @@ dark_status dark_decay_step(const dark_decay_params* p, const void* q, const voi
  *   nearer of the two.  What lies behind a sequence in the operands does not matter; out and the gradients are 0 there.
  *   States are float32, [B, H, dk, dv].  S_in NULL: zero.  S_out NULL: not wanted.  S_out is the state behind the last token; S_out == S_in
  *   updates a state in place.  Any other overlap of a result with an operand or another result is DARK_EINVAL, here and below.
- * dk and dv up to 256, B H L up to 2^28 (else DARK_EUNSUPPORTED); rows of whole 16 bytes are faster.  L == 0: the state is passed on.
+ * dk and dv up to 256, B H up to 2^22, B H L up to 2^28, with DARK_BLHD H max(dk, dv) up to 2^22; backward with dk above 64 fewer than 2^23 chunks of 64 rows
+ * (fp32: 32), each sequence's last one counted whole (else DARK_EUNSUPPORTED).  Rows of whole 16 bytes are faster.  L == 0: the state is passed on.
  *
  * Arithmetic: products on the matrix units, with fp32 sums, of operands that are sums of bf16 numbers: 24 bits of whatever has 32 (states,
  * corrections, fp32 operands), the operands themselves where they are bf16.  What goes into a bf16 output alone keeps 16 bits.  Outputs and gradients do not depend on which others are wanted.

@@ -10,8 +10,9 @@ namespace delta {
 namespace {
 
 constexpr int kMostWidth = 256;
-constexpr long long kMostRows = 1LL << 28;   // and so at most 2^23 chunks, a workgroup of 256 threads each
-constexpr long long kMostGroups = 1 << 22;
+constexpr long long kMostRows = 1LL << 28;
+constexpr long long kMostHeads = 1 << 22;        // 768 threads each at most
+constexpr long long kMostThreads = 1LL << 32;    // of a launch in one dimension, less one
 
 // ---------------------------------------------------------------------------
 // One token.  With D = a S: u = beta (v - D^T k), S' = D + k u^T, out = scale (D^T q + (q . k) u): one reduction over the rows for both
@@ -114,13 +115,20 @@ static dark_status check_params(const dark_delta_params* p, Problem* out) {
   if (p->layout != DARK_BHLD && p->layout != DARK_BLHD) return DARK_EINVAL;
   if (!(p->scale >= 0.f) || std::isinf(p->scale)) return DARK_EINVAL;
   const long long heads = (long long)p->B * p->H;
-  if (p->dk > kMostWidth || p->dv > kMostWidth || heads > kMostGroups || (heads > 0 && p->L > kMostRows / heads)) return DARK_EUNSUPPORTED;
+  if (p->dk > kMostWidth || p->dv > kMostWidth || heads > kMostHeads || (heads > 0 && p->L > kMostRows / heads)) return DARK_EUNSUPPORTED;
   // a chunk's rows are addressed by 32-bit offsets: 64 rows of all heads stay under 2^31 bytes
   if (p->layout == DARK_BLHD && (long long)p->H * (p->dk > p->dv ? p->dk : p->dv) > (1 << 22)) return DARK_EUNSUPPORTED;
   out->p = *p;
   out->scale = p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)p->dk);
   out->st = nullptr;
   return DARK_OK;
+}
+
+// A chunk's triangles take 256 threads: 2^28 rows make 12.4 million chunks at most, of sequences of 65 rows in fp32.  Its gradients (k_delta_grad) take 512
+// where keys are wider than 64.
+static bool too_many_chunks(const Problem& pb) {
+  const int C = chunk_of(pb.p.io_dtype);
+  return pb.BH() * ((pb.p.L + C - 1) / C) * (inner_of(pb.p.dk) > 64 ? 512 : 256) >= kMostThreads;
 }
 
 static Args args_of(const Problem& pb) {
@@ -231,7 +239,7 @@ extern "C" {
 
 size_t dark_delta_workspace_bytes(const dark_delta_params* p, int backward) {
   delta::Problem pb;
-  if (delta::check_params(p, &pb) != DARK_OK) return 0;
+  if (delta::check_params(p, &pb) != DARK_OK || (backward != 0 && delta::too_many_chunks(pb))) return 0;
   return measure(pb, backward != 0);
 }
 
@@ -276,6 +284,7 @@ dark_status dark_delta_bwd(const dark_delta_params* p, const void* Q, const void
                            void* dK, void* dV, float* dlog_gate, float* dbeta, float* dS_in, void* ws, size_t ws_bytes, void* hip_stream) {
   delta::Problem pb;
   DARK_TRY(delta::check_params(p, &pb));
+  if (delta::too_many_chunks(pb)) return DARK_EUNSUPPORTED;
   if (pb.p.B == 0 || (pb.p.L == 0 && dS_in == nullptr)) return DARK_OK;
   if (pb.p.L > 0 && (!Q || !K || !V || !beta || !dOut)) return DARK_EINVAL;
   if (!aligned(Q, 16) || !aligned(K, 16) || !aligned(V, 16) || !aligned(dOut, 16) || !aligned(S_in, 16) || !aligned(dS_out, 16) ||
