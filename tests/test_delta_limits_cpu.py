@@ -19,7 +19,7 @@ def _backward(p):
     return dk.lib().dark_delta_bwd(p, *far, None, 0, None)
 
 
-@pytest.mark.parametrize("heads,L,wide,dtype", [(4129776, 65, 128, dk.DARK_F32), (4129776, 65, 256, dk.DARK_F32), (2767376, 97, 65, dk.DARK_F32), (1 << 22, 64, 128, dk.DARK_F32)])
+@pytest.mark.parametrize("heads,L,wide,dtype", [(4129776, 65, 128, dk.DARK_F32), (4129776, 65, 256, dk.DARK_F32), (2767375, 97, 65, dk.DARK_F32), (1 << 22, 64, 128, dk.DARK_F32)])
 def test_more_chunks_than_a_launch_holds(heads, L, wide, dtype):
     # the gradients' kernel has 512 threads for a chunk of 32 rows where keys are wider than 64: 2^32 threads from 2^23 chunks on
     assert heads * L <= 1 << 28 and heads * -(-L // 32) * 512 >= 1 << 32
