@@ -793,11 +793,12 @@ def dark_sample(logits, uniform=None, *, temperature=1.0, top_k=0, top_p=1.0, mi
     settings = (temperature, top_k, top_p, min_p)
     tensor = [x if isinstance(x, torch.Tensor) and x.dim() > 0 else None for x in settings]
     t, k, p, q = (0 if y is not None else x for x, y in zip(settings, tensor))
-    key = ("sample", logits.shape, logits.dtype, float(t), int(k), float(p), float(q))
+    k = min(max(int(k), 0), 2 ** 31 - 1)   # the parameter block has 32 bits
+    key = ("sample", logits.shape, logits.dtype, float(t), k, float(p), float(q))
     plan = _plans.get(key)
     if plan is None:
         B, V = logits.shape
-        plan = (SampleParams(B, V, _dtype_code(logits), int(k), float(t), float(p), float(q)), 0)
+        plan = (SampleParams(B, V, _dtype_code(logits), k, float(t), float(p), float(q)), 0)
         _keep_plan(key, plan)
     params, shape = plan[0], logits.shape[:1]
     _require(uniform, f32, shape, "uniform")
