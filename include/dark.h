@@ -386,8 +386,8 @@ dark_status dark_decay_step(const dark_decay_params* p, const void* q, const voi
  *
  * Arithmetic: products on the matrix units, with fp32 sums, of operands that are sums of bf16 numbers: 24 bits of whatever has 32 (states,
  * corrections, fp32 operands), the operands themselves where they are bf16.  What goes into a bf16 output alone keeps 16 bits.  Outputs and gradients do not depend on which others are wanted.
- * An element of K, V, log_gate or beta that is not finite makes the outputs from its row on not finite, in its column at least for V, and may
- * make those of up to 63 rows before it so.
+ * An element of K, V, log_gate (but for -infinity) or beta that is not finite makes the outputs from its row on and S_out not finite, in its column at least for V,
+ * and may make those of up to 63 rows before it so; one of Q those of its row, and of no other chunk.
  */
 typedef struct {
   int32_t B, H, L;        /* batch, heads, rows of a sequence */
@@ -407,8 +407,10 @@ dark_status dark_delta_fwd(const dark_delta_params* p, const void* Q, const void
 /*
  * Gradients of sum(out dOut) + sum(S_out dS_out).  dS_out NULL: zero.  dQ, dK, dV have the element type and layout of what they belong to;
  * dlog_gate, dbeta and dS_in are float32.  All are overwritten; each may be NULL (skipped).  Nothing is needed from the forward
- * call.  The gradient of a gate of exp(log_gate) == 0 is 0.  An element that is not finite makes the gradients of its sequence not finite
- * from its chunk of 64 rows on, or up to it, or both.
+ * call.  The gradient of a gate of exp(log_gate) == 0 is 0.
+ * An element that is not finite makes gradients of its sequence not finite: one of V dQ, dK and dbeta from its row on, and dlog_gate behind it; one of Q or
+ * dOut dK, dV, dlog_gate and dbeta up to its row, and dS_in (of dOut: dV and dS_in in its column at least, and dQ in its row); one of K, log_gate or beta both, but
+ * for dbeta in a beta's own row.  Other rows of its chunk of 64 (fp32: 32) may become so too, those of other chunks do not.
  */
 dark_status dark_delta_bwd(const dark_delta_params* p, const void* Q, const void* K, const void* V, const float* log_gate,
                            const float* beta, const int32_t* lengths, const float* S_in, const void* dOut, const float* dS_out,
