@@ -195,7 +195,7 @@ __device__ __forceinline__ float logit_of(u64 e) { return value_of((unsigned)(e 
 __device__ __forceinline__ int token_of(u64 e) { return (int)~(unsigned)e; }
 
 struct Shared {
-  u64 list[kList], sorted[kCounted];
+  u64 list[kList];
   u64 mass[kBins];
   unsigned count[kBins];
   double sums[kWaves], scan[kWaves], weights[kSmall];
@@ -369,9 +369,8 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     if (out_logprob != nullptr) out_logprob[b] = (float)log(w / all);
   };
 
-  bool done = k == 0 && !by_p;
   bool summed = false;   // whether `sum` is that of a thread's weights before the bin that holds the bound, and the list's first s.kept are what is kept of it
-  if (!done && k > 0 && k <= kSmall) {
+  if (k > 0 && k <= kSmall) {
     // The k-th largest of the threads' maxima is at most the k-th largest logit.  Most often it is within a factor of two of the largest: then 64 counters
     // of what lies so many 2^17 units of the last place below that say where it is; else its first 16 bits, four at a time, a wave for each value of them.
     const unsigned most = ordered(top);
@@ -416,61 +415,56 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
       sort(s, n, tid);
       if (wave == 0) {
         double upto = 0.0;
-        u64 e = last_of(n, 0, 0.0, true, k, 0.0, &upto);
-        if (by_p) e = last_of(min(n, k), 0, 0.0, false, 0, (double)p * upto, &upto);
-        if (lane == 0) s.bound = e;
+        last_of(n, 0, 0.0, true, k, 0.0, &upto);
+        if (by_p) last_of(min(n, k), 0, 0.0, false, 0, (double)p * upto, &upto);
       }
       __syncthreads();
-      const int m = s.kept;
-      if (m <= kSmall) {
-        // every kept entry adds up those with lower numbers
-        double w = 0.0;
-        if (tid < m) {
-          w = weight.any(logit_of(s.list[tid]));
-          w = w >= (double)q ? w : 0.0;
-          s.weights[tid] = w;
-        }
-        __syncthreads();
-        double before = 0.0;
-        if (tid < m) {
-          const int own = token_of(s.list[tid]);
-          for (int i = 0; i < m; i += 4)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) before += i + j < m && token_of(s.list[i + j]) < own ? s.weights[i + j] : 0.0;
-        }
-        __syncthreads();
-        if (tid < m) s.weights[tid] = before;
-        __syncthreads();
-        if (wave == 0) {
-          double all = 0.0;
-          for (int i0 = 0; i0 < m; i0 += 64) {
-            const double x = i0 + lane < m ? weight.any(logit_of(s.list[i0 + lane])) : 0.0;
-            all += x >= (double)q ? x : 0.0;
-          }
-          all = wave_sum(all);
-          // the kept entry with the highest number whose sum before it does not exceed u of them all
-          const double target = (double)u * all;
-          int best = -1;
-          float logit = 0.f;
-          for (int i0 = 0; i0 < m; i0 += 64) {
-            if (i0 + lane < m) {
-              const u64 e = s.list[i0 + lane];
-              const double x = weight.any(logit_of(e));
-              if (x >= (double)q && x > 0.0 && s.weights[i0 + lane] <= target && token_of(e) > best) best = token_of(e), logit = logit_of(e);
-            }
-          }
-#pragma unroll
-          for (int o = 32; o > 0; o >>= 1) {
-            const int t = __shfl_xor(best, o, 64);
-            const float x = __shfl_xor(logit, o, 64);
-            if (t > best) best = t, logit = x;
-          }
-          if (lane == 0) finish(best, weight.any(logit), all);
-        }
-        return;
+      const int m = s.kept;   // k at most
+      // every kept entry adds up those with lower numbers
+      double w = 0.0;
+      if (tid < m) {
+        w = weight.any(logit_of(s.list[tid]));
+        w = w >= (double)q ? w : 0.0;
+        s.weights[tid] = w;
       }
-      bound = s.bound;
-      done = true;
+      __syncthreads();
+      double before = 0.0;
+      if (tid < m) {
+        const int own = token_of(s.list[tid]);
+        for (int i = 0; i < m; i += 4)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) before += i + j < m && token_of(s.list[i + j]) < own ? s.weights[i + j] : 0.0;
+      }
+      __syncthreads();
+      if (tid < m) s.weights[tid] = before;
+      __syncthreads();
+      if (wave == 0) {
+        double all = 0.0;
+        for (int i0 = 0; i0 < m; i0 += 64) {
+          const double x = i0 + lane < m ? weight.any(logit_of(s.list[i0 + lane])) : 0.0;
+          all += x >= (double)q ? x : 0.0;
+        }
+        all = wave_sum(all);
+        // the kept entry with the highest number whose sum before it does not exceed u of them all
+        const double target = (double)u * all;
+        int best = -1;
+        float logit = 0.f;
+        for (int i0 = 0; i0 < m; i0 += 64) {
+          if (i0 + lane < m) {
+            const u64 e = s.list[i0 + lane];
+            const double x = weight.any(logit_of(e));
+            if (x >= (double)q && x > 0.0 && s.weights[i0 + lane] <= target && token_of(e) > best) best = token_of(e), logit = logit_of(e);
+          }
+        }
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) {
+          const int t = __shfl_xor(best, o, 64);
+          const float x = __shfl_xor(logit, o, 64);
+          if (t > best) best = t, logit = x;
+        }
+        if (lane == 0) finish(best, weight.any(logit), all);
+      }
+      return;
     }
     __syncthreads();
   }
@@ -488,7 +482,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
     }
     least = (u64)(key + 1) << 32 | 0x80000000u;   // with the highest number
   }
-  if (!done) {
+  if (k > 0 || by_p) {
     // Bins over the logits from the largest down, as far as weights matter beside 1 - top_p of the sum (and further for top_k): 2^fine of them an octave of the
     // weights, 32 at least (as far is 56 octaves at most).  Differences are halved: those of the largest numbers stay finite.
     const float reach = (logf((float)V) + (by_p ? fmaxf(-logf(1.f - p), 0.f) : 0.f) + 3.f) * 1.4426950408889634f;
