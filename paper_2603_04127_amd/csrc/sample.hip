@@ -340,6 +340,9 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   const auto integer = [&](double w) __attribute__((always_inline)) -> u64 { return (u64)__double_as_longlong(fma(w, unit, 4503599627370496.0)) & 0xfffffffffffffull; };
   const auto value_in = [&](u64 sum, int octave) __attribute__((always_inline)) -> double { return (double)sum * __hiloint2double((1023 - bits - octave) << 20, 0); };
 
+  // What the sums before a token are held against.  1 or more: whatever they are, the last token has it, though it may weigh less than their roundings.
+  const auto share_of = [&](double all) __attribute__((always_inline)) -> double { return u < 1.f ? (double)u * all : INFINITY; };
+
   // The list holds all entries of a part of the order, sorted, behind `rank` entries of weight `held`: the last that is kept of them, by rank
   // or by weight (target; the first at least), and the weight up to it.  By one wave.
   const auto last_of = [&](int n, int rank, double held, bool by_rank, int most, double target, double* upto) __attribute__((always_inline)) -> u64 {
@@ -446,7 +449,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
         }
         all = wave_sum(all);
         // the kept entry with the highest number whose sum before it does not exceed u of them all
-        const double target = (double)u * all;
+        const double target = share_of(all);
         int best = -1;
         float logit = 0.f;
         for (int i0 = 0; i0 < m; i0 += 64) {
@@ -749,7 +752,7 @@ __global__ __launch_bounds__(kThreads) void k_sample(const T* __restrict__ logit
   double all = 0.0;
 #pragma unroll
   for (int i = 0; i < kWaves; ++i) all += s.sums[i];
-  double rest = (double)u * all;
+  double rest = share_of(all);
   // the part: the first behind which the sums exceed `rest`; with a random number of 1 or more the last that holds anything
   const auto locate = [&](const double* sums, double& rest) __attribute__((always_inline)) -> int {
     int part = -1;
