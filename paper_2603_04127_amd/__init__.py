@@ -671,7 +671,8 @@ def dark_delta_bwd(Q, K, V, log_gate, beta, dOut, *, lengths=None, state=None, d
                    layout="bhld"):
     """Gradients of sum(out dOut) + sum(state_out dstate) of dark_delta_fwd: a dict of those named in `need` ("dlog_gate" only where
     `log_gate` is given, "dstate", the gradient of the incoming state, only where `state` is), in the types and layouts of what they belong to.
-    `grads`: a dict of preallocated tensors to write into instead."""
+    `grads`: a dict of preallocated tensors to write into instead.  The scratch, 120 KB and more for 64 rows of a head (dark.h), is kept for
+    the stream's next calls."""
     torch = _torch()
     p, nb, gates = _delta_plan(Q, K, V, layout, float(scale), True)
     f32, shape = torch.float32, (p.B, p.H, p.dk, p.dv)

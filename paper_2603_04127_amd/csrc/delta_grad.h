@@ -40,7 +40,8 @@ __device__ static inline float row16_prefix(float v) {
 // A chunk by four or eight waves, two a SIMD: each computes its share of the dk columns of dQ and dK, transposed, so that a lane has four neighbouring columns of
 // a row.  The products with the states go over their dv columns in blocks; the states' operands come straight from memory, since
 // no two waves need the same rows of them.
-// 1536 chunks of 64 x 64 in bf16 take 62 us: 120 KB each, two thirds of it states, their gradients, U and dR in fp32, 3.0 TB/s; 576 of 64 x 128 50 to 57.  Four
+// 1536 chunks of 64 x 64 in bf16 take 64 us: 120 KB each, two thirds of it states, their gradients, U and dR in fp32, 3.1 TB/s, with the waves waiting half of their
+// cycles; 576 of 64 x 128 48 to 57.  Four
 // waves where there are columns for eight (dk of 128) took 69, and operands of all steps at once 78 instead of 65 (dk of 64).
 template <typename T, int D1, bool VEC>
 __global__ __launch_bounds__((64 * GradLds<T, D1>::NW), 2) void k_delta_grad(Args A) {

@@ -12,8 +12,8 @@ namespace delta {
 // T = (I + diag(beta) E)^-1 and P = D o (Q K^T) of every chunk, in operand order; backward their transposes, P times scale.
 // The inverse: blocks of 16 x 16 on the diagonal by substitution, row after row; below it T_rc = -T_rr sum_m A_rm T_mc, by fp32 matrix
 // products, one diagonal of blocks after the other.  Substitution and products are backward stable for any beta and keys.
-// A chunk a workgroup.  Many chunks are bound by memory: 8192 of 64 x 128 in bf16 take 105 us, 62 KB each (K and Q read, T in three planes and P in two
-// written), 4.8 TB/s; 1536 of 64 x 64 22, backward, with T^T and a third plane of P, 26.  Few are bound by the steps one after the other: 208 take 10.
+// A chunk a workgroup.  Many chunks are bound by memory: 8192 of 64 x 128 in bf16 take 104 to 115 us, 62 KB each (K and Q read, T in three planes and P in two
+// written), 4.4 to 4.9 TB/s; 1536 of 64 x 64 22, backward, with T^T and a third plane of P, 27.  Few are bound by the steps one after the other: 208 take 10.
 // ---------------------------------------------------------------------------
 template <typename T, int D1>
 constexpr int prep_lds() {
@@ -190,9 +190,9 @@ __global__ __launch_bounds__(256) void k_delta_prep(Args A) {
 // ---------------------------------------------------------------------------
 // Chunk after chunk.  A wave owns 16 columns of the state, in the accumulators of the products that update it, and takes them through
 // all of a chunk's products by itself: its state is an operand of K S and Q S, R of T R, U of P U and of the update, all without a way
-// through LDS or another wave.  Further waves bring the next chunk's operands to LDS meanwhile: a wave that has its SIMD to itself issues an
-// instruction in five or six cycles, whatever it is, so that the chain from state to state is as long as it has instructions.
-// (bf16, 64 heads of 8192 x 120 and 128: 430 us; 64 heads of 2048 x 256 and 128: 196; fp32, 96 heads of 1024 x 64: 65, backward 90.)
+// through LDS or another wave.  Further waves bring the next chunk's operands to LDS meanwhile: a wave that has its SIMD to itself takes several
+// cycles for an instruction, whatever it is, so that the chain from state to state is as long as it has instructions.
+// (bf16, 64 heads of 8192 x 120 and 128: 418 us; 64 heads of 2048 x 256 and 128: 203; fp32, 96 heads of 1024 x 64: 69, backward 94.)
 // ---------------------------------------------------------------------------
 // A chunk's operands in LDS (NP: planes of P, 0: neither Q nor P), in one buffer or two.  An instruction's own offset reaches 64 KB: a lane has a
 // base for each operand, and the buffers lie beside each other.

@@ -1,15 +1,15 @@
 // The gated delta rule's scans with a wave for each row tile of 16 columns of the state (see delta_scan.h for one wave that does all).
 //
-// A wave takes an instruction in seven to twelve cycles, whatever it is, where the chunks' states hang on each other; what a SIMD does in that
+// A wave by itself takes several cycles for an instruction, whatever it is, where the chunks' states hang on each other; what a SIMD does in that
 // time grows with its waves, and a CU with its SIMDs.  So the 16 columns' work is dealt to a team, four waves for bf16's chunks of 64 rows and two for
 // fp32's of 32: each has one of the chunk's row tiles and a part of the state's rows.  What a wave has as sums and all need as an operand goes
 // through LDS: the state's planes, R, and U, with a barrier behind each.  bf16 rows that fill the tiles are brought by two waves and loads that end in
 // LDS (DIRECT), a part between two barriers: a whole chunk's at once, six instructions each, kept their wave from the first barrier for a third of the
 // chunk.  All others go through the registers of eight waves (of four, with as long between the same barriers: 5 to 13 % more; four where fp32 rows of
 // 128 leave no registers for eight).
-// One wave and a team, DIRECT: prompt of 16 x 777 x 128 42 -> 26 us, prefill of 64 x 8192 x 128 415 -> 320, 24 x 4096 x 64 as training runs it 122 -> 72 and
-// backward 160 -> 100 (two waves a team, with all loads at once: no faster than one).  Heads of 100 and 128 for that prompt 45 -> 38, 8 heads of 1000 x 96 and 80
-// backward 63 -> 39; fp32, 8 heads of 1000 x 64 58 -> 55, backward 70 -> 56.
+// One wave and a team, DIRECT: prompt of 16 x 777 x 128 44 -> 26 us, prefill of 64 x 8192 x 128 425 -> 364, 16 x 2048 of 128 and 256 columns 103 -> 64, training of
+// 24 x 4096 x 64 forward 145 -> 92, backward 169 -> 102 (two waves a team, with all loads at once: no faster than one).  Through registers: heads of 100 and 128 for
+// that prompt 46 -> 39, 8 heads of 1000 x 96 and 80 backward 63 -> 41; fp32, 8 heads of 1000 x 64 64 -> 54, backward 69 -> 55.
 // What is not DIRECT adds up in the same order here and there, so that a sequence's results do not depend on how many others there are.
 #pragma once
 
@@ -618,7 +618,7 @@ __global__ __launch_bounds__((TeamChunks<T, D1, TEAMS, 3, true, DIRECT>::kThread
 }
 
 // Whether a call takes these kernels: DIRECT always; what goes through registers while each team of the launch has a CU to itself (48 heads of 1000 x 96 and
-// 80, 240 teams: 42 us, one wave for 16 columns 53; fp32, 48 heads of 1000 x 64 backward, 384 teams: 102, one wave 68).
+// 80, 240 teams: 42 us, one wave for 16 columns 55; fp32, 48 heads of 1000 x 64 backward, 384 teams: 95, one wave 75).
 constexpr int kCUs = 256;
 static long long teams_of(const Args& a, int cols) { return (long long)a.B * a.H * ((cols + 15) / 16); }
 template <typename T>
@@ -629,7 +629,7 @@ template <typename T>
 static bool teamed_back(const Args& a, bool states) { return direct<T>(a) || (a.dk <= 128 && teams_of(a, a.dvp) * (states ? 2 : 1) <= kCUs); }
 
 // One team a workgroup as long as each of those has a CU to itself: the reads of LDS, 128 bytes a cycle, are what two share (24 x 4096 x 64 with
-// one and two: 78 and 98 us, backward 100 and 124).
+// one and two: 92 and 116 us, backward 102 and 122; 64 x 8192 x 128, 512 teams: 521 and 364).
 template <typename T, int D1, int TEAMS, bool DIRECT, bool VEC>
 static dark_status go_team(const Args& a, hipStream_t st) {
   typedef TeamChunks<T, D1, TEAMS, Kind<T>::kOut, false, DIRECT> L;

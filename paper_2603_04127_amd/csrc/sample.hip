@@ -18,8 +18,8 @@
 // row in 8000 would draw a token's neighbour.
 // What bounds it: of 256 rows of 131071 bf16 logits the first read takes 10 us (6.7 TB/s), a read that asks a comparison of each logit 9, one that weighs
 // each 24 (19 instructions a logit, four waves a SIMD; the matrix of 67 MB lies in the last cache by then), the histogram's 40 (two more for the
-// addition in LDS and its bin).  Together: the largest alone 27 us, top_k 50 31, no filter 37 (weighed in a read of its own behind that for the largest:
-// 47), top_p 0.9 101 (with a read for the list and one for the sum 107); one row of 32000 fp32 logits 8, 12.5, 12 and 29, where the way through the
+// addition in LDS and its bin).  Together: the largest alone 28 us, top_k 50 32, no filter 38 (weighed in a read of its own behind that for the largest:
+// 47), top_p 0.9 105 to 107 (with a read for the list and one for the sum 6 more); one row of 32000 fp32 logits 8, 13, 13 and 30, where the way through the
 // steps counts and not the row (top_k 50 with the bound's bits four at a time alone: 14.4).
 #include <algorithm>
 #include <cmath>
